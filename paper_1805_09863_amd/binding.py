@@ -7,6 +7,7 @@ There is no fallback: if the library is missing, loading it raises.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from typing import Optional
 
@@ -25,7 +26,20 @@ _P = ctypes.c_void_p
 _I = ctypes.c_int
 _SZ = ctypes.c_size_t
 
-# name -> (restype, argtypes), mirroring include/kbest.h and include/kbest_standin.h
+_F = ctypes.c_float
+_L = ctypes.c_int64
+
+
+class _Cache(ctypes.Structure):
+    """kb_cache of include/kbest_cache.h."""
+    _fields_ = [("dtype", ctypes.c_int32), ("heads", ctypes.c_int32), ("dim", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("pages", ctypes.c_int32), ("seqs", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("k", _P), ("v", _P), ("table", _P)]
+
+
+_C = ctypes.POINTER(_Cache)
+
+# name -> (restype, argtypes), mirroring include/kbest.h, include/kbest_standin.h and include/kbest_cache.h
 SIGNATURES = {
     "kb_abi_version": (_I, []),
     "kb_status_string": (ctypes.c_char_p, [_I]),
@@ -56,6 +70,11 @@ SIGNATURES = {
     "kb_standin_alive": (_I, [_I, _P, _I, _I, _P, _P, _P, _P]),
     "kb_standin_next_h": (_I, [_I, _P, _I, _I, _I, _P, _P, _P, _P, _SZ, _P]),
     "kb_standin_step": (_I, [_I, _P, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I, _P, _SZ, _P]),
+    # attention cache (include/kbest_cache.h)
+    "kb_cache_append": (_I, [_C, _I, _P, _I, _P, _L, _P, _L, _P, _L, _I, _I, _P, _P, _F, _P, _P, _P, _P, _P, _P]),
+    "kb_cache_attend_workspace_bytes": (_SZ, [_C, _I, _I, _I, _I]),
+    "kb_cache_attend": (_I, [_C, _I, _P, _I, _P, _L, _F, _P, _P, _I, _P, _P, _P, _P, _P, _SZ, _P]),
+    "kb_cache_evict": (_I, [_C, _I, _P, _P, _I, _I, _I, _P, _P, _P, _P, _I, _P, _P, _P, _P, _P]),
 }
 
 
@@ -616,3 +635,252 @@ def beam_backtrace(S0: int, k: int, T: int, alpha: float, fin: tuple, hist_token
     _check(lib().kb_beam_backtrace(S0, k, T, float(alpha), _ptr(fc), _ptr(fs), _ptr(fl), _ptr(fh), _ptr(hist_token),
                                    _ptr(hist_parent), _ptr(toks), _ptr(ln), _ptr(sc), _ptr(nm), _stream(stream)))
     return toks, ln, sc, nm
+
+
+# ---------------------------------------------------------------- attention cache
+def _same_device(dev, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != dev:
+            raise ValueError(f"{name} is on {t.device}, the cache on {dev}")
+
+
+class _on:
+    """The device of the call's tensors made current around it, where it is not."""
+
+    def __init__(self, dev):
+        self.guard = None if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _cache(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor) -> _Cache:
+    _need(k_cache, "k_cache", dim=4)
+    _need(v_cache, "v_cache", dtype=k_cache.dtype, dim=4)
+    _need(table, "table", dtype=torch.int32, dim=2)
+    if v_cache.shape != k_cache.shape:
+        raise ValueError("k_cache and v_cache must have the same shape")
+    _same_device(k_cache.device, v_cache=v_cache, table=table)
+    pages, heads, page_size, dim = k_cache.shape
+    seqs, max_pages = table.shape
+    return _Cache(_dtype_code(k_cache), heads, dim, page_size, pages, seqs, max_pages, k_cache.data_ptr(),
+                  v_cache.data_ptr(), table.data_ptr())
+
+
+def _need_rows(t: torch.Tensor, name: str, dtype, R: int, heads: Optional[int], dim: int) -> int:
+    """R x heads x dim whose rows may lie apart (part of a wider projection); their distance in values."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a tensor on the GPU")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 3 or t.shape[0] != R or t.shape[2] != dim or (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{name} must be {R} x {'heads' if heads is None else heads} x {dim}, "
+                         f"got {tuple(t.shape)}")
+    heads = t.shape[1]
+    st = t.stride()
+    if (dim > 1 and st[2] != 1) or (heads > 1 and st[1] != dim):
+        raise ValueError(f"{name}: the heads of a row must lie one after the other, without gaps")
+    if R <= 1:
+        return heads * dim
+    if st[0] < heads * dim:
+        raise ValueError(f"{name}: rows must not overlap")
+    return st[0]
+
+
+def cache_append(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, length: torch.Tensor,
+                 k: torch.Tensor, v: torch.Tensor, *, q: Optional[torch.Tensor] = None,
+                 pos: Optional[torch.Tensor] = None, freq: Optional[torch.Tensor] = None, interleaved: bool = False,
+                 amplitude: float = 1.0, seq: Optional[torch.Tensor] = None, n_dev: Optional[torch.Tensor] = None,
+                 position: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
+                 q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """The keys and values of R new tokens into their slots of the cache, queries and
+    keys turned by their rotary positions (kb_cache_append).
+
+    ``k_cache``, ``v_cache`` are pages x heads x page_size x dim (float32 or bfloat16),
+    ``table`` seqs x max_pages int32.  Row r is a token of sequence ``seq[r]`` (r) and
+    goes to slot ``length[r] - 1``.  ``k``, ``v`` are R x heads x dim and ``q`` R x
+    q_heads x dim; their rows may be parts of a wider projection's.  ``freq`` (float64,
+    radians per position, see rotary_frequencies) turns the first ``2 * len(freq)``
+    values of a head, in pairs half of that apart or, ``interleaved``, side by side.
+    ``position`` (int32) and ``weight`` (float32), seqs x heads x slots, receive the new
+    slots' ``pos`` and 0.  Returns the turned queries (``q_out``), None without ``q``.
+    """
+    c = _cache(k_cache, v_cache, table)
+    dev = k_cache.device
+    _need(length, "length", dtype=torch.int32, dim=1)
+    R = length.shape[0]
+    k_stride = _need_rows(k, "k", k_cache.dtype, R, c.heads, c.dim)
+    v_stride = _need_rows(v, "v", k_cache.dtype, R, c.heads, c.dim)
+    q_heads = q_stride = rot = 0
+    if q is not None:
+        q_stride = _need_rows(q, "q", k_cache.dtype, R, None, c.dim)
+        q_heads = q.shape[1]
+        if q_out is None:
+            q_out = torch.empty((R, q_heads, c.dim), dtype=q.dtype, device=dev)
+        _need(q_out, "q_out", dtype=q.dtype, numel=R * q_heads * c.dim)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    if freq is not None:
+        _need(freq, "freq", dtype=torch.float64, dim=1)
+        rot = 2 * freq.shape[0]
+    if pos is not None:
+        _need(pos, "pos", dtype=torch.int32, numel=R)
+    if seq is not None:
+        _need(seq, "seq", dtype=torch.int32, numel=R)
+    if n_dev is not None:
+        _need(n_dev, "n_dev", dtype=torch.int32, numel=1)
+    slots = c.seqs * c.heads * c.max_pages * c.page_size
+    if position is not None:
+        _need(position, "position", dtype=torch.int32, numel=slots)
+    if weight is not None:
+        _need(weight, "weight", dtype=torch.float32, numel=slots)
+    _same_device(dev, length=length, k=k, v=v, q=q, q_out=q_out, freq=freq, pos=pos, seq=seq, n_dev=n_dev,
+                 position=position, weight=weight)
+    with _on(dev):
+        _check(lib().kb_cache_append(c, R, _ptr(n_dev), q_heads, _ptr(q), q_stride, _ptr(k), k_stride, _ptr(v),
+                                     v_stride, rot, int(interleaved), _ptr(pos), _ptr(freq), amplitude, _ptr(seq),
+                                     _ptr(length), _ptr(q_out), _ptr(position), _ptr(weight), _stream(stream, dev)))
+    return q_out
+
+
+def cache_attend_workspace_bytes(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, R: int,
+                                 q_heads: int, max_len: Optional[int] = None, weights: bool = False) -> int:
+    c = _cache(k_cache, v_cache, table)
+    return int(lib().kb_cache_attend_workspace_bytes(c, R, q_heads, max_len or c.max_pages * c.page_size,
+                                                     int(weights)))
+
+
+def cache_attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor,
+                 length: torch.Tensor, *, scale: Optional[float] = None, max_len: Optional[int] = None,
+                 seq: Optional[torch.Tensor] = None, n_dev: Optional[torch.Tensor] = None,
+                 out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                 weight_in: Optional[torch.Tensor] = None, weight_out: Optional[torch.Tensor] = None,
+                 ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Attention of one new token a row (``q``: R x q_heads x dim) over the first
+    ``length[r]`` cached slots of its sequence (kb_cache_attend): returns R x q_heads x dim.
+
+    ``scale`` defaults to 1 / sqrt(dim), ``max_len``, a host-side bound of the lengths,
+    to the slots of the table.  ``lse`` (R x q_heads float32) receives the scores'
+    log-sum-exp.  ``weight_out`` (seqs x heads x slots float32) receives ``weight_in``
+    (zeros; may be the same tensor) plus each slot's probability, summed over the query
+    heads that share a key-value head: what cache_evict goes by.
+    """
+    c = _cache(k_cache, v_cache, table)
+    dev = k_cache.device
+    _need(length, "length", dtype=torch.int32, dim=1)
+    R = length.shape[0]
+    q_stride = _need_rows(q, "q", k_cache.dtype, R, None, c.dim)
+    q_heads = q.shape[1]
+    if out is None:
+        out = torch.empty((R, q_heads, c.dim), dtype=q.dtype, device=dev)
+    _need(out, "out", dtype=q.dtype, numel=R * q_heads * c.dim)
+    if lse is not None:
+        _need(lse, "lse", dtype=torch.float32, numel=R * q_heads)
+    if seq is not None:
+        _need(seq, "seq", dtype=torch.int32, numel=R)
+    if n_dev is not None:
+        _need(n_dev, "n_dev", dtype=torch.int32, numel=1)
+    cap = c.max_pages * c.page_size
+    for t, name in ((weight_in, "weight_in"), (weight_out, "weight_out")):
+        if t is not None:
+            _need(t, name, dtype=torch.float32, numel=c.seqs * c.heads * cap)
+    _same_device(dev, q=q, length=length, out=out, lse=lse, seq=seq, n_dev=n_dev, weight_in=weight_in,
+                 weight_out=weight_out, ws=ws)
+    max_len = cap if max_len is None else max_len
+    L = lib()
+    need = L.kb_cache_attend_workspace_bytes(c, R, q_heads, max_len, weight_out is not None)
+    if ws is None and need > 0:
+        ws = workspace(need, dev)
+    if ws is not None:
+        _need_ws(ws, need)
+    with _on(dev):
+        _check(L.kb_cache_attend(c, R, _ptr(n_dev), q_heads, _ptr(q), q_stride,
+                                 c.dim ** -0.5 if scale is None else scale, _ptr(seq), _ptr(length), max_len,
+                                 _ptr(out), _ptr(lse), _ptr(weight_in), _ptr(weight_out), _ptr(ws),
+                                 0 if ws is None else ws.numel() * ws.element_size(), _stream(stream, dev)))
+    return out
+
+
+def cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, length: torch.Tensor, keep: int, *,
+                weight: torch.Tensor, position: Optional[torch.Tensor] = None, newest: Optional[torch.Tensor] = None,
+                first: int = 0, recent: int = 0, out_table: Optional[torch.Tensor] = None,
+                out: Optional[tuple] = None, n_dev: Optional[torch.Tensor] = None, stream=None):
+    """Sequences' caches back to ``keep`` slots, head by head those of greatest ``weight``
+    and those whose ``position`` is below ``first`` or above ``newest - recent``
+    (kb_cache_evict).  Returns (length, weight, position, source): the new lengths, the
+    kept slots' weights and positions, and the slot each came from.
+
+    Without ``out_table`` the rows move within their own pages; with it (R x pages int32)
+    the kept ones are put there.  ``out`` may supply the four results (position None where
+    ``position`` is; length and, in place, weight and position may be the inputs).
+    """
+    c = _cache(k_cache, v_cache, table)
+    dev = k_cache.device
+    _need(length, "length", dtype=torch.int32, dim=1)
+    R = length.shape[0]
+    slots = c.seqs * c.heads * c.max_pages * c.page_size
+    _need(weight, "weight", dtype=torch.float32, numel=slots)
+    if position is not None:
+        _need(position, "position", dtype=torch.int32, numel=slots)
+    if newest is not None:
+        _need(newest, "newest", dtype=torch.int32, numel=R)
+    if n_dev is not None:
+        _need(n_dev, "n_dev", dtype=torch.int32, numel=1)
+    if out_table is None:
+        out_table = table
+    _need(out_table, "out_table", dtype=torch.int32, dim=2)
+    if out_table.shape[0] < R:
+        raise ValueError(f"out_table has {out_table.shape[0]} rows, {R} needed")
+    out_pages = out_table.shape[1]
+    kept = R * c.heads * out_pages * c.page_size
+    if out is None:
+        shape = (R, c.heads, out_pages * c.page_size)
+        out = (torch.empty(R, dtype=torch.int32, device=dev), torch.zeros(shape, device=dev),
+               None if position is None else torch.full(shape, -1, dtype=torch.int32, device=dev),
+               torch.empty((R, c.heads, max(keep, 0)), dtype=torch.int32, device=dev))
+    if len(out) != 4:
+        raise ValueError("out must hold 4 tensors (length, weight, position, source)")
+    out_length, out_weight, out_position, source = out
+    _need(out_length, "out length", dtype=torch.int32, numel=R)
+    _need(out_weight, "out weight", dtype=torch.float32, numel=kept)
+    if out_position is not None:
+        _need(out_position, "out position", dtype=torch.int32, numel=kept)
+    _need(source, "source", dtype=torch.int32, numel=R * c.heads * keep)
+    _same_device(dev, length=length, weight=weight, position=position, newest=newest, n_dev=n_dev,
+                 out_table=out_table, out_length=out_length, out_weight=out_weight, out_position=out_position,
+                 source=source)
+    with _on(dev):
+        _check(lib().kb_cache_evict(c, R, _ptr(n_dev), _ptr(length), keep, first, recent, _ptr(newest), _ptr(weight),
+                                    _ptr(position), _ptr(out_table), out_pages, _ptr(out_length), _ptr(out_weight),
+                                    _ptr(out_position), _ptr(source), _stream(stream, dev)))
+    return out_length, out_weight, out_position, source
+
+
+def rotary_frequencies(rot_dim: int, *, base: float = 10000.0, factor: float = 1.0,
+                       trained_length: Optional[int] = None, slow: float = 1.0, fast: float = 32.0,
+                       device=None) -> torch.Tensor:
+    """Radians per position of the rot_dim / 2 pairs, float64: base ** (-2 i / rot_dim).
+
+    For contexts ``factor`` times longer than the trained ones every frequency is divided
+    by it; with ``trained_length``, only those of pairs that make at most ``slow`` turns
+    over that length, those of pairs that make ``fast`` and more stay, and the ones
+    between are blended linearly in the number of turns.
+    """
+    if rot_dim < 2 or rot_dim % 2 != 0:
+        raise ValueError(f"rot_dim = {rot_dim}: an even number of values")
+    if not base > 0 or not factor > 0 or not fast > slow or (trained_length is not None and trained_length < 1):
+        raise ValueError(f"base = {base}, factor = {factor}, trained_length = {trained_length}, slow = {slow}, "
+                         f"fast = {fast}")
+    w = base ** (-2.0 * torch.arange(rot_dim // 2, dtype=torch.float64) / rot_dim)
+    if trained_length is None:
+        w = w / factor
+    else:
+        turns = trained_length * w / (2 * math.pi)
+        stay = ((turns - slow) / (fast - slow)).clamp(0.0, 1.0)
+        w = w * stay + w / factor * (1.0 - stay)
+    return w.to(device or "cuda")

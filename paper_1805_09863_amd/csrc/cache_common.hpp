@@ -1,0 +1,86 @@
+// The attention cache on the device: argument blocks and launchers of its
+// three operators, and what their kernels share.
+#pragma once
+
+#include "kb_common.hpp"
+
+namespace kb {
+
+constexpr int kCacheMaxDim = 256;  // largest head size
+
+// A kb_cache as the kernels take it.
+struct CacheView {
+  void* k;               // pages x heads x page_size x dim
+  void* v;
+  const int32_t* table;  // seqs x max_pages
+  int heads, dim, log_ps, pages, seqs, max_pages, cap;  // cap = max_pages << log_ps
+};
+
+struct AppendArgs {
+  CacheView c;
+  int R, q_heads, rot, interleaved;
+  const int32_t* n_dev;
+  const void *q, *k_new, *v_new;
+  int64_t q_stride, k_stride, v_stride;
+  const int32_t* pos;
+  const double* freq;
+  float amplitude;
+  const int32_t* seq;
+  const int32_t* length;
+  void* q_out;
+  int32_t* position;
+  float* weight;
+};
+
+struct AttendArgs {
+  CacheView c;
+  int R, q_heads, max_len;
+  const int32_t* n_dev;
+  const void* q;
+  int64_t q_stride;
+  float scale;
+  const int32_t* seq;
+  const int32_t* length;
+  void* out;
+  float* lse;  // nullable without weights
+  const float* weight_in;
+  float* weight_out;
+};
+
+struct EvictArgs {
+  CacheView c;
+  int R, keep, first, recent, out_max_pages;
+  const int32_t* n_dev;
+  const int32_t* length;
+  const int32_t* newest;
+  const float* weight;
+  const int32_t* position;
+  const int32_t* out_table;
+  int32_t* out_length;
+  float* out_weight;
+  int32_t* out_position;
+  int32_t* source;
+};
+
+hipError_t launch_cache_append(int bf16, const AppendArgs& a, hipStream_t st);
+hipError_t launch_cache_attend(int bf16, const AttendArgs& a, hipStream_t st);
+hipError_t launch_cache_evict(int bf16, const EvictArgs& a, hipStream_t st);
+
+// Row (of dim values, in k or v) of slot t of a sequence whose table row is
+// `pages`, for key-value head `head`; -1 for a hole.  Rows are counted in 32
+// bits (the host refuses pools of 2^31 and more), their bytes in 64.
+__device__ __forceinline__ int cache_row(const CacheView& c, const int32_t* pages, int head, int t) {
+  const int page = pages[t >> c.log_ps];
+  if ((uint32_t)page >= (uint32_t)c.pages) return -1;
+  return ((page * c.heads + head) << c.log_ps) + (t & ((1 << c.log_ps) - 1));
+}
+
+// Table row of row r of a call, -1 where seq names none.
+__device__ __forceinline__ int cache_seq(const CacheView& c, const int32_t* seq, int r) {
+  const int s = seq ? seq[r] : r;
+  return (uint32_t)s < (uint32_t)c.seqs ? s : -1;
+}
+
+__device__ __forceinline__ int rows_of(int R, const int32_t* n_dev) { return n_dev ? min(R, *n_dev) : R; }
+
+}  // namespace kb

@@ -12,6 +12,7 @@
 #include "kbest.h"
 #include "kbest_standin.h"
 #include "kb_launch.hpp"
+#include "kb_status.hpp"
 
 namespace kb {
 hipError_t launch_k1_stage_bf16_L256(int kc, dim3 grid, const K1Args& a, hipStream_t st);
@@ -79,11 +80,10 @@ hipError_t launch_k1(int bf16, int dma, int layout, int kc, dim3 grid, const K1A
 }
 }  // namespace kb
 
-namespace {
+namespace kb {
 
-thread_local std::string g_last_error;
+static thread_local std::string g_last_error;
 
-kb_status fail(kb_status status, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 kb_status fail(kb_status status, const char* fmt, ...) {
   char buf[512];
   va_list ap;
@@ -98,6 +98,16 @@ kb_status ok() {
   g_last_error.clear();
   return KB_OK;
 }
+
+const char* last_error() { return g_last_error.c_str(); }
+
+}  // namespace kb
+
+namespace {
+
+using kb::aligned;
+using kb::fail;
+using kb::ok;
 
 // The projection is planned for MI355X: 256 compute units, one fused
 // workgroup per CU (its LDS and registers allow no more).
@@ -391,8 +401,6 @@ size_t workspace_bytes(int dtype, int N, int H, int V, int k) {
   return std::max(a, std::max(b, c));
 }
 
-bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
-
 kb_status validate_step(int dtype, int N, int H, int V, int k, int S) {
   if (dtype != KB_F32 && dtype != KB_BF16) return fail(KB_ERR_INVALID_ARG, "unknown dtype %d", dtype);
   if (N < 0 || S < 0) return fail(KB_ERR_INVALID_ARG, "negative N (%d) or S (%d)", N, S);
@@ -605,7 +613,7 @@ const char* kb_status_string(kb_status s) {
   }
 }
 
-const char* kb_last_error(void) { return g_last_error.c_str(); }
+const char* kb_last_error(void) { return kb::last_error(); }
 
 kb_status kb_kbest_plan(int dtype, int N, int H, int V, int k, const void* h, const void* W, const float* b,
                         int32_t* plan_out) {
