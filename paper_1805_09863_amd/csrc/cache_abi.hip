@@ -67,6 +67,37 @@ kb_status check_count(int R, int q_heads) {
   return KB_OK;
 }
 
+size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+
+struct AttendPlan {
+  int waves, head_tiles, chunk, splits;
+  size_t score_ld, part_o, part_s, scores, lse, bytes;  // workspace offsets
+};
+
+AttendPlan attend_plan(const kb_cache* c, int R, int q_heads, int max_len, bool weights) {
+  AttendPlan p{};
+  max_len = std::min(max_len, c->max_pages * c->page_size);
+  const int group = q_heads / c->heads;
+  p.head_tiles = (group + 15) / 16;
+  const long long units = (long long)R * c->heads * p.head_tiles;
+  p.waves = max_len <= 64 ? 1 : 4;
+  const long long even = ((long long)max_len * units + 2047) / 2048;
+  p.chunk = (int)std::min<long long>(std::max<long long>((even + 127) / 128 * 128, 256), 1024);
+  p.splits = (max_len + p.chunk - 1) / p.chunk;
+  const size_t rh = (size_t)R * q_heads;
+  if (p.splits > 1) {
+    p.part_s = align_up(rh * p.splits * c->dim * sizeof(float), 256);
+    p.bytes = align_up(p.part_s + rh * p.splits * sizeof(float2), 256);
+  }
+  if (weights) {
+    p.score_ld = align_up(max_len, 32);
+    p.scores = p.bytes;
+    p.lse = align_up(p.scores + rh * p.score_ld * sizeof(float), 256);
+    p.bytes = align_up(p.lse + rh * sizeof(float), 256);
+  }
+  return p;
+}
+
 bool bf16(const kb_cache* c) { return c->dtype == KB_BF16; }
 
 }  // namespace
@@ -110,7 +141,7 @@ size_t kb_cache_attend_workspace_bytes(const kb_cache* cache, int R, int q_heads
   if (check_cache(cache) != KB_OK || q_heads < 1 || q_heads % cache->heads != 0 || max_len < 1 ||
       check_count(R, q_heads) != KB_OK || R == 0)
     return 0;
-  return weights ? (size_t)R * q_heads * sizeof(float) : 0;
+  return attend_plan(cache, R, q_heads, max_len, weights != 0).bytes;
 }
 
 kb_status kb_cache_attend(const kb_cache* cache, int R, const int32_t* n_dev, int q_heads, const void* q,
@@ -132,15 +163,31 @@ kb_status kb_cache_attend(const kb_cache* cache, int R, const int32_t* n_dev, in
   if (!seq && R > cache->seqs) return fail(KB_ERR_INVALID_ARG, "R = %d rows, seqs = %d and no seq", R, cache->seqs);
   if (weight_in && !weight_out) return fail(KB_ERR_INVALID_ARG, "weight_in without weight_out");
   if (weight_out && seq) return fail(KB_ERR_UNSUPPORTED, "weights need a table row for each row (seq NULL)");
-  const size_t need = kb_cache_attend_workspace_bytes(cache, R, q_heads, max_len, weight_out != nullptr);
-  if (need > 0) {
-    if (!workspace) return fail(KB_ERR_WORKSPACE, "workspace is null (%zu bytes needed)", need);
+  const AttendPlan p = attend_plan(cache, R, q_heads, max_len, weight_out != nullptr);
+  if ((long long)R * cache->heads * p.head_tiles * p.splits * p.waves * 64 > UINT32_MAX)  // threads of a launch
+    return fail(KB_ERR_UNSUPPORTED, "R * heads * %d splits too large", p.splits);
+  if (p.bytes > 0) {
+    if (!workspace) return fail(KB_ERR_WORKSPACE, "workspace is null (%zu bytes needed)", p.bytes);
     if (!aligned(workspace, 256)) return fail(KB_ERR_WORKSPACE, "workspace must be 256-byte aligned");
-    if (workspace_bytes < need) return fail(KB_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", workspace_bytes, need);
+    if (workspace_bytes < p.bytes)
+      return fail(KB_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", workspace_bytes, p.bytes);
   }
-  if (weight_out && !lse) lse = static_cast<float*>(workspace);
-  const kb::AttendArgs a{view(cache), R,      q_heads, max_len, n_dev, q,         q_stride,
-                         scale,       seq, length,  out,     lse,   weight_in, weight_out};
+  char* ws = static_cast<char*>(workspace);
+  kb::AttendArgs a{view(cache), R,      q_heads, max_len, n_dev, q,         q_stride,
+                   scale,       seq, length,  out,     lse,   weight_in, weight_out};
+  a.waves = p.waves;
+  a.head_tiles = p.head_tiles;
+  a.chunk = p.chunk;
+  a.splits = p.splits;
+  if (p.splits > 1) {
+    a.part_o = reinterpret_cast<float*>(ws + p.part_o);
+    a.part_s = reinterpret_cast<float2*>(ws + p.part_s);
+  }
+  if (weight_out) {
+    a.scores = reinterpret_cast<float*>(ws + p.scores);
+    a.score_ld = (int64_t)p.score_ld;
+    if (!lse) a.lse = reinterpret_cast<float*>(ws + p.lse);
+  }
   hipError_t e = kb::launch_cache_attend(bf16(cache), a, reinterpret_cast<hipStream_t>(stream));
   if (e != hipSuccess) return fail(KB_ERR_HIP, "cache attention kernel launch: %s", hipGetErrorString(e));
   return ok();
@@ -153,6 +200,8 @@ kb_status kb_cache_evict(const kb_cache* cache, int R, const int32_t* n_dev, con
   kb_status st = check_cache(cache);
   if (st != KB_OK) return st;
   if ((st = check_count(R, cache->heads)) != KB_OK) return st;
+  if ((long long)R * cache->heads * 1024 > UINT32_MAX)  // threads of a launch
+    return fail(KB_ERR_UNSUPPORTED, "R * heads = %lld too large", (long long)R * cache->heads);
   if (keep < 1 || first < 0 || recent < 0 || (long long)first + recent > keep)
     return fail(KB_ERR_INVALID_ARG, "keep = %d, first = %d, recent = %d", keep, first, recent);
   const int cap = cache->max_pages * cache->page_size;

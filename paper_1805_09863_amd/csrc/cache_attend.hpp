@@ -1,0 +1,323 @@
+// Attention of one new token a row over its cached slots, on the matrix cores.
+//
+//   x_t = scale * (q . k_t),   out = sum_t e^(x_t - m) v_t / sum_t e^(x_t - m),   m = max x_t
+//
+// One pass with the running maximum and sum of a softmax: a tile of scores takes (m, s, o) to
+// (m', s a + sum e^(x - m'), o a + sum e^(x - m') v), a = e^(m - m').
+//
+// What bounds it is the cache's stream from memory, 2 dim values a slot and key-value head, which
+// every query head that shares the key-value head takes part in.  So a wave holds the queries of 16
+// such heads in registers (fewer: zeros) and reads each slot once:
+//
+//  - S^T = K Q^T in 16 x 16 blocks, rows slots and columns heads.  A lane's part of the operand K is
+//    16 bytes of one slot's key, loaded straight from the cache: the sum over the head's values may
+//    run in any order, so the lanes of a slot take turns over its 64-byte pieces.
+//  - A lane then has the scores of one head for 4 slots of each block, and that is already its part
+//    of the operand P^T of the second product, O^T = V^T P^T, if the slots are summed over in that
+//    order: probabilities never leave their registers.  o and a have the same head in the lane, so
+//    rescaling is a product a register.
+//  - A lane's part of V^T would be one value of each of its slots.  It loads 16 bytes of each slot
+//    (8 bf16 values; the 16 lanes of a slot read its row from end to end) and picks the value of
+//    each product out of them with byte permutations.
+//
+// bf16: 32 slots a tile, probabilities as two bf16 pieces (the rounding of one alone, 2^-9 of each,
+// would double the error of a rounded output; the second product is not what bounds the kernel).
+// float32: 16 slots a tile, products on the fp32 matrix instruction.
+#pragma once
+
+#include "cache_common.hpp"
+
+namespace kb {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+template <class T>
+struct AttendTile;
+template <>
+struct AttendTile<__bf16> {
+  static constexpr int kSlots = 32;
+};
+template <>
+struct AttendTile<float> {
+  static constexpr int kSlots = 16;
+};
+
+// The largest (the sum) of the four lanes l, l ^ 16, l ^ 32, l ^ 48, in all of them.
+__device__ __forceinline__ float over_groups(float x, bool sum) {
+  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  float u = __uint_as_float(a[0]), w = __uint_as_float(a[1]);
+  x = sum ? u + w : fmaxf(u, w);
+  auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  u = __uint_as_float(b[0]), w = __uint_as_float(b[1]);
+  return sum ? u + w : fmaxf(u, w);
+}
+
+// One (row, key-value head, 16 query heads, run of slots): NW waves, tiles in turn.
+// DC: dim rounded up to a built size.
+template <class T, int DC, int NW>
+__global__ __launch_bounds__(NW * 64, DC * sizeof(T) <= 256 ? 2 : 1) void cache_attend_tiles(AttendArgs a) {
+  constexpr bool kBf16 = sizeof(T) == 2;
+  constexpr int TS = AttendTile<T>::kSlots, NH = TS / 16;   // slots of a tile, 16-slot blocks
+  constexpr int NI = DC * (int)sizeof(T) / 64;              // 64-byte pieces of a key
+  constexpr int VE = kBf16 && DC > 64 ? 8 : 4;              // values of a slot that a lane holds side by side
+  constexpr int NB = (DC + 16 * VE - 1) / (16 * VE);        // such runs of 16 lanes in a row
+  constexpr int VW = VE * (int)sizeof(T) / 4;               // words of them
+  constexpr int NV = TS / 4;                                // slots of a tile that a lane takes values of
+  constexpr int LD = DC + 4;
+  __shared__ float part[NW > 1 ? NW * 16 * LD : 1];
+  __shared__ float2 stat[NW > 1 ? NW * 16 : 1];
+
+  const CacheView& c = a.c;
+  const int lane = threadIdx.x & 63, wave = NW > 1 ? threadIdx.x >> 6 : 0;
+  const int n = lane & 15, g = lane >> 4;  // operand row or column, group of the summed index
+  const int split = blockIdx.x % a.splits, unit = blockIdx.x / a.splits;
+  const int ht = unit % a.head_tiles, kv = unit / a.head_tiles % c.heads, r = unit / a.head_tiles / c.heads;
+  if (r >= rows_of(a.R, a.n_dev)) return;
+  const int group = a.q_heads / c.heads, h0 = kv * group + ht * 16, nh = min(16, group - ht * 16);
+  const int s = cache_seq(c, a.seq, r);
+  const int len = s < 0 || c.pages == 0 ? 0 : max(0, min(a.length[r], min(a.max_len, c.cap)));
+  const int begin = split * a.chunk, end = min(len, begin + a.chunk);
+  if (a.splits > 1 && begin >= end) return;  // the join knows from the length which splits there are
+
+  const int D = c.dim, last = D * (int)sizeof(T) / 16 - 1, vlast = D / VE - 1;
+  const int row_bytes = D * (int)sizeof(T);
+  const int32_t* pages = c.table + (int64_t)max(s, 0) * c.max_pages;
+
+  uint4 q[NI];
+  int koff[NI], voff[NB];
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    q[i] = make_uint4(0, 0, 0, 0);
+    koff[i] = min(4 * i + g, last) * 16;  // past the head's end: its last piece again, times zeros
+    if (n < nh && 4 * i + g <= last) {
+      const T* p = (const T*)a.q + r * a.q_stride + (int64_t)(h0 + n) * D + (4 * i + g) * (16 / (int)sizeof(T));
+      __builtin_memcpy(&q[i], __builtin_assume_aligned(p, sizeof(T)), 16);
+    }
+  }
+#pragma unroll
+  for (int b = 0; b < NB; ++b) voff[b] = min(b * 16 + n, vlast) * VW * 4;
+
+  const float scale2 = a.scale * kL2E;
+  float m = -FLT_MAX, sum = 0.f;
+  f32x4 acc[NB][VE];
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int e = 0; e < VE; ++e) acc[b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  const int first = begin + wave * TS, step = NW * TS;
+  if (first < end) {
+    uint4 kr[NH][NI];
+    uint32_t vr[NV][NB][VW];
+    uint32_t valid;
+    const int tl = lane & (TS - 1);  // the slot of a tile whose page this lane looks up
+    auto page_of = [&](int t0) { return t0 + tl < end ? pages[(t0 + tl) >> c.log_ps] : -1; };
+    // this lane's slot as a row of the cache; a hole's or one past the end: some row of the pool
+    auto row_at = [&](int page, int t0, uint32_t& ok) {
+      const bool there = (uint32_t)page < (uint32_t)c.pages;
+      ok = (uint32_t)__ballot(there) & (uint32_t)((1ull << TS) - 1);
+      return there ? ((page * c.heads + kv) << c.log_ps) + ((t0 + tl) & ((1 << c.log_ps) - 1)) : 0;
+    };
+    auto load_k = [&](int row) {
+#pragma unroll
+      for (int hf = 0; hf < NH; ++hf) {
+        const char* p = (const char*)c.k + (int64_t)__shfl(row, hf * 16 + n) * row_bytes;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) kr[hf][i] = *(const uint4*)(p + koff[i]);
+      }
+    };
+    auto load_v = [&](int row) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const char* p = (const char*)c.v + (int64_t)__shfl(row, (j >> 2) * 16 + g * 4 + (j & 3)) * row_bytes;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) __builtin_memcpy(vr[j][b], __builtin_assume_aligned(p + voff[b], VW * 4), VW * 4);
+      }
+    };
+    int row = row_at(page_of(first), first, valid);
+    int next_page = page_of(first + step);
+    load_k(row);
+    load_v(row);
+
+    for (int t0 = first; t0 < end; t0 += step) {
+      // scores: x[hf][i] is head n, slot t0 + 16 hf + 4 g + i
+      f32x4 x[NH];
+#pragma unroll
+      for (int hf = 0; hf < NH; ++hf) {
+        x[hf] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          if constexpr (kBf16) {
+            bf16x8 ka, qb;
+            __builtin_memcpy(&ka, &kr[hf][i], 16);
+            __builtin_memcpy(&qb, &q[i], 16);
+            x[hf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qb, x[hf], 0, 0, 0);
+          } else {
+            float ka[4], qb[4];
+            __builtin_memcpy(ka, &kr[hf][i], 16);
+            __builtin_memcpy(qb, &q[i], 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[hf] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka[e], qb[e], x[hf], 0, 0, 0);
+          }
+        }
+      }
+      // the next tile's keys are asked for as soon as this one's registers are free, its values
+      // further down: one of the two is always on its way
+      uint32_t next_valid;
+      row = row_at(next_page, t0 + step, next_valid);
+      next_page = page_of(t0 + 2 * step);
+      load_k(row);
+
+      const bool whole = valid == (uint32_t)((1ull << TS) - 1);
+      float top = m;
+#pragma unroll
+      for (int hf = 0; hf < NH; ++hf)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[hf][i] *= scale2;
+          if (!whole && !(valid >> (hf * 16 + g * 4 + i) & 1)) x[hf][i] = -INFINITY;
+          top = fmaxf(top, x[hf][i]);
+        }
+      if (a.scores && n < nh) {
+        float* to = a.scores + ((int64_t)r * a.q_heads + h0 + n) * a.score_ld + t0 + g * 4;
+#pragma unroll
+        for (int hf = 0; hf < NH; ++hf) *(f32x4*)(to + hf * 16) = x[hf];
+      }
+      top = over_groups(top, false);
+      const float keep = exp2_fast(m - top);
+      m = top;
+      sum *= keep;
+#pragma unroll
+      for (int hf = 0; hf < NH; ++hf)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[hf][i] = exp2_fast(x[hf][i] - top);
+          sum += x[hf][i];
+        }
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int e = 0; e < VE; ++e) acc[b][e] *= keep;
+
+      if (!whole) {  // a probability of 0 times whatever lies there
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+          if (!(valid >> ((j >> 2) * 16 + g * 4 + (j & 3)) & 1))
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+              for (int w = 0; w < VW; ++w) vr[j][b][w] = 0;
+      }
+      if constexpr (kBf16) {
+        bf16x8 hi, lo;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          hi[j] = (__bf16)x[j >> 2][j & 3];
+          lo[j] = (__bf16)(x[j >> 2][j & 3] - (float)hi[j]);
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int e = 0; e < VE; ++e) {
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              w[j] = __builtin_amdgcn_perm(vr[2 * j + 1][b][e / 2], vr[2 * j][b][e / 2], e % 2 ? 0x07060302 : 0x05040100);
+            bf16x8 va;
+            __builtin_memcpy(&va, w, 16);
+            acc[b][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, hi, acc[b][e], 0, 0, 0);
+            acc[b][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, lo, acc[b][e], 0, 0, 0);
+          }
+      } else {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int e = 0; e < VE; ++e)
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+              acc[b][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[j][b][e]), x[0][j], acc[b][e], 0, 0, 0);
+      }
+      load_v(row);
+      valid = next_valid;
+    }
+    sum = over_groups(sum, true);
+  }
+
+  // acc[b][e][i]: head n, value (16 b + 4 g + i) VE + e
+  auto finish = [&](int head, int d, float* o, float top, float total) {  // 4 values from d
+    const int64_t rh = (int64_t)r * a.q_heads + h0 + head;
+    if (a.splits > 1) {
+      *(f32x4*)(a.part_o + (rh * a.splits + split) * D + d) = f32x4{o[0], o[1], o[2], o[3]};
+      if (d == 0) a.part_s[rh * a.splits + split] = make_float2(top, total);
+      return;
+    }
+    const float norm = total > 0.f ? 1.f / total : total == 0.f ? 0.f : total;
+    T y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = (T)(o[i] * norm);
+    __builtin_memcpy(__builtin_assume_aligned((T*)a.out + rh * D + d, 4 * sizeof(T)), y, sizeof y);
+    if (d == 0 && a.lse) a.lse[rh] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * (1.f / kL2E);
+  };
+  if constexpr (NW == 1) {
+    if (n >= nh) return;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < VE; e += 4) {
+          const int d = (16 * b + 4 * g + i) * VE + e;
+          float o[4] = {acc[b][e][i], acc[b][e + 1][i], acc[b][e + 2][i], acc[b][e + 3][i]};
+          if (d < D) finish(n, d, o, m, sum);
+        }
+  } else {
+    if (g == 0) stat[wave * 16 + n] = make_float2(m, sum);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < VE; e += 4) {
+          const int d = (16 * b + 4 * g + i) * VE + e;
+          if (n < nh && d < DC)
+            *(f32x4*)&part[(wave * 16 + n) * LD + d] = f32x4{acc[b][e][i], acc[b][e + 1][i], acc[b][e + 2][i], acc[b][e + 3][i]};
+        }
+    __syncthreads();
+    for (int i = threadIdx.x; i < nh * (D / 4); i += NW * 64) {
+      const int head = i / (D / 4), d = i % (D / 4) * 4;
+      float top = -FLT_MAX, total = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < NW; ++w) top = fmaxf(top, stat[w * 16 + head].x);
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const float f = exp2_fast(stat[w * 16 + head].x - top);
+        const f32x4 x = *(const f32x4*)&part[(w * 16 + head) * LD + d];
+        total += f * stat[w * 16 + head].y;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] += f * x[j];
+      }
+      finish(head, d, o, top, total);
+    }
+  }
+}
+
+template <class T, int DC>
+hipError_t launch_attend_tiles(const AttendArgs& a, hipStream_t st) {
+  const dim3 grid((unsigned)a.R * a.c.heads * a.head_tiles * a.splits);
+  if (a.waves == 1)
+    cache_attend_tiles<T, DC, 1><<<grid, dim3(64), 0, st>>>(a);
+  else
+    cache_attend_tiles<T, DC, 4><<<grid, dim3(256), 0, st>>>(a);
+  return hipGetLastError();
+}
+
+template <class T>
+hipError_t launch_attend_dim(const AttendArgs& a, hipStream_t st) {
+  if (a.c.dim <= 64) return launch_attend_tiles<T, 64>(a, st);
+  if (a.c.dim <= 96) return launch_attend_tiles<T, 96>(a, st);
+  if (a.c.dim <= 128) return launch_attend_tiles<T, 128>(a, st);
+  if (a.c.dim <= 192) return launch_attend_tiles<T, 192>(a, st);
+  return launch_attend_tiles<T, 256>(a, st);
+}
+
+}  // namespace kb

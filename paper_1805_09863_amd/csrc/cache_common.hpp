@@ -45,6 +45,14 @@ struct AttendArgs {
   float* lse;  // nullable without weights
   const float* weight_in;
   float* weight_out;
+  // the launch: waves per workgroup, tiles of 16 query heads per key-value head, splits of `chunk` slots
+  int waves, head_tiles, chunk, splits;
+  // workspace: per row, query head and split the partial output (dim floats) and its (max, sum), in base 2
+  // (splits > 1); the scores in base 2, score_ld apart per row and query head (weight_out)
+  float* part_o;
+  float2* part_s;
+  float* scores;
+  int64_t score_ld;
 };
 
 struct EvictArgs {
