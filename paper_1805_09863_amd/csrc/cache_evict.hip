@@ -24,17 +24,14 @@ constexpr int kDigits = 2048, kCopies = 2;
 struct EvictKeys {
   const float* weight;
   const int32_t* position;
-  int first, recent, newest;
-  __device__ __forceinline__ uint32_t operator()(int t) const {
-    const float w = weight[t] + 0.f;  // -0 counts as 0
+  int lo, hi;  // protected: positions below lo or above hi
+  __device__ __forceinline__ uint32_t of(float w, int p) const {
+    w += 0.f;  // -0 counts as 0
     const uint32_t u = __float_as_uint(w);
-    uint32_t key = w != w ? 0 : (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-    if (position) {
-      const int p = position[t];
-      if (p < first || (recent > 0 && (long long)p > (long long)newest - recent)) key = 0xFFFFFFFFu;
-    }
-    return key;
+    const uint32_t key = w == w ? u ^ ((uint32_t)((int)u >> 31) | 0x80000000u) : 0;
+    return (p < lo) | (p > hi) ? 0xFFFFFFFFu : key;
   }
+  __device__ __forceinline__ uint32_t operator()(int t) const { return of(weight[t], position ? position[t] : lo); }
 };
 
 // Exclusive prefix sums over the workgroup; total: the whole sum.
@@ -63,11 +60,11 @@ __device__ __forceinline__ int scan(int x, int* wave_sums, int& total) {
 
 template <int T>
 __global__ __launch_bounds__(T) void cache_evict_select(EvictArgs a, int room) {
-  extern __shared__ uint32_t lds[];  // room keys, later a list of tail slots; room / 64 masks of kept slots
+  extern __shared__ __align__(16) uint32_t lds[];  // room keys, later a list of slots; room / 64 masks and counts of kept slots
   __shared__ __align__(16) int hist[kDigits * kCopies];
-  __shared__ int wsum[T / 64], wsum2[T / 64], pick[3];
+  __shared__ int wsum[T / 64], pick[3];
   const CacheView& c = a.c;
-  const int r = blockIdx.x / c.heads, h = blockIdx.x % c.heads, tid = threadIdx.x;
+  const int r = blockIdx.x / c.heads, h = blockIdx.x % c.heads, tid = threadIdx.x, lane = tid & 63;
   if (r >= rows_of(a.R, a.n_dev)) return;
   const int L = max(0, min(a.length[r], c.cap)), n = min(L, a.keep);
   int32_t* source = a.source + ((int64_t)r * c.heads + h) * a.keep;
@@ -77,9 +74,11 @@ __global__ __launch_bounds__(T) void cache_evict_select(EvictArgs a, int room) {
     return;
   }
   const int64_t at = ((int64_t)r * c.heads + h) * c.cap;
-  const EvictKeys key{a.weight + at, a.position ? a.position + at : nullptr, a.first, a.recent,
-                      a.newest ? a.newest[r] : 0};
+  // (first >= 0, so that a bound below every int32 protects the lowest one too)
+  const long long old = a.recent > 0 ? (long long)a.newest[r] - a.recent : INT_MAX;
+  const EvictKeys key{a.weight + at, a.position ? a.position + at : nullptr, a.first, (int)max(old, (long long)INT_MIN)};
   const bool held = L <= room;  // keys in LDS
+  const bool whole = (((uintptr_t)key.weight | (uintptr_t)key.position) & 15) == 0 && c.cap % 4 == 0;
 
   uint32_t top = 0, mask = 0;
   int need = n, same = L;  // of the `same` slots whose key agrees with top in the bits of mask, keep the lowest `need`
@@ -87,19 +86,70 @@ __global__ __launch_bounds__(T) void cache_evict_select(EvictArgs a, int room) {
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11;
     for (int i = tid * 4; i < kDigits * kCopies; i += T * 4) *(int4*)&hist[i] = make_int4(0, 0, 0, 0);
     __syncthreads();
-    for (int t = tid; t < L; t += T) {
-      const uint32_t x = held && pass > 0 ? lds[t] : key(t);
-      if (held && pass == 0) lds[t] = x;
-      if ((x & mask) == top) atomicAdd(&hist[(x >> shift & ((1u << width) - 1)) * kCopies + (tid & (kCopies - 1))], 1);
+    auto count_in = [&](uint32_t x) {
+      const bool in = (x & mask) == top;
+      const uint64_t ins = __ballot(in);
+      if (ins == 0) return;
+      const int digit = x >> shift & ((1 << width) - 1);
+      if (__popcll(ins) >= 48) {
+        const int one = __ffsll((unsigned long long)ins) - 1;
+        if (__ballot(in & (digit == __builtin_amdgcn_readlane(digit, one))) == ins) {  // equal digits: one adds
+          if (lane == one) atomicAdd(&hist[digit * kCopies], __popcll(ins));
+          return;
+        }
+      }
+      if (in) atomicAdd(&hist[digit * kCopies + (lane & (kCopies - 1))], 1);
+    };
+    if (held && pass > 0) {
+#pragma unroll 8
+      for (int t = tid; t < L; t += T) count_in(lds[t]);
+    } else if (held && whole) {
+      constexpr int U = T / 256;  // 16-byte loads in flight; the last may reach past L, not past the row
+      for (int t0 = tid * 4; t0 < L; t0 += U * T * 4) {
+        float4 w[U];
+        int4 p[U];
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+          const int t = min(t0 + j * T * 4, (L - 1) & ~3);
+          w[j] = *(const float4*)(key.weight + t);
+          p[j] = key.position ? *(const int4*)(key.position + t) : make_int4(key.lo, key.lo, key.lo, key.lo);
+        }
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+          const int t = t0 + j * T * 4;
+          if (t >= L) break;
+          const uint4 x = make_uint4(key.of(w[j].x, p[j].x), key.of(w[j].y, p[j].y), key.of(w[j].z, p[j].z),
+                                     key.of(w[j].w, p[j].w));
+          *(uint4*)&lds[t] = x;
+          count_in(x.x);
+          if (t + 1 < L) count_in(x.y);
+          if (t + 2 < L) count_in(x.z);
+          if (t + 3 < L) count_in(x.w);
+        }
+      }
+    } else {
+      constexpr int U = T / 64;  // loads in flight
+      for (int t0 = tid; t0 < L; t0 += U * T) {
+        uint32_t x[U];
+#pragma unroll
+        for (int j = 0; j < U; ++j) x[j] = key(min(t0 + j * T, L - 1));
+#pragma unroll
+        for (int j = 0; j < U; ++j)
+          if (t0 + j * T < L) {
+            if (held) lds[t0 + j * T] = x[j];
+            count_in(x[j]);
+          }
+      }
     }
     __syncthreads();
     // digits from the largest down, kDigits / T a thread
     constexpr int B = kDigits / T;
     const int d0 = kDigits - 1 - tid * B;
-    int count[B], mine = 0, all;
+    int copy[B * kCopies], count[B], mine = 0, all;
+    __builtin_memcpy(copy, __builtin_assume_aligned(&hist[(d0 - B + 1) * kCopies], 16), sizeof copy);
 #pragma unroll
     for (int j = 0; j < B; ++j) {
-      count[j] = hist[(d0 - j) * kCopies] + hist[(d0 - j) * kCopies + 1];
+      count[j] = copy[(B - 1 - j) * kCopies] + copy[(B - 1 - j) * kCopies + 1];
       mine += count[j];
     }
     int before = scan<T>(mine, wsum, all);
@@ -115,48 +165,72 @@ __global__ __launch_bounds__(T) void cache_evict_select(EvictArgs a, int room) {
   }
 
   if (held) {
-    // Each wave: a run of whole 64-slot strips.
+    // Each wave takes a run of whole 64-slot strips; what is uniform in it stays on the scalar unit.
     constexpr int W = T / 64;
-    const int lane = tid & 63, w = tid >> 6, strips = (L + 63) / 64;
-    const int s0 = (int)((long long)strips * w / W), s1 = (int)((long long)strips * (w + 1) / W);
-    uint64_t* kept = (uint64_t*)(lds + room);
-    const uint64_t below = (1ull << lane) - 1;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6), strips = (L + 63) / 64;
+    const int per = (strips + W - 1) / W, s0 = min(w * per, strips), s1 = min(s0 + per, strips);
+    uint64_t* kept = (uint64_t*)(lds + room);  // each strip's kept slots
+    int* before = (int*)(kept + room / 64);    // and their number in the strips before
+    auto key_at = [&](int t) { return lds[min(t, L - 1)] & mask; };
+    auto below = [](uint64_t m) {  // the lanes of m below this one
+      return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+    };
+
     int ties = 0;  // slots that agree with top, in the strips before
     if (same != need) {
-      for (int s = s0; s < s1; ++s) ties += __popcll(__ballot(s * 64 + lane < L && (lds[s * 64 + lane] & mask) == top));
+      for (int s = s0; s < s1; ++s) ties += __popcll(__ballot((s * 64 + lane < L) & (key_at(s * 64 + lane) == top)));
       int all;
-      const int before = scan<T>(lane == 0 ? ties : 0, wsum, all);
-      ties = __shfl(before, 0);
+      ties = __builtin_amdgcn_readfirstlane(scan<T>(lane == 0 ? ties : 0, wsum, all));
     }
-    int tail = 0, holes = 0;  // kept slots from n on, dropped ones below n
+    uint64_t mine = 0;  // lane j: strip s0 + j (a wave has at most 32)
+#pragma unroll 4
     for (int s = s0; s < s1; ++s) {
       const int t = s * 64 + lane;
-      const uint32_t x = t < L ? lds[t] & mask : 0;
-      const uint64_t tie = __ballot(t < L && x == top);
-      const bool stay = t < L && (x > top || (x == top && ties + __popcll(tie & below) < need));
-      ties += __popcll(tie);
-      const uint64_t m = __ballot(stay);
-      if (lane == 0) kept[s] = m;
-      tail += __popcll(__ballot(stay && t >= n));
-      holes += __popcll(__ballot(!stay && t < n));
+      const uint32_t x = key_at(t);
+      uint64_t m;
+      if (same == need) {
+        m = __ballot((t < L) & (x >= top));
+      } else {
+        const uint64_t tie = __ballot((t < L) & (x == top));
+        m = __ballot((t < L) & ((x > top) | ((x == top) & (ties + below(tie) < need))));
+        ties += __popcll(tie);
+      }
+      mine = lane == s - s0 ? m : mine;
     }
-    if (lane == 0) wsum[w] = tail, wsum2[w] = holes;
+    // scan<T>'s barriers also part the keys' last reads from the list that takes their place
+    int all;
+    const int s = s0 + lane, rank = scan<T>(__popcll(mine), wsum, all);
+    if (s < s1) kept[s] = mine, before[s] = rank;
     __syncthreads();
-    tail = holes = 0;
-    for (int i = 0; i < w; ++i) tail += wsum[i], holes += wsum2[i];
-    // the keys have been read: their place is the list's
-    for (int s = max(s0, n / 64); s < s1; ++s) {
-      const int t = s * 64 + lane;
-      const uint64_t from_n = s * 64 >= n ? ~0ull : ~0ull << (n - s * 64), m = kept[s] & from_n;
-      if (m >> lane & 1) lds[tail + __popcll(m & below)] = t;
-      tail += __popcll(m);
+    // The list of kept slots from n on, where the keys were: a slot's rank among the kept ones less
+    // that of slot n.  Then the places: the j-th dropped slot is t = j + the kept ones before it.
+    const int sn = n / 64;
+    const uint64_t low = (1ull << (n % 64)) - 1;
+    const int kept_below = before[sn] + __popcll(kept[sn] & low);
+    // (32 strips a wave: a lane a strip, bit by bit, 2,100 cycles at 1 slot in 16 kept against 9,500
+    // strip by strip; 8 strips a wave: strip by strip, 1,800 against 3,300)
+    if constexpr (T == 1024) {
+      if (s >= sn && s < s1) {
+        uint64_t m = s == sn ? mine & ~low : mine;
+        for (int i = s == sn ? 0 : rank - kept_below; m != 0; m &= m - 1)
+          lds[i++] = s * 64 + __ffsll((unsigned long long)m) - 1;
+      }
+    } else {
+      for (int z = max(s0, sn); z < s1; ++z) {
+        uint64_t m = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)mine, z - s0) |
+                     (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), z - s0) << 32;
+        const int first = z == sn ? 0 : __builtin_amdgcn_readlane(rank, z - s0) - kept_below;
+        if (z == sn) m &= ~low;
+        if (__builtin_amdgcn_inverse_ballot_w64(m)) lds[first + below(m)] = z * 64 + lane;
+      }
     }
     __syncthreads();
-    for (int s = s0; s < s1 && s * 64 < n; ++s) {
+    for (int s = w; s * 64 < n; s += W) {
       const int t = s * 64 + lane;
-      const uint64_t m = ~kept[s];  // ones at and after n belong to no place
-      if (t < n) source[t] = (m >> lane & 1) ? (int)lds[holes + __popcll(m & below)] : t;
-      holes += __popcll(m);
+      const uint64_t m = kept[s];
+      const bool stays = m >> lane & 1;
+      const int j = t - before[s] - __popcll(m & ((1ull << lane) - 1));
+      if (t < n) source[t] = stays ? t : (int)lds[j];
     }
     return;
   }
@@ -238,14 +312,14 @@ static hipError_t raise_lds_ceiling() {
   if (e != hipSuccess || dev < 0 || dev >= kMaxDevices) return e != hipSuccess ? e : hipErrorInvalidDevice;
   if (done[dev].load(std::memory_order_acquire)) return hipSuccess;
   e = hipFuncSetAttribute(reinterpret_cast<const void*>(&cache_evict_select<1024>),
-                          hipFuncAttributeMaxDynamicSharedMemorySize, kEvictLds * 4 + kEvictLds / 8);
+                          hipFuncAttributeMaxDynamicSharedMemorySize, kEvictLds * 4 + kEvictLds / 64 * 12);
   if (e == hipSuccess) done[dev].store(true, std::memory_order_release);
   return e;
 }
 
 hipError_t launch_cache_evict(int bf16, const EvictArgs& a, hipStream_t st) {
   const int room = min((a.c.cap + 63) / 64 * 64, kEvictLds);
-  const size_t lds = (size_t)room * 4 + room / 8;
+  const size_t lds = (size_t)room * 4 + room / 64 * 12;
   const dim3 grid(a.R * a.c.heads);
   if (room <= kEvictSmall) {
     cache_evict_select<256><<<grid, dim3(256), lds, st>>>(a, room);
