@@ -271,32 +271,34 @@ __global__ __launch_bounds__(T) void cache_evict_select(EvictArgs a, int room) {
   }
 }
 
-// Rows to their places: 16 lanes a row, 16 bytes of key and value each at a time.
+// Rows to their places: 16 lanes a row, 16 bytes of key and value each at a time.  A chain of
+// dependent loads (source, table, row) bounds it where few rows move.
 __global__ __launch_bounds__(256) void cache_evict_move(EvictArgs a, int units) {
   const CacheView& c = a.c;
-  const int r = blockIdx.x / c.heads, h = blockIdx.x % c.heads;
+  const int r = blockIdx.x / c.heads, h = blockIdx.x % c.heads, lane = threadIdx.x % 16;
   if (r >= rows_of(a.R, a.n_dev)) return;
-  const int n = min(max(0, min(a.length[r], c.cap)), a.keep);
+  const int places = min(a.keep, c.cap);
   const int64_t rh = (int64_t)r * c.heads + h;
   const int32_t *source = a.source + rh * a.keep, *from_t = c.table + (int64_t)r * c.max_pages,
                 *to_t = a.out_table + (int64_t)r * a.out_max_pages;
   const int64_t in = rh * c.cap, out = rh * ((int64_t)a.out_max_pages << c.log_ps);
   const uint4 *k = (const uint4*)c.k, *v = (const uint4*)c.v;
-  for (int i = blockIdx.y * 16 + threadIdx.x / 16; i < n; i += gridDim.y * 16) {
-    const int s = source[i];
-    const int from = cache_row(c, from_t, h, s), to = cache_row(c, to_t, h, i);
+  for (int i = blockIdx.y * 16 + threadIdx.x / 16; i < places; i += gridDim.y * 16) {
+    const int s = source[i], to = cache_row(c, to_t, h, i);
+    if (s < 0) break;
+    const int from = cache_row(c, from_t, h, s);
     if (from >= 0 && to >= 0 && from != to)
-      for (int u = threadIdx.x % 16; u < units; u += 16) {
+      for (int u = lane; u < units; u += 16) {
         const uint4 x = k[(int64_t)from * units + u], y = v[(int64_t)from * units + u];
         ((uint4*)c.k)[(int64_t)to * units + u] = x;
         ((uint4*)c.v)[(int64_t)to * units + u] = y;
       }
-    if (threadIdx.x % 16 == 0) {
+    if (lane == 0) {
       a.out_weight[out + i] = a.weight[in + s];
       if (a.position) a.out_position[out + i] = a.position[in + s];
     }
   }
-  if (h == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.out_length[r] = n;
+  if (h == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.out_length[r] = min(max(0, min(a.length[r], c.cap)), a.keep);
 }
 
 // A workgroup of 256 threads holds up to 2,048 keys: its passes are shorter than those of 1,024
@@ -330,8 +332,10 @@ hipError_t launch_cache_evict(int bf16, const EvictArgs& a, hipStream_t st) {
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int blocks = min(1024, (min(a.keep, a.c.cap) + 63) / 64);
-  cache_evict_move<<<dim3(a.R * a.c.heads, blocks), dim3(256), 0, st>>>(a, a.c.dim * (bf16 ? 2 : 4) / 16);
+  // 16 rows a workgroup at a time, and no more workgroups than the card starts in a few microseconds
+  // (512 heads of at most 512 places: 8 blocks each 8.2 us, 16 9.2, 32 13.4)
+  const int pairs = a.R * a.c.heads, blocks = min((min(a.keep, a.c.cap) + 15) / 16, max(1, 4096 / pairs));
+  cache_evict_move<<<dim3(pairs, blocks), dim3(256), 0, st>>>(a, a.c.dim * (bf16 ? 2 : 4) / 16);
   return hipGetLastError();
 }
 
