@@ -131,12 +131,12 @@ def _stream(stream, device: Optional[torch.device] = None) -> int:
     return stream.cuda_stream
 
 
-def _dtype_code(t: torch.Tensor) -> int:
+def _dtype_code(t: torch.Tensor, what: str = "h and W") -> int:
     if t.dtype == torch.float32:
         return KB_F32
     if t.dtype == torch.bfloat16:
         return KB_BF16
-    raise TypeError(f"h and W must be float32 or bfloat16, got {t.dtype}")
+    raise TypeError(f"{what} must be float32 or bfloat16, got {t.dtype}")
 
 
 def _need(t: torch.Tensor, name: str, dtype=None, dim=None, numel=None):
@@ -638,58 +638,83 @@ def beam_backtrace(S0: int, k: int, T: int, alpha: float, fin: tuple, hist_token
 
 
 # ---------------------------------------------------------------- attention cache
-def _same_device(dev, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != dev:
-            raise ValueError(f"{name} is on {t.device}, the cache on {dev}")
+# A step's calls take a few microseconds on the device: their tensors are
+# checked in one expression each, and the message is worked out only for one
+# that fails.
+def _refuse(t, name: str, dtype, numel: int, dev: int):
+    _need(t, name, dtype=dtype, numel=numel)
+    raise ValueError(f"{name} is on {t.device}, the cache on cuda:{dev}")
 
 
-class _on:
-    """The device of the call's tensors made current around it, where it is not."""
+def _ask(t, name: str, dtype, numel: int, dev: int) -> int:
+    """Address of a contiguous tensor of ``dtype`` with at least ``numel`` elements on GPU ``dev``."""
+    try:
+        if t.dtype is dtype and t.get_device() == dev and t.is_contiguous() and t.numel() >= numel:
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    return _refuse(t, name, dtype, numel, dev)
 
-    def __init__(self, dev):
-        self.guard = None if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
+
+class _stay:
+    """The current device is the call's."""
 
     def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
+        pass
 
     def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+        pass
 
 
-def _cache(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor) -> _Cache:
-    _need(k_cache, "k_cache", dim=4)
-    _need(v_cache, "v_cache", dtype=k_cache.dtype, dim=4)
-    _need(table, "table", dtype=torch.int32, dim=2)
-    if v_cache.shape != k_cache.shape:
-        raise ValueError("k_cache and v_cache must have the same shape")
-    _same_device(k_cache.device, v_cache=v_cache, table=table)
+_STAY = _stay()
+_device_now = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _around(dev: int):
+    """The tensors' device made current around a call, where it is not."""
+    return _STAY if _device_now() == dev else torch.cuda.device(dev)
+
+
+def _cache(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor):
+    """(kb_cache, GPU index, type, key-value heads, dim, slots of a sequence, sequences)."""
+    if not isinstance(k_cache, torch.Tensor) or not k_cache.is_cuda:
+        raise TypeError("k_cache must be a tensor on the GPU")
+    dtype, dev = k_cache.dtype, k_cache.get_device()
+    code = _dtype_code(k_cache, "k_cache")
+    kp = _ask(k_cache, "k_cache", dtype, 0, dev)
+    vp = _ask(v_cache, "v_cache", dtype, 0, dev)
+    tp = _ask(table, "table", torch.int32, 0, dev)
+    if k_cache.dim() != 4 or v_cache.shape != k_cache.shape:
+        raise ValueError("k_cache and v_cache must be pages x heads x page_size x dim, the same shape")
+    if table.dim() != 2:
+        raise ValueError("table must be seqs x max_pages")
     pages, heads, page_size, dim = k_cache.shape
     seqs, max_pages = table.shape
-    return _Cache(_dtype_code(k_cache), heads, dim, page_size, pages, seqs, max_pages, k_cache.data_ptr(),
-                  v_cache.data_ptr(), table.data_ptr())
+    return (_Cache(code, heads, dim, page_size, pages, seqs, max_pages, kp, vp, tp), dev, dtype, heads, dim,
+            max_pages * page_size, seqs)
 
 
-def _need_rows(t: torch.Tensor, name: str, dtype, R: int, heads: Optional[int], dim: int) -> int:
-    """R x heads x dim whose rows may lie apart (part of a wider projection); their distance in values."""
+def _ask_rows(t: torch.Tensor, name: str, dtype, R: int, heads: Optional[int], dim: int, dev: int):
+    """(address, distance of two rows in values, heads) of R x heads x dim whose rows may lie apart, as
+    parts of a wider projection's do."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a tensor on the GPU")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.dim() != 3 or t.shape[0] != R or t.shape[2] != dim or (heads is not None and t.shape[1] != heads):
-        raise ValueError(f"{name} must be {R} x {'heads' if heads is None else heads} x {dim}, "
-                         f"got {tuple(t.shape)}")
-    heads = t.shape[1]
-    st = t.stride()
-    if (dim > 1 and st[2] != 1) or (heads > 1 and st[1] != dim):
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, the cache on cuda:{dev}")
+    shape = t.shape
+    if len(shape) != 3 or shape[0] != R or shape[2] != dim or (heads is not None and shape[1] != heads):
+        raise ValueError(f"{name} must be {R} x {'heads' if heads is None else heads} x {dim}, got {tuple(shape)}")
+    heads = shape[1]
+    step, apart, one = t.stride()
+    if one != 1 or (heads > 1 and apart != dim):
         raise ValueError(f"{name}: the heads of a row must lie one after the other, without gaps")
     if R <= 1:
-        return heads * dim
-    if st[0] < heads * dim:
+        step = heads * dim
+    elif step < heads * dim:
         raise ValueError(f"{name}: rows must not overlap")
-    return st[0]
+    return t.data_ptr(), step, heads
 
 
 def cache_append(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, length: torch.Tensor,
@@ -710,49 +735,43 @@ def cache_append(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tens
     ``position`` (int32) and ``weight`` (float32), seqs x heads x slots, receive the new
     slots' ``pos`` and 0.  Returns the turned queries (``q_out``), None without ``q``.
     """
-    c = _cache(k_cache, v_cache, table)
-    dev = k_cache.device
-    _need(length, "length", dtype=torch.int32, dim=1)
-    R = length.shape[0]
-    k_stride = _need_rows(k, "k", k_cache.dtype, R, c.heads, c.dim)
-    v_stride = _need_rows(v, "v", k_cache.dtype, R, c.heads, c.dim)
+    c, dev, dtype, heads, dim, cap, seqs = _cache(k_cache, v_cache, table)
+    i32 = torch.int32
+    lp = _ask(length, "length", i32, 0, dev)
+    R = length.numel()
+    kp, k_stride, _ = _ask_rows(k, "k", dtype, R, heads, dim, dev)
+    vp, v_stride, _ = _ask_rows(v, "v", dtype, R, heads, dim, dev)
     q_heads = q_stride = rot = 0
+    qp = op = fp = None
     if q is not None:
-        q_stride = _need_rows(q, "q", k_cache.dtype, R, None, c.dim)
-        q_heads = q.shape[1]
+        qp, q_stride, q_heads = _ask_rows(q, "q", dtype, R, None, dim, dev)
         if q_out is None:
-            q_out = torch.empty((R, q_heads, c.dim), dtype=q.dtype, device=dev)
-        _need(q_out, "q_out", dtype=q.dtype, numel=R * q_heads * c.dim)
+            q_out = torch.empty((R, q_heads, dim), dtype=dtype, device=q.device)
+        op = _ask(q_out, "q_out", dtype, R * q_heads * dim, dev)
     elif q_out is not None:
         raise ValueError("q_out without q")
     if freq is not None:
-        _need(freq, "freq", dtype=torch.float64, dim=1)
-        rot = 2 * freq.shape[0]
-    if pos is not None:
-        _need(pos, "pos", dtype=torch.int32, numel=R)
-    if seq is not None:
-        _need(seq, "seq", dtype=torch.int32, numel=R)
-    if n_dev is not None:
-        _need(n_dev, "n_dev", dtype=torch.int32, numel=1)
-    slots = c.seqs * c.heads * c.max_pages * c.page_size
-    if position is not None:
-        _need(position, "position", dtype=torch.int32, numel=slots)
-    if weight is not None:
-        _need(weight, "weight", dtype=torch.float32, numel=slots)
-    _same_device(dev, length=length, k=k, v=v, q=q, q_out=q_out, freq=freq, pos=pos, seq=seq, n_dev=n_dev,
-                 position=position, weight=weight)
-    with _on(dev):
-        _check(lib().kb_cache_append(c, R, _ptr(n_dev), q_heads, _ptr(q), q_stride, _ptr(k), k_stride, _ptr(v),
-                                     v_stride, rot, int(interleaved), _ptr(pos), _ptr(freq), amplitude, _ptr(seq),
-                                     _ptr(length), _ptr(q_out), _ptr(position), _ptr(weight), _stream(stream, dev)))
+        fp = _ask(freq, "freq", torch.float64, 0, dev)
+        rot = 2 * freq.numel()
+    pp = None if pos is None else _ask(pos, "pos", i32, R, dev)
+    sp = None if seq is None else _ask(seq, "seq", i32, R, dev)
+    nd = None if n_dev is None else _ask(n_dev, "n_dev", i32, 1, dev)
+    at = None if position is None else _ask(position, "position", i32, seqs * heads * cap, dev)
+    wp = None if weight is None else _ask(weight, "weight", torch.float32, seqs * heads * cap, dev)
+    with _around(dev):
+        status = lib().kb_cache_append(c, R, nd, q_heads, qp, q_stride, kp, k_stride, vp, v_stride, rot,
+                                       1 if interleaved else 0, pp, fp, amplitude, sp, lp, op, at, wp,
+                                       _stream(stream, k_cache.device))
+    if status:
+        _check(status)
     return q_out
 
 
 def cache_attend_workspace_bytes(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, R: int,
                                  q_heads: int, max_len: Optional[int] = None, weights: bool = False) -> int:
-    c = _cache(k_cache, v_cache, table)
-    return int(lib().kb_cache_attend_workspace_bytes(c, R, q_heads, max_len or c.max_pages * c.page_size,
-                                                     int(weights)))
+    """Bytes that cache_attend's ``ws`` needs for R rows of q_heads heads (``weights``: with ``weight_out``)."""
+    c, _, _, _, _, cap, _ = _cache(k_cache, v_cache, table)
+    return int(lib().kb_cache_attend_workspace_bytes(c, R, q_heads, cap if max_len is None else max_len, int(weights)))
 
 
 def cache_attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor,
@@ -768,41 +787,37 @@ def cache_attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, 
     to the slots of the table.  ``lse`` (R x q_heads float32) receives the scores'
     log-sum-exp.  ``weight_out`` (seqs x heads x slots float32) receives ``weight_in``
     (zeros; may be the same tensor) plus each slot's probability, summed over the query
-    heads that share a key-value head: what cache_evict goes by.
+    heads that share a key-value head: what cache_evict goes by.  ``ws`` may supply a
+    workspace of at least ``cache_attend_workspace_bytes`` bytes.
     """
-    c = _cache(k_cache, v_cache, table)
-    dev = k_cache.device
-    _need(length, "length", dtype=torch.int32, dim=1)
-    R = length.shape[0]
-    q_stride = _need_rows(q, "q", k_cache.dtype, R, None, c.dim)
-    q_heads = q.shape[1]
+    c, dev, dtype, heads, dim, cap, seqs = _cache(k_cache, v_cache, table)
+    i32, f32 = torch.int32, torch.float32
+    lp = _ask(length, "length", i32, 0, dev)
+    R = length.numel()
+    qp, q_stride, q_heads = _ask_rows(q, "q", dtype, R, None, dim, dev)
     if out is None:
-        out = torch.empty((R, q_heads, c.dim), dtype=q.dtype, device=dev)
-    _need(out, "out", dtype=q.dtype, numel=R * q_heads * c.dim)
-    if lse is not None:
-        _need(lse, "lse", dtype=torch.float32, numel=R * q_heads)
-    if seq is not None:
-        _need(seq, "seq", dtype=torch.int32, numel=R)
-    if n_dev is not None:
-        _need(n_dev, "n_dev", dtype=torch.int32, numel=1)
-    cap = c.max_pages * c.page_size
-    for t, name in ((weight_in, "weight_in"), (weight_out, "weight_out")):
-        if t is not None:
-            _need(t, name, dtype=torch.float32, numel=c.seqs * c.heads * cap)
-    _same_device(dev, q=q, length=length, out=out, lse=lse, seq=seq, n_dev=n_dev, weight_in=weight_in,
-                 weight_out=weight_out, ws=ws)
-    max_len = cap if max_len is None else max_len
+        out = torch.empty((R, q_heads, dim), dtype=dtype, device=q.device)
+    op = _ask(out, "out", dtype, R * q_heads * dim, dev)
+    ep = None if lse is None else _ask(lse, "lse", f32, R * q_heads, dev)
+    sp = None if seq is None else _ask(seq, "seq", i32, R, dev)
+    nd = None if n_dev is None else _ask(n_dev, "n_dev", i32, 1, dev)
+    wi = None if weight_in is None else _ask(weight_in, "weight_in", f32, seqs * heads * cap, dev)
+    wo = None if weight_out is None else _ask(weight_out, "weight_out", f32, seqs * heads * cap, dev)
+    if max_len is None:
+        max_len = cap
     L = lib()
-    need = L.kb_cache_attend_workspace_bytes(c, R, q_heads, max_len, weight_out is not None)
+    need = L.kb_cache_attend_workspace_bytes(c, R, q_heads, max_len, 0 if wo is None else 1)
     if ws is None and need > 0:
-        ws = workspace(need, dev)
+        ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+    wp, ws_bytes = None, 0
     if ws is not None:
         _need_ws(ws, need)
-    with _on(dev):
-        _check(L.kb_cache_attend(c, R, _ptr(n_dev), q_heads, _ptr(q), q_stride,
-                                 c.dim ** -0.5 if scale is None else scale, _ptr(seq), _ptr(length), max_len,
-                                 _ptr(out), _ptr(lse), _ptr(weight_in), _ptr(weight_out), _ptr(ws),
-                                 0 if ws is None else ws.numel() * ws.element_size(), _stream(stream, dev)))
+        wp, ws_bytes = _ask(ws, "ws", ws.dtype, 0, dev), ws.numel() * ws.element_size()
+    with _around(dev):
+        status = L.kb_cache_attend(c, R, nd, q_heads, qp, q_stride, dim ** -0.5 if scale is None else scale, sp, lp,
+                                   max_len, op, ep, wi, wo, wp, ws_bytes, _stream(stream, k_cache.device))
+    if status:
+        _check(status)
     return out
 
 
@@ -819,46 +834,40 @@ def cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tenso
     the kept ones are put there.  ``out`` may supply the four results (position None where
     ``position`` is; length and, in place, weight and position may be the inputs).
     """
-    c = _cache(k_cache, v_cache, table)
-    dev = k_cache.device
-    _need(length, "length", dtype=torch.int32, dim=1)
-    R = length.shape[0]
-    slots = c.seqs * c.heads * c.max_pages * c.page_size
-    _need(weight, "weight", dtype=torch.float32, numel=slots)
-    if position is not None:
-        _need(position, "position", dtype=torch.int32, numel=slots)
-    if newest is not None:
-        _need(newest, "newest", dtype=torch.int32, numel=R)
-    if n_dev is not None:
-        _need(n_dev, "n_dev", dtype=torch.int32, numel=1)
+    c, dev, _, heads, _, cap, seqs = _cache(k_cache, v_cache, table)
+    i32, f32 = torch.int32, torch.float32
+    lp = _ask(length, "length", i32, 0, dev)
+    R = length.numel()
+    wp = _ask(weight, "weight", f32, seqs * heads * cap, dev)
+    pp = None if position is None else _ask(position, "position", i32, seqs * heads * cap, dev)
+    ne = None if newest is None else _ask(newest, "newest", i32, R, dev)
+    nd = None if n_dev is None else _ask(n_dev, "n_dev", i32, 1, dev)
     if out_table is None:
         out_table = table
-    _need(out_table, "out_table", dtype=torch.int32, dim=2)
-    if out_table.shape[0] < R:
-        raise ValueError(f"out_table has {out_table.shape[0]} rows, {R} needed")
+    tp = _ask(out_table, "out_table", i32, 0, dev)
+    if out_table.dim() != 2 or out_table.shape[0] < R:
+        raise ValueError(f"out_table must have at least {R} rows of pages, got {tuple(out_table.shape)}")
     out_pages = out_table.shape[1]
-    kept = R * c.heads * out_pages * c.page_size
+    out_cap = out_pages * c.page_size
     if out is None:
-        shape = (R, c.heads, out_pages * c.page_size)
-        out = (torch.empty(R, dtype=torch.int32, device=dev), torch.zeros(shape, device=dev),
-               None if position is None else torch.full(shape, -1, dtype=torch.int32, device=dev),
-               torch.empty((R, c.heads, max(keep, 0)), dtype=torch.int32, device=dev))
+        at = k_cache.device
+        shape = (R, heads, out_cap)
+        out = (torch.empty(R, dtype=i32, device=at), torch.zeros(shape, device=at),
+               None if position is None else torch.full(shape, -1, dtype=i32, device=at),
+               torch.empty((R, heads, max(keep, 0)), dtype=i32, device=at))
     if len(out) != 4:
         raise ValueError("out must hold 4 tensors (length, weight, position, source)")
     out_length, out_weight, out_position, source = out
-    _need(out_length, "out length", dtype=torch.int32, numel=R)
-    _need(out_weight, "out weight", dtype=torch.float32, numel=kept)
-    if out_position is not None:
-        _need(out_position, "out position", dtype=torch.int32, numel=kept)
-    _need(source, "source", dtype=torch.int32, numel=R * c.heads * keep)
-    _same_device(dev, length=length, weight=weight, position=position, newest=newest, n_dev=n_dev,
-                 out_table=out_table, out_length=out_length, out_weight=out_weight, out_position=out_position,
-                 source=source)
-    with _on(dev):
-        _check(lib().kb_cache_evict(c, R, _ptr(n_dev), _ptr(length), keep, first, recent, _ptr(newest), _ptr(weight),
-                                    _ptr(position), _ptr(out_table), out_pages, _ptr(out_length), _ptr(out_weight),
-                                    _ptr(out_position), _ptr(source), _stream(stream, dev)))
-    return out_length, out_weight, out_position, source
+    olp = _ask(out_length, "out length", i32, R, dev)
+    owp = _ask(out_weight, "out weight", f32, R * heads * out_cap, dev)
+    opp = None if out_position is None else _ask(out_position, "out position", i32, R * heads * out_cap, dev)
+    sp = _ask(source, "source", i32, R * heads * keep, dev)
+    with _around(dev):
+        status = lib().kb_cache_evict(c, R, nd, lp, keep, first, recent, ne, wp, pp, tp, out_pages, olp, owp, opp, sp,
+                                      _stream(stream, k_cache.device))
+    if status:
+        _check(status)
+    return out
 
 
 def rotary_frequencies(rot_dim: int, *, base: float = 10000.0, factor: float = 1.0,
