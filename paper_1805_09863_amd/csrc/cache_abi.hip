@@ -79,10 +79,20 @@ AttendPlan attend_plan(const kb_cache* c, int R, int q_heads, int max_len, bool 
   max_len = std::min(max_len, c->max_pages * c->page_size);
   const int group = q_heads / c->heads;
   p.head_tiles = (group + 15) / 16;
+  // A unit is a row's slots for 16 query heads.  Where units fill the card and are at most 64 slots long,
+  // one wave takes each (640 rows x 8 heads of 60 slots: 14.2 us, four waves 37.6), else four take its
+  // tiles in turn (5 x 16 of 60: 4.8 us, one wave 6.6).
   const long long units = (long long)R * c->heads * p.head_tiles;
-  p.waves = max_len <= 64 ? 1 : 4;
-  const long long even = ((long long)max_len * units + 2047) / 2048;
-  p.chunk = (int)std::min<long long>(std::max<long long>((even + 127) / 128 * 128, 256), 1024);
+  p.waves = max_len <= 64 && units >= 1024 ? 1 : 4;
+  // Splits cost the join's launch, so up to 512 slots there is one (4 rows x 8 heads of 300: 7.4 us, two
+  // splits 9.4).  Beyond, a split is 256 to 1,024 slots, for 2,048 workgroups at the bound of the
+  // lengths: rows that are shorter than it have fewer, and the longest row's last split ends the call
+  // (64 x 8 of up to 8,192: 90 us at 512 and 1,024 slots, 98 at 256, 94 at 2,048; 17 x 5 of up to 3,001
+  // in float32: 24 us at 256, 32 at 512).  One row's length is mostly its bound: 512 workgroups
+  // (131,072 slots: 97 us, 106 with 2,048).
+  const long long workgroups = R == 1 ? 512 : 2048, most = R == 1 ? 2048 : 1024;
+  const long long even = ((long long)max_len * units + workgroups - 1) / workgroups;
+  p.chunk = max_len <= 512 ? max_len : (int)std::min(std::max((even + 127) / 128 * 128, 256LL), most);
   p.splits = (max_len + p.chunk - 1) / p.chunk;
   const size_t rh = (size_t)R * q_heads;
   if (p.splits > 1) {
@@ -175,6 +185,8 @@ kb_status kb_cache_attend(const kb_cache* cache, int R, const int32_t* n_dev, in
   char* ws = static_cast<char*>(workspace);
   kb::AttendArgs a{view(cache), R,      q_heads, max_len, n_dev, q,         q_stride,
                    scale,       seq, length,  out,     lse,   weight_in, weight_out};
+  // no length counts where there is nothing to attend to
+  a.max_len = cache->pages == 0 || cache->seqs == 0 ? 0 : std::min(max_len, cache->max_pages * cache->page_size);
   a.waves = p.waves;
   a.head_tiles = p.head_tiles;
   a.chunk = p.chunk;

@@ -55,7 +55,7 @@ __device__ __forceinline__ float over_groups(float x, bool sum) {
 // One (row, key-value head, 16 query heads, run of slots): NW waves, tiles in turn.
 // DC: dim rounded up to a built size.
 template <class T, int DC, int NW>
-__global__ __launch_bounds__(NW * 64, DC * sizeof(T) <= 256 ? 2 : 1) void cache_attend_tiles(AttendArgs a) {
+__global__ __launch_bounds__(NW * 64, DC * sizeof(T) > 256 ? 1 : NW == 1 ? 3 : 2) void cache_attend_tiles(AttendArgs a) {
   constexpr bool kBf16 = sizeof(T) == 2;
   constexpr int TS = AttendTile<T>::kSlots, NH = TS / 16;   // slots of a tile, 16-slot blocks
   constexpr int NI = DC * (int)sizeof(T) / 64;              // 64-byte pieces of a key
@@ -70,18 +70,26 @@ __global__ __launch_bounds__(NW * 64, DC * sizeof(T) <= 256 ? 2 : 1) void cache_
   const CacheView& c = a.c;
   const int lane = threadIdx.x & 63, wave = NW > 1 ? threadIdx.x >> 6 : 0;
   const int n = lane & 15, g = lane >> 4;  // operand row or column, group of the summed index
-  const int split = blockIdx.x % a.splits, unit = blockIdx.x / a.splits;
+  // All units' first splits, then all second ones: short rows have no later splits, and workgroups go
+  // to the XCDs in turn, so the splits of a unit side by side would leave some XCDs without work.
+  const int units = a.R * c.heads * a.head_tiles;
+  const int split = blockIdx.x / units, unit = blockIdx.x - split * units;
   const int ht = unit % a.head_tiles, kv = unit / a.head_tiles % c.heads, r = unit / a.head_tiles / c.heads;
   if (r >= rows_of(a.R, a.n_dev)) return;
   const int group = a.q_heads / c.heads, h0 = kv * group + ht * 16, nh = min(16, group - ht * 16);
   const int s = cache_seq(c, a.seq, r);
-  const int len = s < 0 || c.pages == 0 ? 0 : max(0, min(a.length[r], min(a.max_len, c.cap)));
-  const int begin = split * a.chunk, end = min(len, begin + a.chunk);
-  if (a.splits > 1 && begin >= end) return;  // the join knows from the length which splits there are
+  const int32_t* pages = c.table + (int64_t)max(s, 0) * c.max_pages;
+  // The pages of the first two tiles are asked for before the length is known: they, the length and the
+  // queries arrive in one round trip.
+  const int begin = split * a.chunk, first = begin + wave * TS, step = NW * TS;
+  const int tl = lane & (TS - 1);  // the slot of a tile whose page this lane looks up
+  auto page_of = [&](int t0) { return pages[min(t0 + tl, a.max_len - 1) >> c.log_ps]; };
+  int page = -1, next_page = -1;
+  if (a.max_len > 0) page = page_of(first), next_page = page_of(first + step);
+  const int len = s < 0 ? 0 : max(0, min(a.length[r], a.max_len)), end = min(len, begin + a.chunk);
 
   const int D = c.dim, last = D * (int)sizeof(T) / 16 - 1, vlast = D / VE - 1;
   const int row_bytes = D * (int)sizeof(T);
-  const int32_t* pages = c.table + (int64_t)max(s, 0) * c.max_pages;
 
   uint4 q[NI];
   int koff[NI], voff[NB];
@@ -97,6 +105,8 @@ __global__ __launch_bounds__(NW * 64, DC * sizeof(T) <= 256 ? 2 : 1) void cache_
 #pragma unroll
   for (int b = 0; b < NB; ++b) voff[b] = min(b * 16 + n, vlast) * VW * 4;
 
+  if (a.splits > 1 && begin >= end) return;  // the join knows from the length which splits there are
+
   const float scale2 = a.scale * kL2E;
   float m = -FLT_MAX, sum = 0.f;
   f32x4 acc[NB][VE];
@@ -105,16 +115,13 @@ __global__ __launch_bounds__(NW * 64, DC * sizeof(T) <= 256 ? 2 : 1) void cache_
 #pragma unroll
     for (int e = 0; e < VE; ++e) acc[b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  const int first = begin + wave * TS, step = NW * TS;
   if (first < end) {
     uint4 kr[NH][NI];
     uint32_t vr[NV][NB][VW];
     uint32_t valid;
-    const int tl = lane & (TS - 1);  // the slot of a tile whose page this lane looks up
-    auto page_of = [&](int t0) { return t0 + tl < end ? pages[(t0 + tl) >> c.log_ps] : -1; };
     // this lane's slot as a row of the cache; a hole's or one past the end: some row of the pool
     auto row_at = [&](int page, int t0, uint32_t& ok) {
-      const bool there = (uint32_t)page < (uint32_t)c.pages;
+      const bool there = t0 + tl < end && (uint32_t)page < (uint32_t)c.pages;
       ok = (uint32_t)__ballot(there) & (uint32_t)((1ull << TS) - 1);
       return there ? ((page * c.heads + kv) << c.log_ps) + ((t0 + tl) & ((1 << c.log_ps) - 1)) : 0;
     };
@@ -134,8 +141,7 @@ __global__ __launch_bounds__(NW * 64, DC * sizeof(T) <= 256 ? 2 : 1) void cache_
         for (int b = 0; b < NB; ++b) __builtin_memcpy(vr[j][b], __builtin_assume_aligned(p + voff[b], VW * 4), VW * 4);
       }
     };
-    int row = row_at(page_of(first), first, valid);
-    int next_page = page_of(first + step);
+    int row = row_at(page, first, valid);
     load_k(row);
     load_v(row);
 
@@ -161,12 +167,15 @@ __global__ __launch_bounds__(NW * 64, DC * sizeof(T) <= 256 ? 2 : 1) void cache_
           }
         }
       }
-      // the next tile's keys are asked for as soon as this one's registers are free, its values
-      // further down: one of the two is always on its way
+      // The next tile's keys are asked for as soon as this one's registers are free, its values further
+      // down: one of the two is always on its way.  Past the last tile they are a row of the pool again:
+      // a branch around the loads would have the other half wait for them.  A lone wave has few tiles
+      // and is better off without (640 rows of at most 60 slots: 14.2 us, 14.9 with them).
       uint32_t next_valid;
       row = row_at(next_page, t0 + step, next_valid);
       next_page = page_of(t0 + 2 * step);
-      load_k(row);
+      const bool more = NW > 1 || t0 + step < end;
+      if (more) load_k(row);
 
       const bool whole = valid == (uint32_t)((1ull << TS) - 1);
       float top = m;
@@ -237,7 +246,7 @@ __global__ __launch_bounds__(NW * 64, DC * sizeof(T) <= 256 ? 2 : 1) void cache_
             for (int j = 0; j < NV; ++j)
               acc[b][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[j][b][e]), x[0][j], acc[b][e], 0, 0, 0);
       }
-      load_v(row);
+      if (more) load_v(row);
       valid = next_valid;
     }
     sum = over_groups(sum, true);
@@ -303,11 +312,11 @@ __global__ __launch_bounds__(NW * 64, DC * sizeof(T) <= 256 ? 2 : 1) void cache_
 
 template <class T, int DC>
 hipError_t launch_attend_tiles(const AttendArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)a.R * a.c.heads * a.head_tiles * a.splits);
+  const unsigned cells = (unsigned)a.R * a.c.heads * a.head_tiles * a.splits;
   if (a.waves == 1)
-    cache_attend_tiles<T, DC, 1><<<grid, dim3(64), 0, st>>>(a);
+    cache_attend_tiles<T, DC, 1><<<dim3(cells), dim3(64), 0, st>>>(a);
   else
-    cache_attend_tiles<T, DC, 4><<<grid, dim3(256), 0, st>>>(a);
+    cache_attend_tiles<T, DC, 4><<<dim3(cells), dim3(256), 0, st>>>(a);
   return hipGetLastError();
 }
 
