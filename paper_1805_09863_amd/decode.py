@@ -2,9 +2,10 @@
 finished hypotheses (Section 2.1, Algorithm 2) and the naive constant batch
 (Algorithm 1).
 
-The decoder RNN is not part of this library: each row's state h for step t
-comes from a device table indexed by (sentence, step, beam slot), standing in
-for the decoder.  Every output-layer step (projection, fused softmax/k-best,
+The paper's decoder RNN is not part of this library: each row's state h for
+step t comes from a device table indexed by (sentence, step, beam slot),
+standing in for the decoder, or from a decoder that attends to its own past
+(decoder.CachedDecoder).  Every output-layer step (projection, fused softmax/k-best,
 beam merge) and every compaction and state gather runs in libkbest's kernels;
 the decoder stand-in's bookkeeping (EOS mask of the schedule, next states)
 runs in its own small kernels (include/kbest_standin.h).
@@ -18,6 +19,7 @@ from typing import Callable, Optional
 import torch
 
 from . import binding as kbb
+from .decoder import CachedDecoder
 
 
 def _poll_tag(cn, tag: int):
@@ -219,13 +221,85 @@ class BeamSearchResult:
     rows: list = field(default_factory=list)   # live rows decoded at each step
 
 
-def beam_search(h_table: torch.Tensor, W: torch.Tensor, b: torch.Tensor, k: int, T: int, eos: int, *,
-                alpha: float = 0.0, on_step: Optional[Callable] = None, stream=None) -> BeamSearchResult:
+def _check_decoder(decoder: CachedDecoder, W: torch.Tensor, start: torch.Tensor):
+    kbb._need(start, "start", dtype=torch.int32, dim=1, numel=1)
+    if decoder.H != W.shape[0] or decoder.embed.shape[0] < W.shape[1] or decoder.embed.dtype != W.dtype:
+        raise ValueError("the decoder's states, words or type are not those of W")
+    if decoder.embed.device != W.device or start.device != W.device:
+        raise ValueError("decoder, start and W must be on one device")
+    if int(start.min()) < 0 or int(start.max()) >= decoder.embed.shape[0]:
+        raise ValueError("start holds tokens that the decoder has no embedding of")
+
+
+class _TableStates:
+    """beam_search's next states from the table of the decoder stand-in."""
+
+    def __init__(self, h_table: torch.Tensor, k: int, T: int, S0: int, stream):
+        self.table, self.k, self.T, self.S0, self.stream = h_table, k, T, S0, stream
+        self.dtype, self.H, self.device = h_table.dtype, h_table.shape[1], h_table.device
+
+    def first(self, out):
+        i32 = dict(dtype=torch.int32, device=self.device)
+        kbb.standin_next_h(self.table, torch.arange(self.S0, **i32) * self.k, torch.arange(self.S0, **i32), self.k,
+                           self.T, 0, self.S0, out=out, stream=self.stream)
+
+    def next(self, t, rows, n_dev, tok, par, keep, sid, out):
+        kbb.standin_next_h(self.table, keep, sid, self.k, self.T, t, rows, n_dev=n_dev, out=out, stream=self.stream)
+
+
+class _CachedStates:
+    """beam_search's next states from a decoder with an attention cache.
+
+    Pages of one slot: the token that row i decodes at step t has page t * M0 + i, so a
+    continuation shares its parent's past by a copy of the parent's row of the table, and no
+    key or value moves.  Rows are sized by the step's upper bound and counted on the device."""
+
+    def __init__(self, decoder: CachedDecoder, start: torch.Tensor, k: int, T: int, stream):
+        self.decoder, self.start, self.stream = decoder, start, stream
+        self.dtype, self.H, self.device = decoder.embed.dtype, decoder.H, decoder.embed.device
+        self.M0 = M0 = start.numel() * k
+        i32 = dict(dtype=torch.int32, device=self.device)
+        self.kv = decoder.cache(T * M0, 1)
+        self.table, self.table_nx = (torch.zeros((M0, T), **i32) for _ in range(2))
+        self.rows = torch.arange(M0, **i32)
+        # rows past a step's count hold stale tokens and parents: always valid ones
+        self.tok, self.par = torch.zeros(M0, **i32), torch.zeros(M0, **i32)
+        self.pos, self.length = torch.zeros(M0, **i32), torch.ones(M0, **i32)
+
+    def _step(self, t, rows, n_dev, out):
+        self.table[:rows, t] = self.rows[:rows] + t * self.M0
+        self.decoder.step(self.tok[:rows], self.pos[:rows], self.length[:rows], *self.kv, self.table, max_len=t + 1,
+                          n_dev=n_dev, out=out[:rows])
+
+    def first(self, out):
+        with torch.cuda.stream(self.stream):
+            n = self.start.numel()
+            self.tok[:n] = self.start
+            self._step(0, n, None, out)
+
+    def next(self, t, rows, n_dev, tok, par, keep, sid, out):
+        with torch.cuda.stream(self.stream):
+            gather = dict(n_dev=n_dev, n_max=rows, stream=self.stream)
+            kbb.gather_rows(tok[:rows].view(rows, 1), keep, out=self.tok.view(-1, 1), **gather)
+            kbb.gather_rows(par[:rows].view(rows, 1), keep, out=self.par.view(-1, 1), **gather)
+            kbb.gather_rows(self.table, self.par, out=self.table_nx, **gather)
+            self.table, self.table_nx = self.table_nx, self.table
+            self.pos.fill_(t)
+            self.length.fill_(t + 1)
+            self._step(t, rows, n_dev, out)
+
+
+def beam_search(h_table: Optional[torch.Tensor], W: torch.Tensor, b: torch.Tensor, k: int, T: int, eos: int, *,
+                alpha: float = 0.0, decoder: Optional[CachedDecoder] = None, start: Optional[torch.Tensor] = None,
+                on_step: Optional[Callable] = None, stream=None) -> BeamSearchResult:
     """Beam search with per-hypothesis end of sentence (Section 2.1, Algorithm 2).
 
     ``h_table`` is (S0*T*k) x H on the device: row (s*T + t)*k + r is the state
     of the hypothesis in slot r (its rank in the sentence's beam) of sentence s
-    at step t, the decoder stand-in.  Every sentence starts from one hypothesis
+    at step t, the decoder stand-in.  With ``decoder`` (h_table None) the states are
+    its: every sentence starts from the token ``start[s]`` (int32, on the GPU), and a
+    hypothesis attends to its own tokens so far, which hypotheses of one sentence share
+    in the attention cache.  Every sentence starts from one hypothesis
     (slot 0, score 0) with a beam of k.  Each step: the output layer
     (kb_kbest_step), kb_beam_finish (history, finished store, beam shrink),
     kb_compact_beams, the gathers of the surviving scores, sentence ids and
@@ -239,11 +313,20 @@ def beam_search(h_table: torch.Tensor, W: torch.Tensor, b: torch.Tensor, k: int,
     """
     dev = W.device
     H, V = W.shape
-    S0 = h_table.shape[0] // (T * k)
-    if h_table.shape[0] != S0 * T * k or S0 == 0:
-        raise ValueError("h_table must hold S0 * T * k rows")
+    if (h_table is None) == (decoder is None):
+        raise ValueError("either h_table or decoder gives the states")
     if stream is None:
         stream = torch.cuda.current_stream(dev)
+    if decoder is None:
+        S0 = h_table.shape[0] // (T * k)
+        if h_table.shape[0] != S0 * T * k or S0 == 0:
+            raise ValueError("h_table must hold S0 * T * k rows")
+        states = _TableStates(h_table, k, T, S0, stream)
+    else:
+        _check_decoder(decoder, W, start)
+        S0 = start.numel()
+        with torch.cuda.stream(stream):
+            states = _CachedStates(decoder, start, k, T, stream)
     M0 = S0 * k
     i32 = dict(dtype=torch.int32, device=dev)
     dt = kbb._dtype_code(W)
@@ -252,7 +335,7 @@ def beam_search(h_table: torch.Tensor, W: torch.Tensor, b: torch.Tensor, k: int,
     tok = torch.empty(M0, **i32)
     par = torch.empty(M0, **i32)
     sc = torch.empty(M0, dtype=torch.float32, device=dev)
-    h_cur = torch.empty((M0, H), dtype=h_table.dtype, device=dev)
+    h_cur = torch.empty((M0, H), dtype=states.dtype, device=dev)
     alive = torch.empty(M0, dtype=torch.uint8, device=dev)
     keep = [torch.empty(M0, **i32), torch.empty(M0, **i32)]
     cnt = torch.empty(2, **i32)
@@ -268,9 +351,8 @@ def beam_search(h_table: torch.Tensor, W: torch.Tensor, b: torch.Tensor, k: int,
     off = torch.arange(S0 + 1, **i32)                  # one row per sentence at the start
     cnt_host = torch.empty(2, dtype=torch.int32, pin_memory=True)
     ready = torch.cuda.Event()
-    # step 0's states: slot 0 of every sentence
-    kbb.standin_next_h(h_table, torch.arange(S0, **i32) * k, torch.arange(S0, **i32), k, T, 0, S0, out=h_cur,
-                       stream=stream)
+    # step 0's states: one hypothesis of every sentence
+    states.first(h_cur)
     out = BeamSearchResult(None, None, None, None)
     S, N, t, cur, prev_base = S0, S0, 0, 0, 0
     while S > 0 and t < T:
@@ -298,7 +380,7 @@ def beam_search(h_table: torch.Tensor, W: torch.Tensor, b: torch.Tensor, k: int,
         kbb.gather_rows(beam[:S].view(S, 1), ksent, n_dev=cnt[1:2], n_max=S, out=beam_nx.view(S0, 1),
                         stream=stream)
         if t + 1 < T:
-            kbb.standin_next_h(h_table, keep[cur], sid, k, T, t + 1, S * k, n_dev=cnt[0:1], out=h_cur, stream=stream)
+            states.next(t + 1, S * k, cnt[0:1], tok, par, keep[cur], sid, h_cur)
         _wait(ready)                                   # the step's one host sync
         N, S = (int(x) for x in cnt_host.tolist())
         prev, prev_nx = prev_nx, prev
@@ -314,3 +396,76 @@ def beam_search(h_table: torch.Tensor, W: torch.Tensor, b: torch.Tensor, k: int,
     out.fin = fin
     out.hist = (hist_tok, hist_par)
     return out
+
+
+@dataclass
+class GreedyResult:
+    tokens: torch.Tensor      # S0 x T int32: each sentence's tokens, EOS included, then -1
+    length: torch.Tensor      # S0 int32
+    steps: int = 0
+    evictions: int = 0
+
+
+def greedy_search(decoder: CachedDecoder, W: torch.Tensor, b: torch.Tensor, start: torch.Tensor, T: int, eos: int, *,
+                  keep: Optional[int] = None, first: int = 1, recent: Optional[int] = None, every: int = 16,
+                  page_size: int = 16, on_step: Optional[Callable] = None, stream=None) -> GreedyResult:
+    """Greedy decoding (Algorithm 5) of a constant batch (Algorithm 1) with a decoder that
+    attends to its own past: each step appends the last tokens to the cache, attends
+    (decoder.step) and takes the best word of every row (kb_argmax_step), until every
+    sentence has produced ``eos`` or has T tokens.
+
+    ``keep``: the cache of a sentence is held to a budget.  Whenever it has ``every`` more
+    slots than that, it goes back to ``keep`` (kb_cache_evict): the ``first`` and the
+    ``recent`` (by default keep // 2) newest tokens stay, and those of the others that
+    have received most attention.
+
+    ``on_step(t, state)`` is called after each step's attention with a dict of its device
+    tensors.
+    """
+    dev = W.device
+    H, V = W.shape
+    _check_decoder(decoder, W, start)
+    if T < 1 or every < 1 or (keep is not None and keep < 1):
+        raise ValueError(f"T = {T}, keep = {keep}, every = {every}")
+    if recent is None:
+        recent = 0 if keep is None else min(keep // 2, max(keep - first, 0))
+    if stream is None:
+        stream = torch.cuda.current_stream(dev)
+    S0 = start.numel()
+    i32 = dict(dtype=torch.int32, device=dev)
+    most = T if keep is None else min(T, keep + every)
+    cols = -(-most // page_size)
+    with torch.cuda.stream(stream):
+        kv = decoder.cache(S0 * cols, page_size)
+        table = torch.arange(S0 * cols, **i32).view(S0, cols)
+        length, pos, tok = torch.zeros(S0, **i32), torch.full((S0,), -1, **i32), start.clone()
+        tokens, ended = torch.full((S0, T), -1, **i32), torch.zeros(S0, dtype=torch.bool, device=dev)
+        position = weight = evicted = None
+        if keep is not None:
+            position = torch.zeros((S0, decoder.kv_heads, cols * page_size), **i32)
+            weight = torch.zeros((S0, decoder.kv_heads, cols * page_size), device=dev)
+            evicted = (length, weight, position, torch.empty((S0, decoder.kv_heads, keep), **i32))
+        ws = kbb.workspace(kbb.argmax_workspace_bytes(kbb._dtype_code(W), S0, H, V), dev)
+        logit = torch.empty(S0, dtype=torch.float32, device=dev)
+        slots, res = 0, GreedyResult(tokens, None)
+        for t in range(T):
+            if keep is not None and slots == keep + every:
+                kbb.cache_evict(*kv, table, length, keep, weight=weight, position=position, newest=pos, first=first,
+                                recent=recent, out=evicted, stream=stream)
+                slots = keep
+                res.evictions += 1
+            length += 1
+            pos += 1
+            slots += 1
+            h = decoder.step(tok, pos, length, *kv, table, max_len=slots, position=position, weight=weight)
+            kbb.argmax_step(h, W, b, out=(tok, logit), ws=ws, stream=stream)
+            if on_step is not None:
+                on_step(t, dict(h=h, k=kv[0], v=kv[1], table=table, length=length, pos=pos, token=tok, slots=slots,
+                                position=position, weight=weight))
+            tokens[:, t] = torch.where(ended, -1, tok)
+            ended |= tok == eos
+            res.steps = t + 1
+            if bool(ended.all()):                          # the step's one host sync
+                break
+        res.length = (tokens >= 0).sum(1).to(torch.int32)
+    return res

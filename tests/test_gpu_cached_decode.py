@@ -1,0 +1,173 @@
+"""The decode loops over a decoder with an attention cache (decoder.CachedDecoder): beam search whose
+hypotheses share their past through page tables, greedy search with and without a budget.
+
+Float64 recomputation of the decoder from its weights, whole sequences at once, without any cache; a
+step's log-probabilities hold to the output layer's float32 tolerance of 1e-4 (tests/gpu_util.py), a
+sequence's to that times its length.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache_oracle as co
+from tests.gpu_util import TOL
+
+pytestmark = pytest.mark.gpu
+H, V, Q, KV, D = 64, 500, 4, 2, 16
+EOS = 3
+
+
+@pytest.fixture(scope="module")
+def kb():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_1805_09863_amd as kb
+    kb.lib()
+    return kb
+
+
+def make(dtype=torch.float32, seed=0, eos_bias=1.5):
+    from paper_1805_09863_amd.decoder import CachedDecoder
+    g = torch.Generator().manual_seed(seed)
+    r = lambda *s: torch.randn(s, generator=g)  # noqa: E731
+    embed, Wqkv, Wo = r(V, H), r(H, (Q + 2 * KV) * D) * 1.5 / H ** 0.5, r(Q * D, H) / (Q * D) ** 0.5
+    W, b = r(H, V) * 1.2 / H ** 0.5, (torch.rand(V, generator=g) - 0.5) * 0.2
+    b[EOS] += eos_bias
+    dec = CachedDecoder(embed.to(dtype).cuda(), Wqkv.to(dtype).cuda(), Wo.to(dtype).cuda(), Q, KV)
+    return dec, W.to(dtype).cuda(), b.cuda()
+
+
+def f64(t):
+    return t.detach().cpu().double().numpy()
+
+
+def states(dec, tokens):
+    """h of every position of one sequence of tokens, in float64."""
+    embed, Wqkv, Wo, freq = f64(dec.embed), f64(dec.Wqkv), f64(dec.Wo), f64(dec.freq)
+    x = embed[tokens]
+    qkv = (x @ Wqkv).reshape(len(tokens), Q + 2 * KV, D)
+    turned = np.stack([[co.rotate(qkv[t, h], t, freq, False, 1.0) for h in range(Q + KV)] for t in range(len(tokens))])
+    out = np.zeros((len(tokens), Q, D))
+    for t in range(len(tokens)):
+        for h in range(Q):
+            kv = h // (Q // KV)
+            s = turned[:t + 1, Q + kv] @ turned[t, h] * D ** -0.5
+            p = np.exp(s - s.max())
+            out[t, h] = p / p.sum() @ qkv[:t + 1, Q + KV + kv]
+    return x + out.reshape(len(tokens), -1) @ Wo
+
+
+def log_probs(h, W, b):
+    x = h @ f64(W) + f64(b)
+    m = x.max(-1, keepdims=True)
+    return x - m - np.log(np.exp(x - m).sum(-1, keepdims=True))
+
+
+@pytest.mark.parametrize("k,T", [(1, 12), (4, 20), (7, 9)])
+def test_beam_search_scores_are_the_sequences(kb, k, T):
+    """Each translation's score is the sum of its tokens' log-probabilities, the decoder run over it as a whole: a
+    hypothesis that had attended to another's tokens, or at another position, would not have it."""
+    from paper_1805_09863_amd.decode import beam_search
+    dec, W, b = make(seed=k)
+    start = torch.tensor([5, 9, 5, 77, 0], dtype=torch.int32, device="cuda")
+    res = beam_search(None, W, b, k, T, EOS, decoder=dec, start=start, alpha=0.6)
+    torch.cuda.synchronize()
+    for s in range(len(start)):
+        n = int(res.length[s])
+        tok = res.tokens[s, :n].tolist()
+        assert n >= 1 and (tok[-1] == EOS or n == T) and EOS not in tok[:-1]
+        lp = log_probs(states(dec, [int(start[s])] + tok[:-1]), W, b)
+        score = sum(lp[i, w] for i, w in enumerate(tok))
+        assert abs(score - float(res.score[s])) <= TOL["f32"] * n
+    assert torch.equal(res.tokens[0], res.tokens[2])       # the same start, the same search
+    assert res.steps > 2 and (k == 1 or len(set(res.rows)) > 1)
+
+
+def test_beam_search_on_a_stream_and_in_bf16(kb):
+    from paper_1805_09863_amd.decode import beam_search
+    dec, W, b = make(torch.bfloat16, seed=3)
+    start = torch.tensor([5, 9, 11], dtype=torch.int32, device="cuda")
+    a = beam_search(None, W, b, 3, 15, EOS, decoder=dec, start=start)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    c = beam_search(None, W, b, 3, 15, EOS, decoder=dec, start=start, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(a.tokens, c.tokens) and torch.equal(a.score, c.score)
+    assert torch.all(a.length >= 1) and torch.all(torch.isfinite(a.score))
+
+
+def test_greedy_search_is_beam_one(kb):
+    """Greedy tokens are those of a beam of one and the best words of the recomputed states; a budget that is never
+    reached changes nothing."""
+    from paper_1805_09863_amd.decode import beam_search, greedy_search
+    dec, W, b = make(seed=8)
+    start = torch.tensor([1, 2, 4, 8, 16, 32], dtype=torch.int32, device="cuda")
+    T = 25
+    a = greedy_search(dec, W, b, start, T, EOS)
+    c = beam_search(None, W, b, 1, T, EOS, decoder=dec, start=start)
+    d = greedy_search(dec, W, b, start, T, EOS, keep=T, page_size=1)
+    assert torch.equal(a.tokens, c.tokens) and torch.equal(a.length, c.length)
+    assert torch.equal(a.tokens, d.tokens) and d.evictions == 0
+    for s in range(len(start)):
+        tok = a.tokens[s, :int(a.length[s])].tolist()
+        lp = log_probs(states(dec, [int(start[s])] + tok[:-1]), W, b)
+        for i, w in enumerate(tok):
+            assert lp[i, w] >= lp[i].max() - 2 * TOL["f32"]
+
+
+def test_greedy_search_within_a_budget(kb):
+    """Every step's states from the cache as it is then, in float64; the first and the newest tokens are in it, no
+    position twice, and its length stays within the budget and what is added between evictions."""
+    from paper_1805_09863_amd.decode import greedy_search
+    dec, W, b = make(seed=9, eos_bias=-4.0)
+    embed, Wqkv, Wo, freq = f64(dec.embed), f64(dec.Wqkv), f64(dec.Wo), f64(dec.freq)
+    start = torch.tensor([7, 8, 9], dtype=torch.int32, device="cuda")
+    last = [start.tolist()]
+    keep, every, first, recent, page, T = 20, 7, 2, 6, 8, 90
+    lengths = []
+
+    def on_step(t, st):
+        n = st["length"].tolist()
+        assert n == [st["slots"]] * 3 and st["pos"].tolist() == [t] * 3
+        lengths.append(n[0])
+        x = embed[last[0]]
+        q = (x @ Wqkv).reshape(3, -1, D)[:, :Q]
+        q = np.stack([[co.rotate(q[s, h], t, freq, False, 1.0) for h in range(Q)] for s in range(3)])
+        # the cache of this step is whole: the new token's keys and values are in it, nothing was evicted since
+        out = co.attend(q, f64(st["k"]), f64(st["v"]), st["table"].cpu().numpy(), np.array(n), D ** -0.5)[0]
+        err = np.abs(x + out.reshape(3, -1) @ Wo - f64(st["h"])).max()
+        assert err <= TOL["f32"], f"step {t}: {err}"
+        where = st["position"].cpu().numpy()
+        for s in range(3):
+            for h in range(KV):
+                there = where[s, h, :n[s]].tolist()
+                assert len(set(there)) == n[s] and max(there) == t
+                assert set(range(min(first, t + 1))) <= set(there)
+                assert set(range(max(0, t + 1 - recent), t + 1)) <= set(there)
+        last[0] = st["token"].tolist()
+
+    res = greedy_search(dec, W, b, start, T, EOS, keep=keep, every=every, first=first, recent=recent, page_size=page,
+                        on_step=on_step)
+    assert res.steps == T and res.evictions > 5
+    assert max(lengths) == keep + every and lengths[-1] < T
+
+
+def test_refusals(kb):
+    from paper_1805_09863_amd.decode import beam_search, greedy_search
+    from paper_1805_09863_amd.decoder import CachedDecoder
+    dec, W, b = make()
+    start = torch.tensor([1], dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        beam_search(None, W, b, 2, 5, EOS)
+    with pytest.raises(TypeError):
+        beam_search(None, W, b, 2, 5, EOS, decoder=dec)
+    with pytest.raises(ValueError):
+        beam_search(None, W[:32].contiguous(), b, 2, 5, EOS, decoder=dec, start=start)
+    with pytest.raises(ValueError):
+        greedy_search(dec, W, b, start + V, 5, EOS)
+    with pytest.raises(ValueError):
+        greedy_search(dec, W, b, start, 5, EOS, keep=0)
+    with pytest.raises(ValueError):
+        CachedDecoder(dec.embed, dec.Wqkv, dec.Wo, 3, 2)
+    with pytest.raises(ValueError):
+        CachedDecoder(dec.embed, dec.Wqkv[:, :-1].contiguous(), dec.Wo, Q, KV)
