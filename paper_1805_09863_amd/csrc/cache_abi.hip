@@ -70,8 +70,8 @@ kb_status check_count(int R, int q_heads) {
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 struct AttendPlan {
-  int waves, head_tiles, chunk, splits;
-  size_t score_ld, part_o, part_s, scores, lse, bytes;  // workspace offsets
+  int waves, head_tiles, chunk, splits, shares;
+  size_t score_ld, part_o, part_s, row_before, scores, lse, bytes;  // workspace offsets
 };
 
 AttendPlan attend_plan(const kb_cache* c, int R, int q_heads, int max_len, bool weights) {
@@ -84,20 +84,20 @@ AttendPlan attend_plan(const kb_cache* c, int R, int q_heads, int max_len, bool 
   // tiles in turn (5 x 16 of 60: 4.8 us, one wave 6.6).
   const long long units = (long long)R * c->heads * p.head_tiles;
   p.waves = max_len <= 64 && units >= 1024 ? 1 : 4;
-  // Splits cost the join's launch, so up to 512 slots there is one (4 rows x 8 heads of 300: 7.4 us, two
-  // splits 9.4).  Beyond, a split is 256 to 1,024 slots, for 2,048 workgroups at the bound of the
-  // lengths: rows that are shorter than it have fewer, and the longest row's last split ends the call
-  // (64 x 8 of up to 8,192: 90 us at 512 and 1,024 slots, 98 at 256, 94 at 2,048; 17 x 5 of up to 3,001
-  // in float32: 24 us at 256, 32 at 512).  One row's length is mostly its bound: 512 workgroups
-  // (131,072 slots: 97 us, 106 with 2,048).
-  const long long workgroups = R == 1 ? 512 : 2048, most = R == 1 ? 2048 : 1024;
-  const long long even = ((long long)max_len * units + workgroups - 1) / workgroups;
-  p.chunk = max_len <= 512 ? max_len : (int)std::min(std::max((even + 127) / 128 * 128, 256LL), most);
+  // More than 512 slots are shared out: 256 workgroups take equal parts of all rows (64 x 8 of up to 8,192:
+  // 77 us, splits of 1,024 slots 94; 128 x 8 of 4,096: 376, splits 396; one row of 131,072: 99 either way;
+  // 512 workgroups 79, 375 and 100).  Up to 512, where the join's launch would cost more than it gives (4 x
+  // 8 of 300: 8.3 us, shared out 11.5), each row is one workgroup's; and with more rows than the shares'
+  // kernel can add up, splits of 1,024 slots are.
+  p.shares = max_len > 512 && R <= kb::kShareRows ? 256 : 0;
+  p.chunk = p.shares > 0 || max_len <= 512 ? max_len : 1024;
   p.splits = (max_len + p.chunk - 1) / p.chunk;
   const size_t rh = (size_t)R * q_heads;
-  if (p.splits > 1) {
-    p.part_s = align_up(rh * p.splits * c->dim * sizeof(float), 256);
-    p.bytes = align_up(p.part_s + rh * p.splits * sizeof(float2), 256);
+  const size_t parts = p.shares > 0 ? (size_t)p.shares * 2 * 16 : p.splits > 1 ? rh * p.splits : 0;
+  if (parts > 0) {
+    p.part_s = align_up(parts * c->dim * sizeof(float), 256);
+    p.row_before = align_up(p.part_s + parts * sizeof(float2), 256);
+    p.bytes = align_up(p.row_before + (p.shares > 0 ? ((size_t)R + 1) * sizeof(int) : 0), 256);
   }
   if (weights) {
     p.score_ld = align_up(max_len, 32);
@@ -191,9 +191,11 @@ kb_status kb_cache_attend(const kb_cache* cache, int R, const int32_t* n_dev, in
   a.head_tiles = p.head_tiles;
   a.chunk = p.chunk;
   a.splits = p.splits;
-  if (p.splits > 1) {
+  a.shares = a.max_len > 0 ? p.shares : 0;
+  if (p.splits > 1 || p.shares > 0) {
     a.part_o = reinterpret_cast<float*>(ws + p.part_o);
     a.part_s = reinterpret_cast<float2*>(ws + p.part_s);
+    a.row_before = reinterpret_cast<int*>(ws + p.row_before);
   }
   if (weight_out) {
     a.scores = reinterpret_cast<float*>(ws + p.scores);
