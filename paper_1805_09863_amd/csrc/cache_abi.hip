@@ -84,13 +84,14 @@ AttendPlan attend_plan(const kb_cache* c, int R, int q_heads, int max_len, bool 
   // tiles in turn (5 x 16 of 60: 4.8 us, one wave 6.6).
   const long long units = (long long)R * c->heads * p.head_tiles;
   p.waves = max_len <= 64 && units >= 1024 ? 1 : 4;
-  // More than 512 slots are shared out: 256 workgroups take equal parts of all rows (64 x 8 of up to 8,192:
-  // 77 us, splits of 1,024 slots 94; 128 x 8 of 4,096: 376, splits 396; one row of 131,072: 99 either way;
-  // 512 workgroups 79, 375 and 100).  Up to 512, where the join's launch would cost more than it gives (4 x
-  // 8 of 300: 8.3 us, shared out 11.5), each row is one workgroup's; and with more rows than the shares'
-  // kernel can add up, splits of 1,024 slots are.
-  p.shares = max_len > 512 && R <= kb::kShareRows ? 256 : 0;
-  p.chunk = p.shares > 0 || max_len <= 512 ? max_len : 1024;
+  // Beyond 6 steps of the four waves the slots are shared out: 256 workgroups take equal parts of all rows
+  // (64 x 8 of up to 8,192: 77 us, splits of 1,024 slots 94; 128 x 8 of 4,096: 376, splits 396; one row of
+  // 131,072: 99 either way; 512 workgroups 79, 375 and 100).  Up to there, where the join's launch would cost
+  // more than it gives (4 x 8 of 300: 7.4 us, shared out 11.5; 1 x 8 of 600: 9.7 and 11.2), each row is one
+  // workgroup's; and with more rows than the shares' kernel can add up, splits of 1,024 slots are.
+  const int step = c->dtype == KB_BF16 ? 128 : 64;
+  p.shares = max_len > 6 * step && R <= kb::kShareRows ? 256 : 0;
+  p.chunk = p.shares > 0 ? max_len : std::min(max_len, R <= kb::kShareRows ? 6 * step : 1024);
   p.splits = (max_len + p.chunk - 1) / p.chunk;
   const size_t rh = (size_t)R * q_heads;
   const size_t parts = p.shares > 0 ? (size_t)p.shares * 2 * 16 : p.splits > 1 ? rh * p.splits : 0;

@@ -62,6 +62,7 @@ struct AttendRun {
   static constexpr int VE = kBf16 && DC > 64 ? 8 : 4;             // values of a slot that a lane holds side by side
   static constexpr int NB = (DC + 16 * VE - 1) / (16 * VE);       // such runs of 16 lanes in a row
   static constexpr int VW = VE * (int)sizeof(T) / 4;              // words of them
+  typedef uint32_t Words __attribute__((ext_vector_type(VW)));
   static constexpr int NV = TS / 4;                               // slots of a tile that a lane takes values of
   static constexpr int LD = DC + 4;
   static constexpr int kStep = NW * TS;                           // slots that the waves take at a time
@@ -91,30 +92,30 @@ struct AttendRun {
     const int row_bytes = D * (int)sizeof(T);
 
     uint4 q[NI];
-    int koff[NI], voff[NB];
-  #pragma unroll
+    int voff[NB];
+    const int g16 = g * 16, last16 = last * 16;  // past the head's end: its last piece again, times zeros
+#pragma unroll
     for (int i = 0; i < NI; ++i) {
       q[i] = make_uint4(0, 0, 0, 0);
-      koff[i] = min(4 * i + g, last) * 16;  // past the head's end: its last piece again, times zeros
       if (n < nh && 4 * i + g <= last) {
         const T* p = (const T*)a.q + r * a.q_stride + (int64_t)(h0 + n) * D + (4 * i + g) * (16 / (int)sizeof(T));
         __builtin_memcpy(&q[i], __builtin_assume_aligned(p, sizeof(T)), 16);
       }
     }
-  #pragma unroll
+#pragma unroll
     for (int b = 0; b < NB; ++b) voff[b] = min(b * 16 + n, vlast) * VW * 4;
 
     const float scale2 = a.scale * kL2E;
     float m = -FLT_MAX, sum = 0.f;
     f32x4 acc[NB][VE];
-  #pragma unroll
+#pragma unroll
     for (int b = 0; b < NB; ++b)
-  #pragma unroll
+#pragma unroll
       for (int e = 0; e < VE; ++e) acc[b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
 
     if (first < end) {
       uint4 kr[NH][NI];
-      uint32_t vr[NV][NB][VW];
+      Words vr[NV][NB];
       uint32_t valid;
       // this lane's slot as a row of the cache; a hole's or one past the end: some row of the pool
       auto row_at = [&](int page, int t0, uint32_t& ok) {
@@ -123,19 +124,19 @@ struct AttendRun {
         return there ? ((page * c.heads + kv) << c.log_ps) + ((t0 + tl) & ((1 << c.log_ps) - 1)) : 0;
       };
       auto load_k = [&](int row) {
-  #pragma unroll
+#pragma unroll
         for (int hf = 0; hf < NH; ++hf) {
           const char* p = (const char*)c.k + (int64_t)__shfl(row, hf * 16 + n) * row_bytes;
-  #pragma unroll
-          for (int i = 0; i < NI; ++i) kr[hf][i] = *(const uint4*)(p + koff[i]);
+#pragma unroll
+          for (int i = 0; i < NI; ++i) kr[hf][i] = *(const uint4*)(p + min(4 * i * 16 + g16, last16));
         }
       };
       auto load_v = [&](int row) {
-  #pragma unroll
+#pragma unroll
         for (int j = 0; j < NV; ++j) {
           const char* p = (const char*)c.v + (int64_t)__shfl(row, (j >> 2) * 16 + g * 4 + (j & 3)) * row_bytes;
-  #pragma unroll
-          for (int b = 0; b < NB; ++b) __builtin_memcpy(vr[j][b], __builtin_assume_aligned(p + voff[b], VW * 4), VW * 4);
+#pragma unroll
+          for (int b = 0; b < NB; ++b) vr[j][b] = *(const Words*)(p + voff[b]);
         }
       };
       int row = row_at(page, first, valid);
@@ -145,10 +146,10 @@ struct AttendRun {
       for (int t0 = first; t0 < end; t0 += step) {
         // scores: x[hf][i] is head n, slot t0 + 16 hf + 4 g + i
         f32x4 x[NH];
-  #pragma unroll
+#pragma unroll
         for (int hf = 0; hf < NH; ++hf) {
           x[hf] = f32x4{0.f, 0.f, 0.f, 0.f};
-  #pragma unroll
+#pragma unroll
           for (int i = 0; i < NI; ++i) {
             if constexpr (kBf16) {
               bf16x8 ka, qb;
@@ -159,7 +160,7 @@ struct AttendRun {
               float ka[4], qb[4];
               __builtin_memcpy(ka, &kr[hf][i], 16);
               __builtin_memcpy(qb, &q[i], 16);
-  #pragma unroll
+#pragma unroll
               for (int e = 0; e < 4; ++e) x[hf] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka[e], qb[e], x[hf], 0, 0, 0);
             }
           }
@@ -176,9 +177,9 @@ struct AttendRun {
 
         const bool whole = valid == (uint32_t)((1ull << TS) - 1);
         float top = m;
-  #pragma unroll
+#pragma unroll
         for (int hf = 0; hf < NH; ++hf)
-  #pragma unroll
+#pragma unroll
           for (int i = 0; i < 4; ++i) {
             x[hf][i] *= scale2;
             if (!whole && !(valid >> (hf * 16 + g * 4 + i) & 1)) x[hf][i] = -INFINITY;
@@ -186,47 +187,46 @@ struct AttendRun {
           }
         if (a.scores && n < nh) {
           float* to = a.scores + ((int64_t)r * a.q_heads + h0 + n) * a.score_ld + t0 + g * 4;
-  #pragma unroll
+#pragma unroll
           for (int hf = 0; hf < NH; ++hf) *(f32x4*)(to + hf * 16) = x[hf];
         }
         top = over_groups(top, false);
         const float keep = exp2_fast(m - top);
         m = top;
         sum *= keep;
-  #pragma unroll
+#pragma unroll
         for (int hf = 0; hf < NH; ++hf)
-  #pragma unroll
+#pragma unroll
           for (int i = 0; i < 4; ++i) {
             x[hf][i] = exp2_fast(x[hf][i] - top);
             sum += x[hf][i];
           }
-  #pragma unroll
+#pragma unroll
         for (int b = 0; b < NB; ++b)
-  #pragma unroll
+#pragma unroll
           for (int e = 0; e < VE; ++e) acc[b][e] *= keep;
 
         if (!whole) {  // a probability of 0 times whatever lies there
-  #pragma unroll
-          for (int j = 0; j < NV; ++j)
-            if (!(valid >> ((j >> 2) * 16 + g * 4 + (j & 3)) & 1))
-  #pragma unroll
-              for (int b = 0; b < NB; ++b)
-  #pragma unroll
-                for (int w = 0; w < VW; ++w) vr[j][b][w] = 0;
+#pragma unroll
+          for (int j = 0; j < NV; ++j) {
+            const uint32_t there = 0u - (valid >> ((j >> 2) * 16 + g * 4 + (j & 3)) & 1);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) vr[j][b] &= there;
+          }
         }
         if constexpr (kBf16) {
           bf16x8 hi, lo;
-  #pragma unroll
+#pragma unroll
           for (int j = 0; j < 8; ++j) {
             hi[j] = (__bf16)x[j >> 2][j & 3];
             lo[j] = (__bf16)(x[j >> 2][j & 3] - (float)hi[j]);
           }
-  #pragma unroll
+#pragma unroll
           for (int b = 0; b < NB; ++b)
-  #pragma unroll
+#pragma unroll
             for (int e = 0; e < VE; ++e) {
               uint32_t w[4];
-  #pragma unroll
+#pragma unroll
               for (int j = 0; j < 4; ++j)
                 w[j] = __builtin_amdgcn_perm(vr[2 * j + 1][b][e / 2], vr[2 * j][b][e / 2], e % 2 ? 0x07060302 : 0x05040100);
               bf16x8 va;
@@ -235,11 +235,11 @@ struct AttendRun {
               acc[b][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, lo, acc[b][e], 0, 0, 0);
             }
         } else {
-  #pragma unroll
+#pragma unroll
           for (int b = 0; b < NB; ++b)
-  #pragma unroll
+#pragma unroll
             for (int e = 0; e < VE; ++e)
-  #pragma unroll
+#pragma unroll
               for (int j = 0; j < NV; ++j)
                 acc[b][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[j][b][e]), x[0][j], acc[b][e], 0, 0, 0);
         }
@@ -260,18 +260,18 @@ struct AttendRun {
       const int64_t rh = (int64_t)r * a.q_heads + h0 + head;
       const float norm = total > 0.f ? 1.f / total : total == 0.f ? 0.f : total;
       T y[4];
-  #pragma unroll
+#pragma unroll
       for (int i = 0; i < 4; ++i) y[i] = (T)(o[i] * norm);
       __builtin_memcpy(__builtin_assume_aligned((T*)a.out + rh * D + d, 4 * sizeof(T)), y, sizeof y);
       if (d == 0 && a.lse) a.lse[rh] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * (1.f / kL2E);
     };
     if constexpr (NW == 1) {
       if (n >= nh) return;
-  #pragma unroll
+#pragma unroll
       for (int b = 0; b < NB; ++b)
-  #pragma unroll
+#pragma unroll
         for (int i = 0; i < 4; ++i)
-  #pragma unroll
+#pragma unroll
           for (int e = 0; e < VE; e += 4) {
             const int d = (16 * b + 4 * g + i) * VE + e;
             float o[4] = {acc[b][e][i], acc[b][e + 1][i], acc[b][e + 2][i], acc[b][e + 3][i]};
@@ -282,11 +282,11 @@ struct AttendRun {
       float2* stat = lds.stat;
       __syncthreads();  // the run before has been read
       if (g == 0) stat[wave * 16 + n] = make_float2(m, sum);
-  #pragma unroll
+#pragma unroll
       for (int b = 0; b < NB; ++b)
-  #pragma unroll
+#pragma unroll
         for (int i = 0; i < 4; ++i)
-  #pragma unroll
+#pragma unroll
           for (int e = 0; e < VE; e += 4) {
             const int d = (16 * b + 4 * g + i) * VE + e;
             if (n < nh && d < DC)
@@ -296,14 +296,14 @@ struct AttendRun {
       for (int i = threadIdx.x; i < nh * (D / 4); i += NW * 64) {
         const int head = i / (D / 4), d = i % (D / 4) * 4;
         float top = -FLT_MAX, total = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  #pragma unroll
+#pragma unroll
         for (int w = 0; w < NW; ++w) top = fmaxf(top, stat[w * 16 + head].x);
-  #pragma unroll
+#pragma unroll
         for (int w = 0; w < NW; ++w) {
           const float f = exp2_fast(stat[w * 16 + head].x - top);
           const f32x4 x = *(const f32x4*)&part[(w * 16 + head) * LD + d];
           total += f * stat[w * 16 + head].y;
-  #pragma unroll
+#pragma unroll
           for (int j = 0; j < 4; ++j) o[j] += f * x[j];
         }
         finish(head, d, o, top, total);
@@ -312,7 +312,7 @@ struct AttendRun {
   }
 };
 
-// A row's splits of a.chunk slots each a workgroup (NW = 1: a wave) of their own.
+// A row's splits of a.chunk slots each a workgroup of their own; NW = 1: a wave for a whole row.
 template <class T, int DC, int NW>
 __global__ __launch_bounds__(NW * 64, DC * sizeof(T) > 256 ? 1 : NW == 1 ? 3 : 2) void cache_attend_splits(AttendArgs a) {
   using Run = AttendRun<T, DC, NW>;
@@ -320,7 +320,8 @@ __global__ __launch_bounds__(NW * 64, DC * sizeof(T) > 256 ? 1 : NW == 1 ? 3 : 2
   const CacheView& c = a.c;
   // All units' first splits, then all second ones: short rows have no later splits, and workgroups go
   // to the XCDs in turn, so the splits of a unit side by side would leave some XCDs without work.
-  const int units = a.R * c.heads * a.head_tiles, split = blockIdx.x / units, unit = blockIdx.x - split * units;
+  const int units = a.R * c.heads * a.head_tiles, split = NW == 1 ? 0 : blockIdx.x / units;
+  const int unit = blockIdx.x - split * units;
   const int ht = unit % a.head_tiles, kv = unit / a.head_tiles % c.heads, r = unit / a.head_tiles / c.heads;
   if (r >= rows_of(a.R, a.n_dev)) return;
   const int s = cache_seq(c, a.seq, r);
@@ -332,8 +333,12 @@ __global__ __launch_bounds__(NW * 64, DC * sizeof(T) > 256 ? 1 : NW == 1 ? 3 : 2
   if (a.max_len > 0) page = Run::page_of(a, pages, first), next_page = Run::page_of(a, pages, first + Run::kStep);
   const int len = s < 0 ? 0 : max(0, min(a.length[r], a.max_len)), end = min(len, begin + a.chunk);
   if (a.splits > 1 && begin >= end) return;  // the join knows from the length which splits there are
-  const int64_t rh = (int64_t)r * a.q_heads + kv * (a.q_heads / c.heads) + ht * 16;
-  Run::run(a, lds, pages, r, kv, ht, begin, end, page, next_page, a.splits > 1 ? rh * a.splits + split : -1, a.splits);
+  if constexpr (NW == 1) {
+    Run::run(a, lds, pages, r, kv, ht, 0, len, page, next_page, -1, 0);
+  } else {
+    const int64_t rh = (int64_t)r * a.q_heads + kv * (a.q_heads / c.heads) + ht * 16;
+    Run::run(a, lds, pages, r, kv, ht, begin, end, page, next_page, a.splits > 1 ? rh * a.splits + split : -1, a.splits);
+  }
 }
 
 // Equal shares of all rows' slots: see AttendShares (cache_common.hpp).

@@ -157,6 +157,38 @@ def test_attend_long(kb, dtype, R, q_heads, heads, dim, page, length):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("R,q_heads,heads,dim,page,most,long", [
+    (60, 40, 2, 64, 16, 2000, 8),      # cut rows and whole ones, empty ones among them, two tiles of query heads
+    (300, 3, 3, 24, 1, 40, 1),         # one long row among short ones
+    (1024, 2, 1, 16, 8, 30, 3),        # as many rows as shares take
+    (1030, 2, 1, 16, 8, 30, 3),        # more: splits
+    (520, 4, 2, 128, 4, 60, 0),        # many short rows: a wave each
+    (520, 6, 2, 80, 1, 60, 0),
+])
+def test_attend_batches(kb, dtype, R, q_heads, heads, dim, page, most, long):
+    """Batches of very different lengths, rows from the device's count on left alone."""
+    g = torch.Generator().manual_seed(R + most)
+    n = torch.randint(0, most + 1, (R,), generator=g).to(torch.int32)
+    at = torch.randperm(R, generator=g)[:long]
+    n[at] = torch.randint(900, 2500, (long,), generator=g).to(torch.int32)
+    cap = int(n.max())
+    k, v, table = make_cache(g, dtype, R, heads, dim, page, cap, spare=0, dirty=R < 100)
+    if R < 100:
+        fill(g, k, v, table, n)
+    q = torch.randn((R, q_heads, dim), generator=g).to(dtype)
+    out, lse, _ = check_attend(kb, q, k, v, table, n)
+    part = torch.full_like(out, 5)
+    part_lse = torch.full_like(lse, 5)
+    count = R * 2 // 3
+    kb.cache_attend(q.cuda(), k.cuda(), v.cuda(), table.cuda(), n.cuda(), out=part, lse=part_lse,
+                    n_dev=torch.tensor([count], dtype=torch.int32, device="cuda"))
+    assert torch.all(part[count:] == 5) and torch.all(part_lse[count:] == 5)
+    # the count moves the shares' ends, and with them where a row's sums are joined
+    near = 2 * (int(n.max()) * U + 2.0 ** -16) * float(v.float().abs().max()) + ROUND[dtype] * float(out.abs().max()) * 2
+    assert float((part[:count].float() - out[:count].float()).abs().max()) <= near
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("page", [1, 16, 64])
 def test_attend_holes(kb, dtype, page):
     """Pages outside the pool at the start, in the middle, at the end and everywhere; lengths past the table."""
