@@ -24,7 +24,9 @@
  *  - Keys and values that no slot of a row's length refers to may hold
  *    anything, NaN and infinities included.
  *  - Results do not depend on the order in which workgroups run: no
- *    floating-point atomics.
+ *    floating-point atomics.  The same call gives the same bits; in
+ *    kb_cache_attend a row's last bits may differ with the lengths of the
+ *    other rows, which move the places where its sums are cut and joined.
  */
 #ifndef KBEST_CACHE_H
 #define KBEST_CACHE_H
@@ -111,7 +113,7 @@ kb_status kb_cache_append(const kb_cache* cache, int R, const int32_t* n_dev, in
  *   q_heads      a multiple of the cache's heads.
  *   q            rows of q_heads x dim values, q_stride values apart, aligned
  *                to the element.
- *   scale        finite.
+ *   scale        finite, below 2e38 in magnitude.
  *   seq          nullable, R int32: table row of each row (r itself where
  *                NULL); rows may share one, as drafted tokens with lengths of
  *                their own do.
@@ -128,7 +130,10 @@ kb_status kb_cache_append(const kb_cache* cache, int R, const int32_t* n_dev, in
  *                (KB_ERR_UNSUPPORTED otherwise) and R <= seqs.
  *   workspace    kb_cache_attend_workspace_bytes(...) bytes, 256-byte
  *                aligned scratch (NULL allowed where that is 0); weights:
- *                nonzero where weight_out is given.
+ *                nonzero where weight_out is given.  The bytes never shrink
+ *                with R or max_len, so those of the largest call serve all.
+ *                With weights they are at least 4 R q_heads max_len: give
+ *                max_len where the table has far more slots than are used.
  */
 size_t kb_cache_attend_workspace_bytes(const kb_cache* cache, int R, int q_heads, int max_len, int weights);
 kb_status kb_cache_attend(const kb_cache* cache, int R, const int32_t* n_dev, int q_heads, const void* q,

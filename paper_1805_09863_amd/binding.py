@@ -675,6 +675,15 @@ def _around(dev: int):
     return _STAY if _device_now() == dev else torch.cuda.device(dev)
 
 
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    """Memory of the stream that the call runs on: what the caller's current stream has freed may still be
+    in use there, and what is dropped after the call is still in use on the call's."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _cache(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor):
     """(kb_cache, GPU index, type, key-value heads, dim, slots of a sequence, sequences)."""
     if not isinstance(k_cache, torch.Tensor) or not k_cache.is_cuda:
@@ -746,7 +755,7 @@ def cache_append(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tens
     if q is not None:
         qp, q_stride, q_heads = _ask_rows(q, "q", dtype, R, None, dim, dev)
         if q_out is None:
-            q_out = torch.empty((R, q_heads, dim), dtype=dtype, device=q.device)
+            q_out = _empty((R, q_heads, dim), dtype, q.device, stream)
         op = _ask(q_out, "q_out", dtype, R * q_heads * dim, dev)
     elif q_out is not None:
         raise ValueError("q_out without q")
@@ -796,7 +805,7 @@ def cache_attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, 
     R = length.numel()
     qp, q_stride, q_heads = _ask_rows(q, "q", dtype, R, None, dim, dev)
     if out is None:
-        out = torch.empty((R, q_heads, dim), dtype=dtype, device=q.device)
+        out = _empty((R, q_heads, dim), dtype, q.device, stream)
     op = _ask(out, "out", dtype, R * q_heads * dim, dev)
     ep = None if lse is None else _ask(lse, "lse", f32, R * q_heads, dev)
     sp = None if seq is None else _ask(seq, "seq", i32, R, dev)
@@ -808,7 +817,7 @@ def cache_attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, 
     L = lib()
     need = L.kb_cache_attend_workspace_bytes(c, R, q_heads, max_len, 0 if wo is None else 1)
     if ws is None and need > 0:
-        ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+        ws = _empty(need, torch.uint8, q.device, stream)
     wp, ws_bytes = None, 0
     if ws is not None:
         _need_ws(ws, need)
@@ -850,11 +859,11 @@ def cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tenso
     out_pages = out_table.shape[1]
     out_cap = out_pages * c.page_size
     if out is None:
-        at = k_cache.device
-        shape = (R, heads, out_cap)
-        out = (torch.empty(R, dtype=i32, device=at), torch.zeros(shape, device=at),
-               None if position is None else torch.full(shape, -1, dtype=i32, device=at),
-               torch.empty((R, heads, max(keep, 0)), dtype=i32, device=at))
+        at, shape = k_cache.device, (R, heads, out_cap)
+        with torch.cuda.stream(stream):
+            out = (torch.empty(R, dtype=i32, device=at), torch.zeros(shape, device=at),
+                   None if position is None else torch.full(shape, -1, dtype=i32, device=at),
+                   torch.empty((R, heads, max(keep, 0)), dtype=i32, device=at))
     if len(out) != 4:
         raise ValueError("out must hold 4 tensors (length, weight, position, source)")
     out_length, out_weight, out_position, source = out

@@ -69,6 +69,8 @@ kb_status check_count(int R, int q_heads) {
 
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
+constexpr int kShares = 256;  // workgroups, a multiple of the 8 XCDs
+
 struct AttendPlan {
   int waves, head_tiles, chunk, splits, shares;
   size_t score_ld, part_o, part_s, row_before, scores, lse, bytes;  // workspace offsets
@@ -90,15 +92,16 @@ AttendPlan attend_plan(const kb_cache* c, int R, int q_heads, int max_len, bool 
   // more than it gives (4 x 8 of 300: 7.4 us, shared out 11.5; 1 x 8 of 600: 9.7 and 11.2), each row is one
   // workgroup's; and with more rows than the shares' kernel can add up, splits of 1,024 slots are.
   const int step = c->dtype == KB_BF16 ? 128 : 64;
-  p.shares = max_len > 6 * step && R <= kb::kShareRows ? 256 : 0;
+  p.shares = max_len > 6 * step && R <= kb::kShareRows ? kShares : 0;
   p.chunk = p.shares > 0 ? max_len : std::min(max_len, R <= kb::kShareRows ? 6 * step : 1024);
   p.splits = (max_len + p.chunk - 1) / p.chunk;
   const size_t rh = (size_t)R * q_heads;
-  const size_t parts = p.shares > 0 ? (size_t)p.shares * 2 * 16 : p.splits > 1 ? rh * p.splits : 0;
+  // (never less for more rows or longer ones: a workspace for the largest call serves all)
+  const size_t parts = p.shares > 0 || p.splits > 1 ? std::max((size_t)kShares * 2 * 16, p.splits > 1 ? rh * p.splits : 0) : 0;
   if (parts > 0) {
     p.part_s = align_up(parts * c->dim * sizeof(float), 256);
     p.row_before = align_up(p.part_s + parts * sizeof(float2), 256);
-    p.bytes = align_up(p.row_before + (p.shares > 0 ? ((size_t)R + 1) * sizeof(int) : 0), 256);
+    p.bytes = align_up(p.row_before + ((size_t)R + 1) * sizeof(int), 256);
   }
   if (weights) {
     p.score_ld = align_up(max_len, 32);
@@ -165,7 +168,7 @@ kb_status kb_cache_attend(const kb_cache* cache, int R, const int32_t* n_dev, in
     return fail(KB_ERR_INVALID_ARG, "q_heads = %d is no multiple of heads = %d", q_heads, cache->heads);
   if ((st = check_count(R, q_heads)) != KB_OK) return st;
   if (max_len < 1) return fail(KB_ERR_INVALID_ARG, "max_len = %d < 1", max_len);
-  if (!isfinite(scale)) return fail(KB_ERR_INVALID_ARG, "scale is not finite");
+  if (!isfinite(scale * kb::kL2E)) return fail(KB_ERR_INVALID_ARG, "scale is not finite, or too large");
   if (R == 0) return ok();
   if ((st = check_pointers(cache)) != KB_OK) return st;
   if ((st = check_rows("q", cache, q, q_stride, q_heads)) != KB_OK) return st;

@@ -93,6 +93,7 @@ def test_append_refused(kw, status):
 
 @pytest.mark.parametrize("kw,status", [
     (dict(q_heads=0), INVALID), (dict(q_heads=3), INVALID), (dict(max_len=0), INVALID), (dict(scale=math.inf), INVALID),
+    (dict(scale=-3e38), INVALID),
     (dict(q=None), INVALID), (dict(q=F + 1), INVALID), (dict(q_stride=100), INVALID), (dict(length=None), INVALID),
     (dict(out=None), INVALID), (dict(out=F + 4), INVALID), (dict(R=9), INVALID), (dict(weight_in=F), INVALID),
     (dict(weight_out=F, seq=F), UNSUPPORTED), (dict(weight_out=F, ws=None), WORKSPACE),
@@ -123,6 +124,18 @@ def test_attend_workspace_is_a_function_of_the_shape():
     assert need(cache(), 4, 4, 160, 1) == need(cache(), 4, 4, 160, 1) > 0
     assert need(cache(), 0, 4, 160, 1) == 0
     assert need(cache(dim=12), 4, 4, 160, 1) == need(cache(), 4, 3, 160, 1) == need(cache(), 4, 4, 0, 1) == 0
+
+
+def test_attend_workspace_of_the_largest_call_serves_all():
+    need = binding.lib().kb_cache_attend_workspace_bytes
+    for weights in (0, 1):
+        for dtype in (0, 1):
+            c = cache(dtype=dtype, max_pages=600, seqs=5000)
+            by_rows = [need(c, R, 4, 5000, weights) for R in (1, 7, 500, 1023, 1024, 1025, 1026, 5000)]
+            by_len = [need(c, R, 4, n, weights) for R in (3, 2000)
+                      for n in (1, 64, 65, 384, 385, 768, 769, 1024, 1025, 5000, 9600, 10 ** 6)]
+            assert by_rows == sorted(by_rows) and by_len[:12] == sorted(by_len[:12]) and by_len[12:] == sorted(by_len[12:])
+            assert by_rows[0] > 0 and by_rows[-1] < 2 ** 31
 
 
 def test_binding_refuses_host_tensors():

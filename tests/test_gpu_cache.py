@@ -270,6 +270,34 @@ def test_attend_repeats_and_leaves_rows_alone(kb):
     assert torch.all(out[4:] == 9) and torch.all(lse2[4:] == 9) and torch.equal(w3[4:], w[4:])
 
 
+def test_results_lie_in_memory_of_the_calls_stream(kb):
+    """Calls on a side stream that allocate for themselves take no memory that the current stream has freed but
+    still reads."""
+    g = torch.Generator().manual_seed(12)
+    R, Q, heads, dim, page, L = 64, 8, 2, 128, 16, 1500
+    k, v, table = make_cache(g, torch.float32, R, heads, dim, page, L, dirty=False)
+    k, v, table = k.cuda(), v.cuda(), table.cuda()
+    n = torch.full((R,), L, dtype=torch.int32, device="cuda")
+    q = torch.randn((R, Q, dim), generator=g).cuda()
+    w = torch.zeros((R, heads, table.shape[1] * page), device="cuda")
+    sizes = [kb.cache_attend_workspace_bytes(k, v, table, R, Q, weights=True) // 4, R * Q * dim,
+             R * heads * table.shape[1] * page, R * heads * 1000]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    read = [torch.ones(m, device="cuda") for m in sizes]
+    copies = [torch.empty_like(x) for x in read]
+    torch.cuda.synchronize()
+    torch.cuda._sleep(20_000_000)          # about 10 ms of the current stream
+    for x, y in zip(read, copies):
+        y.copy_(x)
+    del read, x
+    kb.cache_attend(q, k, v, table, n, weight_out=w, stream=side)
+    kb.cache_append(k, v, table, n, q[:, :2], q[:, :2], q=q, stream=side)
+    kb.cache_evict(k, v, table, n, 1000, weight=w, stream=side)
+    torch.cuda.synchronize()
+    assert all(bool((y == 1).all()) for y in copies)
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("q_heads,heads,dim,rot,pairs,page,gap", [
     (4, 2, 128, 128, False, 16, 0), (4, 2, 128, 64, True, 1, 0), (3, 1, 72, 24, False, 8, 0),
