@@ -43,6 +43,7 @@ extern "C" {
 #define KB_CACHE_MAX_DIM 256       /* largest head size                      */
 #define KB_CACHE_MAX_PAGE 1024     /* largest page_size                      */
 #define KB_CACHE_MAX_SLOTS (1 << 24) /* largest max_pages * page_size        */
+#define KB_CACHE_MAX_EVICT (1 << 19) /* the largest that kb_cache_evict takes */
 
 /* A cache: filled by the caller, read on the host during a call only. */
 typedef struct kb_cache {
@@ -175,6 +176,7 @@ kb_status kb_cache_attend(const kb_cache* cache, int R, const int32_t* n_dev, in
  *   out_position the same for position; NULL where position is.
  *   source       R x heads x keep int32: the slot that each kept place's row
  *                came from, -1 from n on.
+ * Caches of more than KB_CACHE_MAX_EVICT slots a sequence: KB_ERR_UNSUPPORTED.
  */
 kb_status kb_cache_evict(const kb_cache* cache, int R, const int32_t* n_dev, const int32_t* length, int keep, int first,
                          int recent, const int32_t* newest, const float* weight, const int32_t* position,

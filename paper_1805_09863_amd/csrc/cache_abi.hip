@@ -15,7 +15,7 @@ using kb::aligned;
 using kb::fail;
 using kb::ok;
 
-static_assert(kb::kCacheMaxDim == KB_CACHE_MAX_DIM, "one limit");
+static_assert(kb::kCacheMaxDim == KB_CACHE_MAX_DIM && kb::kEvictMax == KB_CACHE_MAX_EVICT, "the same limits");
 
 kb_status check_cache(const kb_cache* c) {
   if (!c) return fail(KB_ERR_INVALID_ARG, "null cache");
@@ -223,6 +223,8 @@ kb_status kb_cache_evict(const kb_cache* cache, int R, const int32_t* n_dev, con
   if (keep < 1 || first < 0 || recent < 0 || (long long)first + recent > keep)
     return fail(KB_ERR_INVALID_ARG, "keep = %d, first = %d, recent = %d", keep, first, recent);
   const int cap = cache->max_pages * cache->page_size;
+  if (cap > KB_CACHE_MAX_EVICT)
+    return fail(KB_ERR_UNSUPPORTED, "max_pages * page_size = %d exceeds %d", cap, KB_CACHE_MAX_EVICT);
   if (out_max_pages < 1 || (long long)out_max_pages * cache->page_size < std::min(keep, cap))
     return fail(KB_ERR_INVALID_ARG, "out_max_pages = %d of %d slots hold no %d", out_max_pages, cache->page_size,
                 std::min(keep, cap));

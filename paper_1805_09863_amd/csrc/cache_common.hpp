@@ -6,7 +6,8 @@
 
 namespace kb {
 
-constexpr int kCacheMaxDim = 256;  // largest head size
+constexpr int kCacheMaxDim = 256;     // largest head size
+constexpr int kEvictMax = 1 << 19;    // most slots of a sequence that eviction takes: their masks fit LDS
 
 // A kb_cache as the kernels take it.
 struct CacheView {

@@ -11,14 +11,14 @@
 // and stay in LDS; the two counters a digit keep a wave whose weights share their exponent from
 // adding to one address 64 times in turn; kept slots are bit masks, 64 slots each, so that the
 // ordered part needs three barriers in all.  Lengths above kEvictLds take their keys from memory in
-// every pass and go through the ordered part 1,024 slots at a time.
+// every pass.
 #include <atomic>
 
 #include "cache_common.hpp"
 
 namespace kb {
 
-constexpr int kEvictLds = 32768;  // keys that fit: 128 KB of LDS, next to 16 KB of counters
+constexpr int kEvictLds = 32768;  // keys that fit: 128 KB of LDS, next to 16 KB of counters and 6 KB of masks
 constexpr int kDigits = 2048, kCopies = 2;
 
 struct EvictKeys {
@@ -60,7 +60,7 @@ __device__ __forceinline__ int scan(int x, int* wave_sums, int& total) {
 
 template <int T>
 __global__ __launch_bounds__(T) void cache_evict_select(EvictArgs a, int room) {
-  extern __shared__ __align__(16) uint32_t lds[];  // room keys, later a list of slots; room / 64 masks and counts of kept slots
+  extern __shared__ __align__(16) uint32_t lds[];  // keys, later a list of slots (lengths up to room); a mask and a count each 64 slots
   __shared__ __align__(16) int hist[kDigits * kCopies];
   __shared__ int wsum[T / 64], pick[3];
   const CacheView& c = a.c;
@@ -164,27 +164,30 @@ __global__ __launch_bounds__(T) void cache_evict_select(EvictArgs a, int room) {
     need = pick[1], same = pick[2];
   }
 
-  if (held) {
-    // Each wave takes a run of whole 64-slot strips; what is uniform in it stays on the scalar unit.
-    constexpr int W = T / 64;
-    const int w = __builtin_amdgcn_readfirstlane(tid >> 6), strips = (L + 63) / 64;
-    const int per = (strips + W - 1) / W, s0 = min(w * per, strips), s1 = min(s0 + per, strips);
-    uint64_t* kept = (uint64_t*)(lds + room);  // each strip's kept slots
-    int* before = (int*)(kept + room / 64);    // and their number in the strips before
-    auto key_at = [&](int t) { return lds[min(t, L - 1)] & mask; };
-    auto below = [](uint64_t m) {  // the lanes of m below this one
-      return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
-    };
+  // Each wave takes a run of whole 64-slot strips; what is uniform in it stays on the scalar unit.
+  constexpr int W = T / 64;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6), strips = (L + 63) / 64;
+  const int per = (strips + W - 1) / W, s0 = min(w * per, strips), s1 = min(s0 + per, strips);
+  const int marks = held ? room / 64 : strips;
+  uint64_t* kept = (uint64_t*)(lds + (held ? room : 0));  // each strip's kept slots
+  int* before = (int*)(kept + marks);                     // and their number in the strips before
+  auto key_at = [&](int t) { return (held ? lds[min(t, L - 1)] : key(min(t, L - 1))) & mask; };
+  auto below = [](uint64_t m) {  // the lanes of m below this one
+    return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+  };
 
-    int ties = 0;  // slots that agree with top, in the strips before
-    if (same != need) {
-      for (int s = s0; s < s1; ++s) ties += __popcll(__ballot((s * 64 + lane < L) & (key_at(s * 64 + lane) == top)));
-      int all;
-      ties = __builtin_amdgcn_readfirstlane(scan<T>(lane == 0 ? ties : 0, wsum, all));
-    }
-    uint64_t mine = 0;  // lane j: strip s0 + j (a wave has at most 32)
+  int all, ties = 0;  // slots that agree with top, in the strips before
+  if (same != need) {
 #pragma unroll 4
-    for (int s = s0; s < s1; ++s) {
+    for (int s = s0; s < s1; ++s) ties += __popcll(__ballot((s * 64 + lane < L) & (key_at(s * 64 + lane) == top)));
+    ties = __builtin_amdgcn_readfirstlane(scan<T>(lane == 0 ? ties : 0, wsum, all));
+  }
+  int count = 0;  // of the wave's kept slots
+  uint64_t mine = 0;
+  for (int batch = s0; batch < s1; batch += 64) {  // lane j: strip batch + j; with keys in LDS there is one batch
+    mine = 0;
+#pragma unroll 4
+    for (int s = batch; s < min(s1, batch + 64); ++s) {
       const int t = s * 64 + lane;
       const uint32_t x = key_at(t);
       uint64_t m;
@@ -195,79 +198,73 @@ __global__ __launch_bounds__(T) void cache_evict_select(EvictArgs a, int room) {
         m = __ballot((t < L) & ((x > top) | ((x == top) & (ties + below(tie) < need))));
         ties += __popcll(tie);
       }
-      mine = lane == s - s0 ? m : mine;
+      mine = lane == s - batch ? m : mine;
     }
-    // scan<T>'s barriers also part the keys' last reads from the list that takes their place
-    int all;
-    const int s = s0 + lane, rank = scan<T>(__popcll(mine), wsum, all);
-    if (s < s1) kept[s] = mine, before[s] = rank;
-    __syncthreads();
-    // The list of kept slots from n on, where the keys were: a slot's rank among the kept ones less
-    // that of slot n.  Then the places: the j-th dropped slot is t = j + the kept ones before it.
-    const int sn = n / 64;
-    const uint64_t low = (1ull << (n % 64)) - 1;
-    const int kept_below = before[sn] + __popcll(kept[sn] & low);
-    // (32 strips a wave: a lane a strip, bit by bit, 2,100 cycles at 1 slot in 16 kept against 9,500
-    // strip by strip; 8 strips a wave: strip by strip, 1,800 against 3,300)
+    int sum = __popcll(mine);
+    const int own = sum;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int z = __shfl_up(sum, d);
+      if (lane >= d) sum += z;
+    }
+    if (batch + lane < s1) kept[batch + lane] = mine, before[batch + lane] = count + sum - own;
+    count += __shfl(sum, 63);
+  }
+  // scan<T>'s barriers also part the keys' last reads from the list that takes their place
+  count = scan<T>(lane == 0 ? count : 0, wsum, all);
+  count = __shfl(count, 0);
+  for (int s = s0 + lane; s < s1; s += 64) before[s] += count;
+  __syncthreads();
+
+  // A place t < n of a kept slot is its own; that of a dropped one, the j-th, j = t less the kept ones before
+  // it, is the j-th kept slot from n on.
+  const int sn = n / 64;
+  const uint64_t low = (1ull << (n % 64)) - 1;
+  const int kept_below = before[sn] + __popcll(kept[sn] & low);
+  if (held) {
+    // Those in a list where the keys were: a slot's rank among the kept ones less that of slot n.  (32 strips a
+    // wave: a lane a strip, bit by bit, 2,100 cycles at 1 slot in 16 kept against 9,500 strip by strip; 8
+    // strips a wave: strip by strip, 1,800 against 3,300.)
+    const int s = s0 + lane, rank = s < s1 ? before[s] - kept_below : 0;
     if constexpr (T == 1024) {
       if (s >= sn && s < s1) {
         uint64_t m = s == sn ? mine & ~low : mine;
-        for (int i = s == sn ? 0 : rank - kept_below; m != 0; m &= m - 1)
+        for (int i = s == sn ? 0 : rank; m != 0; m &= m - 1)
           lds[i++] = s * 64 + __ffsll((unsigned long long)m) - 1;
       }
     } else {
       for (int z = max(s0, sn); z < s1; ++z) {
         uint64_t m = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)mine, z - s0) |
                      (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), z - s0) << 32;
-        const int first = z == sn ? 0 : __builtin_amdgcn_readlane(rank, z - s0) - kept_below;
+        const int first = z == sn ? 0 : __builtin_amdgcn_readlane(rank, z - s0);
         if (z == sn) m &= ~low;
         if (__builtin_amdgcn_inverse_ballot_w64(m)) lds[first + below(m)] = z * 64 + lane;
       }
     }
     __syncthreads();
-    for (int s = w; s * 64 < n; s += W) {
-      const int t = s * 64 + lane;
-      const uint64_t m = kept[s];
-      const bool stays = m >> lane & 1;
-      const int j = t - before[s] - __popcll(m & ((1ull << lane) - 1));
-      if (t < n) source[t] = stays ? t : (int)lds[j];
+  }
+  for (int s = w; s * 64 < n; s += W) {
+    const int t = s * 64 + lane;
+    const uint64_t m = kept[s];
+    const bool stays = m >> lane & 1;
+    const int j = t - before[s] - __popcll(m & ((1ull << lane) - 1));
+    int from = t;
+    if (t < n && !stays) {
+      if (held) {
+        from = lds[j];
+      } else {
+        // the last strip with at most kept_below + j kept slots before it, then the bit of that rank
+        int lo = sn, hi = strips;
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) / 2;
+          if (before[mid] <= kept_below + j) lo = mid; else hi = mid;
+        }
+        uint64_t bits = kept[lo];
+        for (int i = kept_below + j - before[lo]; i > 0; --i) bits &= bits - 1;
+        from = lo * 64 + __ffsll((unsigned long long)bits) - 1;
+      }
     }
-    return;
-  }
-
-  // The kept slots from n on, ascending, to the front of source; and the number of ties below n.
-  int ties = 0, ties_below = 0, moved = 0, all;
-  for (int t0 = 0; t0 < L; t0 += T) {
-    const int t = t0 + tid;
-    const uint32_t x = t < L ? key(t) & mask : 0;
-    const bool tie = t < L && x == top;
-    const int rank = ties + scan<T>(tie, wsum, all);
-    ties += all;
-    scan<T>(tie && t < n, wsum, all);
-    ties_below += all;
-    const bool move = t >= n && t < L && (x > top || (tie && rank < need));
-    const int to = moved + scan<T>(move, wsum, all);
-    if (move) source[to] = t;
-    moved += all;
-  }
-  __syncthreads();
-  // Places n - 1 .. 0: a kept slot's own number, a dropped one's the tail slot of its rank.  The
-  // j-th dropped place is at j or above, so in descending order no entry of the list is
-  // overwritten before it is read.
-  int above = 0, ties_above = 0;
-  for (int e = n; e > 0; e -= T) {
-    const int t = e - 1 - tid;
-    const uint32_t x = t >= 0 ? key(t) & mask : 0;
-    const bool tie = t >= 0 && x == top;
-    const int tr = ties_below - 1 - (ties_above + scan<T>(tie, wsum, all));
-    ties_above += all;
-    const bool drop = t >= 0 && !(x > top || (tie && tr < need));
-    const int j = moved - 1 - (above + scan<T>(drop, wsum, all));
-    above += all;
-    const int s = drop ? source[j] : t;
-    __syncthreads();
-    if (t >= 0) source[t] = s;
-    __syncthreads();
+    if (t < n) source[t] = from;
   }
 }
 
@@ -320,8 +317,8 @@ static hipError_t raise_lds_ceiling() {
 }
 
 hipError_t launch_cache_evict(int bf16, const EvictArgs& a, hipStream_t st) {
-  const int room = min((a.c.cap + 63) / 64 * 64, kEvictLds);
-  const size_t lds = (size_t)room * 4 + room / 64 * 12;
+  const int strips = (a.c.cap + 63) / 64, room = min(strips * 64, kEvictLds);
+  const size_t lds = max((size_t)room * 4 + room / 64 * 12, (size_t)strips * 12);
   const dim3 grid(a.R * a.c.heads);
   if (room <= kEvictSmall) {
     cache_evict_select<256><<<grid, dim3(256), lds, st>>>(a, room);

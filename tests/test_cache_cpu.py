@@ -119,6 +119,12 @@ def test_evict_refused(kw, status):
     assert evict(**kw) == status
 
 
+def test_evict_refuses_longer_caches():
+    big = dict(max_pages=(1 << 19) // 16 + 1)
+    assert evict(cache(**big), out_max_pages=big["max_pages"]) == UNSUPPORTED
+    assert attend(cache(**big), R=0) == OK
+
+
 def test_attend_workspace_is_a_function_of_the_shape():
     need = binding.lib().kb_cache_attend_workspace_bytes
     assert need(cache(), 4, 4, 160, 1) == need(cache(), 4, 4, 160, 1) > 0

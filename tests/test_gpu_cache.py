@@ -457,14 +457,15 @@ def test_evict_ties_and_special_values(kb):
     run_evict(kb, k, v, table, length, keep, w, position=position, newest=newest, first=0, recent=5)
 
 
-def test_evict_long(kb):
-    """Longer than any buffer on the chip: 70,000 slots down to 20,000 and to 3."""
-    g = torch.Generator().manual_seed(2)
-    L = 70000
-    k, v, table = make_cache(g, torch.bfloat16, 2, 2, 8, 128, L, dirty=False)
-    length = torch.tensor([L, 33333], dtype=torch.int32)
-    w = (torch.rand((2, 2, table.shape[1] * 128), generator=g) * 5000).round()
-    for keep in (20000, 3):
+@pytest.mark.parametrize("L,keeps", [(70000, (20000, 3, 69999)), (300001, (150000,)), (1 << 19, (1000,))])
+def test_evict_long(kb, L, keeps):
+    """Longer than what keys fit the chip, up to the longest; ties across wave and strip borders."""
+    g = torch.Generator().manual_seed(L)
+    k, v, table = make_cache(g, torch.bfloat16, 2, 1, 8, 128, L, dirty=False)
+    length = torch.tensor([L, L // 2 - 1], dtype=torch.int32)
+    w = (torch.rand((2, 1, table.shape[1] * 128), generator=g) * 5000).round()
+    w[1] = 1
+    for keep in keeps:
         run_evict(kb, k, v, table, length, keep, w)
 
 
