@@ -69,10 +69,8 @@ kb_status check_count(int R, int q_heads) {
 
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
-constexpr int kShares = 256;  // workgroups, a multiple of the 8 XCDs
-
 struct AttendPlan {
-  int waves, head_tiles, chunk, splits, shares;
+  int waves, head_tiles, chunk, splits, shared;
   size_t score_ld, part_o, part_s, row_before, scores, lse, bytes;  // workspace offsets
 };
 
@@ -92,12 +90,12 @@ AttendPlan attend_plan(const kb_cache* c, int R, int q_heads, int max_len, bool 
   // more than it gives (4 x 8 of 300: 7.4 us, shared out 11.5; 1 x 8 of 600: 9.7 and 11.2), each row is one
   // workgroup's; and with more rows than the shares' kernel can add up, splits of 1,024 slots are.
   const int step = c->dtype == KB_BF16 ? 128 : 64;
-  p.shares = max_len > 6 * step && R <= kb::kShareRows ? kShares : 0;
-  p.chunk = p.shares > 0 ? max_len : std::min(max_len, R <= kb::kShareRows ? 6 * step : 1024);
+  p.shared = max_len > 6 * step && R <= kb::kShareRows;
+  p.chunk = p.shared ? max_len : std::min(max_len, R <= kb::kShareRows ? 6 * step : 1024);
   p.splits = (max_len + p.chunk - 1) / p.chunk;
   const size_t rh = (size_t)R * q_heads;
   // (never less for more rows or longer ones: a workspace for the largest call serves all)
-  const size_t parts = p.shares > 0 || p.splits > 1 ? std::max((size_t)kShares * 2 * 16, p.splits > 1 ? rh * p.splits : 0) : 0;
+  const size_t parts = p.shared || p.splits > 1 ? std::max((size_t)kb::kShares * 2 * 16, p.splits > 1 ? rh * p.splits : 0) : 0;
   if (parts > 0) {
     p.part_s = align_up(parts * c->dim * sizeof(float), 256);
     p.row_before = align_up(p.part_s + parts * sizeof(float2), 256);
@@ -195,8 +193,8 @@ kb_status kb_cache_attend(const kb_cache* cache, int R, const int32_t* n_dev, in
   a.head_tiles = p.head_tiles;
   a.chunk = p.chunk;
   a.splits = p.splits;
-  a.shares = a.max_len > 0 ? p.shares : 0;
-  if (p.splits > 1 || p.shares > 0) {
+  a.shared = a.max_len > 0 && p.shared;
+  if (p.splits > 1 || p.shared) {
     a.part_o = reinterpret_cast<float*>(ws + p.part_o);
     a.part_s = reinterpret_cast<float2*>(ws + p.part_s);
     a.row_before = reinterpret_cast<int*>(ws + p.row_before);

@@ -350,7 +350,7 @@ __global__ __launch_bounds__(256, DC * sizeof(T) > 256 ? 1 : 2) void cache_atten
   const CacheView& c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, rows = rows_of(a.R, a.n_dev);
   // each XCD a run of neighbouring shares
-  const int b = (blockIdx.x & 7) * (a.shares / 8) + (blockIdx.x >> 3);
+  const int b = (blockIdx.x & 7) * (kShares / 8) + (blockIdx.x >> 3);
 
   // The rows' costs in steps, and their sums before each row.
   constexpr int RT = kShareRows / 256;
@@ -382,7 +382,7 @@ __global__ __launch_bounds__(256, DC * sizeof(T) > 256 ? 1 : 2) void cache_atten
     if (w < tid >> 6) before += wave_sum[w];
     all += wave_sum[w];
   }
-  const AttendShares shares(all, c.heads * a.head_tiles, a.shares);
+  const AttendShares shares(all, c.heads * a.head_tiles);
   const bool idle = b >= shares.shares;
   long long x = idle ? 0 : shares.begin(b);
   const long long x_end = idle ? 0 : shares.begin(b + 1);
@@ -419,8 +419,8 @@ __global__ __launch_bounds__(256, DC * sizeof(T) > 256 ? 1 : 2) void cache_atten
 template <class T, int DC>
 hipError_t launch_attend_built(const AttendArgs& a, hipStream_t st) {
   const unsigned cells = (unsigned)a.R * a.c.heads * a.head_tiles * a.splits;
-  if (a.shares > 0)
-    cache_attend_shares<T, DC><<<dim3(a.shares), dim3(256), 0, st>>>(a);
+  if (a.shared)
+    cache_attend_shares<T, DC><<<dim3(kShares), dim3(256), 0, st>>>(a);
   else if (a.waves == 1)
     cache_attend_splits<T, DC, 1><<<dim3(cells), dim3(64), 0, st>>>(a);
   else

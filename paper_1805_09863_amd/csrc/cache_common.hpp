@@ -47,8 +47,8 @@ struct AttendArgs {
   const float* weight_in;
   float* weight_out;
   // the launch: waves per workgroup, tiles of 16 query heads per key-value head, splits of `chunk` slots; or
-  // (shares > 0) that many equal shares of all rows' slots
-  int waves, head_tiles, chunk, splits, shares;
+  // (shared) equal shares of all rows' slots
+  int waves, head_tiles, chunk, splits, shared;
   // workspace: partial outputs (dim floats) and their (max, sum), in base 2: one per row, query head and
   // split (splits > 1), or 16 query heads' two per share, and the costs before each row; the scores in base
   // 2, score_ld apart per row and query head (weight_out)
@@ -57,29 +57,35 @@ struct AttendArgs {
   int* row_before;
   float* scores;
   int64_t score_ld;
+  int weight_blocks;  // of the second launch, a (row, key-value head); the others join
 };
 
 // Attention's slots in equal shares, where lengths differ or splits would start and end too often.
 // Every (key-value head, 16 query heads), one after the other, has all rows in order; a row costs its
 // steps (the slots that a workgroup takes at a time) and kStart more for starting on it (64 x 8 of up to
 // 8,192 slots: 77 us at 1, 80 at 2, 84 at 4).
-// Share b is the b-th of `shares` equal parts of all of it, one workgroup's: a row within one share is
+// Share b is the b-th of kShares equal parts of all of it, one workgroup's: a row within one share is
 // finished there, one that shares cut leaves a partial in each, which the join adds up.  A share cuts at
 // most two: the one it starts within and the one it ends within.
 constexpr int kShareRows = 1024;
+constexpr int kShares = 256;  // workgroups; a power of two and a multiple of the 8 XCDs
 struct AttendShares {
   long long total;
   int shares;  // no more than total: none is empty
   // all: the cost of all rows, for one (key-value head, 16 query heads); columns: how many of these there are
-  __device__ __forceinline__ AttendShares(int all, int columns, int most)
-      : total((long long)all * columns), shares((int)min((long long)most, total)) {}
+  __device__ __forceinline__ AttendShares(int all, int columns)
+      : total((long long)all * columns), shares((int)min((long long)kShares, total)) {}
   static constexpr int kStart = 1;
   static __device__ __forceinline__ int cost(int len, int step) { return (len + step - 1) / step + kStart; }
   // The first slot of a row at place o of its cost; the start's places come first.
   static __device__ __forceinline__ int slot(int o, int step) { return max(o - kStart, 0) * step; }
-  __device__ __forceinline__ long long begin(int b) const { return b * total / shares; }
+  __device__ __forceinline__ long long begin(int b) const { return shares < kShares ? b : b * total / kShares; }
   // The share that x lies in: the largest b with begin(b) <= x.
-  __device__ __forceinline__ int of(long long x) const { return (int)(((x + 1) * shares - 1) / total); }
+  __device__ __forceinline__ int of(long long x) const {
+    if (shares < kShares) return (int)x;
+    const long long n = (x + 1) * kShares - 1;
+    return total <= UINT_MAX / kShares ? (int)((uint32_t)n / (uint32_t)total) : (int)(n / total);
+  }
   static __device__ __forceinline__ int64_t partial(int b, int o0) { return 2 * (int64_t)b + (o0 == 0 ? 1 : 0); }
 };
 
@@ -99,7 +105,7 @@ struct EvictArgs {
 };
 
 hipError_t launch_cache_append(int bf16, const AppendArgs& a, hipStream_t st);
-hipError_t launch_cache_attend(int bf16, const AttendArgs& a, hipStream_t st);
+hipError_t launch_cache_attend(int bf16, AttendArgs& a, hipStream_t st);
 hipError_t launch_cache_evict(int bf16, const EvictArgs& a, hipStream_t st);
 
 // Row (of dim values, in k or v) of slot t of a sequence whose table row is
