@@ -429,6 +429,8 @@ def greedy_search(decoder: CachedDecoder, W: torch.Tensor, b: torch.Tensor, star
         raise ValueError(f"T = {T}, keep = {keep}, every = {every}")
     if recent is None:
         recent = 0 if keep is None else min(keep // 2, max(keep - first, 0))
+    if keep is not None and (first < 0 or recent < 0 or first + recent > keep):
+        raise ValueError(f"first = {first} and recent = {recent} of keep = {keep}")
     if stream is None:
         stream = torch.cuda.current_stream(dev)
     S0 = start.numel()

@@ -168,6 +168,8 @@ def test_refusals(kb):
     with pytest.raises(ValueError):
         greedy_search(dec, W, b, start, 5, EOS, keep=0)
     with pytest.raises(ValueError):
+        greedy_search(dec, W, b, start, 5, EOS, keep=4, first=3, recent=2)
+    with pytest.raises(ValueError):
         CachedDecoder(dec.embed, dec.Wqkv, dec.Wo, 3, 2)
     with pytest.raises(ValueError):
         CachedDecoder(dec.embed, dec.Wqkv[:, :-1].contiguous(), dec.Wo, Q, KV)
