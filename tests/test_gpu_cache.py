@@ -405,6 +405,7 @@ def run_evict(kb, k, v, table, length, keep, weight, position=None, newest=None,
 @pytest.mark.parametrize("heads,dim,page,cap,keep,first,recent", [
     (1, 8, 1, 40, 16, 0, 0), (2, 64, 16, 300, 256, 4, 64), (3, 72, 8, 1100, 500, 0, 100), (1, 128, 64, 2100, 1, 0, 1),
     (2, 256, 4, 70, 69, 69, 0), (1, 40, 1024, 5000, 1024, 3, 7), (2, 16, 2, 1500, 1400, 0, 0), (1, 8, 32, 20, 64, 1, 1),
+    (2, 16, 1, 1101, 300, 1, 20), (3, 8, 1, 2503, 2400, 0, 5),
 ])
 def test_evict(kb, dtype, heads, dim, page, cap, keep, first, recent):
     g = torch.Generator().manual_seed(cap + keep)
@@ -467,6 +468,62 @@ def test_evict_long(kb, L, keeps):
     w[1] = 1
     for keep in keeps:
         run_evict(kb, k, v, table, length, keep, w)
+
+
+@pytest.mark.parametrize("count", [0, -1, -2 ** 31])
+def test_no_rows_on_the_device(kb, count):
+    """A device count of none or less: every output stays as it was."""
+    g = torch.Generator().manual_seed(6)
+    for cap in (40, 2000):
+        k, v, table = (x.cuda() for x in make_cache(g, torch.float32, 3, 2, 64, 8, cap, dirty=False))
+        n = torch.full((3,), cap, dtype=torch.int32, device="cuda")
+        nd = torch.tensor([count], dtype=torch.int32, device="cuda")
+        x = torch.randn((3, 4, 64), generator=g).cuda()
+        w = torch.ones((3, 2, table.shape[1] * 8), device="cuda")
+        keep = [t.clone() for t in (k, v, w)]
+        out, lse, q_out = torch.full_like(x, 7), torch.full((3, 4), 7.0, device="cuda"), torch.full_like(x, 7)
+        res = (torch.full((3,), 7, dtype=torch.int32, device="cuda"), w, None,
+               torch.full((3, 2, 9), 7, dtype=torch.int32, device="cuda"))
+        kb.cache_append(k, v, table, n, x[:, :2], x[:, 2:], q=x, q_out=q_out, weight=w, n_dev=nd)
+        kb.cache_attend(x, k, v, table, n, out=out, lse=lse, weight_out=w, n_dev=nd)
+        kb.cache_evict(k, v, table, n, 9, weight=w, out=res, n_dev=nd)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((k, v, w), keep))
+        for t in (out, lse, q_out, res[0], res[3]):
+            assert bool((t == 7).all())
+
+
+def test_attend_replayed_over_other_lengths(kb):
+    """A graph of the shared-out attention, captured at some lengths, replayed at others and other tables: the work
+    is shared out anew from what is on the device."""
+    g = torch.Generator().manual_seed(14)
+    R, Q, heads, dim, page, cap = 9, 6, 2, 64, 16, 2500
+    k, v, table = make_cache(g, torch.bfloat16, R, heads, dim, page, cap, dirty=False)
+    q = torch.randn((R, Q, dim), generator=g).bfloat16()
+    dk, dv, dt, dq = k.cuda(), v.cuda(), table.cuda(), q.cuda()
+    n = torch.full((R,), 100, dtype=torch.int32, device="cuda")
+    w = torch.zeros((R, heads, dt.shape[1] * page), device="cuda")
+    out, lse = torch.zeros_like(dq), torch.zeros((R, Q), device="cuda")
+    ws = torch.empty(kb.cache_attend_workspace_bytes(dk, dv, dt, R, Q, weights=True), dtype=torch.uint8, device="cuda")
+    call = lambda o, e, x: kb.cache_attend(dq, dk, dv, dt, n, out=o, lse=e, weight_out=x, ws=ws)  # noqa: E731
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call(out, lse, w)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out, lse, w)
+    for i in range(6):
+        n.copy_(torch.randint(0, cap + 1, (R,), generator=g).to(torch.int32) if i != 3 else torch.zeros(R).int())
+        dt.copy_(table[torch.randperm(R, generator=g)])
+        graph.replay()
+        a, b, c = torch.zeros_like(out), torch.zeros_like(lse), w.clone()
+        torch.cuda.synchronize()
+        call(a, b, c)
+        torch.cuda.synchronize()
+        assert torch.equal(a, out) and torch.equal(b, lse) and torch.equal(c, w), f"replay {i}"
+    check_attend(kb, q, k, v, dt.cpu(), n.cpu(), weights=True)
 
 
 def test_run_together_under_a_graph(kb):
