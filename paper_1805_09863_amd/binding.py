@@ -656,51 +656,46 @@ def _ask(t, name: str, dtype, numel: int, dev: int) -> int:
     return _refuse(t, name, dtype, numel, dev)
 
 
-class _stay:
-    """The current device is the call's."""
-
-    def __enter__(self):
-        pass
-
-    def __exit__(self, *exc):
-        pass
-
-
-_STAY = _stay()
 _device_now = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _around(dev: int):
-    """The tensors' device made current around a call, where it is not."""
-    return _STAY if _device_now() == dev else torch.cuda.device(dev)
+def _run(fn, dev: int, stream, *args):
+    """fn(*args, stream) with the tensors' device current; an error raised."""
+    st = _raw_stream(dev) if stream is None and _raw_stream is not None else _stream(stream, torch.device("cuda", dev))
+    if _device_now() == dev:
+        status = fn(*args, st)
+    else:
+        with torch.cuda.device(dev):
+            status = fn(*args, st)
+    if status:
+        _check(status)
 
 
-def _empty(shape, dtype, device, stream) -> torch.Tensor:
+def _empty(like: torch.Tensor, shape, stream, dtype=None) -> torch.Tensor:
     """Memory of the stream that the call runs on: what the caller's current stream has freed may still be
     in use there, and what is dropped after the call is still in use on the call's."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
 
 
 def _cache(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor):
     """(kb_cache, GPU index, type, key-value heads, dim, slots of a sequence, sequences)."""
     if not isinstance(k_cache, torch.Tensor) or not k_cache.is_cuda:
         raise TypeError("k_cache must be a tensor on the GPU")
-    dtype, dev = k_cache.dtype, k_cache.get_device()
-    code = _dtype_code(k_cache, "k_cache")
+    dtype, dev, shape = k_cache.dtype, k_cache.get_device(), k_cache.shape
     kp = _ask(k_cache, "k_cache", dtype, 0, dev)
     vp = _ask(v_cache, "v_cache", dtype, 0, dev)
     tp = _ask(table, "table", torch.int32, 0, dev)
-    if k_cache.dim() != 4 or v_cache.shape != k_cache.shape:
+    if len(shape) != 4 or v_cache.shape != shape:
         raise ValueError("k_cache and v_cache must be pages x heads x page_size x dim, the same shape")
     if table.dim() != 2:
         raise ValueError("table must be seqs x max_pages")
-    pages, heads, page_size, dim = k_cache.shape
+    pages, heads, page_size, dim = shape
     seqs, max_pages = table.shape
-    return (_Cache(code, heads, dim, page_size, pages, seqs, max_pages, kp, vp, tp), dev, dtype, heads, dim,
-            max_pages * page_size, seqs)
+    return (_Cache(_dtype_code(k_cache, "k_cache"), heads, dim, page_size, pages, seqs, max_pages, kp, vp, tp), dev,
+            dtype, heads, dim, max_pages * page_size, seqs)
 
 
 def _ask_rows(t: torch.Tensor, name: str, dtype, R: int, heads: Optional[int], dim: int, dev: int):
@@ -755,7 +750,7 @@ def cache_append(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tens
     if q is not None:
         qp, q_stride, q_heads = _ask_rows(q, "q", dtype, R, None, dim, dev)
         if q_out is None:
-            q_out = _empty((R, q_heads, dim), dtype, q.device, stream)
+            q_out = _empty(q, (R, q_heads, dim), stream)
         op = _ask(q_out, "q_out", dtype, R * q_heads * dim, dev)
     elif q_out is not None:
         raise ValueError("q_out without q")
@@ -767,12 +762,8 @@ def cache_append(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tens
     nd = None if n_dev is None else _ask(n_dev, "n_dev", i32, 1, dev)
     at = None if position is None else _ask(position, "position", i32, seqs * heads * cap, dev)
     wp = None if weight is None else _ask(weight, "weight", torch.float32, seqs * heads * cap, dev)
-    with _around(dev):
-        status = lib().kb_cache_append(c, R, nd, q_heads, qp, q_stride, kp, k_stride, vp, v_stride, rot,
-                                       1 if interleaved else 0, pp, fp, amplitude, sp, lp, op, at, wp,
-                                       _stream(stream, k_cache.device))
-    if status:
-        _check(status)
+    _run(lib().kb_cache_append, dev, stream, c, R, nd, q_heads, qp, q_stride, kp, k_stride, vp, v_stride, rot,
+         1 if interleaved else 0, pp, fp, amplitude, sp, lp, op, at, wp)
     return q_out
 
 
@@ -805,7 +796,7 @@ def cache_attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, 
     R = length.numel()
     qp, q_stride, q_heads = _ask_rows(q, "q", dtype, R, None, dim, dev)
     if out is None:
-        out = _empty((R, q_heads, dim), dtype, q.device, stream)
+        out = _empty(q, (R, q_heads, dim), stream)
     op = _ask(out, "out", dtype, R * q_heads * dim, dev)
     ep = None if lse is None else _ask(lse, "lse", f32, R * q_heads, dev)
     sp = None if seq is None else _ask(seq, "seq", i32, R, dev)
@@ -817,16 +808,13 @@ def cache_attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, 
     L = lib()
     need = L.kb_cache_attend_workspace_bytes(c, R, q_heads, max_len, 0 if wo is None else 1)
     if ws is None and need > 0:
-        ws = _empty(need, torch.uint8, q.device, stream)
+        ws = _empty(q, need, stream, torch.uint8)
     wp, ws_bytes = None, 0
     if ws is not None:
         _need_ws(ws, need)
         wp, ws_bytes = _ask(ws, "ws", ws.dtype, 0, dev), ws.numel() * ws.element_size()
-    with _around(dev):
-        status = L.kb_cache_attend(c, R, nd, q_heads, qp, q_stride, dim ** -0.5 if scale is None else scale, sp, lp,
-                                   max_len, op, ep, wi, wo, wp, ws_bytes, _stream(stream, k_cache.device))
-    if status:
-        _check(status)
+    _run(L.kb_cache_attend, dev, stream, c, R, nd, q_heads, qp, q_stride, dim ** -0.5 if scale is None else scale, sp,
+         lp, max_len, op, ep, wi, wo, wp, ws_bytes)
     return out
 
 
@@ -871,11 +859,8 @@ def cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tenso
     owp = _ask(out_weight, "out weight", f32, R * heads * out_cap, dev)
     opp = None if out_position is None else _ask(out_position, "out position", i32, R * heads * out_cap, dev)
     sp = _ask(source, "source", i32, R * heads * keep, dev)
-    with _around(dev):
-        status = lib().kb_cache_evict(c, R, nd, lp, keep, first, recent, ne, wp, pp, tp, out_pages, olp, owp, opp, sp,
-                                      _stream(stream, k_cache.device))
-    if status:
-        _check(status)
+    _run(lib().kb_cache_evict, dev, stream, c, R, nd, lp, keep, first, recent, ne, wp, pp, tp, out_pages, olp, owp, opp,
+         sp)
     return out
 
 

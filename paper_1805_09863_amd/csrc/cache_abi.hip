@@ -95,7 +95,8 @@ AttendPlan attend_plan(const kb_cache* c, int R, int q_heads, int max_len, bool 
   p.splits = (max_len + p.chunk - 1) / p.chunk;
   const size_t rh = (size_t)R * q_heads;
   // (never less for more rows or longer ones: a workspace for the largest call serves all)
-  const size_t parts = p.shared || p.splits > 1 ? std::max((size_t)kb::kShares * 2 * 16, p.splits > 1 ? rh * p.splits : 0) : 0;
+  const size_t least = (size_t)kb::kShares * 2 * 16;
+  const size_t parts = p.splits > 1 ? std::max(least, rh * p.splits) : p.shared ? least : 0;
   if (parts > 0) {
     p.part_s = align_up(parts * c->dim * sizeof(float), 256);
     p.row_before = align_up(p.part_s + parts * sizeof(float2), 256);

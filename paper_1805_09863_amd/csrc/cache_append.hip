@@ -60,7 +60,9 @@ __global__ __launch_bounds__(kAppendT) void cache_append_rows(AppendArgs a) {
     __builtin_memcpy(&x, __builtin_assume_aligned(p, sizeof(Piece)), sizeof(Piece));
     return x;
   };
-  auto store = [](T* p, const Piece& x) { __builtin_memcpy(__builtin_assume_aligned(p, sizeof(Piece)), &x, sizeof(Piece)); };
+  auto store = [](T* p, const Piece& x) {
+    __builtin_memcpy(__builtin_assume_aligned(p, sizeof(Piece)), &x, sizeof(Piece));
+  };
 
   // a turned item: V pairs, in two pieces that lie half the turned part apart or side by side
   const int per = half / V, turned = H * per;

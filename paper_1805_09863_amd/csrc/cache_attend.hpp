@@ -228,7 +228,8 @@ struct AttendRun {
               uint32_t w[4];
 #pragma unroll
               for (int j = 0; j < 4; ++j)
-                w[j] = __builtin_amdgcn_perm(vr[2 * j + 1][b][e / 2], vr[2 * j][b][e / 2], e % 2 ? 0x07060302 : 0x05040100);
+                w[j] = __builtin_amdgcn_perm(vr[2 * j + 1][b][e / 2], vr[2 * j][b][e / 2],
+                                             e % 2 ? 0x07060302 : 0x05040100);
               bf16x8 va;
               __builtin_memcpy(&va, w, 16);
               acc[b][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, hi, acc[b][e], 0, 0, 0);
@@ -241,7 +242,8 @@ struct AttendRun {
             for (int e = 0; e < VE; ++e)
 #pragma unroll
               for (int j = 0; j < NV; ++j)
-                acc[b][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[j][b][e]), x[0][j], acc[b][e], 0, 0, 0);
+                acc[b][e] =
+                    __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[j][b][e]), x[0][j], acc[b][e], 0, 0, 0);
         }
         if (more) load_v(row);
         valid = next_valid;
@@ -290,7 +292,8 @@ struct AttendRun {
           for (int e = 0; e < VE; e += 4) {
             const int d = (16 * b + 4 * g + i) * VE + e;
             if (n < nh && d < DC)
-              *(f32x4*)&part[(wave * 16 + n) * LD + d] = f32x4{acc[b][e][i], acc[b][e + 1][i], acc[b][e + 2][i], acc[b][e + 3][i]};
+              *(f32x4*)&part[(wave * 16 + n) * LD + d] =
+                  f32x4{acc[b][e][i], acc[b][e + 1][i], acc[b][e + 2][i], acc[b][e + 3][i]};
           }
       __syncthreads();
       for (int i = threadIdx.x; i < nh * (D / 4); i += NW * 64) {
@@ -314,7 +317,8 @@ struct AttendRun {
 
 // A row's splits of a.chunk slots each a workgroup of their own; NW = 1: a wave for a whole row.
 template <class T, int DC, int NW>
-__global__ __launch_bounds__(NW * 64, DC * sizeof(T) > 256 ? 1 : NW == 1 ? 3 : 2) void cache_attend_splits(AttendArgs a) {
+__global__ __launch_bounds__(NW * 64, DC * sizeof(T) > 256 ? 1 : NW == 1 ? 3 : 2)
+void cache_attend_splits(AttendArgs a) {
   using Run = AttendRun<T, DC, NW>;
   __shared__ typename Run::Lds lds;
   const CacheView& c = a.c;
@@ -337,7 +341,8 @@ __global__ __launch_bounds__(NW * 64, DC * sizeof(T) > 256 ? 1 : NW == 1 ? 3 : 2
     Run::run(a, lds, pages, r, kv, ht, 0, len, page, next_page, -1, 0);
   } else {
     const int64_t rh = (int64_t)r * a.q_heads + kv * (a.q_heads / c.heads) + ht * 16;
-    Run::run(a, lds, pages, r, kv, ht, begin, end, page, next_page, a.splits > 1 ? rh * a.splits + split : -1, a.splits);
+    Run::run(a, lds, pages, r, kv, ht, begin, end, page, next_page, a.splits > 1 ? rh * a.splits + split : -1,
+             a.splits);
   }
 }
 

@@ -60,7 +60,8 @@ __device__ __forceinline__ int scan(int x, int* wave_sums, int& total) {
 
 template <int T>
 __global__ __launch_bounds__(T) void cache_evict_select(EvictArgs a, int room) {
-  extern __shared__ __align__(16) uint32_t lds[];  // keys, later a list of slots (lengths up to room); a mask and a count each 64 slots
+  // keys, later a list of slots (lengths up to room); a mask and a count for each 64 slots
+  extern __shared__ __align__(16) uint32_t lds[];
   __shared__ __align__(16) int hist[kDigits * kCopies];
   __shared__ int wsum[T / 64], pick[3];
   const CacheView& c = a.c;
@@ -76,7 +77,8 @@ __global__ __launch_bounds__(T) void cache_evict_select(EvictArgs a, int room) {
   const int64_t at = ((int64_t)r * c.heads + h) * c.cap;
   // (first >= 0, so that a bound below every int32 protects the lowest one too)
   const long long old = a.recent > 0 ? (long long)a.newest[r] - a.recent : INT_MAX;
-  const EvictKeys key{a.weight + at, a.position ? a.position + at : nullptr, a.first, (int)max(old, (long long)INT_MIN)};
+  const EvictKeys key{a.weight + at, a.position ? a.position + at : nullptr, a.first,
+                      (int)max(old, (long long)INT_MIN)};
   const bool held = L <= room;  // keys in LDS
   const bool whole = (((uintptr_t)key.weight | (uintptr_t)key.position) & 15) == 0 && c.cap % 4 == 0;
 
