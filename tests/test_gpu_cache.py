@@ -493,6 +493,59 @@ def test_no_rows_on_the_device(kb, count):
             assert bool((t == 7).all())
 
 
+@pytest.mark.parametrize("pages,seqs,R", [(0, 4, 4), (3, 0, 4), (0, 0, 1100)])
+def test_empty_pools_and_tables(kb, pages, seqs, R):
+    """No pages or no sequences: nothing to attend to, nowhere to store, whatever the lengths say."""
+    shape = (pages, 2, 16, 64)
+    for cols in (1, 200):
+        k, v = (torch.full(shape, math.nan, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        table = torch.zeros((seqs, cols), dtype=torch.int32, device="cuda")
+        n = torch.full((R,), 10, dtype=torch.int32, device="cuda")
+        seq = None if seqs else torch.zeros(R, dtype=torch.int32, device="cuda")
+        q = torch.ones((R, 4, 64), dtype=torch.bfloat16, device="cuda")
+        lse = torch.zeros((R, 4), device="cuda")
+        kb.cache_append(k, v, table, n, q[:, :2], q[:, 2:], q=q, seq=seq)
+        out = kb.cache_attend(q, k, v, table, n, lse=lse, seq=seq)
+        torch.cuda.synchronize()
+        assert bool((out == 0).all()) and bool((lse == -math.inf).all())
+        assert pages == 0 or bool(torch.isnan(k).all())
+    if seqs:
+        w = torch.rand((seqs, 2, 3200), device="cuda")
+        got = kb.cache_evict(k, v, table, n, 4, weight=w)
+        assert got[0].tolist() == [4] * R
+        assert torch.equal(got[1][:, :, :4].sort().values, w[:, :, :10].topk(4).values.sort().values)
+
+
+def test_offsets_past_32_bits(kb):
+    """The last pages of a pool of more than 2^32 bytes and 2^31 values give what the same pages of a small one do."""
+    g = torch.Generator().manual_seed(16)
+    R, Q, heads, dim, page, cap = 3, 8, 2, 256, 64, 1000
+    k, v, table = make_cache(g, torch.bfloat16, R, heads, dim, page, cap, spare=0, dirty=False)
+    pages = k.shape[0]
+    big_pages = 2 ** 31 // (heads * page * dim) + 40000
+    assert big_pages * heads * page * dim * 2 > 2 ** 32 and big_pages * heads * page < 2 ** 31
+    k, v, table = k.cuda(), v.cuda(), table.cuda()
+    bk, bv = (torch.empty((big_pages,) + tuple(k.shape[1:]), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    at = torch.arange(big_pages - pages, big_pages, device="cuda")
+    bk[at], bv[at] = k, v
+    far = (table + big_pages - pages).to(torch.int32)
+    n = torch.tensor([1000, 999, 64], dtype=torch.int32, device="cuda")
+    x = torch.randn((R, Q + 2 * heads, dim), generator=g).bfloat16().cuda()
+    pos, freq = n - 1, kb.rotary_frequencies(dim)
+    res = []
+    for kc, vc, t in ((k, v, table), (bk, bv, far)):
+        w = torch.zeros((R, heads, t.shape[1] * page), device="cuda")
+        q = kb.cache_append(kc, vc, t, n, x[:, Q:Q + heads], x[:, Q + heads:], q=x[:, :Q], pos=pos, freq=freq)
+        lse = torch.zeros((R, Q), device="cuda")
+        out = kb.cache_attend(q, kc, vc, t, n, lse=lse, weight_out=w)
+        ev = kb.cache_evict(kc, vc, t, n, 300, weight=w)
+        res.append((q, out, lse, w, ev[0], ev[1], ev[3]))
+    torch.cuda.synchronize()
+    for a, b in zip(*res):
+        assert torch.equal(a, b)
+    assert torch.equal(bk[at], k) and torch.equal(bv[at], v)
+
+
 def test_attend_replayed_over_other_lengths(kb):
     """A graph of the shared-out attention, captured at some lengths, replayed at others and other tables: the work
     is shared out anew from what is on the device."""
