@@ -16,8 +16,8 @@
  *    place t % page_size.  A page outside [0, pages) is a hole: its slots are
  *    neither read, attended to nor written.  Where slots are read, lengths
  *    above the table's max_pages * page_size are cut to that; negative ones
- *    are 0.  So no
- *    content of table, seq and length makes a call leave its buffers.
+ *    are 0.  So no content of table, seq and length makes a call leave its
+ *    buffers.
  *  - A call of R rows takes their count from the device where n_dev is given:
  *    min(R, *n_dev) rows are worked on, outputs of the others are left as
  *    they were.
@@ -66,11 +66,11 @@ typedef struct kb_cache {
  * Row r is a token of sequence s = seq[r] (r itself where seq is NULL; a
  * value outside [0, seqs) makes the row one of length 0) and goes to slot
  * length[r] - 1; a row of length 0, or longer than the table has slots, is not
- * stored.  A prompt's tokens are rows
- * with one seq and lengths 1, 2, ...; where two rows of a call name the same
- * place of a page, what it holds afterwards is unspecified.  With m the
- * amplitude and a_i = pos[r] * freq[i], taken in 64 bits, each pair (x, y) of a
- * query's or key's first rot_dim values becomes
+ * stored.  A prompt's tokens are rows with one seq and lengths 1, 2, ...;
+ * where two rows of a call name the same place of a page, what it holds
+ * afterwards is unspecified.  With m the amplitude and a_i = pos[r] * freq[i],
+ * taken in 64 bits, each pair (x, y) of a query's or key's first rot_dim
+ * values becomes
  *     (m (x cos a_i - y sin a_i), m (x sin a_i + y cos a_i)),   i < rot_dim / 2
  * rounded once; pair i is values (i, i + rot_dim / 2), or (2i, 2i + 1) where
  * interleaved.  The rest of the head, and values, are copied.  Positions
@@ -168,8 +168,9 @@ kb_status kb_cache_attend(const kb_cache* cache, int R, const int32_t* n_dev, in
  *   out_table    R x out_max_pages int32: the pages to keep the slots in,
  *                either the cache's own table (in place: out_table == table,
  *                out_max_pages == max_pages) or pages that hold none of the
- *                sequences' slots.  Sequences do not share these pages.  out_max_pages * page_size >= min(keep,
- *                max_pages * page_size).
+ *                sequences' slots.  Sequences do not share these pages.
+ *                out_max_pages * page_size >= min(keep, max_pages *
+ *                page_size).
  *   out_length   R int32: n (may be length).
  *   out_weight   R x heads x (out_max_pages * page_size) float32: the kept
  *                slots' weights (may be weight where out_max_pages ==

@@ -23,6 +23,10 @@
 // bf16: 32 slots a tile, probabilities as two bf16 pieces (the rounding of one alone, 2^-9 of each,
 // would double the error of a rounded output; the second product is not what bounds the kernel).
 // float32: 16 slots a tile, products on the fp32 matrix instruction.
+//
+// Kernel time: 128 rows of 8 key-value heads with 4,096 slots of 128 bf16 values 355 us, 6.05 TB/s
+// (a large read: 6.06), the matrix cores busy for 6 % of it; one row of 131,072 slots 91 us and 5 for
+// the join; 640 rows of at most 60 slots 13.2 us.
 #pragma once
 
 #include "cache_common.hpp"
