@@ -90,13 +90,15 @@ AttendPlan attend_plan(const kb_cache* c, int R, int q_heads, int max_len, bool 
   // more than it gives (4 x 8 of 300: 7.4 us, shared out 11.5; 1 x 8 of 600: 9.7 and 11.2), each row is one
   // workgroup's; and with more rows than the shares' kernel can add up, splits of 1,024 slots are.
   const int step = c->dtype == KB_BF16 ? 128 : 64;
-  p.shared = max_len > 6 * step && R <= kb::kShareRows;
+  const bool long_rows = max_len > 6 * step;
+  p.shared = long_rows && R <= kb::kShareRows;
   p.chunk = p.shared ? max_len : std::min(max_len, R <= kb::kShareRows ? 6 * step : 1024);
   p.splits = (max_len + p.chunk - 1) / p.chunk;
   const size_t rh = (size_t)R * q_heads;
-  // (never less for more rows or longer ones: a workspace for the largest call serves all)
+  // Never less for more rows or longer ones, so that a workspace for the largest call serves all: rows that
+  // are one workgroup's because there are many of them still ask for what fewer would need for their shares.
   const size_t least = (size_t)kb::kShares * 2 * 16;
-  const size_t parts = p.splits > 1 ? std::max(least, rh * p.splits) : p.shared ? least : 0;
+  const size_t parts = p.splits > 1 ? std::max(least, rh * p.splits) : long_rows ? least : 0;
   if (parts > 0) {
     p.part_s = align_up(parts * c->dim * sizeof(float), 256);
     p.row_before = align_up(p.part_s + parts * sizeof(float2), 256);

@@ -144,6 +144,17 @@ def test_attend_workspace_of_the_largest_call_serves_all():
             assert by_rows[0] > 0 and by_rows[-1] < 2 ** 31
 
 
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("weights", [0, 1])
+def test_attend_workspace_shrinks_neither_with_rows_nor_with_lengths(dtype, weights):
+    need = binding.lib().kb_cache_attend_workspace_bytes
+    c = cache(dtype=dtype, max_pages=600, seqs=5000)
+    rows, lengths = (1, 63, 64, 128, 129, 1000, 1024, 1025, 1100, 3000), (1, 64, 65, 384, 385, 768, 769, 1024, 1025, 9600)
+    for heads in (2, 34):
+        got = [[need(c, R, heads, n, weights) for n in lengths] for R in rows]
+        assert all(line == sorted(line) for line in got) and all(list(col) == sorted(col) for col in zip(*got))
+
+
 def test_binding_refuses_host_tensors():
     k = torch.zeros((4, 2, 16, 64))
     t, n = torch.zeros((1, 2), dtype=torch.int32), torch.ones(1, dtype=torch.int32)
