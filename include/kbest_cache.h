@@ -122,7 +122,8 @@ kb_status kb_cache_append(const kb_cache* cache, int R, const int32_t* n_dev, in
  *   length       R int32: slots to attend to, the new token's included.
  *   max_len      host-side bound of the lengths: longer ones are cut to it.
  *                At least 1; the work is split for it.
- *   out          R x q_heads x dim, 16-byte aligned.
+ *   out          R x q_heads x dim, 16-byte aligned; overlaps neither q nor the
+ *                cache.
  *   lse          nullable, R x q_heads float32: log sum_t exp(score).
  *   weight_out   nullable, seqs x heads x (max_pages * page_size) float32:
  *                weight_out[r, head, t] = weight_in[r, head, t] + the sum of

@@ -656,6 +656,7 @@ def _ask(t, name: str, dtype, numel: int, dev: int) -> int:
     return _refuse(t, name, dtype, numel, dev)
 
 
+_INT_MAX = 2 ** 31 - 1
 _device_now = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
@@ -694,6 +695,8 @@ def _cache(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor):
         raise ValueError("table must be seqs x max_pages")
     pages, heads, page_size, dim = shape
     seqs, max_pages = table.shape
+    if pages > _INT_MAX or seqs > _INT_MAX or max_pages > _INT_MAX:  # ctypes would cut them to 32 bits
+        raise ValueError(f"{pages} pages, a table of {seqs} x {max_pages}: beyond 32 bits")
     return (_Cache(_dtype_code(k_cache, "k_cache"), heads, dim, page_size, pages, seqs, max_pages, kp, vp, tp), dev,
             dtype, heads, dim, max_pages * page_size, seqs)
 
@@ -771,7 +774,8 @@ def cache_attend_workspace_bytes(k_cache: torch.Tensor, v_cache: torch.Tensor, t
                                  q_heads: int, max_len: Optional[int] = None, weights: bool = False) -> int:
     """Bytes that cache_attend's ``ws`` needs for R rows of q_heads heads (``weights``: with ``weight_out``)."""
     c, _, _, _, _, cap, _ = _cache(k_cache, v_cache, table)
-    return int(lib().kb_cache_attend_workspace_bytes(c, R, q_heads, cap if max_len is None else max_len, int(weights)))
+    max_len = cap if max_len is None else min(max_len, cap)
+    return int(lib().kb_cache_attend_workspace_bytes(c, R, q_heads, max_len, int(weights)))
 
 
 def cache_attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor,
@@ -803,7 +807,7 @@ def cache_attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, 
     nd = None if n_dev is None else _ask(n_dev, "n_dev", i32, 1, dev)
     wi = None if weight_in is None else _ask(weight_in, "weight_in", f32, seqs * heads * cap, dev)
     wo = None if weight_out is None else _ask(weight_out, "weight_out", f32, seqs * heads * cap, dev)
-    if max_len is None:
+    if max_len is None or max_len > cap:
         max_len = cap
     L = lib()
     need = L.kb_cache_attend_workspace_bytes(c, R, q_heads, max_len, 0 if wo is None else 1)
@@ -832,6 +836,8 @@ def cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tenso
     ``position`` is; length and, in place, weight and position may be the inputs).
     """
     c, dev, _, heads, _, cap, seqs = _cache(k_cache, v_cache, table)
+    if keep > _INT_MAX:
+        raise ValueError(f"keep = {keep}: beyond 32 bits")
     i32, f32 = torch.int32, torch.float32
     lp = _ask(length, "length", i32, 0, dev)
     R = length.numel()

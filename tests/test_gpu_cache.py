@@ -225,6 +225,39 @@ def test_attend_shared_sequences(kb, dtype):
     assert torch.equal(a, b)
 
 
+def test_bounds_past_32_bits(kb):
+    """A bound of the lengths above the table's slots is the table's slots, whatever its low 32 bits are; a
+    budget that C cannot hold is refused."""
+    g = torch.Generator().manual_seed(77)
+    k, v, table = make_cache(g, torch.float32, 2, 1, 16, 4, 40)
+    length = torch.tensor([40, 33], dtype=torch.int32)
+    fill(g, k, v, table, length)
+    q = torch.randn(2, 2, 16, generator=g).cuda()
+    dk, dv, dt, dl = k.cuda(), v.cuda(), table.cuda(), length.cuda()
+    want = kb.cache_attend(q, dk, dv, dt, dl)
+    got = kb.cache_attend(q, dk, dv, dt, dl, max_len=2 ** 32 + 5)
+    assert torch.equal(got, want)
+    assert kb.cache_attend_workspace_bytes(dk, dv, dt, 2, 2, 2 ** 32 + 5, True) == kb.cache_attend_workspace_bytes(
+        dk, dv, dt, 2, 2, weights=True)
+    with pytest.raises(ValueError, match="32 bits"):
+        kb.cache_evict(dk, dv, dt, dl, 2 ** 32 + 4, weight=torch.zeros(2, 1, 40, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_workspace_for_many_rows_serves_fewer(kb, dtype):
+    """1,100 rows of up to 1,000 slots are a workgroup's each, 1,000 of the same lengths are shared out."""
+    g = torch.Generator().manual_seed(78)
+    k, v, table = make_cache(g, dtype, 1100, 1, 16, 8, 1000)
+    length = torch.randint(0, 1001, (1100,), generator=g, dtype=torch.int32)
+    length[0], length[1] = 1000, 0
+    fill(g, k, v, table, length)
+    q = torch.randn(1100, 1, 16, generator=g).to(dtype)
+    ws = torch.empty(kb.cache_attend_workspace_bytes(k.cuda(), v.cuda(), table.cuda(), 1100, 1), dtype=torch.uint8,
+                     device="cuda")
+    check_attend(kb, q, k, v, table, length, ws=ws)
+    check_attend(kb, q[:1000], k, v, table, length[:1000], ws=ws)
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
 def test_attend_large_scores(kb, dtype):
     """Scores far apart and far from zero: one slot takes all the weight, at the first, a middle and the last place,
