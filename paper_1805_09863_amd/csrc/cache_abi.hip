@@ -245,8 +245,9 @@ kb_status kb_cache_evict(const kb_cache* cache, int R, const int32_t* n_dev, con
   if ((out_weight == weight || (position && out_position == position)) && out_max_pages != cache->max_pages)
     return fail(KB_ERR_INVALID_ARG, "out_weight and out_position of another row length cannot be weight and position");
   const kb::EvictArgs a{view(cache), R,      keep,     first,     recent,     out_max_pages, n_dev,        length,
-                        newest,      weight, position, out_table, out_length, out_weight,    out_position, source};
-  hipError_t e = kb::launch_cache_evict(bf16(cache), a, reinterpret_cast<hipStream_t>(stream));
+                        newest,      weight, position, out_table, out_length, out_weight,    out_position, source,
+                        cache->dim * (bf16(cache) ? 2 : 4) / 16};
+  hipError_t e = kb::launch_cache_evict(a, reinterpret_cast<hipStream_t>(stream));
   if (e != hipSuccess) return fail(KB_ERR_HIP, "cache eviction kernel launch: %s", hipGetErrorString(e));
   return ok();
 }

@@ -102,11 +102,12 @@ struct EvictArgs {
   float* out_weight;
   int32_t* out_position;
   int32_t* source;
+  int units;  // 16-byte pieces of a row
 };
 
 hipError_t launch_cache_append(int bf16, const AppendArgs& a, hipStream_t st);
 hipError_t launch_cache_attend(int bf16, AttendArgs& a, hipStream_t st);
-hipError_t launch_cache_evict(int bf16, const EvictArgs& a, hipStream_t st);
+hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t st);
 
 // Row (of dim values, in k or v) of slot t of a sequence whose table row is
 // `pages`, for key-value head `head`; -1 for a hole.  Rows are counted in 32

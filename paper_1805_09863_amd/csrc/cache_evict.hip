@@ -5,7 +5,7 @@
 // the top, 11, 11 and 10 bits a pass: T, the bits settled so far of it, and how many of the slots
 // that agree with T in them are kept (the lowest ones).  A pass that needs every slot of the digit
 // it picks is the last.  The kept slots from n on then fill the places of the dropped slots below
-// n, and a second kernel moves the rows.
+// n; the workgroup moves the rows itself, or a second launch does.
 //
 // What bounds the selection is the chain of its passes, not the weights' bytes: keys are read once
 // and stay in LDS; the two counters a digit keep a wave whose weights share their exponent from
@@ -13,8 +13,9 @@
 // ordered part needs three barriers in all.  Lengths above kEvictLds take their keys from memory in
 // every pass.
 //
-// Kernel time: 4 sequences of 8 heads and 32,768 slots, 32 workgroups, 29 us to select and 13.3 us to
-// move 67 MB in and out (5.0 TB/s); 16 sequences of 8 heads and 257 slots 7.4 and 3.1 us.
+// Kernel time: 16 sequences of 8 heads, 257 slots to 256, 8.4 us (with a second launch 7.4 and 3.1);
+// 64 sequences of 8 heads, up to 1,100 to 512, 14.0 us (9 and 7.8); 4 sequences of 8 heads, 32,768 to
+// 2,048, 32 workgroups, 28.5 us and a second launch's 13.0 to move 67 MB in and out (5.1 TB/s).
 #include <atomic>
 
 #include "cache_common.hpp"
@@ -61,7 +62,52 @@ __device__ __forceinline__ int scan(int x, int* wave_sums, int& total) {
   return before + y - x;
 }
 
-template <int T>
+// The lanes of m below this one.
+__device__ __forceinline__ int lanes_below(uint64_t m) {
+  return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+}
+
+// A wave's places t of head h of row r (live: t < n), whose rows come from slots `from`: weights, positions,
+// and the rows that move, 16 lanes a row, kUnroll times 4 rows in flight.
+__device__ __forceinline__ void put_places(const EvictArgs& a, int r, int h, int t, int from, bool live) {
+  constexpr int kUnroll = 4;
+  const CacheView& c = a.c;
+  const int lane = threadIdx.x & 63, units = a.units;
+  int at = -1, to = -1;
+  if (live) {
+    const int64_t rh = (int64_t)r * c.heads + h, in = rh * c.cap + from;
+    const int64_t out = rh * ((int64_t)a.out_max_pages << c.log_ps) + t;
+    a.out_weight[out] = a.weight[in];
+    if (a.position) a.out_position[out] = a.position[in];
+    at = cache_row(c, c.table + (int64_t)r * c.max_pages, h, from);
+    to = cache_row(c, a.out_table + (int64_t)r * a.out_max_pages, h, t);
+  }
+  const bool moves = at >= 0 && to >= 0 && at != to;
+  const uint64_t m = __ballot(moves);
+  const int count = __popcll(m), rank = lanes_below(m), lane_to = (moves ? rank : count + lane - rank) * 4;
+  at = __builtin_amdgcn_ds_permute(lane_to, at);  // those that move first
+  to = __builtin_amdgcn_ds_permute(lane_to, to);
+  typedef uint32_t Piece __attribute__((ext_vector_type(4)));
+  Piece *k = (Piece*)c.k, *v = (Piece*)c.v;
+  for (int i0 = 0; i0 < count; i0 += 4 * kUnroll)
+    for (int u0 = 0; u0 < units; u0 += 16) {  // past the last row or its end: that one again
+      const int u = min(u0 + (lane & 15), units - 1);
+      Piece x[kUnroll], y[kUnroll];
+      int64_t put[kUnroll];
+#pragma unroll
+      for (int j = 0; j < kUnroll; ++j) {
+        const int i = min(i0 + 4 * j + (lane >> 4), count - 1);
+        const int64_t get = (int64_t)__shfl(at, i) * units + u;
+        put[j] = (int64_t)__shfl(to, i) * units + u;
+        x[j] = k[get], y[j] = v[get];
+      }
+#pragma unroll
+      for (int j = 0; j < kUnroll; ++j) k[put[j]] = x[j], v[put[j]] = y[j];
+    }
+}
+
+// MOVE: the workgroup moves its rows itself.
+template <int T, bool MOVE>
 __global__ __launch_bounds__(T) void cache_evict_select(EvictArgs a, int room) {
   // keys, later a list of slots (lengths up to room); a mask and a count for each 64 slots
   extern __shared__ __align__(16) uint32_t lds[];
@@ -73,8 +119,18 @@ __global__ __launch_bounds__(T) void cache_evict_select(EvictArgs a, int room) {
   const int L = max(0, min(a.length[r], c.cap)), n = min(L, a.keep);
   int32_t* source = a.source + ((int64_t)r * c.heads + h) * a.keep;
   for (int i = n + tid; i < a.keep; i += T) source[i] = -1;
+  if (MOVE && h == 0 && tid == 0 && a.out_length != a.length) a.out_length[r] = n;
+  constexpr int W = T / 64;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // places that a wave takes at a time: fewer where their rows would keep few waves busy
+  const int run = !MOVE || n >= W * 64 ? 64 : n >= W * 32 ? 32 : 16;
   if (L == n) {
-    for (int i = tid; i < n; i += T) source[i] = i;
+    for (int t0 = w * run; t0 < n; t0 += W * run) {
+      const int t = t0 + lane;
+      const bool live = lane < run && t < n;
+      if (live) source[t] = t;
+      if constexpr (MOVE) put_places(a, r, h, t, t, live);
+    }
     return;
   }
   const int64_t at = ((int64_t)r * c.heads + h) * c.cap;
@@ -170,16 +226,12 @@ __global__ __launch_bounds__(T) void cache_evict_select(EvictArgs a, int room) {
   }
 
   // Each wave takes a run of whole 64-slot strips; what is uniform in it stays on the scalar unit.
-  constexpr int W = T / 64;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6), strips = (L + 63) / 64;
+  const int strips = (L + 63) / 64;
   const int per = (strips + W - 1) / W, s0 = min(w * per, strips), s1 = min(s0 + per, strips);
   const int marks = held ? room / 64 : strips;
   uint64_t* kept = (uint64_t*)(lds + (held ? room : 0));  // each strip's kept slots
   int* before = (int*)(kept + marks);                     // and their number in the strips before
   auto key_at = [&](int t) { return (held ? lds[min(t, L - 1)] : key(min(t, L - 1))) & mask; };
-  auto below = [](uint64_t m) {  // the lanes of m below this one
-    return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
-  };
 
   int all, ties = 0;  // slots that agree with top, in the strips before
   if (same != need) {
@@ -200,7 +252,7 @@ __global__ __launch_bounds__(T) void cache_evict_select(EvictArgs a, int room) {
         m = __ballot((t < L) & (x >= top));
       } else {
         const uint64_t tie = __ballot((t < L) & (x == top));
-        m = __ballot((t < L) & ((x > top) | ((x == top) & (ties + below(tie) < need))));
+        m = __ballot((t < L) & ((x > top) | ((x == top) & (ties + lanes_below(tie) < need))));
         ties += __popcll(tie);
       }
       mine = lane == s - batch ? m : mine;
@@ -243,18 +295,18 @@ __global__ __launch_bounds__(T) void cache_evict_select(EvictArgs a, int room) {
                      (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), z - s0) << 32;
         const int first = z == sn ? 0 : __builtin_amdgcn_readlane(rank, z - s0);
         if (z == sn) m &= ~low;
-        if (__builtin_amdgcn_inverse_ballot_w64(m)) lds[first + below(m)] = z * 64 + lane;
+        if (__builtin_amdgcn_inverse_ballot_w64(m)) lds[first + lanes_below(m)] = z * 64 + lane;
       }
     }
     __syncthreads();
   }
-  for (int s = w; s * 64 < n; s += W) {
-    const int t = s * 64 + lane;
+  for (int t0 = w * run; t0 < n; t0 += W * run) {
+    const int t = t0 + lane, s = t0 / 64, bit = t & 63;
     const uint64_t m = kept[s];
-    const bool stays = m >> lane & 1;
-    const int j = t - before[s] - __popcll(m & ((1ull << lane) - 1));
+    const bool live = lane < run && t < n, stays = m >> bit & 1;
+    const int j = t - before[s] - __popcll(m & ((1ull << bit) - 1));
     int from = t;
-    if (t < n && !stays) {
+    if (live && !stays) {
       if (held) {
         from = lds[j];
       } else {
@@ -269,14 +321,19 @@ __global__ __launch_bounds__(T) void cache_evict_select(EvictArgs a, int room) {
         from = lo * 64 + __ffsll((unsigned long long)bits) - 1;
       }
     }
-    if (t < n) source[t] = from;
+    if (live) source[t] = from;
+    if constexpr (MOVE) put_places(a, r, h, t, from, live);
   }
 }
 
-// Rows to their places: 16 lanes a row, 16 bytes of key and value each at a time.  A chain of
-// dependent loads (source, table, row) bounds it where few rows move.
-__global__ __launch_bounds__(256) void cache_evict_move(EvictArgs a, int units) {
+__device__ __forceinline__ int kept_of(const EvictArgs& a, int r) {
+  return min(max(0, min(a.length[r], a.c.cap)), a.keep);
+}
+
+// Rows to their places by the whole card: 16 lanes a row, 16 bytes of key and value each at a time.
+__global__ __launch_bounds__(256) void cache_evict_move(EvictArgs a) {
   const CacheView& c = a.c;
+  const int units = a.units;
   const int r = blockIdx.x / c.heads, h = blockIdx.x % c.heads, lane = threadIdx.x % 16;
   if (r >= rows_of(a.R, a.n_dev)) return;
   const int places = min(a.keep, c.cap);
@@ -300,44 +357,71 @@ __global__ __launch_bounds__(256) void cache_evict_move(EvictArgs a, int units) 
       if (a.position) a.out_position[out + i] = a.position[in + s];
     }
   }
-  if (h == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.out_length[r] = min(max(0, min(a.length[r], c.cap)), a.keep);
+  if (h == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.out_length[r] = kept_of(a, r);
+}
+
+// New lengths in place of the old ones, which every head's workgroup above reads.
+__global__ __launch_bounds__(256) void cache_evict_lengths(EvictArgs a) {
+  const int r = blockIdx.x * 256 + threadIdx.x;
+  if (r < rows_of(a.R, a.n_dev)) a.out_length[r] = kept_of(a, r);
 }
 
 // A workgroup of 256 threads holds up to 2,048 keys: its passes are shorter than those of 1,024
 // threads, and more workgroups share a unit.
 constexpr int kEvictSmall = 2048;
 
-// Raises the kernel's LDS ceiling, once per device.
-static hipError_t raise_lds_ceiling() {
+// Raises the long kernel's LDS ceiling, once per device.
+template <bool MOVE>
+hipError_t raise_lds_ceiling() {
   constexpr int kMaxDevices = 64;
   static std::atomic<bool> done[kMaxDevices];
   int dev = -1;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess || dev < 0 || dev >= kMaxDevices) return e != hipSuccess ? e : hipErrorInvalidDevice;
   if (done[dev].load(std::memory_order_acquire)) return hipSuccess;
-  e = hipFuncSetAttribute(reinterpret_cast<const void*>(&cache_evict_select<1024>),
+  e = hipFuncSetAttribute(reinterpret_cast<const void*>(&cache_evict_select<1024, MOVE>),
                           hipFuncAttributeMaxDynamicSharedMemorySize, kEvictLds * 4 + kEvictLds / 64 * 12);
   if (e == hipSuccess) done[dev].store(true, std::memory_order_release);
   return e;
 }
 
-hipError_t launch_cache_evict(int bf16, const EvictArgs& a, hipStream_t st) {
+template <bool MOVE>
+hipError_t launch_select(const EvictArgs& a, hipStream_t st) {
   const int strips = (a.c.cap + 63) / 64, room = min(strips * 64, kEvictLds);
   const size_t lds = max((size_t)room * 4 + room / 64 * 12, (size_t)strips * 12);
   const dim3 grid(a.R * a.c.heads);
   if (room <= kEvictSmall) {
-    cache_evict_select<256><<<grid, dim3(256), lds, st>>>(a, room);
+    cache_evict_select<256, MOVE><<<grid, dim3(256), lds, st>>>(a, room);
   } else {
-    const hipError_t e = raise_lds_ceiling();
+    const hipError_t e = raise_lds_ceiling<MOVE>();
     if (e != hipSuccess) return e;
-    cache_evict_select<1024><<<grid, dim3(1024), lds, st>>>(a, room);
+    cache_evict_select<1024, MOVE><<<grid, dim3(1024), lds, st>>>(a, room);
   }
-  hipError_t e = hipGetLastError();
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t st) {
+  const int pairs = a.R * a.c.heads, places = min(a.keep, a.c.cap);
+  // A workgroup moves its head's rows itself where there are workgroups for half the card (512 heads, 4,112
+  // slots to 4,096: 36 us, with a second launch 97; 128 heads, 2,000 to 1,500: 25 and 27), or it has little to
+  // move (32 heads of 300 slots to 256 elsewhere, 128 KB: 10.0 and 11.0; of 4,112 to 4,096, 8 KB: 16.9 and
+  // 18.7), else the whole card does (32 heads, 32,768 slots to 2,048, 1 MB: 40 us, by the workgroups 53; of
+  // 4,352 to 4,096, 128 KB: 22.7 and 25.4).
+  const int most = a.out_table == a.c.table ? min(places, a.c.cap - places) : places;  // rows of a head that move
+  const int64_t few = a.c.cap <= kEvictSmall ? 128 << 10 : 32 << 10;
+  if (pairs >= 128 || (int64_t)most * a.units * 32 <= few) {
+    const hipError_t e = launch_select<true>(a, st);
+    if (e != hipSuccess || a.out_length != a.length) return e;
+    cache_evict_lengths<<<(a.R + 255) / 256, 256, 0, st>>>(a);
+    return hipGetLastError();
+  }
+  const hipError_t e = launch_select<false>(a, st);
   if (e != hipSuccess) return e;
-  // 16 rows a workgroup at a time, and no more workgroups than the card starts in a few microseconds
-  // (512 heads of at most 512 places: 8 blocks each 8.2 us, 16 9.2, 32 13.4)
-  const int pairs = a.R * a.c.heads, blocks = min((min(a.keep, a.c.cap) + 15) / 16, max(1, 4096 / pairs));
-  cache_evict_move<<<dim3(pairs, blocks), dim3(256), 0, st>>>(a, a.c.dim * (bf16 ? 2 : 4) / 16);
+  // 16 rows a workgroup at a time, and 16 workgroups a CU (rows of 128 values: as fast as 8 or 32, with 4 it is
+  // 131 us instead of 119 for 96 heads, 32,768 slots to 4,096; 8 heads, 131,072 to 65,536, rows of 8 values:
+  // 282 us, with 8 a CU 318)
+  const int blocks = min((places + 15) / 16, max(1, 4096 / pairs));
+  cache_evict_move<<<dim3(pairs, blocks), dim3(256), 0, st>>>(a);
   return hipGetLastError();
 }
 

@@ -491,6 +491,39 @@ def test_evict_ties_and_special_values(kb):
     run_evict(kb, k, v, table, length, keep, w, position=position, newest=newest, first=0, recent=5)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("R,heads,dim,page,cap,keeps", [
+    (17, 8, 64, 16, 300, (1, 20, 63, 64, 65, 130, 256)),   # many heads: the selecting workgroups move the rows
+    (43, 3, 16, 4, 2100, (100, 513, 1100)),                # the same, 16 waves each
+    (2, 2, 256, 1, 2300, (500, 1150)),                     # few heads with much to move: a second launch does
+    (127, 1, 72, 32, 700, (300,)),
+    (1, 1, 256, 8, 200, (3, 64, 100)),                     # few with little
+])
+def test_evict_by_either_mover(kb, dtype, R, heads, dim, page, cap, keeps):
+    """Rows moved by the workgroups that select them and by a launch of their own: in place, over the inputs,
+    counted on the device, and elsewhere, with rows that are within the budget."""
+    g = torch.Generator().manual_seed(R + cap)
+    length = torch.randint(0, cap + 1, (R,), generator=g, dtype=torch.int32)
+    length[0] = cap
+    k, v, table = make_cache(g, dtype, R, heads, dim, page, cap, dirty=False)
+    slots = table.shape[1] * page
+    weight = torch.rand((R, heads, slots), generator=g).round(decimals=2)  # (with ties)
+    position = torch.stack([torch.randperm(slots, generator=g) for _ in range(R * heads)])
+    position = position.view(R, heads, slots).to(torch.int32)
+    args = dict(position=position, newest=torch.full((R,), slots - 1, dtype=torch.int32))
+    for keep in keeps:
+        args.update(first=keep // 8, recent=keep // 4)
+        run_evict(kb, k, v, table, length, keep, weight, own=True, **args)
+        run_evict(kb, k, v, table, length, keep, weight, own=True, n=R - R // 3, **args)
+        run_evict(kb, k, v, table, length, keep, weight, n=R // 2, **args)
+        cols = -(-keep // page)
+        more = torch.randn((R * cols,) + tuple(k.shape[1:]), generator=g).to(dtype)
+        out_table = (torch.randperm(R * cols, generator=g) + k.shape[0]).to(torch.int32).view(R, cols)
+        out_table[0, 0] = -7
+        run_evict(kb, torch.cat([k, more]), torch.cat([v, more]), table, length, keep, weight, out_table=out_table,
+                  **args)
+
+
 @pytest.mark.parametrize("L,keeps", [(70000, (20000, 3, 69999)), (300001, (150000,)), (1 << 19, (1000,))])
 def test_evict_long(kb, L, keeps):
     """Longer than what keys fit the chip, up to the longest; ties across wave and strip borders."""
