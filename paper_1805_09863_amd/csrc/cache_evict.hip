@@ -9,20 +9,21 @@
 //
 // What bounds the selection is the chain of its passes, not the weights' bytes: keys are read once
 // and stay in LDS; the two counters a digit keep a wave whose weights share their exponent from
-// adding to one address 64 times in turn; kept slots are bit masks, 64 slots each, so that the
-// ordered part needs three barriers in all.  Lengths above kEvictLds take their keys from memory in
-// every pass.
+// adding to one address 64 times in turn; the slots kept and those still open are bit masks, 32 slots
+// a thread's word, so that the ordered part needs few barriers and later digits are counted of the
+// open slots alone.  Lengths above kEvictLds take their keys from memory where these do from LDS.
 //
 // Kernel time: 16 sequences of 8 heads, 257 slots to 256, 8.4 us (with a second launch 7.4 and 3.1);
-// 64 sequences of 8 heads, up to 1,100 to 512, 14.0 us (9 and 7.8); 4 sequences of 8 heads, 32,768 to
-// 2,048, 32 workgroups, 28.5 us and a second launch's 13.0 to move 67 MB in and out (5.1 TB/s).
+// 64 sequences of 8 heads, up to 1,100 to 512, 12.8 us (9 and 7.8); 4 sequences of 8 heads, 32,768 to
+// 2,048, 32 workgroups, 18.3 us (7.6 to read and count the first digit, 5.0 for the second, 2.4 for the
+// first masks) and a second launch's 13.0 to move 67 MB in and out (5.1 TB/s).
 #include <atomic>
 
 #include "cache_common.hpp"
 
 namespace kb {
 
-constexpr int kEvictLds = 32768;  // keys that fit: 128 KB of LDS, next to 16 KB of counters and 6 KB of masks
+constexpr int kEvictLds = 32768;  // keys that fit: 128 KB of LDS, next to 16 KB of counters and 8 KB of masks
 constexpr int kDigits = 2048, kCopies = 2;
 
 struct EvictKeys {
@@ -109,7 +110,7 @@ __device__ __forceinline__ void put_places(const EvictArgs& a, int r, int h, int
 // MOVE: the workgroup moves its rows itself.
 template <int T, bool MOVE>
 __global__ __launch_bounds__(T) void cache_evict_select(EvictArgs a, int room) {
-  // keys, later a list of slots (lengths up to room); a mask and a count for each 64 slots
+  // keys, later a list of slots (lengths up to room); two masks, one later a count, for each 32 slots
   extern __shared__ __align__(16) uint32_t lds[];
   __shared__ __align__(16) int hist[kDigits * kCopies];
   __shared__ int wsum[T / 64], pick[3];
@@ -141,69 +142,27 @@ __global__ __launch_bounds__(T) void cache_evict_select(EvictArgs a, int room) {
   const bool held = L <= room;  // keys in LDS
   const bool whole = (((uintptr_t)key.weight | (uintptr_t)key.position) & 15) == 0 && c.cap % 4 == 0;
 
-  uint32_t top = 0, mask = 0;
-  int need = n, same = L;  // of the `same` slots whose key agrees with top in the bits of mask, keep the lowest `need`
-  for (int pass = 0; pass < 3 && same != need; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11;
-    for (int i = tid * 4; i < kDigits * kCopies; i += T * 4) *(int4*)&hist[i] = make_int4(0, 0, 0, 0);
-    __syncthreads();
-    auto count_in = [&](uint32_t x) {
-      const bool in = (x & mask) == top;
-      const uint64_t ins = __ballot(in);
-      if (ins == 0) return;
-      const int digit = x >> shift & ((1 << width) - 1);
-      if (__popcll(ins) >= 48) {
-        const int one = __ffsll((unsigned long long)ins) - 1;
-        if (__ballot(in & (digit == __builtin_amdgcn_readlane(digit, one))) == ins) {  // equal digits: one adds
-          if (lane == one) atomicAdd(&hist[digit * kCopies], __popcll(ins));
-          return;
-        }
-      }
-      if (in) atomicAdd(&hist[digit * kCopies + (lane & (kCopies - 1))], 1);
-    };
-    if (held && pass > 0) {
-#pragma unroll 8
-      for (int t = tid; t < L; t += T) count_in(lds[t]);
-    } else if (held && whole) {
-      constexpr int U = T / 256;  // 16-byte loads in flight; the last may reach past L, not past the row
-      for (int t0 = tid * 4; t0 < L; t0 += U * T * 4) {
-        float4 w[U];
-        int4 p[U];
-#pragma unroll
-        for (int j = 0; j < U; ++j) {
-          const int t = min(t0 + j * T * 4, (L - 1) & ~3);
-          w[j] = *(const float4*)(key.weight + t);
-          p[j] = key.position ? *(const int4*)(key.position + t) : make_int4(key.lo, key.lo, key.lo, key.lo);
-        }
-#pragma unroll
-        for (int j = 0; j < U; ++j) {
-          const int t = t0 + j * T * 4;
-          if (t >= L) break;
-          const uint4 x = make_uint4(key.of(w[j].x, p[j].x), key.of(w[j].y, p[j].y), key.of(w[j].z, p[j].z),
-                                     key.of(w[j].w, p[j].w));
-          *(uint4*)&lds[t] = x;
-          count_in(x.x);
-          if (t + 1 < L) count_in(x.y);
-          if (t + 2 < L) count_in(x.z);
-          if (t + 3 < L) count_in(x.w);
-        }
-      }
-    } else {
-      constexpr int U = T / 64;  // loads in flight
-      for (int t0 = tid; t0 < L; t0 += U * T) {
-        uint32_t x[U];
-#pragma unroll
-        for (int j = 0; j < U; ++j) x[j] = key(min(t0 + j * T, L - 1));
-#pragma unroll
-        for (int j = 0; j < U; ++j)
-          if (t0 + j * T < L) {
-            if (held) lds[t0 + j * T] = x[j];
-            count_in(x[j]);
-          }
+  // Counts of digits; equal digits of a wave: one lane adds.
+  auto add = [&](bool in, int digit) {
+    const uint64_t ins = __ballot(in);
+    if (ins == 0) return;
+    if (__popcll(ins) >= 48) {
+      const int one = __ffsll((unsigned long long)ins) - 1;
+      if (__ballot(in & (digit == __builtin_amdgcn_readlane(digit, one))) == ins) {
+        if (lane == one) atomicAdd(&hist[digit * kCopies], __popcll(ins));
+        return;
       }
     }
+    if (in) atomicAdd(&hist[digit * kCopies + (lane & (kCopies - 1))], 1);
+  };
+  auto clear = [&] {
+    for (int i = tid * 4; i < kDigits * kCopies; i += T * 4) *(int4*)&hist[i] = make_int4(0, 0, 0, 0);
     __syncthreads();
-    // digits from the largest down, kDigits / T a thread
+  };
+  int need = n, same = L;  // of the `same` slots whose key agrees with T in the bits settled, keep the lowest `need`
+  // The digit of T, from the largest down, kDigits / T a thread.
+  auto pick_digit = [&] {
+    __syncthreads();
     constexpr int B = kDigits / T;
     const int d0 = kDigits - 1 - tid * B;
     int copy[B * kCopies], count[B], mine = 0, all;
@@ -220,108 +179,198 @@ __global__ __launch_bounds__(T) void cache_evict_select(EvictArgs a, int room) {
       before += count[j];
     }
     __syncthreads();
-    top |= (uint32_t)pick[0] << shift;
-    mask |= ((1u << width) - 1) << shift;
     need = pick[1], same = pick[2];
-  }
+    return (uint32_t)pick[0];
+  };
 
-  // Each wave takes a run of whole 64-slot strips; what is uniform in it stays on the scalar unit.
-  const int strips = (L + 63) / 64;
-  const int per = (strips + W - 1) / W, s0 = min(w * per, strips), s1 = min(s0 + per, strips);
-  const int marks = held ? room / 64 : strips;
-  uint64_t* kept = (uint64_t*)(lds + (held ? room : 0));  // each strip's kept slots
-  int* before = (int*)(kept + marks);                     // and their number in the strips before
-  auto key_at = [&](int t) { return (held ? lds[min(t, L - 1)] : key(min(t, L - 1))) & mask; };
-
-  int all, ties = 0;  // slots that agree with top, in the strips before
-  if (same != need) {
-#pragma unroll 4
-    for (int s = s0; s < s1; ++s) ties += __popcll(__ballot((s * 64 + lane < L) & (key_at(s * 64 + lane) == top)));
-    ties = __builtin_amdgcn_readfirstlane(scan<T>(lane == 0 ? ties : 0, wsum, all));
-  }
-  int count = 0;  // of the wave's kept slots
-  uint64_t mine = 0;
-  for (int batch = s0; batch < s1; batch += 64) {  // lane j: strip batch + j; with keys in LDS there is one batch
-    mine = 0;
-#pragma unroll 4
-    for (int s = batch; s < min(s1, batch + 64); ++s) {
-      const int t = s * 64 + lane;
-      const uint32_t x = key_at(t);
-      uint64_t m;
-      if (same == need) {
-        m = __ballot((t < L) & (x >= top));
-      } else {
-        const uint64_t tie = __ballot((t < L) & (x == top));
-        m = __ballot((t < L) & ((x > top) | ((x == top) & (ties + lanes_below(tie) < need))));
-        ties += __popcll(tie);
-      }
-      mine = lane == s - batch ? m : mine;
-    }
-    int sum = __popcll(mine);
-    const int own = sum;
+  clear();
+  if (held && whole) {
+    constexpr int U = T / 256;  // 16-byte loads in flight; the last may reach past L, not past the row
+    for (int t0 = tid * 4; t0 < L; t0 += U * T * 4) {
+      float4 x[U];
+      int4 p[U];
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int z = __shfl_up(sum, d);
-      if (lane >= d) sum += z;
+      for (int j = 0; j < U; ++j) {
+        const int t = min(t0 + j * T * 4, (L - 1) & ~3);
+        x[j] = *(const float4*)(key.weight + t);
+        p[j] = key.position ? *(const int4*)(key.position + t) : make_int4(key.lo, key.lo, key.lo, key.lo);
+      }
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        const int t = t0 + j * T * 4;
+        if (t >= L) break;
+        const uint4 y = make_uint4(key.of(x[j].x, p[j].x), key.of(x[j].y, p[j].y), key.of(x[j].z, p[j].z),
+                                   key.of(x[j].w, p[j].w));
+        *(uint4*)&lds[t] = y;
+        const uint32_t d[4] = {y.x >> 21, y.y >> 21, y.z >> 21, y.w >> 21};
+        if (t + 4 <= L) {  // one test for the four: a test each costs more than the counting
+          const uint32_t f = __builtin_amdgcn_readfirstlane(d[0]);
+          const uint64_t on = __ballot(true);
+          if (__ballot(((d[0] ^ f) | (d[1] ^ f) | (d[2] ^ f) | (d[3] ^ f)) == 0) == on) {
+            if (lane == __ffsll((unsigned long long)on) - 1) atomicAdd(&hist[f * kCopies], 4 * __popcll(on));
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) atomicAdd(&hist[d[i] * kCopies + (lane & (kCopies - 1))], 1);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 3; ++i)
+            if (t + i < L) atomicAdd(&hist[d[i] * kCopies], 1);
+        }
+      }
     }
-    if (batch + lane < s1) kept[batch + lane] = mine, before[batch + lane] = count + sum - own;
-    count += __shfl(sum, 63);
+  } else {
+    constexpr int U = T / 64;  // loads in flight
+    for (int t0 = tid; t0 < L; t0 += U * T) {
+      uint32_t x[U];
+#pragma unroll
+      for (int j = 0; j < U; ++j) x[j] = key(min(t0 + j * T, L - 1));
+#pragma unroll
+      for (int j = 0; j < U; ++j)
+        if (t0 + j * T < L) {
+          if (held) lds[t0 + j * T] = x[j];
+          add(true, x[j] >> 21);
+        }
+    }
   }
-  // scan<T>'s barriers also part the keys' last reads from the list that takes their place
-  count = scan<T>(lane == 0 ? count : 0, wsum, all);
-  count = __shfl(count, 0);
-  for (int s = s0 + lane; s < s1; s += 64) before[s] += count;
+  uint32_t low_key = pick_digit() << 21, high_key = low_key | ((1u << 21) - 1);  // the keys that agree with T
+
+  const int strips = (L + 63) / 64, words = (L + 31) / 32;
+  uint32_t* marks = lds + (held ? room : 0);  // a strip's 2 words of kept slots, 2 of open ones
+  auto word = [](int i) { return i / 2 * 4 + (i & 1); };  // word i of the kept slots; its open ones 2 on
+  auto key_at = [&](int t) { return held ? lds[t] : key(t); };
+  // The slots kept for a key above those that agree with T, and those that agree, the open ones.  With keys in
+  // LDS a thread takes a word, its 16-byte pieces in an order that has a wave read from all banks (a strip a
+  // wave, by ballots: 12,600 cycles for 512 strips, this 5,000); keys in memory are read in their order.
+  auto mark = [&] {
+    if (held) {
+      for (int i = tid; i < strips * 2; i += T) {
+        const int left = L - i * 32;
+        const uint32_t in = left >= 32 ? ~0u : left > 0 ? (1u << left) - 1 : 0;
+        uint32_t more = 0, least = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int at = ((j + i) & 7) * 4;
+          const uint4 x = *(const uint4*)&lds[i * 32 + at];
+          auto four = [&](auto f) {
+            uint32_t b = f(x.w);
+            b = b + b + f(x.z);
+            b = b + b + f(x.y);
+            return b + b + f(x.x);
+          };
+          more |= four([&](uint32_t k) { return k > high_key; }) << at;
+          least |= four([&](uint32_t k) { return k >= low_key; }) << at;
+        }
+        marks[word(i)] = more & in, marks[word(i) + 2] = least & ~more & in;
+      }
+      return;
+    }
+    for (int s = w; s < strips; s += W) {
+      const uint32_t x = key(min(s * 64 + lane, L - 1));
+      const uint64_t in = s * 64 + 64 <= L ? ~0ull : (1ull << (L & 63)) - 1;
+      const uint64_t more = __ballot(x > high_key) & in, open = __ballot(x >= low_key) & in & ~more;
+      if (lane == 0)
+        *(uint4*)&marks[s * 4] =
+            make_uint4((uint32_t)more, (uint32_t)(more >> 32), (uint32_t)open, (uint32_t)(open >> 32));
+    }
+  };
+  // Where few of many slots are open, the next digits are counted of them alone, a thread a word (32 heads of
+  // 32,768 slots: 27 us, 33 of all slots; with all slots open 54 and 44; 128 heads of 257 slots 10.9 and 8.0).
+  // It takes its bits from the lane's number on, so that the keys that a wave reads lie in many banks.
+  const bool few = T == 1024 && same < L / 4;
+  const int turn = lane & 31;
+  auto open_of = [&](int i) { return __builtin_rotateright32(i < words ? marks[word(i) + 2] : 0, turn); };
+  auto slot_of = [&](int i, uint32_t bits) { return i * 32 + ((__ffs(bits) - 1 + turn) & 31); };
+  if (few) mark();
+  for (int pass = 1; pass < 3 && same != need; ++pass) {
+    const int shift = pass == 1 ? 10 : 0, digits = pass == 1 ? 2047 : 1023;
+    clear();
+    if (few) {
+      for (int i = tid; i - tid < words; i += T)
+        for (uint32_t bits = open_of(i); __ballot(bits != 0) != 0; bits &= bits - 1)
+          add(bits != 0, bits != 0 ? key_at(slot_of(i, bits)) >> shift & digits : 0);
+    } else {
+#pragma unroll 8
+      for (int t = tid; t < L; t += T) {
+        const uint32_t x = key_at(t);
+        add((x >= low_key) & (x <= high_key), x >> shift & digits);
+      }
+    }
+    low_key |= pick_digit() << shift, high_key = low_key | ((1u << shift) - 1);
+    if (few)
+      for (int i = tid; i < words; i += T) {
+        uint32_t more = 0, open = 0;
+        for (uint32_t bits = open_of(i); bits != 0; bits &= bits - 1) {
+          const int t = slot_of(i, bits);
+          const uint32_t x = key_at(t);
+          more |= (uint32_t)(x > high_key) << (t & 31);
+          open |= (uint32_t)((x >= low_key) & (x <= high_key)) << (t & 31);
+        }
+        marks[word(i)] |= more, marks[word(i) + 2] = open;
+      }
+  }
+  if (!few) mark();
+  __syncthreads();
+
+  // Open slots are kept, or the lowest `need` of them; each word's kept slots in the words before in the
+  // open ones' place.
+  int ties = 0, total = 0;
+  for (int i0 = 0; i0 < words; i0 += T) {
+    const int i = i0 + tid;
+    uint32_t open = i < words ? marks[word(i) + 2] : 0;
+    int all;
+    if (same != need) {
+      const int take = max(need - ties - scan<T>(__popc(open), wsum, all), 0);
+      ties += all;
+      if (take < __popc(open)) {
+        uint32_t rest = open;
+        for (int j = 0; j < take; ++j) rest &= rest - 1;
+        open &= ~rest;
+      }
+    }
+    const uint32_t mine = i < words ? marks[word(i)] | open : 0;
+    const int before = total + scan<T>(__popc(mine), wsum, all);
+    total += all;
+    if (i < words) marks[word(i)] = mine, marks[word(i) + 2] = before;
+  }
   __syncthreads();
 
   // A place t < n of a kept slot is its own; that of a dropped one, the j-th, j = t less the kept ones before
   // it, is the j-th kept slot from n on.
-  const int sn = n / 64;
-  const uint64_t low = (1ull << (n % 64)) - 1;
-  const int kept_below = before[sn] + __popcll(kept[sn] & low);
-  if (held) {
-    // Those in a list where the keys were: a slot's rank among the kept ones less that of slot n.  (32 strips a
-    // wave: a lane a strip, bit by bit, 2,100 cycles at 1 slot in 16 kept against 9,500 strip by strip; 8
-    // strips a wave: strip by strip, 1,800 against 3,300.)
-    const int s = s0 + lane, rank = s < s1 ? before[s] - kept_below : 0;
-    if constexpr (T == 1024) {
-      if (s >= sn && s < s1) {
-        uint64_t m = s == sn ? mine & ~low : mine;
-        for (int i = s == sn ? 0 : rank; m != 0; m &= m - 1)
-          lds[i++] = s * 64 + __ffsll((unsigned long long)m) - 1;
-      }
-    } else {
-      for (int z = max(s0, sn); z < s1; ++z) {
-        uint64_t m = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)mine, z - s0) |
-                     (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), z - s0) << 32;
-        const int first = z == sn ? 0 : __builtin_amdgcn_readlane(rank, z - s0);
-        if (z == sn) m &= ~low;
-        if (__builtin_amdgcn_inverse_ballot_w64(m)) lds[first + lanes_below(m)] = z * 64 + lane;
-      }
+  const int wn = n / 32;
+  const uint32_t low = (1u << (n % 32)) - 1;
+  const int kept_below = (int)marks[word(wn) + 2] + __popc(marks[word(wn)] & low);
+  if (held) {  // those in a list where the keys were
+    for (int i = wn + tid; i < words; i += T) {
+      uint32_t m = i == wn ? marks[word(i)] & ~low : marks[word(i)];
+      for (int j = i == wn ? 0 : (int)marks[word(i) + 2] - kept_below; m != 0; m &= m - 1) lds[j++] = i * 32 + __ffs(m) - 1;
     }
     __syncthreads();
   }
   for (int t0 = w * run; t0 < n; t0 += W * run) {
-    const int t = t0 + lane, s = t0 / 64, bit = t & 63;
-    const uint64_t m = kept[s];
-    const bool live = lane < run && t < n, stays = m >> bit & 1;
-    const int j = t - before[s] - __popcll(m & ((1ull << bit) - 1));
+    const int t = t0 + lane, bit = t & 31;
+    const bool live = lane < run && t < n;
     int from = t;
-    if (live && !stays) {
-      if (held) {
-        from = lds[j];
-      } else {
-        // the last strip with at most kept_below + j kept slots before it, then the bit of that rank
-        int lo = sn, hi = strips;
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) / 2;
-          if (before[mid] <= kept_below + j) lo = mid; else hi = mid;
+    if (live) {
+      const uint32_t m = marks[word(t / 32)];
+      const int j = t - (int)marks[word(t / 32) + 2] - __popc(m & ((1u << bit) - 1));
+      if (!(m >> bit & 1)) {
+        if (held) {
+          from = lds[j];
+        } else {
+          // the last word with at most kept_below + j kept slots before it, then the bit of that rank
+          int lo = wn, hi = words;
+          while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if ((int)marks[word(mid) + 2] <= kept_below + j) lo = mid; else hi = mid;
+          }
+          uint32_t bits = marks[word(lo)];
+          for (int i = kept_below + j - (int)marks[word(lo) + 2]; i > 0; --i) bits &= bits - 1;
+          from = lo * 32 + __ffs(bits) - 1;
         }
-        uint64_t bits = kept[lo];
-        for (int i = kept_below + j - before[lo]; i > 0; --i) bits &= bits - 1;
-        from = lo * 64 + __ffsll((unsigned long long)bits) - 1;
       }
+      source[t] = from;
     }
-    if (live) source[t] = from;
     if constexpr (MOVE) put_places(a, r, h, t, from, live);
   }
 }
@@ -380,7 +429,7 @@ hipError_t raise_lds_ceiling() {
   if (e != hipSuccess || dev < 0 || dev >= kMaxDevices) return e != hipSuccess ? e : hipErrorInvalidDevice;
   if (done[dev].load(std::memory_order_acquire)) return hipSuccess;
   e = hipFuncSetAttribute(reinterpret_cast<const void*>(&cache_evict_select<1024, MOVE>),
-                          hipFuncAttributeMaxDynamicSharedMemorySize, kEvictLds * 4 + kEvictLds / 64 * 12);
+                          hipFuncAttributeMaxDynamicSharedMemorySize, kEvictLds * 4 + kEvictLds / 64 * 16);
   if (e == hipSuccess) done[dev].store(true, std::memory_order_release);
   return e;
 }
@@ -388,7 +437,7 @@ hipError_t raise_lds_ceiling() {
 template <bool MOVE>
 hipError_t launch_select(const EvictArgs& a, hipStream_t st) {
   const int strips = (a.c.cap + 63) / 64, room = min(strips * 64, kEvictLds);
-  const size_t lds = max((size_t)room * 4 + room / 64 * 12, (size_t)strips * 12);
+  const size_t lds = max((size_t)room * 4 + room / 64 * 16, (size_t)strips * 16);
   const dim3 grid(a.R * a.c.heads);
   if (room <= kEvictSmall) {
     cache_evict_select<256, MOVE><<<grid, dim3(256), lds, st>>>(a, room);
