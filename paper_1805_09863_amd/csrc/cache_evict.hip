@@ -275,9 +275,10 @@ __global__ __launch_bounds__(T) void cache_evict_select(EvictArgs a, int room) {
     }
   };
   // Where few of many slots are open, the next digits are counted of them alone, a thread a word (32 heads of
-  // 32,768 slots: 27 us, 33 of all slots; with all slots open 54 and 44; 128 heads of 257 slots 10.9 and 8.0).
-  // It takes its bits from the lane's number on, so that the keys that a wave reads lie in many banks.
-  const bool few = T == 1024 && same < L / 4;
+  // 32,768 slots: 27 us, 33 of all slots; with all slots open 54 and 44; of 4,112 slots 18.5 and 15.8, of
+  // 16,384 22.3 and 22.4, of 257 10.9 and 8.0).  It takes its bits from the lane's number on, so that the keys
+  // that a wave reads lie in many banks.
+  const bool few = T == 1024 && L >= 16 * T && same < L / 4;
   const int turn = lane & 31;
   auto open_of = [&](int i) { return __builtin_rotateright32(i < words ? marks[word(i) + 2] : 0, turn); };
   auto slot_of = [&](int i, uint32_t bits) { return i * 32 + ((__ffs(bits) - 1 + turn) & 31); };
@@ -451,14 +452,14 @@ hipError_t launch_select(const EvictArgs& a, hipStream_t st) {
 
 hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t st) {
   const int pairs = a.R * a.c.heads, places = min(a.keep, a.c.cap);
-  // A workgroup moves its head's rows itself where there are workgroups for half the card (512 heads, 4,112
-  // slots to 4,096: 36 us, with a second launch 97; 128 heads, 2,000 to 1,500: 25 and 27), or it has little to
-  // move (32 heads of 300 slots to 256 elsewhere, 128 KB: 10.0 and 11.0; of 4,112 to 4,096, 8 KB: 16.9 and
-  // 18.7), else the whole card does (32 heads, 32,768 slots to 2,048, 1 MB: 40 us, by the workgroups 53; of
-  // 4,352 to 4,096, 128 KB: 22.7 and 25.4).
+  // A workgroup moves its head's rows itself where there is one for each CU (512 heads, 4,112 slots to 4,096:
+  // 34 us, with a second launch 95), or for a quarter of them and up to 512 KB of keys and values to move each
+  // (64 heads, 8,192 to 7,168: 35 and 40; 128 heads, 32,768 to 2,048, 1 MB: 85 and 69), or little to move (32
+  // heads, 300 to 256, 22 KB: 9.2 and 10.8; 4,112 to 4,096, 8 KB: 15.9 and 18.1); else the whole card does (32
+  // heads, 32,768 to 2,048, 1 MB: 42.8 and 30.5; 4,224 to 4,096, 64 KB: 21.3 and 19.3).
   const int most = a.out_table == a.c.table ? min(places, a.c.cap - places) : places;  // rows of a head that move
-  const int64_t few = a.c.cap <= kEvictSmall ? 128 << 10 : 32 << 10;
-  if (pairs >= 128 || (int64_t)most * a.units * 32 <= few) {
+  const int64_t bytes = (int64_t)most * a.units * 32, little = a.c.cap <= kEvictSmall ? 128 << 10 : 32 << 10;
+  if (pairs >= 256 || bytes <= (pairs >= 64 ? 512 << 10 : little)) {
     const hipError_t e = launch_select<true>(a, st);
     if (e != hipSuccess || a.out_length != a.length) return e;
     cache_evict_lengths<<<(a.R + 255) / 256, 256, 0, st>>>(a);

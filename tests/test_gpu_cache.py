@@ -536,6 +536,27 @@ def test_evict_long(kb, L, keeps):
         run_evict(kb, k, v, table, length, keep, w)
 
 
+@pytest.mark.parametrize("L,keep", [(16384, 5000), (20001, 20000), (30017, 2048), (32768, 31)])
+def test_evict_of_many_slots_with_few_open(kb, L, keep):
+    """After the first digit few slots are open, spread (row 0), side by side (row 1) or equal (row 2); all of
+    them in row 3, and no more than a quarter short of none in row 4."""
+    g = torch.Generator().manual_seed(L)
+    k, v, table = make_cache(g, torch.bfloat16, 5, 1, 8, 128, L, dirty=False)
+    slots = table.shape[1] * 128
+    length = torch.full((5,), L, dtype=torch.int32)
+    w = torch.rand((5, 1, slots), generator=g).clamp_min(1e-6) ** -0.7
+    rank = torch.arange(slots, dtype=torch.float32)
+    w[1, 0] = torch.where((rank - L + keep).abs() < L // 10, 1 + (rank % 500) / 4096, torch.where(rank < L - keep, 0.1, 9.0))
+    w[2, 0] = torch.where((rank - L + keep).abs() < L // 10, 1.0, torch.where(rank < L - keep, 0.1, 9.0))
+    w[3] = 1
+    w[4] = torch.rand(slots, generator=g)
+    for own in (False, True):
+        run_evict(kb, k, v, table, length, keep, w, own=own)
+    position = torch.stack([torch.randperm(slots, generator=g) for _ in range(5)]).view(5, 1, slots).to(torch.int32)
+    newest = torch.full((5,), slots - 1, dtype=torch.int32)
+    run_evict(kb, k, v, table, length, keep, w, position=position, newest=newest, first=4, recent=keep // 4)
+
+
 @pytest.mark.parametrize("count", [0, -1, -2 ** 31])
 def test_no_rows_on_the_device(kb, count):
     """A device count of none or less: every output stays as it was."""
