@@ -65,12 +65,12 @@ typedef struct kb_cache {
  *
  * Row r is a token of sequence s = seq[r] (r itself where seq is NULL; a
  * value outside [0, seqs) makes the row one of length 0) and goes to slot
- * length[r] - 1; a row of length 0, or longer than the table has slots, is not
- * stored.  A prompt's tokens are rows with one seq and lengths 1, 2, ...;
- * where two rows of a call name the same place of a page, what it holds
- * afterwards is unspecified.  With m the amplitude and a_i = pos[r] * freq[i],
- * taken in 64 bits, each pair (x, y) of a query's or key's first rot_dim
- * values becomes
+ * length[r] - 1; a row whose length is below 1, or longer than the table has
+ * slots, is not stored.  A prompt's tokens are rows with one seq and lengths
+ * 1, 2, ...; where two rows of a call name the same place of a page, what it
+ * holds afterwards is unspecified.  With m the amplitude and a_i = pos[r] *
+ * freq[i], taken in 64 bits, each pair (x, y) of a query's or key's first
+ * rot_dim values becomes
  *     (m (x cos a_i - y sin a_i), m (x sin a_i + y cos a_i)),   i < rot_dim / 2
  * rounded once; pair i is values (i, i + rot_dim / 2), or (2i, 2i + 1) where
  * interleaved.  The rest of the head, and values, are copied.  Positions

@@ -12,6 +12,7 @@
 // Kernel time: 8,200 tokens of 32 + 8 + 8 heads of 128 bf16 values 36.9 us, 202 MB in and out at
 // 5.5 TB/s (a large copy: 4.8 to 5.2); 5 tokens 3.4 us.
 #include "cache_common.hpp"
+#include "cache_slot.hpp"
 
 namespace kb {
 
@@ -41,8 +42,8 @@ __global__ __launch_bounds__(kAppendT) void cache_append_rows(AppendArgs a) {
   const int D = c.dim, half = a.rot / 2, H = a.q_heads + c.heads;
   const int s = cache_seq(c, a.seq, r);
   const int len = a.length[r];
-  const int pos = a.pos ? a.pos[r] : len - 1;
-  int slot = s < 0 || len > c.cap ? -1 : len - 1;
+  int slot = s < 0 ? -1 : new_slot(len, c.cap);
+  const int pos = a.pos ? a.pos[r] : slot;
   int64_t row = 0;
   if (slot >= 0) {
     row = cache_row(c, c.table + (int64_t)s * c.max_pages, 0, slot);
