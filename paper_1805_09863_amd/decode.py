@@ -90,20 +90,28 @@ def decode_loop(h_table: torch.Tensor, W: torch.Tensor, b: torch.Tensor, lengths
     until on_step returns.  In the compacted loop ``S_launch`` and
     ``N_launch`` give the sizes the step was launched with, ``token_launch``
     and ``score_launch`` its whole outputs.
+
+    All work is ``stream``'s (the current one by default): the inputs have to be ready in its order,
+    and it is the current stream within on_step.
     """
+    if lengths.numel() == 0:
+        return LoopStats()
+    if stream is None:
+        stream = torch.cuda.current_stream(W.device)
+    with torch.cuda.stream(stream):      # buffers are filled, used and given back in the loop's order
+        return _decode_loop(h_table, W, b, lengths, prev0, k, T, compact, on_step, stream)
+
+
+def _decode_loop(h_table, W, b, lengths, prev0, k, T, compact, on_step, stream) -> LoopStats:
     dev = W.device
     beam = k
     S0 = lengths.numel()
     H, V = W.shape
     stats = LoopStats()
-    if S0 == 0:
-        return stats
     len_host = lengths.cpu().tolist()
     Lmax = max(len_host)
     if Lmax > T or min(len_host) < 1:
         raise ValueError("lengths must lie in [1, T]")
-    if stream is None:
-        stream = torch.cuda.current_stream(dev)
     M0 = S0 * k
     lengths = lengths.to(device=dev, dtype=torch.int32).contiguous()
     # the plan (and so the workspace) depends on the row count, which shrinks
@@ -272,21 +280,19 @@ class _CachedStates:
                           n_dev=n_dev, out=out[:rows])
 
     def first(self, out):
-        with torch.cuda.stream(self.stream):
-            n = self.start.numel()
-            self.tok[:n] = self.start
-            self._step(0, n, None, out)
+        n = self.start.numel()
+        self.tok[:n] = self.start
+        self._step(0, n, None, out)
 
     def next(self, t, rows, n_dev, tok, par, keep, sid, out):
-        with torch.cuda.stream(self.stream):
-            gather = dict(n_dev=n_dev, n_max=rows, stream=self.stream)
-            kbb.gather_rows(tok[:rows].view(rows, 1), keep, out=self.tok.view(-1, 1), **gather)
-            kbb.gather_rows(par[:rows].view(rows, 1), keep, out=self.par.view(-1, 1), **gather)
-            kbb.gather_rows(self.table, self.par, out=self.table_nx, **gather)
-            self.table, self.table_nx = self.table_nx, self.table
-            self.pos.fill_(t)
-            self.length.fill_(t + 1)
-            self._step(t, rows, n_dev, out)
+        gather = dict(n_dev=n_dev, n_max=rows, stream=self.stream)
+        kbb.gather_rows(tok[:rows].view(rows, 1), keep, out=self.tok.view(-1, 1), **gather)
+        kbb.gather_rows(par[:rows].view(rows, 1), keep, out=self.par.view(-1, 1), **gather)
+        kbb.gather_rows(self.table, self.par, out=self.table_nx, **gather)
+        self.table, self.table_nx = self.table_nx, self.table
+        self.pos.fill_(t)
+        self.length.fill_(t + 1)
+        self._step(t, rows, n_dev, out)
 
 
 def beam_search(h_table: Optional[torch.Tensor], W: torch.Tensor, b: torch.Tensor, k: int, T: int, eos: int, *,
@@ -310,13 +316,21 @@ def beam_search(h_table: Optional[torch.Tensor], W: torch.Tensor, b: torch.Tenso
 
     ``on_step(t, state)`` is called after each step's kb_beam_finish with a
     dict of the step's device tensors (before the batch is compacted).
+
+    All work is ``stream``'s (the current one by default): the inputs have to be ready in its order,
+    and it is the current stream within on_step.
     """
-    dev = W.device
-    H, V = W.shape
     if (h_table is None) == (decoder is None):
         raise ValueError("either h_table or decoder gives the states")
     if stream is None:
-        stream = torch.cuda.current_stream(dev)
+        stream = torch.cuda.current_stream(W.device)
+    with torch.cuda.stream(stream):      # buffers are filled, used and given back in the loop's order
+        return _beam_search(h_table, W, b, k, T, eos, alpha, decoder, start, on_step, stream)
+
+
+def _beam_search(h_table, W, b, k, T, eos, alpha, decoder, start, on_step, stream) -> BeamSearchResult:
+    dev = W.device
+    H, V = W.shape
     if decoder is None:
         S0 = h_table.shape[0] // (T * k)
         if h_table.shape[0] != S0 * T * k or S0 == 0:
@@ -325,8 +339,7 @@ def beam_search(h_table: Optional[torch.Tensor], W: torch.Tensor, b: torch.Tenso
     else:
         _check_decoder(decoder, W, start)
         S0 = start.numel()
-        with torch.cuda.stream(stream):
-            states = _CachedStates(decoder, start, k, T, stream)
+        states = _CachedStates(decoder, start, k, T, stream)
     M0 = S0 * k
     i32 = dict(dtype=torch.int32, device=dev)
     dt = kbb._dtype_code(W)
@@ -371,8 +384,7 @@ def beam_search(h_table: Optional[torch.Tensor], W: torch.Tensor, b: torch.Tenso
                             prev_keep=keep[1 - cur][:N] if t > 0 else None, prev_base=prev_base, base=base,
                             hist_token=hist_tok, hist_parent=hist_par, fin=fin, S=S, N=N))
         kbb.compact_beams(alive[:S * k], S, k, out=(keep[cur], cnt[0:1], noff, ksent, cnt[1:2]), stream=stream)
-        with torch.cuda.stream(stream):                # the copy runs on the loop's stream
-            cnt_host.copy_(cnt, non_blocking=True)
+        cnt_host.copy_(cnt, non_blocking=True)
         ready.record(stream)
         kbb.gather_rows(sc[:S * k].view(S * k, 1), keep[cur], n_dev=cnt[0:1], n_max=S * k,
                         out=prev_nx.view(M0, 1), stream=stream)
@@ -421,18 +433,22 @@ def greedy_search(decoder: CachedDecoder, W: torch.Tensor, b: torch.Tensor, star
 
     ``on_step(t, state)`` is called after each step's attention with a dict of its device
     tensors.
+
+    All work is ``stream``'s (the current one by default): the inputs have to be ready in its order,
+    and it is the current stream within on_step.
     """
     dev = W.device
     H, V = W.shape
-    _check_decoder(decoder, W, start)
+    if stream is None:
+        stream = torch.cuda.current_stream(dev)
+    with torch.cuda.stream(stream):
+        _check_decoder(decoder, W, start)
     if T < 1 or every < 1 or (keep is not None and keep < 1):
         raise ValueError(f"T = {T}, keep = {keep}, every = {every}")
     if recent is None:
         recent = 0 if keep is None else min(keep // 2, max(keep - first, 0))
     if keep is not None and (first < 0 or recent < 0 or first + recent > keep):
         raise ValueError(f"first = {first} and recent = {recent} of keep = {keep}")
-    if stream is None:
-        stream = torch.cuda.current_stream(dev)
     S0 = start.numel()
     i32 = dict(dtype=torch.int32, device=dev)
     most = T if keep is None else min(T, keep + every)
