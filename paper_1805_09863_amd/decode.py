@@ -287,6 +287,7 @@ class _CachedStates:
     def next(self, t, rows, n_dev, tok, par, keep, sid, out):
         gather = dict(n_dev=n_dev, n_max=rows, stream=self.stream)
         kbb.gather_rows(tok[:rows].view(rows, 1), keep, out=self.tok.view(-1, 1), **gather)
+        self.tok.clamp_(min=0)           # -1 where a sentence had fewer continuations than its beam: any word's state
         kbb.gather_rows(par[:rows].view(rows, 1), keep, out=self.par.view(-1, 1), **gather)
         kbb.gather_rows(self.table, self.par, out=self.table_nx, **gather)
         self.table, self.table_nx = self.table_nx, self.table
@@ -305,7 +306,8 @@ def beam_search(h_table: Optional[torch.Tensor], W: torch.Tensor, b: torch.Tenso
     at step t, the decoder stand-in.  With ``decoder`` (h_table None) the states are
     its: every sentence starts from the token ``start[s]`` (int32, on the GPU), and a
     hypothesis attends to its own tokens so far, which hypotheses of one sentence share
-    in the attention cache.  Every sentence starts from one hypothesis
+    in the attention cache; one of score -inf and token -1, where a sentence has fewer
+    continuations of probability above 0 than its beam, goes on as word 0.  Every sentence starts from one hypothesis
     (slot 0, score 0) with a beam of k.  Each step: the output layer
     (kb_kbest_step), kb_beam_finish (history, finished store, beam shrink),
     kb_compact_beams, the gathers of the surviving scores, sentence ids and
@@ -424,7 +426,7 @@ def greedy_search(decoder: CachedDecoder, W: torch.Tensor, b: torch.Tensor, star
     """Greedy decoding (Algorithm 5) of a constant batch (Algorithm 1) with a decoder that
     attends to its own past: each step appends the last tokens to the cache, attends
     (decoder.step) and takes the best word of every row (kb_argmax_step), until every
-    sentence has produced ``eos`` or has T tokens.
+    sentence has produced ``eos`` or has T tokens.  Scores that are all NaN give some word.
 
     ``keep``: the cache of a sentence is held to a budget.  Whenever it has ``every`` more
     slots than that, it goes back to ``keep`` (kb_cache_evict): the ``first`` and the
@@ -477,6 +479,7 @@ def greedy_search(decoder: CachedDecoder, W: torch.Tensor, b: torch.Tensor, star
             slots += 1
             h = decoder.step(tok, pos, length, *kv, table, max_len=slots, position=position, weight=weight)
             kbb.argmax_step(h, W, b, out=(tok, logit), ws=ws, stream=stream)
+            tok.clamp_(0, V - 1)                           # a row of NaN has no best word: any
             if on_step is not None:
                 on_step(t, dict(h=h, k=kv[0], v=kv[1], table=table, length=length, pos=pos, token=tok, slots=slots,
                                 position=position, weight=weight))
