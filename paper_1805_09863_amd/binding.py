@@ -657,6 +657,15 @@ def _ask(t, name: str, dtype, numel: int, dev: int) -> int:
 
 
 _INT_MAX = 2 ** 31 - 1
+
+
+def _refuse_sizes(**sizes):
+    """Raised before ctypes would cut a size to 32 bits."""
+    for name, x in sizes.items():
+        if not -_INT_MAX <= x <= _INT_MAX:
+            raise ValueError(f"{name} = {x}: beyond 32 bits")
+
+
 _device_now = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
@@ -695,8 +704,8 @@ def _cache(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor):
         raise ValueError("table must be seqs x max_pages")
     pages, heads, page_size, dim = shape
     seqs, max_pages = table.shape
-    if pages > _INT_MAX or seqs > _INT_MAX or max_pages > _INT_MAX:  # ctypes would cut them to 32 bits
-        raise ValueError(f"{pages} pages, a table of {seqs} x {max_pages}: beyond 32 bits")
+    if max(pages, heads, page_size, dim, seqs, max_pages) > _INT_MAX:
+        _refuse_sizes(pages=pages, heads=heads, page_size=page_size, dim=dim, seqs=seqs, max_pages=max_pages)
     return (_Cache(_dtype_code(k_cache, "k_cache"), heads, dim, page_size, pages, seqs, max_pages, kp, vp, tp), dev,
             dtype, heads, dim, max_pages * page_size, seqs)
 
@@ -714,6 +723,8 @@ def _ask_rows(t: torch.Tensor, name: str, dtype, R: int, heads: Optional[int], d
     if len(shape) != 3 or shape[0] != R or shape[2] != dim or (heads is not None and shape[1] != heads):
         raise ValueError(f"{name} must be {R} x {'heads' if heads is None else heads} x {dim}, got {tuple(shape)}")
     heads = shape[1]
+    if R > _INT_MAX or heads > _INT_MAX:
+        _refuse_sizes(rows=R, **{f"heads of {name}": heads})
     step, apart, one = t.stride()
     if one != 1 or (heads > 1 and apart != dim):
         raise ValueError(f"{name}: the heads of a row must lie one after the other, without gaps")
@@ -760,6 +771,8 @@ def cache_append(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tens
     if freq is not None:
         fp = _ask(freq, "freq", torch.float64, 0, dev)
         rot = 2 * freq.numel()
+        if rot > _INT_MAX:
+            _refuse_sizes(**{"values that freq turns": rot})
     pp = None if pos is None else _ask(pos, "pos", i32, R, dev)
     sp = None if seq is None else _ask(seq, "seq", i32, R, dev)
     nd = None if n_dev is None else _ask(n_dev, "n_dev", i32, 1, dev)
@@ -775,6 +788,7 @@ def cache_attend_workspace_bytes(k_cache: torch.Tensor, v_cache: torch.Tensor, t
     """Bytes that cache_attend's ``ws`` needs for R rows of q_heads heads (``weights``: with ``weight_out``)."""
     c, _, _, _, _, cap, _ = _cache(k_cache, v_cache, table)
     max_len = cap if max_len is None else min(max_len, cap)
+    _refuse_sizes(R=R, q_heads=q_heads, max_len=max_len)
     return int(lib().kb_cache_attend_workspace_bytes(c, R, q_heads, max_len, int(weights)))
 
 
@@ -809,6 +823,8 @@ def cache_attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, 
     wo = None if weight_out is None else _ask(weight_out, "weight_out", f32, seqs * heads * cap, dev)
     if max_len is None or max_len > cap:
         max_len = cap
+    elif max_len < 1:
+        _refuse_sizes(max_len=max_len)
     L = lib()
     need = L.kb_cache_attend_workspace_bytes(c, R, q_heads, max_len, 0 if wo is None else 1)
     if ws is None and need > 0:
@@ -836,11 +852,11 @@ def cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tenso
     ``position`` is; length and, in place, weight and position may be the inputs).
     """
     c, dev, _, heads, _, cap, seqs = _cache(k_cache, v_cache, table)
-    if keep > _INT_MAX:
-        raise ValueError(f"keep = {keep}: beyond 32 bits")
     i32, f32 = torch.int32, torch.float32
     lp = _ask(length, "length", i32, 0, dev)
     R = length.numel()
+    if max(keep, first, recent, R) > _INT_MAX or min(keep, first, recent) < 0:
+        _refuse_sizes(keep=keep, first=first, recent=recent, rows=R)
     wp = _ask(weight, "weight", f32, seqs * heads * cap, dev)
     pp = None if position is None else _ask(position, "position", i32, seqs * heads * cap, dev)
     ne = None if newest is None else _ask(newest, "newest", i32, R, dev)
@@ -851,6 +867,8 @@ def cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tenso
     if out_table.dim() != 2 or out_table.shape[0] < R:
         raise ValueError(f"out_table must have at least {R} rows of pages, got {tuple(out_table.shape)}")
     out_pages = out_table.shape[1]
+    if out_pages > _INT_MAX:
+        _refuse_sizes(**{"columns of out_table": out_pages})
     out_cap = out_pages * c.page_size
     if out is None:
         at, shape = k_cache.device, (R, heads, out_cap)

@@ -25,3 +25,115 @@ def test_the_append_takes_its_slot_from_there():
     with open(os.path.join(CSRC, "cache_append.hip")) as f:
         src = f.read()
     assert "new_slot(len, c.cap)" in src and "len - 1" not in src
+
+
+# ---------------------------------------------------------------- sizes that C takes in 32 bits
+torch = pytest.importorskip("torch")
+kb = pytest.importorskip("paper_1805_09863_amd")
+from paper_1805_09863_amd import binding  # noqa: E402
+
+
+class Shaped:
+    """A tensor on the GPU as far as its sizes go: nothing of it exists."""
+    is_cuda, dtype, device = True, torch.float32, "cuda:0"
+
+    def __init__(self, *shape, dtype=torch.float32):
+        self.shape, self.dtype = torch.Size(shape), dtype
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        n = 1
+        for x in self.shape:
+            n *= x
+        return n
+
+    def stride(self):
+        s, n = [], 1
+        for x in reversed(self.shape):
+            s.append(n)
+            n *= max(x, 1)
+        return tuple(reversed(s))
+
+    def get_device(self):
+        return 0
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 4096
+
+    def element_size(self):
+        return 4
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The calls that reach the library, none of them made."""
+    made = []
+
+    def run(fn, dev, stream, *args):
+        assert len(args) + 1 == len(fn.argtypes)
+        made.append(args)
+    monkeypatch.setattr(binding, "_run", run)
+    monkeypatch.setattr(binding.torch, "Tensor", Shaped)
+    return made
+
+
+I32 = torch.int32
+
+
+def cache(seqs=8, heads=2, dim=64, page=16, pages=100, cols=10):
+    return Shaped(pages, heads, page, dim), Shaped(pages, heads, page, dim), Shaped(seqs, cols, dtype=I32)
+
+
+def evict(keep, R=8, out_cols=10, **kw):
+    k, v, t = cache()
+    n = max(keep, 1) if keep <= 10 ** 6 else 32
+    out = (Shaped(R, dtype=I32), Shaped(8, 2, 160), None, Shaped(R, 2, n, dtype=I32))
+    more = {} if out_cols == 10 else dict(out_table=Shaped(R, out_cols, dtype=I32))
+    return kb.cache_evict(k, v, t, Shaped(R, dtype=I32), keep, weight=Shaped(8, 2, 160), out=out, **more, **kw)
+
+
+def attend(R=8, q_heads=4, max_len=160, c=None):
+    k, v, t = c or cache()
+    q = Shaped(R, q_heads, k.shape[3])
+    return kb.cache_attend(q, k, v, t, Shaped(R, dtype=I32), max_len=max_len, out=q, ws=Shaped(1 << 40),
+                           seq=Shaped(R, dtype=I32))
+
+
+def append(R=8, q_heads=4, pairs=32, c=None):
+    k, v, t = c or cache()
+    x = Shaped(R, k.shape[1], k.shape[3])
+    q = Shaped(R, q_heads, k.shape[3])
+    return kb.cache_append(k, v, t, Shaped(R, dtype=I32), x, x, q=q, q_out=q, freq=Shaped(pairs, dtype=torch.float64),
+                           pos=Shaped(R, dtype=I32), seq=Shaped(R, dtype=I32))
+
+
+def test_sizes_within_32_bits_reach_the_library(calls):
+    evict(32, first=1, recent=4)
+    attend()
+    append()
+    attend(max_len=2 ** 40)                              # longer than the table: the table's slots
+    assert len(calls) == 4 and calls[0][4:7] == (32, 1, 4) and calls[1][9] == calls[3][9] == 160
+
+
+@pytest.mark.parametrize("call", [
+    lambda: evict(2 ** 32 + 4), lambda: evict(-2 ** 32 + 5), lambda: evict(2 ** 31), lambda: evict(-2 ** 31 - 1),
+    lambda: evict(32, first=2 ** 32), lambda: evict(32, first=-2 ** 32 + 1), lambda: evict(32, recent=2 ** 32 + 4),
+    lambda: evict(32, recent=-2 ** 32), lambda: evict(32, R=2 ** 32 + 2), lambda: evict(32, out_cols=2 ** 32 + 10),
+    lambda: attend(max_len=-2 ** 32 + 5), lambda: attend(R=2 ** 32 + 1), lambda: attend(q_heads=2 ** 32 + 4),
+    lambda: attend(c=cache(heads=2 ** 32 + 2, pages=0), q_heads=2), lambda: attend(c=cache(dim=2 ** 32 + 64, pages=0)),
+    lambda: attend(c=cache(page=2 ** 32 + 16, pages=0)),
+    lambda: append(R=2 ** 32 + 1), lambda: append(q_heads=2 ** 32 + 4), lambda: append(pairs=2 ** 31 + 16),
+    lambda: kb.cache_attend_workspace_bytes(*cache(), 2 ** 32 + 1, 4),
+    lambda: kb.cache_attend_workspace_bytes(*cache(), 8, 2 ** 32 + 4),
+    lambda: kb.cache_attend_workspace_bytes(*cache(), 8, 4, -2 ** 32 + 5),
+    lambda: kb.cache_attend_workspace_bytes(*cache(), -2 ** 32 + 5, 4),
+])
+def test_sizes_past_32_bits_are_refused(calls, call):
+    with pytest.raises(ValueError, match="32 bits"):
+        call()
+    assert not calls
