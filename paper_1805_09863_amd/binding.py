@@ -656,7 +656,24 @@ def _ask(t, name: str, dtype, numel: int, dev: int) -> int:
     return _refuse(t, name, dtype, numel, dev)
 
 
+def _ask_as(t, name: str, dtype, shape: tuple, dev: int) -> int:
+    """_ask for a tensor of ``shape``, or of more rows of the same dimensions, or laid out as that is: flat, or
+    divided otherwise along the same rows.  A last dimension that is longer is another distance of two rows."""
+    try:
+        if t.shape == shape and t.dtype is dtype and t.get_device() == dev and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    p, inner, got = _ask(t, name, dtype, math.prod(shape), dev), shape[1:], t.shape
+    if (len(got) <= 1 or got[-len(inner):] == inner or got[1:] == inner[1:]
+            or math.prod(got[1:]) == math.prod(inner) and (len(got) == 2 or got[1] == inner[0])):
+        return p
+    raise ValueError(f"{name} must have rows of {' x '.join(map(str, inner))}, got {tuple(got)}")
+
+
 _INT_MAX = 2 ** 31 - 1
+_I32, _F32 = torch.int32, torch.float32
+_CODES = {torch.float32: KB_F32, torch.bfloat16: KB_BF16}
 
 
 def _refuse_sizes(**sizes):
@@ -697,16 +714,19 @@ def _cache(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor):
     dtype, dev, shape = k_cache.dtype, k_cache.get_device(), k_cache.shape
     kp = _ask(k_cache, "k_cache", dtype, 0, dev)
     vp = _ask(v_cache, "v_cache", dtype, 0, dev)
-    tp = _ask(table, "table", torch.int32, 0, dev)
+    tp = _ask(table, "table", _I32, 0, dev)
     if len(shape) != 4 or v_cache.shape != shape:
         raise ValueError("k_cache and v_cache must be pages x heads x page_size x dim, the same shape")
     if table.dim() != 2:
         raise ValueError("table must be seqs x max_pages")
     pages, heads, page_size, dim = shape
     seqs, max_pages = table.shape
-    if max(pages, heads, page_size, dim, seqs, max_pages) > _INT_MAX:
+    if pages | heads | page_size | dim | seqs | max_pages > _INT_MAX:
         _refuse_sizes(pages=pages, heads=heads, page_size=page_size, dim=dim, seqs=seqs, max_pages=max_pages)
-    return (_Cache(_dtype_code(k_cache, "k_cache"), heads, dim, page_size, pages, seqs, max_pages, kp, vp, tp), dev,
+    code = _CODES.get(dtype)
+    if code is None:
+        _dtype_code(k_cache, "k_cache")
+    return (_Cache(code, heads, dim, page_size, pages, seqs, max_pages, kp, vp, tp), dev,
             dtype, heads, dim, max_pages * page_size, seqs)
 
 
@@ -723,7 +743,7 @@ def _ask_rows(t: torch.Tensor, name: str, dtype, R: int, heads: Optional[int], d
     if len(shape) != 3 or shape[0] != R or shape[2] != dim or (heads is not None and shape[1] != heads):
         raise ValueError(f"{name} must be {R} x {'heads' if heads is None else heads} x {dim}, got {tuple(shape)}")
     heads = shape[1]
-    if R > _INT_MAX or heads > _INT_MAX:
+    if R | heads > _INT_MAX:
         _refuse_sizes(rows=R, **{f"heads of {name}": heads})
     step, apart, one = t.stride()
     if one != 1 or (heads > 1 and apart != dim):
@@ -754,8 +774,7 @@ def cache_append(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tens
     slots' ``pos`` and 0.  Returns the turned queries (``q_out``), None without ``q``.
     """
     c, dev, dtype, heads, dim, cap, seqs = _cache(k_cache, v_cache, table)
-    i32 = torch.int32
-    lp = _ask(length, "length", i32, 0, dev)
+    lp = _ask(length, "length", _I32, 0, dev)
     R = length.numel()
     kp, k_stride, _ = _ask_rows(k, "k", dtype, R, heads, dim, dev)
     vp, v_stride, _ = _ask_rows(v, "v", dtype, R, heads, dim, dev)
@@ -765,7 +784,7 @@ def cache_append(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tens
         qp, q_stride, q_heads = _ask_rows(q, "q", dtype, R, None, dim, dev)
         if q_out is None:
             q_out = _empty(q, (R, q_heads, dim), stream)
-        op = _ask(q_out, "q_out", dtype, R * q_heads * dim, dev)
+        op = _ask_as(q_out, "q_out", dtype, (R, q_heads, dim), dev)
     elif q_out is not None:
         raise ValueError("q_out without q")
     if freq is not None:
@@ -773,11 +792,11 @@ def cache_append(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tens
         rot = 2 * freq.numel()
         if rot > _INT_MAX:
             _refuse_sizes(**{"values that freq turns": rot})
-    pp = None if pos is None else _ask(pos, "pos", i32, R, dev)
-    sp = None if seq is None else _ask(seq, "seq", i32, R, dev)
-    nd = None if n_dev is None else _ask(n_dev, "n_dev", i32, 1, dev)
-    at = None if position is None else _ask(position, "position", i32, seqs * heads * cap, dev)
-    wp = None if weight is None else _ask(weight, "weight", torch.float32, seqs * heads * cap, dev)
+    pp = None if pos is None else _ask(pos, "pos", _I32, R, dev)
+    sp = None if seq is None else _ask(seq, "seq", _I32, R, dev)
+    nd = None if n_dev is None else _ask(n_dev, "n_dev", _I32, 1, dev)
+    at = None if position is None else _ask_as(position, "position", _I32, (seqs, heads, cap), dev)
+    wp = None if weight is None else _ask_as(weight, "weight", _F32, (seqs, heads, cap), dev)
     _run(lib().kb_cache_append, dev, stream, c, R, nd, q_heads, qp, q_stride, kp, k_stride, vp, v_stride, rot,
          1 if interleaved else 0, pp, fp, amplitude, sp, lp, op, at, wp)
     return q_out
@@ -809,18 +828,17 @@ def cache_attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, 
     workspace of at least ``cache_attend_workspace_bytes`` bytes.
     """
     c, dev, dtype, heads, dim, cap, seqs = _cache(k_cache, v_cache, table)
-    i32, f32 = torch.int32, torch.float32
-    lp = _ask(length, "length", i32, 0, dev)
+    lp = _ask(length, "length", _I32, 0, dev)
     R = length.numel()
     qp, q_stride, q_heads = _ask_rows(q, "q", dtype, R, None, dim, dev)
     if out is None:
         out = _empty(q, (R, q_heads, dim), stream)
-    op = _ask(out, "out", dtype, R * q_heads * dim, dev)
-    ep = None if lse is None else _ask(lse, "lse", f32, R * q_heads, dev)
-    sp = None if seq is None else _ask(seq, "seq", i32, R, dev)
-    nd = None if n_dev is None else _ask(n_dev, "n_dev", i32, 1, dev)
-    wi = None if weight_in is None else _ask(weight_in, "weight_in", f32, seqs * heads * cap, dev)
-    wo = None if weight_out is None else _ask(weight_out, "weight_out", f32, seqs * heads * cap, dev)
+    op = _ask_as(out, "out", dtype, (R, q_heads, dim), dev)
+    ep = None if lse is None else _ask_as(lse, "lse", _F32, (R, q_heads), dev)
+    sp = None if seq is None else _ask(seq, "seq", _I32, R, dev)
+    nd = None if n_dev is None else _ask(n_dev, "n_dev", _I32, 1, dev)
+    wi = None if weight_in is None else _ask_as(weight_in, "weight_in", _F32, (seqs, heads, cap), dev)
+    wo = None if weight_out is None else _ask_as(weight_out, "weight_out", _F32, (seqs, heads, cap), dev)
     if max_len is None or max_len > cap:
         max_len = cap
     elif max_len < 1:
@@ -852,18 +870,17 @@ def cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tenso
     ``position`` is; length and, in place, weight and position may be the inputs).
     """
     c, dev, _, heads, _, cap, seqs = _cache(k_cache, v_cache, table)
-    i32, f32 = torch.int32, torch.float32
-    lp = _ask(length, "length", i32, 0, dev)
+    lp = _ask(length, "length", _I32, 0, dev)
     R = length.numel()
-    if max(keep, first, recent, R) > _INT_MAX or min(keep, first, recent) < 0:
+    if not 0 <= keep | first | recent | R <= _INT_MAX:
         _refuse_sizes(keep=keep, first=first, recent=recent, rows=R)
-    wp = _ask(weight, "weight", f32, seqs * heads * cap, dev)
-    pp = None if position is None else _ask(position, "position", i32, seqs * heads * cap, dev)
-    ne = None if newest is None else _ask(newest, "newest", i32, R, dev)
-    nd = None if n_dev is None else _ask(n_dev, "n_dev", i32, 1, dev)
+    wp = _ask_as(weight, "weight", _F32, (seqs, heads, cap), dev)
+    pp = None if position is None else _ask_as(position, "position", _I32, (seqs, heads, cap), dev)
+    ne = None if newest is None else _ask(newest, "newest", _I32, R, dev)
+    nd = None if n_dev is None else _ask(n_dev, "n_dev", _I32, 1, dev)
     if out_table is None:
         out_table = table
-    tp = _ask(out_table, "out_table", i32, 0, dev)
+    tp = _ask(out_table, "out_table", _I32, 0, dev)
     if out_table.dim() != 2 or out_table.shape[0] < R:
         raise ValueError(f"out_table must have at least {R} rows of pages, got {tuple(out_table.shape)}")
     out_pages = out_table.shape[1]
@@ -873,16 +890,16 @@ def cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tenso
     if out is None:
         at, shape = k_cache.device, (R, heads, out_cap)
         with torch.cuda.stream(stream):
-            out = (torch.empty(R, dtype=i32, device=at), torch.zeros(shape, device=at),
-                   None if position is None else torch.full(shape, -1, dtype=i32, device=at),
-                   torch.empty((R, heads, max(keep, 0)), dtype=i32, device=at))
+            out = (torch.empty(R, dtype=_I32, device=at), torch.zeros(shape, device=at),
+                   None if position is None else torch.full(shape, -1, dtype=_I32, device=at),
+                   torch.empty((R, heads, max(keep, 0)), dtype=_I32, device=at))
     if len(out) != 4:
         raise ValueError("out must hold 4 tensors (length, weight, position, source)")
     out_length, out_weight, out_position, source = out
-    olp = _ask(out_length, "out length", i32, R, dev)
-    owp = _ask(out_weight, "out weight", f32, R * heads * out_cap, dev)
-    opp = None if out_position is None else _ask(out_position, "out position", i32, R * heads * out_cap, dev)
-    sp = _ask(source, "source", i32, R * heads * keep, dev)
+    olp = _ask(out_length, "out length", _I32, R, dev)
+    owp = _ask_as(out_weight, "out weight", _F32, (R, heads, out_cap), dev)
+    opp = None if out_position is None else _ask_as(out_position, "out position", _I32, (R, heads, out_cap), dev)
+    sp = _ask_as(source, "source", _I32, (R, heads, keep), dev) if keep > 0 else _ask(source, "source", _I32, 0, dev)
     _run(lib().kb_cache_evict, dev, stream, c, R, nd, lp, keep, first, recent, ne, wp, pp, tp, out_pages, olp, owp, opp,
          sp)
     return out

@@ -137,3 +137,59 @@ def test_sizes_past_32_bits_are_refused(calls, call):
     with pytest.raises(ValueError, match="32 bits"):
         call()
     assert not calls
+
+
+# ---------------------------------------------------------------- rows that lie otherwise than the call takes them
+def with_weights(name, *shape):
+    """The call that takes the argument, with a tensor of this shape; the others as they should be.  8 sequences of
+    2 heads and 160 slots, 4 query heads of 64 values, 40 slots kept, into pages of 48 slots a sequence."""
+    k, v, t = cache()
+    n, q, w, p = Shaped(8, dtype=I32), Shaped(8, 4, 64), Shaped(8, 2, 160), Shaped(8, 2, 160, dtype=I32)
+    x = Shaped(*shape, dtype=I32 if name in ("position", "source", "out position") else torch.float32)
+    if name in ("q_out", "append weight", "append position"):
+        kw = dict(q_out=q, weight=w, position=p)
+        kw[name.split()[-1]] = x if name != "append position" else Shaped(*shape, dtype=I32)
+        return kb.cache_append(k, v, t, n, Shaped(8, 2, 64), Shaped(8, 2, 64), q=q, **kw)
+    if name in ("out", "lse", "weight_in", "weight_out"):
+        kw = dict(out=q, lse=Shaped(8, 4), weight_in=w, weight_out=w, ws=Shaped(1 << 30))
+        kw[name] = x
+        return kb.cache_attend(q, k, v, t, n, **kw)
+    kw = dict(weight=w, position=p)
+    out = {"length": n, "out weight": Shaped(8, 2, 48), "out position": Shaped(8, 2, 48, dtype=I32),
+           "source": Shaped(8, 2, 40, dtype=I32)}
+    (kw if name in kw else out)[name] = x
+    return kb.cache_evict(k, v, t, n, 40, out_table=Shaped(8, 3, dtype=I32), out=tuple(out.values()), **kw)
+
+
+ROWS = {"q_out": (4, 64), "out": (4, 64), "lse": (4,), "append weight": (2, 160), "append position": (2, 160),
+        "weight_in": (2, 160), "weight_out": (2, 160), "weight": (2, 160), "position": (2, 160), "out weight": (2, 48),
+        "out position": (2, 48), "source": (2, 40)}
+
+
+@pytest.mark.parametrize("name", ROWS)
+def test_rows_that_lie_as_the_call_takes_them(calls, name):
+    *heads, last = ROWS[name]
+    n = heads[0] if heads else 1
+    shapes = [(8, *ROWS[name]), (9, *ROWS[name]), (8 * n * last,), (8 * n * last + 7,), (8, n * last), (8 * n, last),
+              (3, 8, *ROWS[name])]
+    if heads:
+        shapes.append((8, n, last // 4, 4))
+    for shape in shapes:
+        with_weights(name, *shape)
+    assert len(calls) == len(shapes)
+
+
+@pytest.mark.parametrize("name", ROWS)
+def test_rows_further_apart_are_refused(calls, name):
+    *heads, last = ROWS[name]
+    n = heads[0] if heads else 1
+    shapes = [(8, *heads, last + 32), (8, *heads, 2 * last), (8, n * last + 8), (8 * n, last + 16)]
+    if heads:
+        shapes += [(8, n + 2, last), (8, 2 * n, last // 2), (8, n, last // 4, 8)]
+    for shape in shapes:
+        with pytest.raises(ValueError, match="rows of"):
+            with_weights(name, *shape)
+    for shape in ((7, *ROWS[name]), (8 * n * last - 1,)):
+        with pytest.raises(ValueError, match="needed"):
+            with_weights(name, *shape)
+    assert not calls

@@ -44,3 +44,22 @@ def test_append_stores_no_token_without_a_slot(kb, dtype, page, turned):
     assert bool((position[R - 1, :, 4] == (R - 1 if turned else 4)).all()) and bool((weight[R - 1, :, 4] == 0).all())
     position[R - 1, :, 4], weight[R - 1, :, 4] = -9, 5
     assert bool((position == -9).all()) and bool((weight == 5).all())
+
+
+def test_weights_of_another_row_length_are_refused(kb):
+    """A table of 50 slots and weights of 64 a row: refused, not addressed at 50; flat memory is taken as it lies."""
+    R, heads, dim, page, cols = 3, 2, 32, 2, 25
+    k, v = (torch.randn(R * cols, heads, page, dim, device="cuda") for _ in range(2))
+    table = torch.arange(R * cols, dtype=torch.int32, device="cuda").view(R, cols)
+    n = i32(50, 7, 33)
+    q = torch.randn(R, 4, dim, device="cuda")
+    want = torch.zeros(R, heads, 50, device="cuda")
+    kb.cache_attend(q, k, v, table, n, weight_out=want)
+    with pytest.raises(ValueError, match="rows of 2 x 50"):
+        kb.cache_attend(q, k, v, table, n, weight_out=torch.zeros(R, heads, 64, device="cuda"))
+    with pytest.raises(ValueError, match="rows of 2 x 50"):
+        kb.cache_evict(k, v, table, n, 10, weight=torch.zeros(R, heads, 64, device="cuda"))
+    for shape in ((R * heads * 50 + 3,), (R, heads, cols, page), (R * heads, 50)):
+        got = torch.zeros(shape, device="cuda")
+        kb.cache_attend(q, k, v, table, n, weight_out=got)
+        assert torch.equal(got.flatten()[:R * heads * 50], want.flatten())
