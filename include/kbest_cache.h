@@ -14,10 +14,10 @@
  *
  *  - Slot t of sequence s lies in page table[s * max_pages + t / page_size],
  *    place t % page_size.  A page outside [0, pages) is a hole: its slots are
- *    neither read, attended to nor written.  Where slots are read, lengths
- *    above the table's max_pages * page_size are cut to that; negative ones
- *    are 0.  So no content of table, seq and length makes a call leave its
- *    buffers.
+ *    neither read, attended to nor written (kb_cache_evict counts them as
+ *    slots all the same, see there).  Where slots are read, lengths above the
+ *    table's max_pages * page_size are cut to that; negative ones are 0.  So
+ *    no content of table, seq and length makes a call leave its buffers.
  *  - A call of R rows takes their count from the device where n_dev is given:
  *    min(R, *n_dev) rows are worked on, outputs of the others are left as
  *    they were.
@@ -157,6 +157,16 @@ kb_status kb_cache_attend(const kb_cache* cache, int R, const int32_t* n_dev, in
  * values as possible move.  The order of a sequence's slots is then no longer
  * that of its tokens, which attention does not depend on; `position` keeps
  * it.  Rows are moved by the bits.
+ *
+ * Every slot below length, and every place below n of out_table, is to have a
+ * page: attention over the n places is then attention over the kept slots.
+ * Slots are ranked and placed by weight and position alone, and holes are not
+ * looked for.  A kept slot that is a hole takes its weight and position to its
+ * place, which goes on holding the key and value that lay there, to be
+ * attended to if it has a page; a kept row whose place is a hole is lost.  A
+ * sequence that has given pages up is therefore closed up first: its table's
+ * remaining pages moved to the front, with the rows of weight and position
+ * that go with them, and length cut to their slots.
  *
  *   length       R int32.
  *   keep         slots to keep, >= 1; first, recent >= 0, first + recent <=

@@ -866,7 +866,9 @@ def cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tenso
     kept slots' weights and positions, and the slot each came from.
 
     Without ``out_table`` the rows move within their own pages; with it (R x pages int32)
-    the kept ones are put there.  ``out`` may supply the four results (position None where
+    the kept ones are put there.  Every slot below ``length`` and every place that is
+    kept must have a page: holes are not looked for, and one among them leaves a place
+    whose weight and position are not those of the row in it.  ``out`` may supply the four results (position None where
     ``position`` is; length and, in place, weight and position may be the inputs).
     """
     c, dev, _, heads, _, cap, seqs = _cache(k_cache, v_cache, table)
