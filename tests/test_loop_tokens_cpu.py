@@ -1,5 +1,6 @@
-"""What the decode loops hand to a decoder as tokens, with the library's calls replaced by host ones: always rows of its
-embedding, also where a step has no word to give (-1 of the k-best, 2^31 - 1 of the argmax)."""
+"""What the decode loops hand to a decoder, with the library's calls replaced by host ones: tokens are always rows of its
+embedding, also where a step has no word to give (-1 of the k-best, 2^31 - 1 of the argmax); a budget that the search
+never comes to takes no memory."""
 import pytest
 import torch
 
@@ -49,3 +50,14 @@ def test_greedy_search_feeds_words_where_there_is_none(monkeypatch):
     for token in dec.seen:
         assert int(token.min()) >= 0 and int(token.max()) < V
     assert int(res.tokens.max()) < V
+
+
+def test_greedy_search_with_a_budget_past_all_memory(monkeypatch):
+    def argmax_step(h, W, b, *, out, ws, stream):
+        out[0].fill_(5)
+    monkeypatch.setattr(decode.kbb, "argmax_step", argmax_step)
+    monkeypatch.setattr(decode, "_check_decoder", lambda *a: None)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda dev=None: None)
+    start = torch.tensor([1, 2], dtype=torch.int32)
+    res = decode.greedy_search(Decoder(), torch.zeros(H, V), torch.zeros(V), start, 4, 3, keep=10 ** 13)
+    assert res.tokens.tolist() == [[5] * 4] * 2 and res.evictions == 0
