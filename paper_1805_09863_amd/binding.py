@@ -892,7 +892,7 @@ def cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tenso
     if out is None:
         at, shape = k_cache.device, (R, heads, out_cap)
         with torch.cuda.stream(stream):
-            out = (torch.empty(R, dtype=_I32, device=at), torch.zeros(shape, device=at),
+            out = (torch.empty(R, dtype=_I32, device=at), torch.zeros(shape, dtype=_F32, device=at),
                    None if position is None else torch.full(shape, -1, dtype=_I32, device=at),
                    torch.empty((R, heads, max(keep, 0)), dtype=_I32, device=at))
     if len(out) != 4:

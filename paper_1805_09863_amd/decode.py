@@ -463,7 +463,7 @@ def greedy_search(decoder: CachedDecoder, W: torch.Tensor, b: torch.Tensor, star
         position = weight = evicted = None
         if keep is not None:
             position = torch.zeros((S0, decoder.kv_heads, cols * page_size), **i32)
-            weight = torch.zeros((S0, decoder.kv_heads, cols * page_size), device=dev)
+            weight = torch.zeros((S0, decoder.kv_heads, cols * page_size), dtype=torch.float32, device=dev)
             evicted = (length, weight, position, torch.empty((S0, decoder.kv_heads, min(keep, T)), **i32))
         ws = kbb.workspace(kbb.argmax_workspace_bytes(kbb._dtype_code(W), S0, H, V), dev)
         logit = torch.empty(S0, dtype=torch.float32, device=dev)

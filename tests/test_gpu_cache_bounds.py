@@ -63,3 +63,17 @@ def test_weights_of_another_row_length_are_refused(kb):
         got = torch.zeros(shape, device="cuda")
         kb.cache_attend(q, k, v, table, n, weight_out=got)
         assert torch.equal(got.flatten()[:R * heads * 50], want.flatten())
+
+
+def test_an_evictions_own_results_under_another_default_type(kb):
+    k, v = (torch.randn(6, 1, 4, 16, device="cuda") for _ in range(2))
+    table = torch.arange(6, dtype=torch.int32, device="cuda").view(2, 3)
+    w = torch.rand(2, 1, 12, device="cuda")
+    want = w.topk(5).values.sort().values
+    torch.set_default_dtype(torch.float64)
+    try:
+        n, weight, position, source = kb.cache_evict(k, v, table, i32(12, 12), 5, weight=w)
+    finally:
+        torch.set_default_dtype(torch.float32)
+    assert n.tolist() == [5, 5] and position is None and weight.dtype == torch.float32
+    assert torch.equal(weight[:, :, :5].sort().values, want)

@@ -1,6 +1,6 @@
 """What the decode loops hand to a decoder, with the library's calls replaced by host ones: tokens are always rows of its
 embedding, also where a step has no word to give (-1 of the k-best, 2^31 - 1 of the argmax); a budget that the search
-never comes to takes no memory."""
+never comes to takes no memory; weights are float32 whatever torch's default type."""
 import pytest
 import torch
 
@@ -17,8 +17,9 @@ class Decoder:
     def cache(self, pages, page_size):
         return tuple(torch.zeros(pages, 1, page_size, 8) for _ in range(2))
 
-    def step(self, token, pos, length, k_cache, v_cache, table, *, out=None, **kw):
+    def step(self, token, pos, length, k_cache, v_cache, table, *, out=None, weight=None, **kw):
         self.seen.append(token.clone())
+        self.weight = weight
         return self.embed[token.long()] if out is None else out
 
 
@@ -61,3 +62,18 @@ def test_greedy_search_with_a_budget_past_all_memory(monkeypatch):
     start = torch.tensor([1, 2], dtype=torch.int32)
     res = decode.greedy_search(Decoder(), torch.zeros(H, V), torch.zeros(V), start, 4, 3, keep=10 ** 13)
     assert res.tokens.tolist() == [[5] * 4] * 2 and res.evictions == 0
+
+
+def test_greedy_search_under_another_default_type(monkeypatch):
+    def argmax_step(h, W, b, *, out, ws, stream):
+        out[0].fill_(5)
+    monkeypatch.setattr(decode.kbb, "argmax_step", argmax_step)
+    monkeypatch.setattr(decode, "_check_decoder", lambda *a: None)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda dev=None: None)
+    dec, W, b = Decoder(), torch.zeros(H, V), torch.zeros(V)
+    torch.set_default_dtype(torch.float64)
+    try:
+        decode.greedy_search(dec, W, b, torch.tensor([1, 2], dtype=torch.int32), 4, 3, keep=3, every=9)
+    finally:
+        torch.set_default_dtype(torch.float32)
+    assert dec.weight.dtype == torch.float32
