@@ -202,6 +202,9 @@ def _decode_loop(h_table, W, b, lengths, prev0, k, T, compact, on_step, stream) 
             off, noff, offp, noffp = noff, off, noffp, offp
             h_cur, h_nx, hp, hnp = h_nx, h_cur, hnp, hp
             t += 1
+        # the last step launched has yet to write its counts into pinned memory that is given back here
+        last = len(stats.launch_rows) - 1
+        _poll_tag(cnt_np[last % 2], last + 1)
     else:
         while t < Lmax:
             kbb.kbest_step(h_cur, W, b, prev, off, k, S=S0,

@@ -81,3 +81,26 @@ def test_a_loop_beside_a_busy_stream(kb, name):
     assert len(got) == len(want) and all(torch.equal(a.to("cpu"), b.to("cpu")) for a, b in zip(got, want))
     torch.cuda.synchronize()
     assert all(bool((y == 1).all()) for y in copies)
+
+
+def test_a_compacted_loop_writes_nothing_once_it_has_returned(kb):
+    """Its last step, launched for a batch that turns out to be empty, is held up on the device: the pinned memory of
+    its counts, given back when the loop returns, keeps what the next owner writes."""
+    from paper_1805_09863_amd.decode import decode_loop
+    work = wl.make_loop_workload(S=6, V=1001, H=64, T=8, Lmin=3, Lmax=3, seed=6)
+    bf16 = lambda a: torch.from_numpy(a.view("int16")).view(torch.bfloat16).cuda()  # noqa: E731
+    args = (bf16(work.h_table().reshape(-1, work.H)), bf16(work.W), torch.from_numpy(work.b).cuda(),
+            torch.from_numpy(work.lengths).cuda(), torch.from_numpy(work.prev0).cuda(), work.k, work.T)
+    decode_loop(*args)
+    torch.cuda.synchronize()
+    steps = []
+
+    def on_step(t, st):
+        steps.append(t)
+        if t == 2:
+            torch.cuda._sleep(40_000_000)      # about 20 ms before the step after the last
+    decode_loop(*args, on_step=on_step)
+    assert steps == [0, 1, 2]
+    owned = [torch.full((3,), -5, dtype=torch.int32, pin_memory=True) for _ in range(8)]
+    torch.cuda.synchronize()
+    assert all(x.tolist() == [-5] * 3 for x in owned)
