@@ -71,7 +71,7 @@ size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 struct AttendPlan {
   int waves, head_tiles, chunk, splits, shared;
-  size_t score_ld, part_o, part_s, row_before, scores, lse, bytes;  // workspace offsets
+  size_t score_ld, part_o, part_s, row_before, scores, finished, bytes;  // workspace offsets
 };
 
 AttendPlan attend_plan(const kb_cache* c, int R, int q_heads, int max_len, bool weights) {
@@ -107,8 +107,8 @@ AttendPlan attend_plan(const kb_cache* c, int R, int q_heads, int max_len, bool 
   if (weights) {
     p.score_ld = align_up(max_len, 32);
     p.scores = p.bytes;
-    p.lse = align_up(p.scores + rh * p.score_ld * sizeof(float), 256);
-    p.bytes = align_up(p.lse + rh * sizeof(float), 256);
+    p.finished = align_up(p.scores + rh * p.score_ld * sizeof(float), 256);
+    p.bytes = align_up(p.finished + rh * sizeof(float2), 256);
   }
   return p;
 }
@@ -205,7 +205,7 @@ kb_status kb_cache_attend(const kb_cache* cache, int R, const int32_t* n_dev, in
   if (weight_out) {
     a.scores = reinterpret_cast<float*>(ws + p.scores);
     a.score_ld = (int64_t)p.score_ld;
-    if (!lse) a.lse = reinterpret_cast<float*>(ws + p.lse);
+    a.finished = reinterpret_cast<float2*>(ws + p.finished);
   }
   hipError_t e = kb::launch_cache_attend(bf16(cache), a, reinterpret_cast<hipStream_t>(stream));
   if (e != hipSuccess) return fail(KB_ERR_HIP, "cache attention kernel launch: %s", hipGetErrorString(e));

@@ -102,12 +102,13 @@ __device__ __forceinline__ void join(const AttendArgs& a, int block) {
   if (d == 0 && a.lse) a.lse[rh] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * (1.f / kL2E);
 }
 
-// One (row, key-value head): weight_out = weight_in + sum over the sharing query heads of e^(x - lse), from the
-// stored scores, 4 slots a thread, 16 query heads at a time.  Their log-sum-exps, in base 2, are worked out
-// again from the partials, a wave a head: the join need not have run.
+// One (row, key-value head): weight_out = weight_in + sum over the sharing query heads of e^(x - m) / sum, from
+// the stored scores, 4 slots a thread, 16 query heads at a time.  The maxima m and sums of those that the pass has
+// not finished are worked out again from the partials, a wave a head: the join need not have run.  (x less the
+// log-sum-exp would cost a rounding of that one's size in every weight.)
 template <class Parts>
 __device__ __forceinline__ void weights(const AttendArgs& a, int block) {
-  __shared__ float lse[16];
+  __shared__ float2 stat[16];  // m, 1 / sum
   const CacheView& c = a.c;
   const int pairs = a.R * c.heads, y = block / pairs, pair = block - y * pairs;  // short rows have no later blocks
   const int r = pair / c.heads, kv = pair - r * c.heads, group = a.q_heads / c.heads, lane = threadIdx.x & 63;
@@ -120,17 +121,19 @@ __device__ __forceinline__ void weights(const AttendArgs& a, int block) {
     const int nh = min(16, group - ht * 16);
     const Parts parts(a, r, kv, ht);
     for (int n = threadIdx.x >> 6; n < nh; n += 4) {
-      float top = -FLT_MAX, total = 0.f;
-      if (!parts.finished()) {
-        for (int p = lane; p < parts.P; p += 64) top = fmaxf(top, a.part_s[parts.at(p, n)].x);
-        for (int i = 32; i > 0; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
-        for (int p = lane; p < parts.P; p += 64) {
-          const float2 stat = a.part_s[parts.at(p, n)];
-          total += exp2_fast(stat.x - top) * stat.y;
-        }
-        for (int i = 32; i > 0; i >>= 1) total += __shfl_xor(total, i);
+      if (parts.finished()) {
+        if (lane == 0) stat[n] = a.finished[rh + n];
+        continue;
       }
-      if (lane == 0) lse[n] = parts.finished() ? a.lse[rh + n] * kL2E : top + __builtin_amdgcn_logf(total);
+      float top = -FLT_MAX, total = 0.f;
+      for (int p = lane; p < parts.P; p += 64) top = fmaxf(top, a.part_s[parts.at(p, n)].x);
+      for (int i = 32; i > 0; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
+      for (int p = lane; p < parts.P; p += 64) {
+        const float2 s = a.part_s[parts.at(p, n)];
+        total += exp2_fast(s.x - top) * s.y;
+      }
+      for (int i = 32; i > 0; i >>= 1) total += __shfl_xor(total, i);
+      if (lane == 0) stat[n] = make_float2(top, 1.f / total);
     }
     __syncthreads();
     const float* in = ht == 0 ? a.weight_in : a.weight_out;  // later heads add to what this thread has written
@@ -145,11 +148,12 @@ __device__ __forceinline__ void weights(const AttendArgs& a, int block) {
 #pragma unroll 4
       for (int n = 0; n < nh; ++n) {
         const float4 z = *(const float4*)(a.scores + (rh + n) * a.score_ld + t);  // rows end at whole tiles
+        const float2 s = stat[n];
         const float x[4] = {z.x, z.y, z.z, z.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           there[i] &= x[i] != -INFINITY;  // a hole
-          p[i] += exp2_fast(x[i] - lse[n]);
+          p[i] += exp2_fast(x[i] - s.x) * s.y;
         }
       }
 #pragma unroll

@@ -269,7 +269,10 @@ struct AttendRun {
 #pragma unroll
       for (int i = 0; i < 4; ++i) y[i] = (T)(o[i] * norm);
       __builtin_memcpy(__builtin_assume_aligned((T*)a.out + rh * D + d, 4 * sizeof(T)), y, sizeof y);
-      if (d == 0 && a.lse) a.lse[rh] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * (1.f / kL2E);
+      if (d == 0) {
+        if (a.lse) a.lse[rh] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * (1.f / kL2E);
+        if (a.scores) a.finished[rh] = make_float2(top, norm);
+      }
     };
     if constexpr (NW == 1) {
       if (n >= nh) return;

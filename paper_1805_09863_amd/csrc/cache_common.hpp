@@ -43,19 +43,21 @@ struct AttendArgs {
   const int32_t* seq;
   const int32_t* length;
   void* out;
-  float* lse;  // nullable without weights
+  float* lse;
   const float* weight_in;
   float* weight_out;
   // the launch: waves per workgroup, tiles of 16 query heads per key-value head, splits of `chunk` slots; or
   // (shared) equal shares of all rows' slots
   int waves, head_tiles, chunk, splits, shared;
   // workspace: partial outputs (dim floats) and their (max, sum), in base 2: one per row, query head and
-  // split (splits > 1), or 16 query heads' two per share, and the costs before each row; the scores in base
-  // 2, score_ld apart per row and query head (weight_out)
+  // split (splits > 1), or 16 query heads' two per share, and the costs before each row; with weight_out the
+  // scores in base 2, score_ld apart per row and query head, and the (max, 1 / sum) of those that the pass
+  // finishes
   float* part_o;
   float2* part_s;
   int* row_before;
   float* scores;
+  float2* finished;
   int64_t score_ld;
   int weight_blocks;  // of the second launch, a (row, key-value head); the others join
 };
