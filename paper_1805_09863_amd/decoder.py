@@ -43,6 +43,7 @@ class CachedDecoder:
         shape = (pages, self.kv_heads, page_size, self.dim)
         return tuple(torch.empty(shape, dtype=self.embed.dtype, device=self.embed.device) for _ in range(2))
 
+    @torch.no_grad()
     def step(self, token: torch.Tensor, pos: torch.Tensor, length: torch.Tensor, k_cache, v_cache, table, *,
              max_len: Optional[int] = None, n_dev: Optional[torch.Tensor] = None,
              position: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
@@ -50,7 +51,8 @@ class CachedDecoder:
         """States (rows x H) of one new token a row, its keys and values appended to the cache at
         slot ``length[r] - 1``.  Runs on the current stream.  ``weight`` is added to in place
         (what eviction goes by); rows from ``n_dev[0]`` on append nothing and their states
-        mean nothing.  ``token`` holds row numbers of ``embed`` in all rows."""
+        mean nothing.  ``token`` holds row numbers of ``embed`` in all rows.  Nothing is recorded
+        for a backward pass."""
         x = self.embed.index_select(0, token)
         qkv = (x @ self.Wqkv).view(x.shape[0], -1, self.dim)
         q, k, v = qkv.split([self.q_heads, self.kv_heads, self.kv_heads], 1)

@@ -72,3 +72,19 @@ def test_states_that_are_no_numbers(kb, dtype, rows):
     others = [s for s in range(rows) if s != 1]
     a, c = (f64(r[0].score)[others] for r in runs)
     assert np.abs(a - c).max() <= 2 * T * TOL["f32" if dtype == torch.float32 else "bf16"]
+
+
+def test_searches_over_a_modules_parameters(kb):
+    """The decoder's weights and W as a trained module holds them: the same searches."""
+    from paper_1805_09863_amd.decode import beam_search, greedy_search
+    from paper_1805_09863_amd.decoder import CachedDecoder
+    dec, W, b = make(seed=6)
+    module = CachedDecoder(*(torch.nn.Parameter(x.clone()) for x in (dec.embed, dec.Wqkv, dec.Wo)), dec.q_heads,
+                           dec.kv_heads)
+    start = torch.tensor([5, 9, 11], dtype=torch.int32, device="cuda")
+    runs = []
+    for d, w, c in ((dec, W, b), (module, torch.nn.Parameter(W.clone()), torch.nn.Parameter(b.clone()))):
+        r, o = beam_search(None, w, c, 3, 12, EOS, decoder=d, start=start), greedy_search(d, w, c, start, 12, EOS, keep=6)
+        runs.append((r.tokens, r.score, o.tokens))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) and not y.requires_grad for x, y in zip(*runs))
