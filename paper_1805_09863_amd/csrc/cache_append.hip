@@ -42,8 +42,8 @@ __global__ __launch_bounds__(kAppendT) void cache_append_rows(AppendArgs a) {
   const int D = c.dim, half = a.rot / 2, H = a.q_heads + c.heads;
   const int s = cache_seq(c, a.seq, r);
   const int len = a.length[r];
+  const int pos = a.pos ? a.pos[r] : (int)(uint32_t(len) - 1u);  // (stored only where there is a slot)
   int slot = s < 0 ? -1 : new_slot(len, c.cap);
-  const int pos = a.pos ? a.pos[r] : slot;
   int64_t row = 0;
   if (slot >= 0) {
     row = cache_row(c, c.table + (int64_t)s * c.max_pages, 0, slot);
