@@ -712,9 +712,15 @@ def _cache(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor):
     if not isinstance(k_cache, torch.Tensor) or not k_cache.is_cuda:
         raise TypeError("k_cache must be a tensor on the GPU")
     dtype, dev, shape = k_cache.dtype, k_cache.get_device(), k_cache.shape
-    kp = _ask(k_cache, "k_cache", dtype, 0, dev)
-    vp = _ask(v_cache, "v_cache", dtype, 0, dev)
-    tp = _ask(table, "table", _I32, 0, dev)
+    try:
+        whole = (k_cache.is_contiguous() and v_cache.dtype is dtype and v_cache.get_device() == dev
+                 and v_cache.is_contiguous() and table.dtype is _I32 and table.get_device() == dev
+                 and table.is_contiguous())
+    except AttributeError:
+        whole = False
+    if not whole:
+        for t, name, kind in ((k_cache, "k_cache", dtype), (v_cache, "v_cache", dtype), (table, "table", _I32)):
+            _ask(t, name, kind, 0, dev)
     if len(shape) != 4 or v_cache.shape != shape:
         raise ValueError("k_cache and v_cache must be pages x heads x page_size x dim, the same shape")
     if table.dim() != 2:
@@ -726,8 +732,8 @@ def _cache(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor):
     code = _CODES.get(dtype)
     if code is None:
         _dtype_code(k_cache, "k_cache")
-    return (_Cache(code, heads, dim, page_size, pages, seqs, max_pages, kp, vp, tp), dev,
-            dtype, heads, dim, max_pages * page_size, seqs)
+    return (_Cache(code, heads, dim, page_size, pages, seqs, max_pages, k_cache.data_ptr(), v_cache.data_ptr(),
+                   table.data_ptr()), dev, dtype, heads, dim, max_pages * page_size, seqs)
 
 
 def _ask_rows(t: torch.Tensor, name: str, dtype, R: int, heads: Optional[int], dim: int, dev: int):
