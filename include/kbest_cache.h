@@ -110,7 +110,8 @@ kb_status kb_cache_append(const kb_cache* cache, int R, const int32_t* n_dev, in
  * head h / (q_heads / heads).  A row with no such slot gets zeros and lse
  * -inf.  Scores, softmax and sums are float32; probabilities enter the second
  * product with at least 16 significand bits.  NaN or infinite queries, keys
- * or values of attended slots give unspecified values in that row.
+ * or values of attended slots, and scores of 2e38 and more in magnitude, give
+ * unspecified values in that row.
  *
  *   q_heads      a multiple of the cache's heads.
  *   q            rows of q_heads x dim values, q_stride values apart, aligned

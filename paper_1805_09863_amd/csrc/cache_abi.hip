@@ -79,16 +79,19 @@ AttendPlan attend_plan(const kb_cache* c, int R, int q_heads, int max_len, bool 
   max_len = std::min(max_len, c->max_pages * c->page_size);
   const int group = q_heads / c->heads;
   p.head_tiles = (group + 15) / 16;
+  // (Times are whole calls on the device, replayed from a graph of ten over two caches in turn; bf16 heads of
+  // 128 but where stated.)
   // A unit is a row's slots for 16 query heads.  Where units fill the card and are at most 64 slots long,
-  // one wave takes each (640 rows x 8 heads of 60 slots: 14.2 us, four waves 37.6), else four take its
-  // tiles in turn (5 x 16 of 60: 4.8 us, one wave 6.6).
+  // one wave takes each (640 rows x 8 heads of up to 60 slots: 14.2 us, four waves 27.5), else four take its
+  // tiles in turn (5 x 16 of up to 60, float32 heads of 64: 5.1 us, one wave 6.8).
   const long long units = (long long)R * c->heads * p.head_tiles;
   p.waves = max_len <= 64 && units >= 1024 ? 1 : 4;
   // Beyond 6 steps of the four waves the slots are shared out: 256 workgroups take equal parts of all rows
-  // (64 x 8 of up to 8,192: 77 us, splits of 1,024 slots 94; 128 x 8 of 4,096: 376, splits 396; one row of
-  // 131,072: 99 either way; 512 workgroups 79, 375 and 100).  Up to there, where the join's launch would cost
-  // more than it gives (4 x 8 of 300: 7.4 us, shared out 11.5; 1 x 8 of 600: 9.7 and 11.2), each row is one
-  // workgroup's; and with more rows than the shares' kernel can add up, splits of 1,024 slots are.
+  // (64 x 8 of up to 8,192: 59 us, splits of 1,024 slots 71; 128 x 8 of 4,096: 377, splits 395; one row of
+  // 131,072: 103 and 104; 512 workgroups 58, 374 and 104).  Up to there, where the join's launch would cost
+  // more than it gives (4 x 8 of 300: 7.6 us, shared out 10.9; 1 x 8 of 600: 9.8 and 10.4; in float32, whose steps
+  // are half as long, 4 x 8 of 300: 12.7 and 12.2), each row is one workgroup's; and with more rows than the
+  // shares' kernel can add up, splits of 1,024 slots are.
   const int step = c->dtype == KB_BF16 ? 128 : 64;
   const bool long_rows = max_len > 6 * step;
   p.shared = long_rows && R <= kb::kShareRows;

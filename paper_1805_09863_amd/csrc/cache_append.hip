@@ -9,8 +9,8 @@
 // turn or copy them in pieces of V values, 16 bytes where every row starts at 16 bytes and the
 // turned part is whole pairs of pieces, else one value.
 //
-// Kernel time: 8,200 tokens of 32 + 8 + 8 heads of 128 bf16 values 36.9 us, 202 MB in and out at
-// 5.5 TB/s (a large copy: 4.8 to 5.2); 5 tokens 3.4 us.
+// Kernel time, the least of 20: 8,200 tokens of 32 + 8 + 8 heads of 128 bf16 values 37.0 us, 202 MB in and out
+// at 5.5 TB/s (a large copy: 4.8 to 5.2); 5 tokens 3.3 us.
 #include "cache_common.hpp"
 #include "cache_slot.hpp"
 

@@ -24,8 +24,8 @@
 // would double the error of a rounded output; the second product is not what bounds the kernel).
 // float32: 16 slots a tile, products on the fp32 matrix instruction.
 //
-// Kernel time: 128 rows of 8 key-value heads with 4,096 slots of 128 bf16 values 355 us, 6.05 TB/s
-// (a large read: 6.06), the matrix cores busy for 6 % of it; one row of 131,072 slots 91 us and 5 for
+// Kernel time, the least of 20: 128 rows of 8 key-value heads with 4,096 slots of 128 bf16 values 355 us,
+// 6.05 TB/s (a large read: 6.06), the matrix cores busy for 6 % of it; one row of 131,072 slots 91 us, and 5 for
 // the join; 640 rows of at most 60 slots 13.2 us.
 #pragma once
 
@@ -172,7 +172,8 @@ struct AttendRun {
         // The next tile's keys are asked for as soon as this one's registers are free, its values further
         // down: one of the two is always on its way.  Past the last tile they are a row of the pool again:
         // a branch around the loads would have the other half wait for them.  A lone wave has few tiles
-        // and is better off without (640 rows of at most 60 slots: 14.2 us, 14.9 with them).
+        // and is better off without (a call of 640 rows of at most 60 slots, on the device: 14.2 us, 14.8 with
+        // them).
         uint32_t next_valid;
         row = row_at(next_page, t0 + step, next_valid);
         next_page = page_of(a, pages, t0 + 2 * step);

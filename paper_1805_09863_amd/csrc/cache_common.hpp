@@ -64,8 +64,8 @@ struct AttendArgs {
 
 // Attention's slots in equal shares, where lengths differ or splits would start and end too often.
 // Every (key-value head, 16 query heads), one after the other, has all rows in order; a row costs its
-// steps (the slots that a workgroup takes at a time) and kStart more for starting on it (64 x 8 of up to
-// 8,192 slots: 77 us at 1, 80 at 2, 84 at 4).
+// steps (the slots that a workgroup takes at a time) and kStart more for starting on it (a call of 64 x 8 of up
+// to 8,192 slots: 59 us at 1, 56 at 2, 60 at 4; with weights 82, 83 and 87).
 // Share b is the b-th of kShares equal parts of all of it, one workgroup's: a row within one share is
 // finished there, one that shares cut leaves a partial in each, which the join adds up.  A share cuts at
 // most two: the one it starts within and the one it ends within.

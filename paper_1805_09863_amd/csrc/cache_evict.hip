@@ -13,10 +13,11 @@
 // a thread's word, so that the ordered part needs few barriers and later digits are counted of the
 // open slots alone.  Lengths above kEvictLds take their keys from memory where these do from LDS.
 //
-// Kernel time: 16 sequences of 8 heads, 257 slots to 256, 8.4 us (with a second launch 7.4 and 3.1);
-// 64 sequences of 8 heads, up to 1,100 to 512, 12.8 us (9 and 7.8); 4 sequences of 8 heads, 32,768 to
-// 2,048, 32 workgroups, 18.3 us (7.6 to read and count the first digit, 5.0 for the second, 2.4 for the
-// first masks) and a second launch's 13.0 to move 67 MB in and out (5.1 TB/s).
+// Kernel time, the least of 20: 16 sequences of 8 heads, 257 slots to 256, 8.4 us; 64 sequences of 8 heads, up to
+// 1,100 to 512, 12.7 us; 4 sequences of 8 heads, 32,768 to 2,048, 32 workgroups, 18.5 us (7.6 to read and count
+// the first digit, 5.0 for the second, 2.4 for the first masks) and a second launch's 13.1 to move 67 MB in and
+// out (5.1 TB/s).  Where choices are compared below, times are whole calls on the device, all launches of them,
+// replayed from a graph of ten over two caches in turn.
 #include <atomic>
 
 #include "cache_common.hpp"
@@ -274,10 +275,10 @@ __global__ __launch_bounds__(T) void cache_evict_select(EvictArgs a, int room) {
             make_uint4((uint32_t)more, (uint32_t)(more >> 32), (uint32_t)open, (uint32_t)(open >> 32));
     }
   };
-  // Where few of many slots are open, the next digits are counted of them alone, a thread a word (32 heads of
-  // 32,768 slots: 27 us, 33 of all slots; with all slots open 54 and 44; of 4,112 slots 18.5 and 15.8, of
-  // 16,384 22.3 and 22.4, of 257 10.9 and 8.0).  It takes its bits from the lane's number on, so that the keys
-  // that a wave reads lie in many banks.
+  // Where few of many slots are open, the next digits are counted of them alone, a thread a word (32 heads, to
+  // 2,048 slots elsewhere, of 32,768: 33.1 us, 39.8 of all slots; with all slots open 54.9 and 45.5; of 16,384:
+  // 28.7 and 31.2; of 4,112: 26.3 and 24.8; 128 heads of 257: 12.2 and 9.3).  It takes its bits from the lane's
+  // number on, so that the keys that a wave reads lie in many banks.
   const bool few = T == 1024 && L >= 16 * T && same < L / 4;
   const int turn = lane & 31;
   auto open_of = [&](int i) { return __builtin_rotateright32(i < words ? marks[word(i) + 2] : 0, turn); };
@@ -453,10 +454,11 @@ hipError_t launch_select(const EvictArgs& a, hipStream_t st) {
 hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t st) {
   const int pairs = a.R * a.c.heads, places = min(a.keep, a.c.cap);
   // A workgroup moves its head's rows itself where there is one for each CU (512 heads, 4,112 slots to 4,096:
-  // 34 us, with a second launch 95), or for a quarter of them and up to 512 KB of keys and values to move each
-  // (64 heads, 8,192 to 7,168: 35 and 40; 128 heads, 32,768 to 2,048, 1 MB: 85 and 69), or little to move (32
-  // heads, 300 to 256, 22 KB: 9.2 and 10.8; 4,112 to 4,096, 8 KB: 15.9 and 18.1); else the whole card does (32
-  // heads, 32,768 to 2,048, 1 MB: 42.8 and 30.5; 4,224 to 4,096, 64 KB: 21.3 and 19.3).
+  // 35.7 us, with a second launch 98.4), or for a quarter of them and up to 512 KB of keys and values to move each
+  // (64 heads, 8,192 to 7,168: 36.6 and 41.7; 128 heads, 32,768 to 2,048, 1 MB: 88.8 and 82.8), or little to move
+  // (128 heads, 257 to 256, 512 bytes: 9.3 and 11.8; 32 heads, 300 to 256, 22 KB: 9.9 and 11.5; 4,112 to 4,096, 8 KB:
+  // 16.8 and 18.5); else the whole card does (32 heads, 32,768 to 2,048, 1 MB: 45.2 and 33.1; 4,224 to 4,096, 64 KB:
+  // 22.2 and 19.7).
   const int most = a.out_table == a.c.table ? min(places, a.c.cap - places) : places;  // rows of a head that move
   const int64_t bytes = (int64_t)most * a.units * 32, little = a.c.cap <= kEvictSmall ? 128 << 10 : 32 << 10;
   if (pairs >= 256 || bytes <= (pairs >= 64 ? 512 << 10 : little)) {
@@ -467,9 +469,8 @@ hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t st) {
   }
   const hipError_t e = launch_select<false>(a, st);
   if (e != hipSuccess) return e;
-  // 16 rows a workgroup at a time, and 16 workgroups a CU (rows of 128 values: as fast as 8 or 32, with 4 it is
-  // 131 us instead of 119 for 96 heads, 32,768 slots to 4,096; 8 heads, 131,072 to 65,536, rows of 8 values:
-  // 282 us, with 8 a CU 318)
+  // 16 rows a workgroup at a time, and 16 workgroups a CU (as fast as 8 or 32; with 4 it is 124 us instead of 112
+  // for 96 heads, 32,768 slots to 4,096 of 128 values, and 273 instead of 257 for 8 heads, 131,072 to 65,536 of 8)
   const int blocks = min((places + 15) / 16, max(1, 4096 / pairs));
   cache_evict_move<<<dim3(pairs, blocks), dim3(256), 0, st>>>(a);
   return hipGetLastError();
