@@ -208,6 +208,15 @@ def workspace(nbytes: int, device=None) -> torch.Tensor:
     return torch.empty(max(int(nbytes), 1), dtype=torch.uint8, device=device or "cuda")
 
 
+def _empty(like: torch.Tensor, shape, stream, dtype=None) -> torch.Tensor:
+    """Memory of the stream that the call runs on: what the caller's current stream has freed may still be
+    in use there, and what is dropped after the call is still in use on the call's."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(stream):
+        return like.new_empty(shape, dtype=dtype)
+
+
 def kbest_step(h: torch.Tensor, W: torch.Tensor, b: torch.Tensor, prev_score: torch.Tensor,
                sent_offsets: torch.Tensor, k: int, *, S: Optional[int] = None,
                out: Optional[tuple] = None, ws: Optional[torch.Tensor] = None,
@@ -236,15 +245,15 @@ def kbest_step(h: torch.Tensor, W: torch.Tensor, b: torch.Tensor, prev_score: to
         raise ValueError("sent_offsets must have S+1 entries")
     dev = h.device
     if out is None:
-        tok = torch.empty((S, k), dtype=torch.int32, device=dev)
-        par = torch.empty((S, k), dtype=torch.int32, device=dev)
-        sc = torch.empty((S, k), dtype=torch.float32, device=dev)
+        tok = _empty(h, (S, k), stream, torch.int32)
+        par = _empty(h, (S, k), stream, torch.int32)
+        sc = _empty(h, (S, k), stream, torch.float32)
     else:
         _need_outs(out, ("token", "parent", "score"), (torch.int32, torch.int32, torch.float32), S * k)
         tok, par, sc = out
     need = kbest_workspace_bytes(dt, N, H, V, k, S)
     if ws is None:
-        ws = workspace(need, dev)
+        ws = _empty(h, max(need, 1), stream, torch.uint8)
     _need_ws(ws, need)
     if row_lse is not None:
         _need(row_lse, "row_lse", dtype=torch.float32, numel=N)
@@ -305,14 +314,14 @@ def argmax_step(h: torch.Tensor, W: torch.Tensor, b: torch.Tensor, *, out: Optio
     if H2 != H or b.shape[0] != V:
         raise ValueError("shape mismatch among h, W, b")
     if out is None:
-        tok = torch.empty(N, dtype=torch.int32, device=h.device)
-        val = torch.empty(N, dtype=torch.float32, device=h.device)
+        tok = _empty(h, N, stream, torch.int32)
+        val = _empty(h, N, stream, torch.float32)
     else:
         _need_outs(out, ("token", "logit"), (torch.int32, torch.float32), N)
         tok, val = out
     need = argmax_workspace_bytes(dt, N, H, V)
     if ws is None:
-        ws = workspace(need, h.device)
+        ws = _empty(h, max(need, 1), stream, torch.uint8)
     _need_ws(ws, need)
     _check(lib().kb_argmax_step(dt, N, H, V, _ptr(h), _ptr(W), _ptr(b), _ptr(tok), _ptr(val), _ptr(ws),
                                 ws.numel() * ws.element_size(), _stream(stream)))
@@ -340,13 +349,12 @@ def kbest_step_unfused(h: torch.Tensor, W: torch.Tensor, b: torch.Tensor, prev_s
     V = W.shape[1]
     S = sent_offsets.shape[0] - 1
     if out is None:
-        out = tuple(torch.empty((S, k), dtype=t, device=h.device)
-                    for t in (torch.int32, torch.int32, torch.float32))
+        out = tuple(_empty(h, (S, k), stream, t) for t in (torch.int32, torch.int32, torch.float32))
     _need_outs(out, ("token", "parent", "score"), (torch.int32, torch.int32, torch.float32), S * k)
     tok, par, sc = out
     need = unfused_workspace_bytes(dt, N, H, V, k, S)
     if ws is None:
-        ws = workspace(need, h.device)
+        ws = _empty(h, max(need, 1), stream, torch.uint8)
     _need_ws(ws, need)
     if row_lse is not None:
         _need(row_lse, "row_lse", dtype=torch.float32, numel=N)
@@ -378,14 +386,13 @@ def compact_batch(alive: torch.Tensor, entry_sentence: Optional[torch.Tensor] = 
     """
     _need(alive, "alive", dtype=torch.uint8, dim=1)
     M = alive.numel()
-    dev = alive.device
     if entry_sentence is not None:
         _need(entry_sentence, "entry_sentence", dtype=torch.int32, dim=1, numel=M)
     if out is None:
-        keep = torch.empty(max(M, 1), dtype=torch.int32, device=dev)
-        kept = torch.empty(1, dtype=torch.int32, device=dev)
-        noff = torch.empty(M + 1, dtype=torch.int32, device=dev) if entry_sentence is not None else None
-        nS = torch.empty(1, dtype=torch.int32, device=dev) if entry_sentence is not None else None
+        keep = _empty(alive, max(M, 1), stream, torch.int32)
+        kept = _empty(alive, 1, stream, torch.int32)
+        noff = _empty(alive, M + 1, stream, torch.int32) if entry_sentence is not None else None
+        nS = _empty(alive, 1, stream, torch.int32) if entry_sentence is not None else None
     else:
         keep, kept, noff, nS = out
         _need(keep, "keep_idx", dtype=torch.int32, numel=M)
@@ -396,7 +403,7 @@ def compact_batch(alive: torch.Tensor, entry_sentence: Optional[torch.Tensor] = 
             _need(nS, "new_S", dtype=torch.int32, numel=1)
     need = compact_workspace_bytes(M)
     if ws is None and need > 0:
-        ws = workspace(need, dev)
+        ws = _empty(alive, need, stream, torch.uint8)
     if ws is not None:
         _need_ws(ws, need)
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
@@ -415,13 +422,9 @@ def compact_beams(alive: torch.Tensor, S: int, k: int, *, out: Optional[tuple] =
     _need(alive, "alive", dtype=torch.uint8)
     if alive.numel() != S * k:
         raise ValueError("alive must have S*k entries")
-    dev = alive.device
     if out is None:
-        keep = torch.empty(max(S * k, 1), dtype=torch.int32, device=dev)
-        kept = torch.empty(1, dtype=torch.int32, device=dev)
-        noff = torch.empty(S + 1, dtype=torch.int32, device=dev)
-        ksent = torch.empty(max(S, 1), dtype=torch.int32, device=dev)
-        nS = torch.empty(1, dtype=torch.int32, device=dev)
+        keep, kept, noff, ksent, nS = (_empty(alive, n, stream, torch.int32)
+                                       for n in (max(S * k, 1), 1, S + 1, max(S, 1), 1))
     else:
         keep, kept, noff, ksent, nS = out
         _need(keep, "keep_idx", dtype=torch.int32, numel=S * k)
@@ -447,7 +450,7 @@ def gather_rows(src: torch.Tensor, idx: torch.Tensor, *, n_dev: Optional[torch.T
         _need(n_dev, "n_dev", dtype=torch.int32, numel=1)
     row_bytes = src[0].numel() * src.element_size() if src.shape[0] > 0 else 0
     if out is None:
-        out = torch.empty((n_max,) + tuple(src.shape[1:]), dtype=src.dtype, device=src.device)
+        out = _empty(src, (n_max,) + tuple(src.shape[1:]), stream)
     _need(out, "out", dtype=src.dtype, numel=n_max * (src[0].numel() if src.shape[0] > 0 else 0))
     if n_max == 0:
         return out
@@ -487,7 +490,7 @@ def shard_partials(h: torch.Tensor, W_shard: torch.Tensor, b_shard: torch.Tensor
     dt = _dtype_code(h)
     need = int(lib().kb_shard_workspace_bytes(dt, N, H, V_shard, k))
     if ws is None:
-        ws = workspace(need, h.device)
+        ws = _empty(h, max(need, 1), stream, torch.uint8)
     _need_ws(ws, need)
     _check(lib().kb_shard_partials(dt, N, H, V_shard, word_base, k, _ptr(h), _ptr(W_shard), _ptr(b_shard),
                                    _ptr(stats), _ptr(lists), _ptr(ws), ws.numel() * ws.element_size(),
@@ -509,8 +512,7 @@ def merge_partials(stats: torch.Tensor, lists: torch.Tensor, P: int, V: int, k: 
     if stats.numel() < P * N * 2 or lists.numel() < P * N * k * 2:
         raise ValueError(f"stats / lists too small for {P} splits")
     if out is None:
-        out = tuple(torch.empty((S, k), dtype=t, device=prev_score.device)
-                    for t in (torch.int32, torch.int32, torch.float32))
+        out = tuple(_empty(prev_score, (S, k), stream, t) for t in (torch.int32, torch.int32, torch.float32))
     _need_outs(out, ("token", "parent", "score"), (torch.int32, torch.int32, torch.float32), S * k)
     tok, par, sc = out
     if row_lse is not None:
@@ -620,10 +622,9 @@ def beam_backtrace(S0: int, k: int, T: int, alpha: float, fin: tuple, hist_token
     """Best finished hypothesis of every sentence by score / len**alpha, and its tokens:
     returns (tokens[S0, T], len[S0], score[S0], normalised score[S0])."""
     fc, fs, fl, fh = fin
-    dev = fc.device
     if out is None:
-        out = (torch.empty((S0, T), dtype=torch.int32, device=dev), torch.empty(S0, dtype=torch.int32, device=dev),
-               torch.empty(S0, dtype=torch.float32, device=dev), torch.empty(S0, dtype=torch.float32, device=dev))
+        out = (_empty(fc, (S0, T), stream, torch.int32), _empty(fc, S0, stream, torch.int32),
+               _empty(fc, S0, stream, torch.float32), _empty(fc, S0, stream, torch.float32))
     for x, nm_, d in ((fc, "fin_count", torch.int32), (fs, "fin_score", torch.float32),
                       (fl, "fin_len", torch.int32), (fh, "fin_hist", torch.int32)):
         _need(x, nm_, dtype=d, numel=S0 * (1 if nm_ == "fin_count" else k))
@@ -696,15 +697,6 @@ def _run(fn, dev: int, stream, *args):
             status = fn(*args, st)
     if status:
         _check(status)
-
-
-def _empty(like: torch.Tensor, shape, stream, dtype=None) -> torch.Tensor:
-    """Memory of the stream that the call runs on: what the caller's current stream has freed may still be
-    in use there, and what is dropped after the call is still in use on the call's."""
-    if stream is None:
-        return like.new_empty(shape, dtype=dtype)
-    with torch.cuda.stream(stream):
-        return like.new_empty(shape, dtype=dtype)
 
 
 def _cache(k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor):
