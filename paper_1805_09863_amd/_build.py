@@ -49,7 +49,7 @@ def _compile(hipcc: str, src: str) -> str:
 # Sources whose inline-assembly memory instructions take scalar operands or
 # rely on an M0 set by an earlier statement: their device assembly is checked
 # for the wait states and M0 uses that the compiler does not handle there.
-ISA_CHECKED = ("k1_wide.hip",)
+ISA_CHECKED = ("k1_wide.hip", "loss_logits_bf16.hip", "loss_logits_f32.hip", "loss_grads_bf16.hip", "loss_grads_f32.hip")
 
 
 def _device_asm(hipcc: str, src: str) -> str:

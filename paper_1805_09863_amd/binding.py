@@ -1,4 +1,4 @@
-"""ctypes binding of libkbest (the C ABI in include/kbest.h).
+"""ctypes binding of libkbest (the C ABI in include/kbest.h, kbest_cache.h and kbest_loss.h).
 
 Argument marshalling only: every step of the output layer runs in the HIP
 kernels of libkbest.  PyTorch supplies device memory and the current stream.
@@ -39,7 +39,7 @@ class _Cache(ctypes.Structure):
 
 _C = ctypes.POINTER(_Cache)
 
-# name -> (restype, argtypes), mirroring include/kbest.h, include/kbest_standin.h and include/kbest_cache.h
+# name -> (restype, argtypes), mirroring include/kbest.h, kbest_standin.h, kbest_cache.h and kbest_loss.h
 SIGNATURES = {
     "kb_abi_version": (_I, []),
     "kb_status_string": (ctypes.c_char_p, [_I]),
@@ -74,6 +74,13 @@ SIGNATURES = {
     "kb_cache_append": (_I, [_C, _I, _P, _I, _P, _L, _P, _L, _P, _L, _I, _I, _P, _P, _F, _P, _P, _P, _P, _P, _P]),
     "kb_cache_attend_workspace_bytes": (_SZ, [_C, _I, _I, _I, _I]),
     "kb_cache_attend": (_I, [_C, _I, _P, _I, _P, _L, _F, _P, _P, _I, _P, _P, _P, _P, _P, _SZ, _P]),
+    # losses of the output layer (include/kbest_loss.h)
+    "kb_loss_workspace_bytes": (_SZ, [_I, _I, _I, _I, _I]),
+    "kb_loss_grad_workspace_bytes": (_SZ, [_I, _I, _I, _I, _I]),
+    "kb_cross_entropy": (_I, [_I, _I, _I, _I, _P, _P, _P, _P, _F, _P, _P, _P, _SZ, _P]),
+    "kb_cross_entropy_grad": (_I, [_I, _I, _I, _I, _P, _P, _P, _P, _F, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "kb_distill": (_I, [_I, _I, _I, _I, _I, _P, _P, _P, _P, _P, _F, _P, _P, _P, _SZ, _P]),
+    "kb_distill_grad": (_I, [_I, _I, _I, _I, _I, _P, _P, _P, _P, _P, _F, _P, _P, _P, _P, _P, _P, _SZ, _P]),
     "kb_cache_evict": (_I, [_C, _I, _P, _P, _I, _I, _I, _P, _P, _P, _P, _I, _P, _P, _P, _P, _P]),
 }
 
@@ -928,3 +935,142 @@ def rotary_frequencies(rot_dim: int, *, base: float = 10000.0, factor: float = 1
         stay = ((turns - slow) / (fast - slow)).clamp(0.0, 1.0)
         w = w * stay + w / factor * (1.0 - stay)
     return w.to(device or "cuda")
+
+
+# ---------------------------------------------------------------- losses of the output layer
+def loss_workspace_bytes(dtype: int, N: int, H: int, V: int, K: int = 1) -> int:
+    """Workspace of ``cross_entropy`` (K = 1) and ``distill``."""
+    return int(lib().kb_loss_workspace_bytes(dtype, N, H, V, K))
+
+
+def loss_grad_workspace_bytes(dtype: int, N: int, H: int, V: int, K: int = 1) -> int:
+    """Workspace of ``cross_entropy_grad`` (K = 1) and ``distill_grad``."""
+    return int(lib().kb_loss_grad_workspace_bytes(dtype, N, H, V, K))
+
+
+def _loss_layer(h, W, b, rows):
+    """Checks the layer and the tensors of one value a row, all on one device; returns (dtype, N, H, V)."""
+    _need(h, "h", dim=2)
+    _need(W, "W", dtype=h.dtype, dim=2)
+    _need(b, "b", dtype=torch.float32, dim=1)
+    dt = _dtype_code(h)
+    N, H = h.shape
+    V = W.shape[1]
+    if W.shape[0] != H or b.shape[0] != V:
+        raise ValueError("shape mismatch among h, W, b")
+    for name, t, dtype, shape in rows:
+        _need(t, name, dtype=dtype)
+        if t.shape != shape:
+            raise ValueError(f"{name} must be {' x '.join(str(n) for n in shape)}, got {tuple(t.shape)}")
+        if t.device != h.device:
+            raise ValueError(f"{name} must be on {h.device}, as h is")
+    if W.device != h.device or b.device != h.device:
+        raise ValueError(f"W and b must be on {h.device}, as h is")
+    return dt, N, H, V
+
+
+def _loss_out(h, N, out, stream):
+    if out is None:
+        return _empty(h, N, stream, torch.float32), _empty(h, N, stream, torch.float32)
+    _need_outs(out, ("loss", "lse"), (torch.float32, torch.float32), N)
+    return out
+
+
+def _grad_out(h, W, b, out, stream):
+    if out is None:
+        return tuple(_empty(t, t.shape, stream, t.dtype) for t in (h, W, b))
+    if len(out) != 3:
+        raise ValueError("out must hold 3 tensors or Nones (dh, dW, db)")
+    if all(t is None for t in out):
+        raise ValueError("out holds no tensor: no gradient is asked for")
+    for t, name, like in zip(out, ("dh", "dW", "db"), (h, W, b)):
+        if t is None:
+            continue
+        _need(t, name, dtype=like.dtype)
+        if t.shape != like.shape:
+            raise ValueError(f"{name} must be {tuple(like.shape)}, got {tuple(t.shape)}")
+    return out
+
+
+def _loss_ws(h, need, ws, stream):
+    if ws is None:
+        ws = _empty(h, max(need, 1), stream, torch.uint8)
+    _need_ws(ws, need)
+    return ws
+
+
+def cross_entropy(h: torch.Tensor, W: torch.Tensor, b: torch.Tensor, target: torch.Tensor, *, smoothing: float = 0.0,
+                  out: Optional[tuple] = None, ws: Optional[torch.Tensor] = None, stream=None):
+    """Cross entropy of the output layer: returns (loss, lse), N float32 each, without storing h W + b.
+
+    ``h`` is N x H, ``W`` H x V (float32 or bfloat16, same type), ``b`` V float32 as for ``kbest_step``;
+    ``target`` N int32, the word of every row (outside 0 .. V - 1: the row is left out, its loss and lse are
+    0).  ``smoothing``: the part of the labels that is spread over all words.  ``out`` may supply (loss, lse),
+    ``ws`` a workspace of at least ``loss_workspace_bytes`` bytes.
+    """
+    N = h.shape[0] if isinstance(h, torch.Tensor) and h.dim() else 0
+    dt, N, H, V = _loss_layer(h, W, b, (("target", target, torch.int32, (N,)),))
+    loss, lse = _loss_out(h, N, out, stream)
+    ws = _loss_ws(h, loss_workspace_bytes(dt, N, H, V), ws, stream)
+    _check(lib().kb_cross_entropy(dt, N, H, V, _ptr(h), _ptr(W), _ptr(b), _ptr(target), smoothing, _ptr(loss),
+                                  _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream, h.device)))
+    return loss, lse
+
+
+def cross_entropy_grad(h: torch.Tensor, W: torch.Tensor, b: torch.Tensor, target: torch.Tensor, lse: torch.Tensor,
+                       grad: torch.Tensor, *, smoothing: float = 0.0, out: Optional[tuple] = None,
+                       ws: Optional[torch.Tensor] = None, stream=None):
+    """Gradients of sum(grad * loss) of ``cross_entropy`` with the same h, W, b, target and smoothing: returns
+    (dh, dW, db), of the types and shapes of h, W and b.
+
+    ``lse`` is what ``cross_entropy`` returned, ``grad`` N float32.  ``out`` may supply (dh, dW, db), with None
+    for what is not wanted; ``ws`` a workspace of at least ``loss_grad_workspace_bytes`` bytes.
+    """
+    N = h.shape[0] if isinstance(h, torch.Tensor) and h.dim() else 0
+    dt, N, H, V = _loss_layer(h, W, b, (("target", target, torch.int32, (N,)), ("lse", lse, torch.float32, (N,)),
+                                        ("grad", grad, torch.float32, (N,))))
+    out = _grad_out(h, W, b, out, stream)
+    ws = _loss_ws(h, loss_grad_workspace_bytes(dt, N, H, V), ws, stream)
+    _check(lib().kb_cross_entropy_grad(dt, N, H, V, _ptr(h), _ptr(W), _ptr(b), _ptr(target), smoothing, _ptr(lse),
+                                       _ptr(grad), _ptr(out[0]), _ptr(out[1]), _ptr(out[2]), _ptr(ws),
+                                       ws.numel() * ws.element_size(), _stream(stream, h.device)))
+    return tuple(out)
+
+
+def distill(h: torch.Tensor, W: torch.Tensor, b: torch.Tensor, token: torch.Tensor, logit: torch.Tensor, *,
+            temperature: float = 1.0, out: Optional[tuple] = None, ws: Optional[torch.Tensor] = None, stream=None):
+    """Distillation from a teacher's best words: returns (loss, lse), N float32 each.
+
+    ``token``, ``logit``: N x K int32 and float32, the teacher's words for every row and their logits (or
+    log-probabilities), in any order; a token outside 0 .. V - 1 or a logit of -inf is no entry, and a row
+    without one is left out.  The loss is temperature^2 times the divergence of softmax(student / temperature)
+    from softmax(logit / temperature); lse is the log-sum-exp of the student's logits / temperature.
+    """
+    shape = (h.shape[0] if isinstance(h, torch.Tensor) and h.dim() else 0,
+             token.shape[1] if isinstance(token, torch.Tensor) and token.dim() == 2 else 0)
+    dt, N, H, V = _loss_layer(h, W, b, (("token", token, torch.int32, shape), ("logit", logit, torch.float32, shape)))
+    K = shape[1]
+    loss, lse = _loss_out(h, N, out, stream)
+    ws = _loss_ws(h, loss_workspace_bytes(dt, N, H, V, K), ws, stream)
+    _check(lib().kb_distill(dt, N, H, V, K, _ptr(h), _ptr(W), _ptr(b), _ptr(token), _ptr(logit), temperature,
+                            _ptr(loss), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(),
+                            _stream(stream, h.device)))
+    return loss, lse
+
+
+def distill_grad(h: torch.Tensor, W: torch.Tensor, b: torch.Tensor, token: torch.Tensor, logit: torch.Tensor,
+                 lse: torch.Tensor, grad: torch.Tensor, *, temperature: float = 1.0, out: Optional[tuple] = None,
+                 ws: Optional[torch.Tensor] = None, stream=None):
+    """Gradients of sum(grad * loss) of ``distill`` with the same arguments: returns (dh, dW, db), as
+    ``cross_entropy_grad`` does; the teacher has none."""
+    shape = (h.shape[0] if isinstance(h, torch.Tensor) and h.dim() else 0,
+             token.shape[1] if isinstance(token, torch.Tensor) and token.dim() == 2 else 0)
+    dt, N, H, V = _loss_layer(h, W, b, (("token", token, torch.int32, shape), ("logit", logit, torch.float32, shape),
+                                        ("lse", lse, torch.float32, shape[:1]), ("grad", grad, torch.float32, shape[:1])))
+    K = shape[1]
+    out = _grad_out(h, W, b, out, stream)
+    ws = _loss_ws(h, loss_grad_workspace_bytes(dt, N, H, V, K), ws, stream)
+    _check(lib().kb_distill_grad(dt, N, H, V, K, _ptr(h), _ptr(W), _ptr(b), _ptr(token), _ptr(logit), temperature,
+                                 _ptr(lse), _ptr(grad), _ptr(out[0]), _ptr(out[1]), _ptr(out[2]), _ptr(ws),
+                                 ws.numel() * ws.element_size(), _stream(stream, h.device)))
+    return tuple(out)

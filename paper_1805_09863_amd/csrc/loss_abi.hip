@@ -1,0 +1,488 @@
+// Host side of the output layer's losses: argument validation, the plan of a
+// call and the entry points declared in include/kbest_loss.h.
+#include <math.h>
+
+#include <algorithm>
+
+#include "kb_status.hpp"
+#include "kbest_loss.h"
+#include "loss_common.hpp"
+
+namespace kb {
+hipError_t launch_loss_logits_bf16(bool grad, int BN, const LossLogitsArgs& a, int blocks, hipStream_t st);
+hipError_t launch_loss_logits_f32(bool grad, int BN, const LossLogitsArgs& a, int blocks, hipStream_t st);
+hipError_t launch_loss_dh_bf16(int BN, const LossGradArgs& a, hipStream_t st);
+hipError_t launch_loss_dh_f32(int BN, const LossGradArgs& a, hipStream_t st);
+hipError_t launch_loss_dw_bf16(int BNh, const LossGradArgs& a, hipStream_t st);
+hipError_t launch_loss_dw_f32(int BNh, const LossGradArgs& a, hipStream_t st);
+}  // namespace kb
+
+namespace {
+
+using kb::aligned;
+using kb::fail;
+using kb::ok;
+
+static_assert(kb::kLossMaxV == KB_LOSS_MAX_V && kb::kLossMaxK == KB_LOSS_MAX_K, "the same limits");
+
+int up(int x, int a) { return (x + a - 1) / a * a; }
+
+// Takes stretches of a workspace, each at a multiple of 256 bytes.
+struct Space {
+  size_t at = 0;
+  size_t take(size_t bytes) {
+    const size_t p = at;
+    at = (at + bytes + 255) / 256 * 256;
+    return p;
+  }
+};
+
+struct Plan {
+  bool bf16, direct;
+  int planes, z;
+  int N, H, V, K;
+  int BN, R, WN, WTM, WTN;  // row tile, how many, and the wave's part
+  int Hp, Hk, BNh;
+  int vt, words0, nb, grid;
+  int piece;                // word tiles of a piece of the vocabulary
+  int pieces;
+  int dh_mt, dh_splits, dw_ntn, dw_splits;
+  // workspace
+  size_t count, map, inv, flag, token, part, known, offs, items, ph, b, wp, stat, sumx, xt, rowp, g, dbp, dh_part, dw_part;
+  size_t stat_piece;        // values of one piece's statistics
+  size_t bytes;
+};
+
+// The plan of a call. `direct`: W is read where it lies; else its pieces are laid out first (float32 in bf16 pieces, odd
+// sizes and addresses with zeros filled up).
+Plan make_plan(int dtype, int N, int H, int V, int K, bool teacher, bool grad, bool w_aligned) {
+  Plan p{};
+  p.bf16 = dtype == KB_BF16;
+  p.planes = p.bf16 ? 1 : 3;
+  p.z = p.bf16 ? 2 : 4;
+  p.N = N, p.H = H, p.V = V, p.K = K;
+  p.BN = N <= 32 ? 32 : N <= 64 ? 64 : N <= 128 ? 128 : 256;
+  p.R = kb::loss_row_tiles(N, p.BN);
+  p.WN = p.BN >= 128 ? 2 : 1;
+  p.WTM = kb::loss_wtm(p.BN);
+  p.WTN = kb::loss_wtn(p.BN);
+  p.BNh = H > 128 ? 256 : 128;
+  p.Hp = up(H, p.BNh);
+  p.Hk = up(H, kb::kLossStage);
+  p.vt = (V + kb::kLossM - 1) / kb::kLossM;
+  p.words0 = p.vt * (kb::kLossM / p.WTM);
+  p.nb = p.BN / p.WTN * p.words0;
+  p.grid = std::max(p.BN == 32 ? 512 : 256, p.R);
+  const bool shape = p.bf16 && H % kb::kLossStage == 0 && V % 8 == 0 && V >= kb::kLossM;
+  p.direct = shape && w_aligned;
+
+  // A piece: as many words as keep its dlogits, and the part of W that is laid out, near the last-level cache's size.
+  // (W at an odd address where its shape needs no laying out: small pieces, so that the workspace need not grow.)
+  const size_t most = (size_t)128 << 20;
+  const size_t w_tile = (size_t)p.Hk * kb::kLossM * 2 * p.planes, g_tile = (size_t)p.R * p.BN * kb::kLossM * 2 * p.planes;
+  size_t tiles = p.vt;
+  if (!p.direct) tiles = std::min(tiles, std::max<size_t>(1, (shape ? most / 16 : most) / w_tile));
+  if (grad) tiles = std::min(tiles, std::max<size_t>(1, most / g_tile));
+  p.pieces = (int)((p.vt + tiles - 1) / tiles);
+  p.piece = (p.vt + p.pieces - 1) / p.pieces;
+  p.pieces = (p.vt + p.piece - 1) / p.piece;
+
+  Space s;
+  p.count = s.take(4);
+  p.map = s.take((size_t)N * 4);
+  p.inv = s.take((size_t)N * 4);
+  if (teacher) {
+    p.flag = s.take(N);
+    p.token = s.take((size_t)N * K * 4);
+    p.part = s.take((size_t)N * K * 4);
+    p.known = s.take((size_t)N * 4);
+  }
+  p.offs = s.take((size_t)p.R * (p.nb + 1) * 4);
+  p.items = s.take((size_t)p.R * p.BN * K * sizeof(kb::LossItem));
+  p.ph = s.take((size_t)p.planes * p.R * p.BN * p.Hp * 2);
+  p.b = s.take((size_t)p.vt * kb::kLossM * 4);
+  if (!p.direct) p.wp = s.take(p.piece * w_tile);
+  if (!grad) {
+    p.stat_piece = (size_t)p.grid * p.BN;
+    p.stat = s.take(p.pieces * p.stat_piece * sizeof(float2));
+    p.sumx = s.take(p.pieces * p.stat_piece * 4);
+    p.xt = s.take((size_t)p.R * p.BN * K * 4);
+  } else {
+    p.rowp = s.take((size_t)p.R * p.BN * sizeof(float2));
+    p.g = s.take(p.piece * g_tile);
+    p.dbp = s.take((size_t)p.R * p.WN * p.vt * kb::kLossM * 4);
+    p.dh_mt = (H + kb::kLossM - 1) / kb::kLossM;
+    p.dh_splits = std::max(1, std::min((p.BN == 32 ? 512 : 256) / (p.R * p.dh_mt), p.piece));
+    p.dh_part = s.take((size_t)p.dh_splits * p.R * p.dh_mt * kb::kLossM * p.BN * 4);
+    p.dw_ntn = p.Hp / p.BNh;
+    const int stages = p.R * p.BN / kb::kLossStage;
+    p.dw_splits = std::max(1, std::min(256 / (p.piece * p.dw_ntn), stages / 8));
+    if (p.dw_splits > 1) p.dw_part = s.take((size_t)p.dw_splits * p.piece * p.dw_ntn * kb::kLossM * p.BNh * 4);
+  }
+  p.bytes = s.at;
+  return p;
+}
+
+kb_status check_sizes(int dtype, int N, int H, int V, int K) {
+  if (dtype != KB_F32 && dtype != KB_BF16) return fail(KB_ERR_INVALID_ARG, "unknown dtype %d", dtype);
+  if (N < 0 || H < 1 || V < 1) return fail(KB_ERR_INVALID_ARG, "N = %d, H = %d, V = %d", N, H, V);
+  if (K < 1 || K > KB_LOSS_MAX_K) return fail(KB_ERR_INVALID_ARG, "K = %d: 1 to %d", K, KB_LOSS_MAX_K);
+  if (V > KB_LOSS_MAX_V || H > KB_LOSS_MAX_H || N > KB_LOSS_MAX_N || (long long)N * K > (1 << 30))
+    return fail(KB_ERR_UNSUPPORTED, "N = %d, H = %d, V = %d, K = %d: beyond the limits", N, H, V, K);
+  return KB_OK;
+}
+
+size_t workspace_bytes(int dtype, int N, int H, int V, int K, bool grad) {
+  if (check_sizes(dtype, N, H, V, K) != KB_OK || N == 0) return 0;
+  return std::max(make_plan(dtype, N, H, V, K, true, grad, true).bytes,
+                  make_plan(dtype, N, H, V, K, true, grad, false).bytes);
+}
+
+// What the two losses have in common.
+struct Call {
+  int dtype, N, H, V, K;
+  const void *h, *W;
+  const float* b;
+  const int32_t* token;
+  const float* logit;  // null: targets
+  float smoothing, temperature;
+  float *loss, *lse;   // forward
+  const float *lse_in, *grad;
+  void *dh, *dW;
+  float* db;
+  void* ws;
+  size_t ws_bytes;
+  hipStream_t st;
+};
+
+kb_status check_call(const Call& c, const Plan& p) {
+  if (!c.h || !c.W || !c.b || !c.token) return fail(KB_ERR_INVALID_ARG, "null h, W, b or words");
+  if (!aligned(c.h, p.z) || !aligned(c.W, p.z) || !aligned(c.b, 4) || !aligned(c.token, 4) || !aligned(c.logit, 4))
+    return fail(KB_ERR_INVALID_ARG, "h, W, b or words not aligned to their type");
+  if (!c.ws) return fail(KB_ERR_WORKSPACE, "workspace is null (%zu bytes needed)", p.bytes);
+  if (!aligned(c.ws, 256)) return fail(KB_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  if (c.ws_bytes < p.bytes) return fail(KB_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", c.ws_bytes, p.bytes);
+  return KB_OK;
+}
+
+struct Work {
+  kb::LossRows rows;
+  char* ws;
+  template <class X>
+  X* at(size_t o) const {
+    return reinterpret_cast<X*>(ws + o);
+  }
+};
+
+#define KB_LAUNCH(what, call)                                                            \
+  do {                                                                                   \
+    const hipError_t e_ = (call);                                                        \
+    if (e_ != hipSuccess) return fail(KB_ERR_HIP, what ": %s", hipGetErrorString(e_));   \
+  } while (0)
+
+// Rows that count, their states, entries and bias laid out.
+kb_status prepare(const Call& c, const Plan& p, Work& w, bool grad) {
+  w.ws = static_cast<char*>(c.ws);
+  kb::LossRows& r = w.rows;
+  r = {c.N, c.H, c.V, c.K, c.token, nullptr, 1.f - c.smoothing, nullptr, w.at<int32_t>(p.map), w.at<int32_t>(p.inv),
+       w.at<int32_t>(p.count)};
+  if (c.logit) {
+    r.token = w.at<int32_t>(p.token);
+    r.part = w.at<float>(p.part);
+    r.flag = w.at<uint8_t>(p.flag);
+    const kb::LossTeacherArgs t{c.N, c.K, c.V, c.token, c.logit, 1.f / c.temperature, w.at<int32_t>(p.token),
+                                w.at<float>(p.part), w.at<float>(p.known), w.at<uint8_t>(p.flag)};
+    KB_LAUNCH("teacher's rows", kb::launch_loss_teacher(t, c.st));
+  }
+  KB_LAUNCH("rows of a loss", kb::launch_loss_rows(r, c.st));
+  kb::LossPackArgs a{};
+  a.rows = r;
+  a.h = c.h;
+  a.ph = w.at<uint16_t>(p.ph);
+  a.ph_plane = (size_t)p.R * p.BN * p.Hp;
+  a.Hp = p.Hp;
+  a.BN = p.BN;
+  a.tiles = p.R;
+  a.nb = p.nb;
+  a.words0 = p.words0;
+  a.offs = w.at<int32_t>(p.offs);
+  a.items = w.at<kb::LossItem>(p.items);
+  if (grad) {
+    a.lse = c.lse_in;
+    a.grad = c.grad;
+    a.grad_scale = c.temperature;  // d loss / dx = T^2 (p - q) / T; 1 for targets
+    a.rowp = w.at<float2>(p.rowp);
+  }
+  KB_LAUNCH("states of a loss", kb::launch_loss_pack(p.bf16, a, c.st));
+  KB_LAUNCH("bias of a loss", kb::launch_loss_pack_b(c.b, c.V, p.vt * kb::kLossM, w.at<float>(p.b), c.st));
+  return KB_OK;
+}
+
+// Side W of a piece that starts at word tile t0 and has `tiles` of them: laid out if it has to be.
+struct PieceW {
+  const uint16_t* p;
+  size_t plane;
+  int ld, cols, rows;
+};
+kb_status piece_w(const Call& c, const Plan& p, const Work& w, int t0, int tiles, PieceW& out) {
+  const int v0 = t0 * kb::kLossM;
+  if (p.direct) {
+    out = {static_cast<const uint16_t*>(c.W) + v0, 0, c.V, c.V - v0, c.H};
+    return KB_OK;
+  }
+  const int Vc = tiles * kb::kLossM;
+  const kb::LossPackWArgs a{c.W, c.H, c.V, v0, Vc, p.Hk, w.at<uint16_t>(p.wp), (size_t)p.Hk * Vc};
+  KB_LAUNCH("weights of a loss", kb::launch_loss_pack_w(p.bf16, a, c.st));
+  out = {a.out, a.plane, Vc, Vc, p.Hk};
+  return KB_OK;
+}
+
+kb::LossLogitsArgs logits_args(const Call& c, const Plan& p, const Work& w, const PieceW& pw, int t0, int tiles) {
+  kb::LossLogitsArgs a{};
+  a.A = pw.p;
+  a.a_plane = pw.plane;
+  a.lda = pw.ld;
+  a.a_cols = pw.cols;
+  a.ph = w.at<uint16_t>(p.ph);
+  a.ph_plane = (size_t)p.R * p.BN * p.Hp;
+  a.Hp = p.Hp;
+  a.Hk = p.Hk;
+  a.b = w.at<float>(p.b) + (size_t)t0 * kb::kLossM;
+  a.words = c.V - t0 * kb::kLossM;
+  a.vt = tiles;
+  a.N = c.N;
+  a.count = w.rows.count;
+  a.grid = p.grid;
+  a.scale = kb::kL2E / c.temperature;
+  a.offs = w.at<int32_t>(p.offs);
+  a.items = w.at<kb::LossItem>(p.items);
+  a.nb = p.nb;
+  a.words0 = p.words0;
+  a.wt0 = t0 * (kb::kLossM / p.WTM);
+  a.K = c.K;
+  a.rest = c.smoothing / (float)c.V;
+  return a;
+}
+
+kb_status forward(const Call& c) {
+  const Plan p = make_plan(c.dtype, c.N, c.H, c.V, c.K, c.logit != nullptr, false, aligned(c.W, 16));
+  kb_status s = check_call(c, p);
+  if (s != KB_OK) return s;
+  if (!c.loss || !c.lse) return fail(KB_ERR_INVALID_ARG, "null loss or lse");
+  if (!aligned(c.loss, 4) || !aligned(c.lse, 4)) return fail(KB_ERR_INVALID_ARG, "loss or lse not aligned to their type");
+  Work w;
+  if ((s = prepare(c, p, w, false)) != KB_OK) return s;
+  const bool smooth = c.smoothing > 0.f;
+  for (int i = 0; i < p.pieces; ++i) {
+    const int t0 = i * p.piece, tiles = std::min(p.piece, p.vt - t0);
+    PieceW pw;
+    if ((s = piece_w(c, p, w, t0, tiles, pw)) != KB_OK) return s;
+    kb::LossLogitsArgs a = logits_args(c, p, w, pw, t0, tiles);
+    a.stat = w.at<float2>(p.stat) + i * p.stat_piece;
+    a.sumx = smooth ? w.at<float>(p.sumx) + i * p.stat_piece : nullptr;
+    a.xt = w.at<float>(p.xt);
+    KB_LAUNCH("logits of a loss", p.bf16 ? kb::launch_loss_logits_bf16(false, p.BN, a, p.grid, c.st)
+                                         : kb::launch_loss_logits_f32(false, p.BN, a, p.grid, c.st));
+  }
+  kb::LossFinishArgs f{};
+  f.rows = w.rows;
+  f.stat = w.at<float2>(p.stat);
+  f.sumx = smooth ? w.at<float>(p.sumx) : nullptr;
+  f.stat_piece = p.stat_piece;
+  f.pieces = p.pieces;
+  f.vt_piece = p.piece;
+  f.vt_last = p.vt - (p.pieces - 1) * p.piece;
+  f.grid = p.grid;
+  f.BN = p.BN;
+  f.xt = w.at<float>(p.xt);
+  f.known = c.logit ? w.at<float>(p.known) : nullptr;
+  f.scale = kb::kL2E / c.temperature;
+  f.inv_t = 1.f / c.temperature;
+  f.rest = c.smoothing / (float)c.V;
+  f.t2 = c.temperature * c.temperature;
+  f.loss = c.loss;
+  f.lse = c.lse;
+  KB_LAUNCH("losses", kb::launch_loss_finish(f, c.st));
+  return ok();
+}
+
+kb_status gradient(const Call& c) {
+  const Plan p = make_plan(c.dtype, c.N, c.H, c.V, c.K, c.logit != nullptr, true, aligned(c.W, 16));
+  kb_status s = check_call(c, p);
+  if (s != KB_OK) return s;
+  if (!c.lse_in || !c.grad) return fail(KB_ERR_INVALID_ARG, "null lse or grad");
+  if (!aligned(c.lse_in, 4) || !aligned(c.grad, 4))
+    return fail(KB_ERR_INVALID_ARG, "lse or grad not aligned to their type");
+  Work w;
+  if ((s = prepare(c, p, w, true)) != KB_OK) return s;
+  const size_t rows = (size_t)p.R * p.BN;
+  const int Vp = p.vt * kb::kLossM;
+  for (int i = 0; i < p.pieces; ++i) {
+    const int t0 = i * p.piece, tiles = std::min(p.piece, p.vt - t0), Vc = tiles * kb::kLossM;
+    PieceW pw;
+    if ((s = piece_w(c, p, w, t0, tiles, pw)) != KB_OK) return s;
+    kb::LossLogitsArgs a = logits_args(c, p, w, pw, t0, tiles);
+    if (!p.bf16) a.scale = 1.f / c.temperature;  // the difference from lse is taken first
+    a.rowp = w.at<float2>(p.rowp);
+    a.g = w.at<uint16_t>(p.g);
+    a.g_plane = rows * Vc;
+    a.gld = Vc;
+    a.dbp = c.db ? w.at<float>(p.dbp) : nullptr;
+    a.db_ld = Vp;
+    a.db0 = t0 * kb::kLossM;
+    KB_LAUNCH("logits of a loss", p.bf16 ? kb::launch_loss_logits_bf16(true, p.BN, a, p.grid, c.st)
+                                         : kb::launch_loss_logits_f32(true, p.BN, a, p.grid, c.st));
+    kb::LossGradArgs g{};
+    g.W = pw.p;
+    g.w_plane = pw.plane;
+    g.ldw = pw.ld;
+    g.w_rows = pw.rows;
+    g.ph = a.ph;
+    g.ph_plane = a.ph_plane;
+    g.Hp = p.Hp;
+    g.H = c.H;
+    g.g = a.g;
+    g.g_plane = a.g_plane;
+    g.gld = Vc;
+    g.N = c.N;
+    g.BN = p.BN;
+    g.count = w.rows.count;
+    g.V = c.V;
+    if (c.dh) {
+      g.words = pw.cols;
+      g.splits = p.dh_splits;
+      g.mt = p.dh_mt;
+      g.part = w.at<float>(p.dh_part);
+      g.add = i > 0;
+      KB_LAUNCH("gradient of the states", p.bf16 ? kb::launch_loss_dh_bf16(p.BN, g, c.st) : kb::launch_loss_dh_f32(p.BN, g, c.st));
+    }
+    if (c.dW) {
+      g.words = c.V - t0 * kb::kLossM;
+      g.splits = p.dw_splits;
+      g.mt = tiles;
+      g.ntn = p.dw_ntn;
+      g.part = p.dw_splits > 1 ? w.at<float>(p.dw_part) : nullptr;
+      g.out = static_cast<char*>(c.dW) + (size_t)t0 * kb::kLossM * p.z;
+      KB_LAUNCH("gradient of the weights", p.bf16 ? kb::launch_loss_dw_bf16(p.BNh, g, c.st) : kb::launch_loss_dw_f32(p.BNh, g, c.st));
+      if (g.part) {
+        kb::LossJoinArgs j{g.part, p.dw_splits, tiles, p.dw_ntn, p.BNh, c.H, std::min(g.words, Vc), 0, nullptr, nullptr,
+                           g.out, c.V};
+        KB_LAUNCH("gradient of the weights", kb::launch_loss_join(p.bf16, j, nullptr, 0, c.st));
+      }
+    }
+  }
+  if (c.dh) {
+    kb::LossJoinArgs j{w.at<float>(p.dh_part), p.dh_splits, p.dh_mt, p.R, p.BN, c.N, c.H, 1, w.rows.map, w.rows.count,
+                       c.dh, c.H};
+    KB_LAUNCH("gradient of the states", kb::launch_loss_join(p.bf16, j, w.rows.inv, c.N, c.st));
+  }
+  if (c.db) KB_LAUNCH("gradient of the bias", kb::launch_loss_db(w.at<float>(p.dbp), p.WN, p.BN, Vp, w.rows.count, c.V, c.db, c.st));
+  return ok();
+}
+
+kb_status run_gradient(const Call& c) {
+  const int z = c.dtype == KB_BF16 ? 2 : 4;
+  if (!c.dh && !c.dW && !c.db) return fail(KB_ERR_INVALID_ARG, "no gradient is asked for");
+  if (!aligned(c.dh, z) || !aligned(c.dW, z) || !aligned(c.db, 4))
+    return fail(KB_ERR_INVALID_ARG, "dh, dW or db not aligned to their type");
+  if (c.N > 0) return gradient(c);
+  if (c.dW) KB_LAUNCH("gradient of the weights", kb::launch_loss_zero(c.dW, (size_t)c.H * c.V * z, c.st));
+  if (c.db) KB_LAUNCH("gradient of the bias", kb::launch_loss_zero(c.db, (size_t)c.V * 4, c.st));
+  return ok();
+}
+
+kb_status check_smoothing(float s) {
+  if (!(s >= 0.f && s < 1.f)) return fail(KB_ERR_INVALID_ARG, "smoothing = %g: 0 <= smoothing < 1", (double)s);
+  return KB_OK;
+}
+
+kb_status check_temperature(float t) {
+  // T^2 and 1 / T are finite and normal
+  if (!(t >= 1e-6f && t <= 1e6f)) return fail(KB_ERR_INVALID_ARG, "temperature = %g: 1e-6 to 1e6", (double)t);
+  return KB_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t kb_loss_workspace_bytes(int dtype, int N, int H, int V, int K) { return workspace_bytes(dtype, N, H, V, K, false); }
+
+size_t kb_loss_grad_workspace_bytes(int dtype, int N, int H, int V, int K) {
+  return workspace_bytes(dtype, N, H, V, K, true);
+}
+
+kb_status kb_cross_entropy(int dtype, int N, int H, int V, const void* h, const void* W, const float* b,
+                           const int32_t* target, float smoothing, float* loss, float* lse, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  kb_status s = check_sizes(dtype, N, H, V, 1);
+  if (s != KB_OK || (s = check_smoothing(smoothing)) != KB_OK) return s;
+  if (N == 0) return ok();
+  Call c{dtype, N, H, V, 1, h, W, b, target};
+  c.smoothing = smoothing;
+  c.temperature = 1.f;
+  c.loss = loss;
+  c.lse = lse;
+  c.ws = workspace;
+  c.ws_bytes = workspace_bytes;
+  c.st = reinterpret_cast<hipStream_t>(stream);
+  return forward(c);
+}
+
+kb_status kb_cross_entropy_grad(int dtype, int N, int H, int V, const void* h, const void* W, const float* b,
+                                const int32_t* target, float smoothing, const float* lse, const float* grad, void* dh,
+                                void* dW, float* db, void* workspace, size_t workspace_bytes, void* stream) {
+  kb_status s = check_sizes(dtype, N, H, V, 1);
+  if (s != KB_OK || (s = check_smoothing(smoothing)) != KB_OK) return s;
+  Call c{dtype, N, H, V, 1, h, W, b, target};
+  c.smoothing = smoothing;
+  c.temperature = 1.f;
+  c.lse_in = lse;
+  c.grad = grad;
+  c.dh = dh;
+  c.dW = dW;
+  c.db = db;
+  c.ws = workspace;
+  c.ws_bytes = workspace_bytes;
+  c.st = reinterpret_cast<hipStream_t>(stream);
+  return run_gradient(c);
+}
+
+kb_status kb_distill(int dtype, int N, int H, int V, int K, const void* h, const void* W, const float* b,
+                     const int32_t* token, const float* logit, float temperature, float* loss, float* lse,
+                     void* workspace, size_t workspace_bytes, void* stream) {
+  kb_status s = check_sizes(dtype, N, H, V, K);
+  if (s != KB_OK || (s = check_temperature(temperature)) != KB_OK) return s;
+  if (N == 0) return ok();
+  if (!logit) return fail(KB_ERR_INVALID_ARG, "null logit");
+  Call c{dtype, N, H, V, K, h, W, b, token, logit};
+  c.temperature = temperature;
+  c.loss = loss;
+  c.lse = lse;
+  c.ws = workspace;
+  c.ws_bytes = workspace_bytes;
+  c.st = reinterpret_cast<hipStream_t>(stream);
+  return forward(c);
+}
+
+kb_status kb_distill_grad(int dtype, int N, int H, int V, int K, const void* h, const void* W, const float* b,
+                          const int32_t* token, const float* logit, float temperature, const float* lse,
+                          const float* grad, void* dh, void* dW, float* db, void* workspace, size_t workspace_bytes,
+                          void* stream) {
+  kb_status s = check_sizes(dtype, N, H, V, K);
+  if (s != KB_OK || (s = check_temperature(temperature)) != KB_OK) return s;
+  if (N > 0 && !logit) return fail(KB_ERR_INVALID_ARG, "null logit");
+  Call c{dtype, N, H, V, K, h, W, b, token, logit};
+  c.temperature = temperature;
+  c.lse_in = lse;
+  c.grad = grad;
+  c.dh = dh;
+  c.dW = dW;
+  c.db = db;
+  c.ws = workspace;
+  c.ws_bytes = workspace_bytes;
+  c.st = reinterpret_cast<hipStream_t>(stream);
+  return run_gradient(c);
+}
+
+}  // extern "C"

@@ -1,0 +1,191 @@
+// The gradients of the output layer's losses from a piece's dlogits: dh = dx W^T over the words, dW = h^T dx over the
+// rows, both with the 256-wide M side on what lies along the result's rows (states of dh, words of dW).
+//
+// A long axis is split where the tiles alone would not fill the card; the parts stay in the order of the registers, 16
+// bytes a lane, and a join adds them up in order.  dh takes the words piece by piece and adds to its parts.
+#pragma once
+
+#include "loss_logits.hpp"
+
+namespace kb {
+
+template <class T>
+__device__ __forceinline__ void part_of(float* part, size_t tile, int i, f32x16& x, bool load) {
+  float4* p = reinterpret_cast<float4*>(part) + (tile * (T::MB * T::NB) + i) * 4 * 256 + threadIdx.x;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    if (load) {
+      const float4 v = p[q * 256];
+      x[4 * q] = v.x, x[4 * q + 1] = v.y, x[4 * q + 2] = v.z, x[4 * q + 3] = v.w;
+    } else {
+      p[q * 256] = make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
+    }
+  }
+}
+
+// One tile of a split; b: the workgroup among `cells`, dealt so that an XCD has neighbours.
+__device__ __forceinline__ int xcd_cell(int cells, int b) {
+  const int x = b & 7, j = b >> 3;
+  return x * (cells >> 3) + min(x, cells & 7) + j;
+}
+
+template <class T, int PASSES>
+__global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_dh(LossGradArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t ring[4 * LossOcc<T, PASSES>::STAGE];
+  const int rows = const_int(a.count);
+  const int R = loss_row_tiles(rows, T::BN), cells = a.splits * R * a.mt;
+  if ((int)blockIdx.x >= cells) return;
+  const int c = xcd_cell(cells, blockIdx.x);
+  const int split = c / (R * a.mt), at = c - split * (R * a.mt), rt = at / a.mt, mt = at - rt * a.mt;
+  // stages of 32 words, the splits' shares of them alike
+  const int stages = a.gld / kLossStage;
+  const int s0 = (int)((long long)stages * split / a.splits), s1 = (int)((long long)stages * (split + 1) / a.splits);
+  const int k0 = s0 * kLossStage, m0 = mt * kLossM;
+  auto tile = [&](int, MmSide& A, MmSide& B) {
+    A = {a.W + (size_t)m0 * a.ldw + k0, a.ldw, a.w_plane, a.w_rows - m0, a.words - k0};
+    B = {a.g + (size_t)rt * T::BN * a.gld + k0, a.gld, a.g_plane, 0, 0};
+  };
+  const size_t part = (size_t)split * (loss_row_tiles(a.N, T::BN) * a.mt) + at;
+  auto init = [&](int, f32x16 (&acc)[T::MB][T::NB]) {
+#pragma unroll
+    for (int i = 0; i < T::MB * T::NB; ++i) {
+      f32x16& x = acc[i / T::NB][i % T::NB];
+      if (a.add) {
+        part_of<T>(a.part, part, i, x, true);
+      } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[r] = 0.f;
+      }
+      in_acc(x);
+    }
+  };
+  auto epi = [&](int, f32x16 (&acc)[T::MB][T::NB], uint32_t) {
+#pragma unroll
+    for (int i = 0; i < T::MB * T::NB; ++i) {
+      in_acc(acc[i / T::NB][i % T::NB]);
+      part_of<T>(a.part, part, i, acc[i / T::NB][i % T::NB], false);
+    }
+  };
+  mm_run<T, false, false, true, PASSES>(lds_addr(ring), 1, s1 - s0, tile, init, epi);
+}
+
+// 8 bf16 values to out, `left` of which exist.
+__device__ __forceinline__ void write8(uint16_t* out, const bf16x8& v, int left) {
+  if (left >= 8 && (uintptr_t)out % 16 == 0) {
+    *reinterpret_cast<bf16x8*>(out) = v;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < left) reinterpret_cast<__bf16*>(out)[i] = v[i];
+}
+
+template <class T, int PASSES>
+__global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_dw(LossGradArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t ring[4 * LossOcc<T, PASSES>::STAGE];
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave % T::WM, wn = wave / T::WM;
+  const int rows = const_int(a.count);
+  const int stages = loss_row_tiles(rows, a.BN) * a.BN / kLossStage;
+  const int c = xcd_cell(gridDim.x, blockIdx.x);
+  // the state tiles of the same words next to each other: they read the same dlogits
+  const int split = c / (a.mt * a.ntn), at = c - split * (a.mt * a.ntn), mt = at / a.ntn, ht = at - mt * a.ntn;
+  const int s0 = (int)((long long)stages * split / a.splits), s1 = (int)((long long)stages * (split + 1) / a.splits);
+  const int m0 = mt * kLossM, n0 = ht * T::BN;
+  auto tile = [&](int, MmSide& A, MmSide& B) {
+    A = {a.g + (size_t)s0 * kLossStage * a.gld + m0, a.gld, a.g_plane, 0, 0};
+    B = {a.ph + (size_t)s0 * kLossStage * a.Hp + n0, a.Hp, a.ph_plane, 0, 0};
+  };
+  auto init = [&](int, f32x16 (&acc)[T::MB][T::NB]) {
+#pragma unroll
+    for (int i = 0; i < T::MB * T::NB; ++i) {
+      f32x16& x = acc[i / T::NB][i % T::NB];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] = 0.f;
+      in_acc(x);
+    }
+  };
+  auto epi = [&](int, f32x16 (&acc)[T::MB][T::NB], uint32_t lds) {
+    if (a.part) {
+#pragma unroll
+      for (int i = 0; i < T::MB * T::NB; ++i) {
+        in_acc(acc[i / T::NB][i % T::NB]);
+        part_of<T>(a.part, c, i, acc[i / T::NB][i % T::NB], false);
+      }
+      return;
+    }
+    if constexpr (PASSES == 1) {
+      store_bf16<T>(acc, 0, lds, [&](int row, int word, const bf16x8& v) {
+        if (n0 + row < a.H && m0 + word < a.words)
+          write8(static_cast<uint16_t*>(a.out) + (size_t)(n0 + row) * a.V + m0 + word, v, a.words - m0 - word);
+      });
+    } else {
+#pragma unroll
+      for (int m = 0; m < T::MB; ++m)
+#pragma unroll
+        for (int n = 0; n < T::NB; ++n) {
+          in_acc(acc[m][n]);
+          const int row = n0 + wn * T::WTN + n * 32 + col;
+          if (row >= a.H) continue;
+          float* out = static_cast<float*>(a.out) + (size_t)row * a.V;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int w = m0 + wm * T::WTM + m * 32 + 8 * i + 4 * half;
+            if (w + 4 <= a.words && (uintptr_t)(out + w) % 16 == 0) {
+              *reinterpret_cast<float4*>(out + w) =
+                  make_float4(acc[m][n][4 * i], acc[m][n][4 * i + 1], acc[m][n][4 * i + 2], acc[m][n][4 * i + 3]);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                if (w + j < a.words) out[w + j] = acc[m][n][4 * i + j];
+            }
+          }
+        }
+    }
+  };
+  mm_run<T, true, true, false, PASSES>(lds_addr(ring), 1, s1 - s0, tile, init, epi);
+}
+
+// The parts of a result added up in order and rounded once.  Workgroup: one block of 32 x 32 of every wave of a tile,
+// in the order of the registers (dh of rows that do not count: zeros, by the last workgroups).
+template <class T, class D>
+__global__ __launch_bounds__(256) void loss_join(LossJoinArgs a, const int32_t* inv, int N, int zero_blocks) {
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
+  const int wave = tid >> 6, wm = wave % T::WM, wn = wave / T::WM;
+  D* out = static_cast<D*>(a.out);
+  const int work = gridDim.x - zero_blocks;
+  if ((int)blockIdx.x >= work) {
+    for (int n = blockIdx.x - work; n < N; n += zero_blocks)
+      if (inv[n] < 0)
+        for (int i = tid; i < a.cols; i += 256) out[(size_t)n * a.ld + i] = (D)0.f;
+    return;
+  }
+  const int rows = a.is_dh ? *a.count : a.rows;
+  const int tiles = a.mt * a.ntn;  // dh: by rows, then states; dW: by words, then states
+  const int tile = blockIdx.x / (T::MB * T::NB), blk = blockIdx.x % (T::MB * T::NB);
+  const int m = blk / T::NB, n = blk % T::NB;
+  const int mt = a.is_dh ? tile % a.mt : tile / a.ntn, nt = a.is_dh ? tile / a.mt : tile % a.ntn;
+  const int row = nt * T::BN + wn * T::WTN + n * 32 + col;
+  const int c0 = mt * kLossM + wm * T::WTM + m * 32 + 4 * half;
+  if (row >= rows) return;
+  float s[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s[i] = 0.f;
+  for (int k = 0; k < a.splits; ++k) {
+    const float4* p = reinterpret_cast<const float4*>(a.part) + (((size_t)k * tiles + tile) * (T::MB * T::NB) + blk) * 4 * 256 + tid;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float4 v = p[q * 256];
+      s[4 * q] += v.x, s[4 * q + 1] += v.y, s[4 * q + 2] += v.z, s[4 * q + 3] += v.w;
+    }
+  }
+  D* to = out + (size_t)(a.is_dh ? a.map[row] : row) * a.ld;
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (c0 + 8 * q + j < a.cols) to[c0 + 8 * q + j] = (D)s[4 * q + j];
+}
+
+}  // namespace kb

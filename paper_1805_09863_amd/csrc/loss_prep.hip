@@ -1,0 +1,373 @@
+// Around the products of the output layer's losses: which rows count and their entries, operands laid out for the
+// DMA pipeline, and the losses from the parts of all splits.
+#include "k3_scan.hpp"
+#include "loss_common.hpp"
+
+namespace kb {
+
+typedef __bf16 bf16x8v __attribute__((ext_vector_type(8)));
+
+// A teacher's row: the softmax over its entries' words of logit / T (an entry whose word is outside the vocabulary or
+// whose logit is -inf is none; entries of the same word are one, the first, with their probabilities' sum), and
+// sum q ln q.  One wave a row, up to two entries a lane.
+__global__ __launch_bounds__(256) void loss_teacher(LossTeacherArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int row = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= a.N) return;
+  int tok[2];
+  float y[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int j = lane + 64 * u;
+    tok[u] = -1;
+    y[u] = -INFINITY;
+    if (j < a.K) {
+      const size_t at = (size_t)row * a.K + j;
+      const int t = a.token[at];
+      const float x = a.logit[at] * a.inv_t;
+      if (t >= 0 && t < a.V && !(x == -INFINITY)) {
+        tok[u] = t;
+        y[u] = x;
+      }
+    }
+  }
+  const bool any = __builtin_amdgcn_ballot_w64(tok[0] >= 0 || tok[1] >= 0) != 0ull;
+  float top = fmaxf(y[0], y[1]);
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+  float e[2], merged[2], total = 0.f;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    e[u] = tok[u] >= 0 ? expf(y[u] - top) : 0.f;
+    merged[u] = 0.f;
+    total += e[u];
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d, 64);
+  // entry i goes to the first entry of its word
+  bool first[2] = {tok[0] >= 0, tok[1] >= 0};
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+    for (int i = 0; i < 64 && i + 64 * u < a.K; ++i) {
+      const int t = __shfl(tok[u], i, 64);
+      const float x = __shfl(e[u], i, 64);
+#pragma unroll
+      for (int w = 0; w < 2; ++w)
+        if (t >= 0 && t == tok[w]) {
+          merged[w] += x;
+          if (i + 64 * u < lane + 64 * w) first[w] = false;
+        }
+    }
+  float known = 0.f;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int j = lane + 64 * u;
+    const float q = first[u] ? merged[u] / total : 0.f;
+    if (q > 0.f) known += q * (logf(merged[u]) - logf(total));
+    if (first[u] && !(q >= 0.f)) known = q;  // NaN stays NaN
+    if (j < a.K) {
+      const size_t at = (size_t)row * a.K + j;
+      a.out_token[at] = first[u] ? tok[u] : -1;
+      a.part[at] = q;
+    }
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) known += __shfl_xor(known, d, 64);
+  if (lane == 0) {
+    a.known[row] = known;
+    a.flag[row] = any;
+  }
+}
+
+// Rows that count, in order (a stable compaction).  One workgroup: 4,096 rows a turn.
+__global__ __launch_bounds__(K3_T) void loss_rows(LossRows a) {
+  __shared__ int wsum[K3_W];
+  auto counts = [&](int n) {
+    if (a.flag) return a.flag[n] != 0;
+    const int t = a.token[n];
+    return t >= 0 && t < a.V;
+  };
+  for (int n = threadIdx.x; n < a.N; n += K3_T)
+    if (!counts(n)) a.inv[n] = -1;
+  const int kept = compact_entries_pass(
+      a.N, counts,
+      [&](int c, int n) {
+        a.map[c] = n;
+        a.inv[n] = c;
+      },
+      wsum);
+  if (threadIdx.x == 0) *a.count = kept;
+}
+
+// x in `planes` bf16 pieces.
+template <int PLANES>
+__device__ __forceinline__ void write_pieces(const float (&x)[8], uint16_t* out, size_t plane) {
+  float r[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r[i] = x[i];
+#pragma unroll
+  for (int p = 0; p < PLANES; ++p) {
+    bf16x8v v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      v[i] = (__bf16)r[i];
+      r[i] -= (float)v[i];
+    }
+    *reinterpret_cast<bf16x8v*>(out + p * plane) = v;
+  }
+}
+
+__device__ __forceinline__ float widen(const uint16_t* p, size_t i) { return __uint_as_float((uint32_t)p[i] << 16); }
+__device__ __forceinline__ float widen(const float* p, size_t i) { return p[i]; }
+
+// n of 8 values from p on, the rest zeros, by the widest loads that the address allows.
+template <class S>
+__device__ __forceinline__ void load8(const S* p, int n, float (&x)[8]) {
+  if (n >= 8 && (uintptr_t)p % 16 == 0) {
+    if constexpr (sizeof(S) == 2) {
+      const uint4 v = *reinterpret_cast<const uint4*>(p);
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      }
+    } else {
+      const float4 v = reinterpret_cast<const float4*>(p)[0], u = reinterpret_cast<const float4*>(p)[1];
+      x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w, x[4] = u.x, x[5] = u.y, x[6] = u.z, x[7] = u.w;
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = i < n ? widen(p, i) : 0.f;
+}
+
+// The packed rows' states in bf16 pieces, as whole row tiles with zeros behind them, and the lists of their entries.
+// Workgroups 0 .. tiles - 1 make a row tile's lists (a counting sort by wave tile; the order within a list is free, as
+// every entry of a row is of another word), the others copy states.
+template <class S, int PLANES>
+__global__ __launch_bounds__(256) void loss_pack(LossPackArgs a, int wtm, int wtn) {
+  extern __shared__ int hist[];  // nb + 1
+  __shared__ int wsum[4];
+  const int rows = *a.rows.count, R = loss_row_tiles(rows, a.BN);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if ((int)blockIdx.x < a.tiles) {
+    const int rt = blockIdx.x, K = a.rows.K;
+    if (rt >= R) return;
+    const int here = min(a.BN, rows - rt * a.BN), n = here * K;
+    for (int i = tid; i <= a.nb; i += 256) hist[i] = 0;
+    if (a.rowp)
+      for (int r = tid; r < a.BN; r += 256) {
+        const int c = rt * a.BN + r;
+        float2 v = make_float2(INFINITY, 0.f);  // no row: probabilities of zero
+        if (r < here) {
+          const int row = a.rows.map[c];
+          v = make_float2(a.lse[row], a.grad[row] * a.grad_scale);
+        }
+        a.rowp[c] = v;
+      }
+    __syncthreads();
+    auto word = [&](int e) { return a.rows.token[(size_t)a.rows.map[rt * a.BN + e / K] * K + e % K]; };
+    auto list = [&](int e, int t) { return (e / K) / wtn * a.words0 + t / wtm; };
+    for (int e = tid; e < n; e += 256) {
+      const int t = word(e);
+      if (t >= 0 && t < a.rows.V) atomicAdd(&hist[list(e, t) + 1], 1);
+    }
+    __syncthreads();
+    // inclusive scan of hist[1 ..]: hist[i] becomes the first item of list i
+    int carry = 0;
+    for (int i0 = 0; i0 < a.nb; i0 += 256) {
+      const int i = i0 + tid;
+      int x = i < a.nb ? hist[i + 1] : 0;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(x, d, 64);
+        if (lane >= d) x += y;
+      }
+      if (lane == 63) wsum[wave] = x;
+      __syncthreads();
+      int before = carry;
+      for (int w = 0; w < wave; ++w) before += wsum[w];
+      carry += wsum[0] + wsum[1] + wsum[2] + wsum[3];
+      if (i < a.nb) hist[i + 1] = before + x;
+      __syncthreads();
+    }
+    int32_t* offs = a.offs + (size_t)rt * (a.nb + 1);
+    for (int i = tid; i <= a.nb; i += 256) offs[i] = hist[i];
+    __syncthreads();
+    LossItem* items = a.items + (size_t)rt * a.BN * K;
+    const int NB = wtn / 32;
+    for (int e = tid; e < n; e += 256) {
+      const int t = word(e);
+      if (t < 0 || t >= a.rows.V) continue;
+      const int at = atomicAdd(&hist[list(e, t)], 1);
+      const int r = (e / K) % wtn, w = t % wtm;
+      const int blk = (w >> 5) * NB + (r >> 5);
+      const int reg = 4 * ((w >> 3) & 3) + (w & 3), l = 32 * ((w >> 2) & 1) + (r & 31);
+      const int row = a.rows.map[rt * a.BN + e / K];
+      LossItem it;
+      it.code = blk << 16 | reg << 8 | l;
+      it.slot = rt * a.BN * K + e;
+      it.part = a.rows.part ? a.rows.part[(size_t)row * K + e % K] : a.rows.target_part;
+      it.unused = 0;
+      items[at] = it;
+    }
+    return;
+  }
+  const int chunks = a.Hp / 8, H = a.rows.H;
+  const long long total = (long long)R * a.BN * chunks;
+  for (long long i = (long long)(blockIdx.x - a.tiles) * 256 + tid; i < total; i += (long long)(gridDim.x - a.tiles) * 256) {
+    const int c = (int)(i / chunks), h0 = (int)(i % chunks) * 8;
+    float x[8];
+    if (c < rows && h0 < H) {
+      load8(static_cast<const S*>(a.h) + (size_t)a.rows.map[c] * H + h0, H - h0, x);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = 0.f;
+    }
+    write_pieces<PLANES>(x, a.ph + (size_t)c * a.Hp + h0, a.ph_plane);
+  }
+}
+
+// A piece of W in bf16 pieces, filled up with zeros.
+template <class S, int PLANES>
+__global__ __launch_bounds__(256) void loss_pack_w(LossPackWArgs a) {
+  const int chunks = a.Vc / 8;
+  const long long total = (long long)a.Hk * chunks;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
+    const int r = (int)(i / chunks), w = (int)(i % chunks) * 8;
+    float x[8];
+    const int n = a.V - a.v0 - w;
+    if (r < a.H && n > 0) {
+      load8(static_cast<const S*>(a.W) + (size_t)r * a.V + a.v0 + w, n, x);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = 0.f;
+    }
+    write_pieces<PLANES>(x, a.out + (size_t)r * a.Vc + w, a.plane);
+  }
+}
+
+__global__ __launch_bounds__(256) void loss_pack_b(const float* b, int V, int Vp, float* out) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < Vp) out[i] = i < V ? b[i] : -INFINITY;
+}
+
+// loss and log-sum-exp of every row, a wave each: M = max m, S = sum s e^((m - M) / T) over all splits, lse = M / T + ln S.
+__global__ __launch_bounds__(256) void loss_finish(LossFinishArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int row = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= a.rows.N) return;
+  const int c = a.rows.inv[row], K = a.rows.K;
+  if (c < 0) {
+    if (lane == 0) a.loss[row] = a.lse[row] = 0.f;
+    return;
+  }
+  const int R = loss_row_tiles(*a.rows.count, a.BN);
+  const int P = loss_splits(a.grid, R, a.vt_piece), last = loss_splits(a.grid, R, a.vt_last);
+  float M = kStatInit, S = 0.f, X = 0.f;
+  for (int p = 0; p < a.pieces; ++p) {
+    const int here = p + 1 < a.pieces ? P : last;
+    for (int i = lane; i < here; i += 64) {
+      const size_t at = p * a.stat_piece + (size_t)c * here + i;
+      const float2 v = a.stat[at];
+      const float m = fmaxf(M, v.x);
+      S = S * exp2f((M - m) * a.scale) + v.y * exp2f((v.x - m) * a.scale);
+      M = m;
+      if (a.sumx) X += a.sumx[at];
+    }
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) {
+    const float mo = __shfl_xor(M, d, 64), so = __shfl_xor(S, d, 64);
+    X += __shfl_xor(X, d, 64);
+    const float m = fmaxf(M, mo);
+    S = S * exp2f((M - m) * a.scale) + so * exp2f((mo - m) * a.scale);
+    M = m;
+  }
+  const float lse = M * a.inv_t + logf(S);
+  float dot = 0.f;
+  for (int j = lane; j < K; j += 64) {
+    const int t = a.rows.token[(size_t)row * K + j];
+    if (t >= 0 && t < a.rows.V) dot += (a.rows.part ? a.rows.part[(size_t)row * K + j] : a.rows.target_part) * a.xt[(size_t)c * K + j];
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) dot += __shfl_xor(dot, d, 64);
+  if (lane == 0) {
+    float l = lse - dot * a.inv_t - a.rest * X;
+    if (a.known) l += a.known[row];
+    a.loss[row] = l * a.t2;
+    a.lse[row] = lse;
+  }
+}
+
+// db: the row tiles' sums, in order.
+__global__ __launch_bounds__(256) void loss_db(const float* dbp, int wave_rows, int BN, int db_ld, const int32_t* count,
+                                               int V, float* db) {
+  const int v = blockIdx.x * 256 + threadIdx.x;
+  if (v >= V) return;
+  const int n = loss_row_tiles(*count, BN) * wave_rows;
+  float s = 0.f;
+  for (int i = 0; i < n; ++i) s += dbp[(size_t)i * db_ld + v];
+  db[v] = s;
+}
+
+__global__ __launch_bounds__(256) void loss_zero(uint16_t* p, size_t n) {
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) p[i] = 0;
+}
+
+hipError_t launch_loss_zero(void* p, size_t bytes, hipStream_t st) {
+  loss_zero<<<dim3(1024), dim3(256), 0, st>>>(static_cast<uint16_t*>(p), bytes / 2);
+  return hipGetLastError();
+}
+
+hipError_t launch_loss_teacher(const LossTeacherArgs& a, hipStream_t st) {
+  loss_teacher<<<dim3((a.N + 3) / 4), dim3(256), 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_loss_rows(const LossRows& a, hipStream_t st) {
+  loss_rows<<<dim3(1), dim3(K3_T), 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_loss_pack(bool bf16, const LossPackArgs& a, hipStream_t st) {
+  const long long most = (long long)loss_row_tiles(a.rows.N, a.BN) * a.BN * (a.Hp / 8);
+  const int copies = (int)((most + 255) / 256 < 4096 ? (most + 255) / 256 : 4096);
+  const dim3 gr(a.tiles + copies);
+  const size_t lds = ((size_t)a.nb + 1) * sizeof(int);
+  const int wtm = loss_wtm(a.BN), wtn = loss_wtn(a.BN);
+  if (bf16)
+    loss_pack<uint16_t, 1><<<gr, dim3(256), lds, st>>>(a, wtm, wtn);
+  else
+    loss_pack<float, 3><<<gr, dim3(256), lds, st>>>(a, wtm, wtn);
+  return hipGetLastError();
+}
+
+hipError_t launch_loss_pack_w(bool bf16, const LossPackWArgs& a, hipStream_t st) {
+  const long long chunks = (long long)a.Hk * (a.Vc / 8);
+  const dim3 gr((unsigned)((chunks + 255) / 256 < 8192 ? (chunks + 255) / 256 : 8192));
+  if (bf16)
+    loss_pack_w<uint16_t, 1><<<gr, dim3(256), 0, st>>>(a);
+  else
+    loss_pack_w<float, 3><<<gr, dim3(256), 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_loss_pack_b(const float* b, int V, int Vp, float* out, hipStream_t st) {
+  loss_pack_b<<<dim3((Vp + 255) / 256), dim3(256), 0, st>>>(b, V, Vp, out);
+  return hipGetLastError();
+}
+
+hipError_t launch_loss_finish(const LossFinishArgs& a, hipStream_t st) {
+  loss_finish<<<dim3((a.rows.N + 3) / 4), dim3(256), 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_loss_db(const float* dbp, int wave_rows, int BN, int db_ld, const int32_t* count, int V, float* db,
+                          hipStream_t st) {
+  loss_db<<<dim3((V + 255) / 256), dim3(256), 0, st>>>(dbp, wave_rows, BN, db_ld, count, V, db);
+  return hipGetLastError();
+}
+
+}  // namespace kb
