@@ -47,7 +47,7 @@
 extern "C" {
 #endif
 
-#define KB_LOSS_MAX_V 524288
+#define KB_LOSS_MAX_V 262144
 #define KB_LOSS_MAX_H 65536
 #define KB_LOSS_MAX_N 4194304
 #define KB_LOSS_MAX_K 128 /* a teacher's entries of a row */

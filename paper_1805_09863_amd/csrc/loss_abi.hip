@@ -15,6 +15,8 @@ hipError_t launch_loss_dh_bf16(int BN, const LossGradArgs& a, hipStream_t st);
 hipError_t launch_loss_dh_f32(int BN, const LossGradArgs& a, hipStream_t st);
 hipError_t launch_loss_dw_bf16(int BNh, const LossGradArgs& a, hipStream_t st);
 hipError_t launch_loss_dw_f32(int BNh, const LossGradArgs& a, hipStream_t st);
+hipError_t launch_loss_both_bf16(const LossGradArgs& h, const LossGradArgs& w, hipStream_t st);
+hipError_t launch_loss_both_f32(const LossGradArgs& h, const LossGradArgs& w, hipStream_t st);
 }  // namespace kb
 
 namespace {
@@ -51,6 +53,7 @@ struct Plan {
   size_t count, map, inv, flag, token, part, known, offs, items, ph, b, wp, stat, sumx, xt, rowp, g, dbp, dh_part, dw_part;
   size_t stat_piece;        // values of one piece's statistics
   size_t bytes;
+  bool both() const { return BN == 256 && BNh == 256; }  // dh and dW in one launch
 };
 
 // The plan of a call. `direct`: W is read where it lies; else its pieces are laid out first (float32 in bf16 pieces, odd
@@ -66,17 +69,18 @@ Plan make_plan(int dtype, int N, int H, int V, int K, bool teacher, bool grad, b
   p.WN = p.BN >= 128 ? 2 : 1;
   p.WTM = kb::loss_wtm(p.BN);
   p.WTN = kb::loss_wtn(p.BN);
-  p.BNh = H > 128 ? 256 : 128;
-  p.Hp = up(H, p.BNh);
+  p.BNh = p.BN <= 128 ? 64 : H > 128 ? 256 : 128;
+  p.Hp = up(H, H > 128 ? 256 : 128);
   p.Hk = up(H, kb::kLossStage);
   p.vt = (V + kb::kLossM - 1) / kb::kLossM;
   p.words0 = p.vt * (kb::kLossM / p.WTM);
-  p.nb = p.BN / p.WTN * p.words0;
+  p.nb = p.BN / p.WTN * p.words0 * kb::loss_blocks(p.BN);
   p.grid = std::max(p.BN == 32 ? 512 : 256, p.R);
   const bool shape = p.bf16 && H % kb::kLossStage == 0 && V % 8 == 0 && V >= kb::kLossM;
   p.direct = shape && w_aligned;
 
-  // A piece: as many words as keep its dlogits, and the part of W that is laid out, near the last-level cache's size.
+  // A piece: as many words as keep its dlogits, and the part of W that is laid out, at 128 MB, half the last-level cache
+  // (8,192 x 1,024 x 90,000, a training pass: 5.87 ms; at 64 MB 6.37, 256 MB 6.12, 1 GB 6.29).
   // (W at an odd address where its shape needs no laying out: small pieces, so that the workspace need not grow.)
   const size_t most = (size_t)128 << 20;
   const size_t w_tile = (size_t)p.Hk * kb::kLossM * 2 * p.planes, g_tile = (size_t)p.R * p.BN * kb::kLossM * 2 * p.planes;
@@ -97,7 +101,7 @@ Plan make_plan(int dtype, int N, int H, int V, int K, bool teacher, bool grad, b
     p.part = s.take((size_t)N * K * 4);
     p.known = s.take((size_t)N * 4);
   }
-  p.offs = s.take((size_t)p.R * (p.nb + 1) * 4);
+  p.offs = s.take((size_t)p.R * (p.nb + 2) * 2);
   p.items = s.take((size_t)p.R * p.BN * K * sizeof(kb::LossItem));
   p.ph = s.take((size_t)p.planes * p.R * p.BN * p.Hp * 2);
   p.b = s.take((size_t)p.vt * kb::kLossM * 4);
@@ -112,12 +116,21 @@ Plan make_plan(int dtype, int N, int H, int V, int K, bool teacher, bool grad, b
     p.g = s.take(p.piece * g_tile);
     p.dbp = s.take((size_t)p.R * p.WN * p.vt * kb::kLossM * 4);
     p.dh_mt = (H + kb::kLossM - 1) / kb::kLossM;
-    p.dh_splits = std::max(1, std::min((p.BN == 32 ? 512 : 256) / (p.R * p.dh_mt), p.piece));
-    p.dh_part = s.take((size_t)p.dh_splits * p.R * p.dh_mt * kb::kLossM * p.BN * 4);
-    p.dw_ntn = p.Hp / p.BNh;
-    const int stages = p.R * p.BN / kb::kLossStage;
-    p.dw_splits = std::max(1, std::min(256 / (p.piece * p.dw_ntn), stages / 8));
-    if (p.dw_splits > 1) p.dw_part = s.take((size_t)p.dw_splits * p.piece * p.dw_ntn * kb::kLossM * p.BNh * 4);
+    p.dw_ntn = (H + p.BNh - 1) / p.BNh;
+    // Stages of 32 steps: of dh along the piece's words, of dW along the rows.
+    const long long st_h = (long long)p.piece * (kb::kLossM / kb::kLossStage), st_w = p.R * p.BN / kb::kLossStage;
+    const long long n_h = (long long)p.R * p.dh_mt, n_w = (long long)p.piece * p.dw_ntn;
+    if (p.both()) {
+      // one launch: every workgroup about its share of all stages, and none of less than 16
+      const long long share = std::max<long long>(16, (n_h * st_h + n_w * st_w) / 256);
+      p.dh_splits = (int)std::max<long long>(1, std::min<long long>((st_h + share / 2) / share, p.piece));
+      p.dw_splits = (int)std::max<long long>(1, (st_w + share / 2) / share);
+    } else {
+      p.dh_splits = (int)std::max<long long>(1, std::min<long long>((p.BN == 32 ? 512 : 256) / n_h, p.piece));
+      p.dw_splits = (int)std::max<long long>(1, std::min<long long>(256 / n_w, st_w / 8));
+    }
+    p.dh_part = s.take((size_t)p.dh_splits * n_h * kb::kLossM * p.BN * 4);
+    if (p.dw_splits > 1) p.dw_part = s.take((size_t)p.dw_splits * n_w * kb::kLossM * p.BNh * 4);
   }
   p.bytes = s.at;
   return p;
@@ -180,7 +193,12 @@ struct Work {
     if (e_ != hipSuccess) return fail(KB_ERR_HIP, what ": %s", hipGetErrorString(e_));   \
   } while (0)
 
-// Rows that count, their states, entries and bias laid out.
+kb::LossPackWArgs piece_pack(const Call& c, const Plan& p, const Work& w, int t0, int tiles) {
+  const int Vc = tiles * kb::kLossM;
+  return {c.W, c.H, c.V, t0 * kb::kLossM, Vc, p.Hk, w.at<uint16_t>(p.wp), (size_t)p.Hk * Vc};
+}
+
+// Rows that count, their states and entries, the bias and the first piece of W laid out.
 kb_status prepare(const Call& c, const Plan& p, Work& w, bool grad) {
   w.ws = static_cast<char*>(c.ws);
   kb::LossRows& r = w.rows;
@@ -194,9 +212,10 @@ kb_status prepare(const Call& c, const Plan& p, Work& w, bool grad) {
                                 w.at<float>(p.part), w.at<float>(p.known), w.at<uint8_t>(p.flag)};
     KB_LAUNCH("teacher's rows", kb::launch_loss_teacher(t, c.st));
   }
-  KB_LAUNCH("rows of a loss", kb::launch_loss_rows(r, c.st));
   kb::LossPackArgs a{};
   a.rows = r;
+  a.find_rows = kb::loss_finds_rows(c.N, p.nb);
+  if (!a.find_rows) KB_LAUNCH("rows of a loss", kb::launch_loss_rows(r, c.st));
   a.h = c.h;
   a.ph = w.at<uint16_t>(p.ph);
   a.ph_plane = (size_t)p.R * p.BN * p.Hp;
@@ -205,8 +224,12 @@ kb_status prepare(const Call& c, const Plan& p, Work& w, bool grad) {
   a.tiles = p.R;
   a.nb = p.nb;
   a.words0 = p.words0;
-  a.offs = w.at<int32_t>(p.offs);
+  a.offs = w.at<uint16_t>(p.offs);
   a.items = w.at<kb::LossItem>(p.items);
+  a.b = c.b;
+  a.bp = w.at<float>(p.b);
+  a.Vp = p.vt * kb::kLossM;
+  if (!p.direct) a.w = piece_pack(c, p, w, 0, p.piece);
   if (grad) {
     a.lse = c.lse_in;
     a.grad = c.grad;
@@ -214,7 +237,6 @@ kb_status prepare(const Call& c, const Plan& p, Work& w, bool grad) {
     a.rowp = w.at<float2>(p.rowp);
   }
   KB_LAUNCH("states of a loss", kb::launch_loss_pack(p.bf16, a, c.st));
-  KB_LAUNCH("bias of a loss", kb::launch_loss_pack_b(c.b, c.V, p.vt * kb::kLossM, w.at<float>(p.b), c.st));
   return KB_OK;
 }
 
@@ -230,10 +252,9 @@ kb_status piece_w(const Call& c, const Plan& p, const Work& w, int t0, int tiles
     out = {static_cast<const uint16_t*>(c.W) + v0, 0, c.V, c.V - v0, c.H};
     return KB_OK;
   }
-  const int Vc = tiles * kb::kLossM;
-  const kb::LossPackWArgs a{c.W, c.H, c.V, v0, Vc, p.Hk, w.at<uint16_t>(p.wp), (size_t)p.Hk * Vc};
-  KB_LAUNCH("weights of a loss", kb::launch_loss_pack_w(p.bf16, a, c.st));
-  out = {a.out, a.plane, Vc, Vc, p.Hk};
+  const kb::LossPackWArgs a = piece_pack(c, p, w, t0, tiles);
+  if (t0 > 0) KB_LAUNCH("weights of a loss", kb::launch_loss_pack_w(p.bf16, a, c.st));
+  out = {a.out, a.plane, a.Vc, a.Vc, p.Hk};
   return KB_OK;
 }
 
@@ -254,7 +275,7 @@ kb::LossLogitsArgs logits_args(const Call& c, const Plan& p, const Work& w, cons
   a.count = w.rows.count;
   a.grid = p.grid;
   a.scale = kb::kL2E / c.temperature;
-  a.offs = w.at<int32_t>(p.offs);
+  a.offs = w.at<uint16_t>(p.offs);
   a.items = w.at<kb::LossItem>(p.items);
   a.nb = p.nb;
   a.words0 = p.words0;
@@ -348,27 +369,33 @@ kb_status gradient(const Call& c) {
     g.BN = p.BN;
     g.count = w.rows.count;
     g.V = c.V;
-    if (c.dh) {
-      g.words = pw.cols;
-      g.splits = p.dh_splits;
-      g.mt = p.dh_mt;
-      g.part = w.at<float>(p.dh_part);
-      g.add = i > 0;
-      KB_LAUNCH("gradient of the states", p.bf16 ? kb::launch_loss_dh_bf16(p.BN, g, c.st) : kb::launch_loss_dh_f32(p.BN, g, c.st));
+    kb::LossGradArgs gh = g, gw = g;
+    gh.words = pw.cols;
+    gh.splits = p.dh_splits;
+    gh.mt = p.dh_mt;
+    gh.part = w.at<float>(p.dh_part);
+    gh.add = i > 0;
+    gw.words = c.V - t0 * kb::kLossM;
+    gw.splits = p.dw_splits;
+    gw.mt = tiles;
+    gw.ntn = p.dw_ntn;
+    gw.part = p.dw_splits > 1 ? w.at<float>(p.dw_part) : nullptr;
+    gw.out = static_cast<char*>(c.dW) + (size_t)t0 * kb::kLossM * p.z;
+    if (c.dh && c.dW && p.both()) {
+      KB_LAUNCH("gradients of a loss",
+                p.bf16 ? kb::launch_loss_both_bf16(gh, gw, c.st) : kb::launch_loss_both_f32(gh, gw, c.st));
+    } else {
+      if (c.dh)
+        KB_LAUNCH("gradient of the states",
+                  p.bf16 ? kb::launch_loss_dh_bf16(p.BN, gh, c.st) : kb::launch_loss_dh_f32(p.BN, gh, c.st));
+      if (c.dW)
+        KB_LAUNCH("gradient of the weights",
+                  p.bf16 ? kb::launch_loss_dw_bf16(p.BNh, gw, c.st) : kb::launch_loss_dw_f32(p.BNh, gw, c.st));
     }
-    if (c.dW) {
-      g.words = c.V - t0 * kb::kLossM;
-      g.splits = p.dw_splits;
-      g.mt = tiles;
-      g.ntn = p.dw_ntn;
-      g.part = p.dw_splits > 1 ? w.at<float>(p.dw_part) : nullptr;
-      g.out = static_cast<char*>(c.dW) + (size_t)t0 * kb::kLossM * p.z;
-      KB_LAUNCH("gradient of the weights", p.bf16 ? kb::launch_loss_dw_bf16(p.BNh, g, c.st) : kb::launch_loss_dw_f32(p.BNh, g, c.st));
-      if (g.part) {
-        kb::LossJoinArgs j{g.part, p.dw_splits, tiles, p.dw_ntn, p.BNh, c.H, std::min(g.words, Vc), 0, nullptr, nullptr,
-                           g.out, c.V};
-        KB_LAUNCH("gradient of the weights", kb::launch_loss_join(p.bf16, j, nullptr, 0, c.st));
-      }
+    if (c.dW && gw.part) {
+      const kb::LossJoinArgs j{gw.part, p.dw_splits, tiles, p.dw_ntn, p.BNh, c.H, std::min(gw.words, Vc), 0, nullptr,
+                               nullptr, gw.out, c.V};
+      KB_LAUNCH("gradient of the weights", kb::launch_loss_join(p.bf16, j, nullptr, 0, c.st));
     }
   }
   if (c.dh) {

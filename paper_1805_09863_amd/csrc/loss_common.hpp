@@ -22,12 +22,14 @@ using LossT32 = LossTile<2, 1, 4, 1>;
 
 constexpr int kLossM = 256;      // words (or states) of a tile's M side
 constexpr int kLossStage = 32;   // contraction steps of a pipeline stage
-constexpr int kLossMaxV = 1 << 19;
+constexpr int kLossMaxV = 1 << 18;
 constexpr int kLossMaxK = 128;
 
-// The wave tile of a row tile BN, for the lists of entries.
-inline int loss_wtm(int BN) { return BN >= 128 ? 128 : 64; }
-inline int loss_wtn(int BN) { return BN >= 128 ? BN / 2 : BN; }
+// The wave's part of a tile with BN rows, for the lists of entries: its extent, and its blocks of 32 x 32 (a multiple of
+// two, and at most sixteen).
+__host__ __device__ inline int loss_wtm(int BN) { return BN >= 128 ? 128 : 64; }
+__host__ __device__ inline int loss_wtn(int BN) { return BN >= 128 ? BN / 2 : BN; }
+__host__ __device__ inline int loss_blocks(int BN) { return loss_wtm(BN) / 32 * (loss_wtn(BN) / 32); }
 
 // Rows that count lie packed: `map` has the original row of each packed one, `inv` the packed row of each
 // original one or -1, *count how many there are.
@@ -42,12 +44,10 @@ struct LossRows {
   int32_t* count;
 };
 
-// An entry in the list of its wave tile: where the wave holds its logit, and what goes with it.
-struct alignas(16) LossItem {
-  int32_t code;   // block (vb * NB + hb) << 16 | register << 8 | lane
-  int32_t slot;   // packed row * K + entry
-  float part;
-  int32_t unused;
+// An entry in the list of its block: where a wave holds its logit, and what goes with it.
+struct alignas(8) LossItem {
+  int32_t code;     // register << 8 | lane
+  int32_t payload;  // forward: packed row * K + entry; gradient: its part of the row's distribution, as float32 bits
 };
 
 struct LossTeacherArgs {
@@ -61,29 +61,36 @@ struct LossTeacherArgs {
   uint8_t* flag;       // N
 };
 
+// A piece of W: words v0 .. v0 + Vc - 1 (those from V on as zeros), Hk rows (those from H on zeros).
+struct LossPackWArgs {
+  const void* W;
+  int H, V, v0, Vc, Hk;
+  uint16_t* out;       // planes x Hk x Vc bf16; null: none
+  size_t plane;
+};
+
 struct LossPackArgs {
   LossRows rows;
+  int find_rows;       // the map has not been made: every workgroup that needs it finds the rows that count by itself
   const void* h;
-  uint16_t* ph;        // planes x Np x Hp bf16
+  uint16_t* ph;        // planes x rows x Hp bf16
   size_t ph_plane;     // values from one plane to the next
   int Hp, BN;
-  // lists of entries by wave tile
-  int tiles, nb;       // row tiles (most), wave tiles of each
+  // lists of entries by block of the waves' tiles
+  int tiles, nb;       // row tiles (most), blocks of each
   int words0;          // wave tiles along the words
-  int32_t* offs;       // tiles x (nb + 1)
+  uint16_t* offs;      // tiles x (nb + 2)
   LossItem* items;     // tiles x BN x K
   // gradient: what the rows' logits are turned into gradients with
   const float* lse;
   const float* grad;
   float grad_scale;
   float2* rowp;        // (log-sum-exp, gradient) of each packed row; null: forward
-};
-
-struct LossPackWArgs {
-  const void* W;
-  int H, V, v0, Vc, Hk;  // words v0 .. v0 + Vc - 1 (those from V on as zeros), Hk rows (those from H on zeros)
-  uint16_t* out;         // planes x Hk x Vc
-  size_t plane;
+  const float* b;
+  float* bp;           // the bias, -inf for the words that fill the last tile up
+  int Vp;
+  LossPackWArgs w;     // the first piece's
+  int states_wg, bias_wg, w_wg;  // workgroups of each kind behind the `tiles` that make lists
 };
 
 // The logits' product: A words x states (states apart by lda), B packed rows.
@@ -101,9 +108,9 @@ struct LossLogitsArgs {
   const int32_t* count;
   int grid;              // workgroups that share the tiles
   float scale;           // log2(e) / T
-  const int32_t* offs;   // lists of entries
+  const uint16_t* offs;  // lists of entries
   const LossItem* items;
-  int nb, words0, wt0;   // wave tiles a row tile, along the words, and of the words before this piece
+  int nb, words0, wt0;   // blocks of a row tile; wave tiles along the words, and of the words before this piece
   int K;
   // forward
   float2* stat;          // [packed row][split] (max, sum) of the piece
@@ -168,12 +175,12 @@ struct LossFinishArgs {
 
 hipError_t launch_loss_teacher(const LossTeacherArgs& a, hipStream_t st);
 hipError_t launch_loss_rows(const LossRows& a, hipStream_t st);
-hipError_t launch_loss_pack(bool bf16, const LossPackArgs& a, hipStream_t st);
+bool loss_finds_rows(int N, int nb);  // launch_loss_pack can do without launch_loss_rows
+hipError_t launch_loss_pack(bool bf16, LossPackArgs a, hipStream_t st);
 hipError_t launch_loss_pack_w(bool bf16, const LossPackWArgs& a, hipStream_t st);
 hipError_t launch_loss_finish(const LossFinishArgs& a, hipStream_t st);
 // inv, N: rows of dh that do not count, filled with zeros (null: none)
 hipError_t launch_loss_join(bool bf16, const LossJoinArgs& a, const int32_t* inv, int N, hipStream_t st);
-hipError_t launch_loss_pack_b(const float* b, int V, int Vp, float* out, hipStream_t st);
 hipError_t launch_loss_zero(void* p, size_t bytes, hipStream_t st);
 hipError_t launch_loss_db(const float* dbp, int wave_rows, int BN, int db_ld, const int32_t* count, int V, float* db,
                           hipStream_t st);

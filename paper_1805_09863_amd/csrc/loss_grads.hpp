@@ -29,13 +29,9 @@ __device__ __forceinline__ int xcd_cell(int cells, int b) {
   return x * (cells >> 3) + min(x, cells & 7) + j;
 }
 
+// Tile c of the `cells` of dh.
 template <class T, int PASSES>
-__global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_dh(LossGradArgs a) {
-  __shared__ __attribute__((aligned(1024))) uint8_t ring[4 * LossOcc<T, PASSES>::STAGE];
-  const int rows = const_int(a.count);
-  const int R = loss_row_tiles(rows, T::BN), cells = a.splits * R * a.mt;
-  if ((int)blockIdx.x >= cells) return;
-  const int c = xcd_cell(cells, blockIdx.x);
+__device__ __forceinline__ void dh_tile(const LossGradArgs& a, uint32_t ring, int R, int c) {
   const int split = c / (R * a.mt), at = c - split * (R * a.mt), rt = at / a.mt, mt = at - rt * a.mt;
   // stages of 32 words, the splits' shares of them alike
   const int stages = a.gld / kLossStage;
@@ -66,7 +62,7 @@ __global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_dh(LossGrad
       part_of<T>(a.part, part, i, acc[i / T::NB][i % T::NB], false);
     }
   };
-  mm_run<T, false, false, true, PASSES>(lds_addr(ring), 1, s1 - s0, tile, init, epi);
+  mm_run<T, false, false, true, PASSES>(ring, 1, s1 - s0, tile, init, epi);
 }
 
 // 8 bf16 values to out, `left` of which exist.
@@ -80,15 +76,13 @@ __device__ __forceinline__ void write8(uint16_t* out, const bf16x8& v, int left)
     if (i < left) reinterpret_cast<__bf16*>(out)[i] = v[i];
 }
 
+// Tile c of the tiles and splits of dW.
 template <class T, int PASSES>
-__global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_dw(LossGradArgs a) {
-  __shared__ __attribute__((aligned(1024))) uint8_t ring[4 * LossOcc<T, PASSES>::STAGE];
+__device__ __forceinline__ void dw_tile(const LossGradArgs& a, uint32_t ring, int rows, int c) {
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave % T::WM, wn = wave / T::WM;
-  const int rows = const_int(a.count);
   const int stages = loss_row_tiles(rows, a.BN) * a.BN / kLossStage;
-  const int c = xcd_cell(gridDim.x, blockIdx.x);
   // the state tiles of the same words next to each other: they read the same dlogits
   const int split = c / (a.mt * a.ntn), at = c - split * (a.mt * a.ntn), mt = at / a.ntn, ht = at - mt * a.ntn;
   const int s0 = (int)((long long)stages * split / a.splits), s1 = (int)((long long)stages * (split + 1) / a.splits);
@@ -144,21 +138,48 @@ __global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_dw(LossGrad
         }
     }
   };
-  mm_run<T, true, true, false, PASSES>(lds_addr(ring), 1, s1 - s0, tile, init, epi);
+  mm_run<T, true, true, false, PASSES>(ring, 1, s1 - s0, tile, init, epi);
 }
 
-// The parts of a result added up in order and rounded once.  Workgroup: one block of 32 x 32 of every wave of a tile,
-// in the order of the registers (dh of rows that do not count: zeros, by the last workgroups).
+template <class T, int PASSES>
+__global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_dh(LossGradArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t ring[4 * LossOcc<T, PASSES>::STAGE];
+  const int R = loss_row_tiles(const_int(a.count), T::BN), cells = a.splits * R * a.mt;
+  if ((int)blockIdx.x < cells) dh_tile<T, PASSES>(a, lds_addr(ring), R, xcd_cell(cells, blockIdx.x));
+}
+
+template <class T, int PASSES>
+__global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_dw(LossGradArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t ring[4 * LossOcc<T, PASSES>::STAGE];
+  dw_tile<T, PASSES>(a, lds_addr(ring), const_int(a.count), xcd_cell(gridDim.x, blockIdx.x));
+}
+
+// Both in one launch, the longer tiles of dh first: neither has to fill the card by itself.
+template <class T, int PASSES>
+__global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_both(LossGradArgs h, LossGradArgs w) {
+  __shared__ __attribute__((aligned(1024))) uint8_t ring[4 * LossOcc<T, PASSES>::STAGE];
+  const int rows = const_int(h.count), R = loss_row_tiles(rows, T::BN);
+  const int ch = h.splits * R * h.mt, cw = w.splits * w.mt * w.ntn;
+  if ((int)blockIdx.x < ch)
+    dh_tile<T, PASSES>(h, lds_addr(ring), R, xcd_cell(ch, blockIdx.x));
+  else if ((int)blockIdx.x < ch + cw)
+    dw_tile<T, PASSES>(w, lds_addr(ring), rows, xcd_cell(cw, blockIdx.x - ch));
+}
+
+// The parts of a result added up in order and rounded once.  A workgroup takes one block of 32 x 32 of every wave of a
+// tile, in the order of the registers: four groups of 256 threads add up every fourth part each, then the four sums.
+// (dh of rows that do not count: zeros, by the last workgroups.)
 template <class T, class D>
-__global__ __launch_bounds__(256) void loss_join(LossJoinArgs a, const int32_t* inv, int N, int zero_blocks) {
-  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
+__global__ __launch_bounds__(1024) void loss_join(LossJoinArgs a, const int32_t* inv, int N, int zero_blocks) {
+  __shared__ float4 sums[4][4][256];
+  const int tid = threadIdx.x & 255, grp = threadIdx.x >> 8, lane = tid & 63, half = lane >> 5, col = lane & 31;
   const int wave = tid >> 6, wm = wave % T::WM, wn = wave / T::WM;
   D* out = static_cast<D*>(a.out);
   const int work = gridDim.x - zero_blocks;
   if ((int)blockIdx.x >= work) {
     for (int n = blockIdx.x - work; n < N; n += zero_blocks)
       if (inv[n] < 0)
-        for (int i = tid; i < a.cols; i += 256) out[(size_t)n * a.ld + i] = (D)0.f;
+        for (int i = threadIdx.x; i < a.cols; i += 1024) out[(size_t)n * a.ld + i] = (D)0.f;
     return;
   }
   const int rows = a.is_dh ? *a.count : a.rows;
@@ -166,26 +187,43 @@ __global__ __launch_bounds__(256) void loss_join(LossJoinArgs a, const int32_t* 
   const int tile = blockIdx.x / (T::MB * T::NB), blk = blockIdx.x % (T::MB * T::NB);
   const int m = blk / T::NB, n = blk % T::NB;
   const int mt = a.is_dh ? tile % a.mt : tile / a.ntn, nt = a.is_dh ? tile / a.mt : tile % a.ntn;
-  const int row = nt * T::BN + wn * T::WTN + n * 32 + col;
-  const int c0 = mt * kLossM + wm * T::WTM + m * 32 + 4 * half;
-  if (row >= rows) return;
-  float s[16];
+  if (nt * T::BN >= rows) return;
+  float4 s[4];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) s[i] = 0.f;
-  for (int k = 0; k < a.splits; ++k) {
-    const float4* p = reinterpret_cast<const float4*>(a.part) + (((size_t)k * tiles + tile) * (T::MB * T::NB) + blk) * 4 * 256 + tid;
+  for (int q = 0; q < 4; ++q) s[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+  const size_t step = (size_t)tiles * (T::MB * T::NB) * 4 * 256;
+  const float4* p = reinterpret_cast<const float4*>(a.part) + ((size_t)tile * (T::MB * T::NB) + blk) * 4 * 256 + tid;
+#pragma unroll 4
+  for (int k = grp; k < a.splits; k += 4) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const float4 v = p[q * 256];
-      s[4 * q] += v.x, s[4 * q + 1] += v.y, s[4 * q + 2] += v.z, s[4 * q + 3] += v.w;
+      const float4 v = p[k * step + q * 256];
+      s[q].x += v.x, s[q].y += v.y, s[q].z += v.z, s[q].w += v.w;
     }
   }
-  D* to = out + (size_t)(a.is_dh ? a.map[row] : row) * a.ld;
 #pragma unroll
-  for (int q = 0; q < 4; ++q)
+  for (int q = 0; q < 4; ++q) sums[grp][q][tid] = s[q];
+  __syncthreads();
+  // group q finishes the register's quarter q: words (states) 8 q + 4 half .. + 3 of the block
+  float4 r = sums[0][grp][tid];
+#pragma unroll
+  for (int k = 1; k < 4; ++k) {
+    const float4 v = sums[k][grp][tid];
+    r.x += v.x, r.y += v.y, r.z += v.z, r.w += v.w;
+  }
+  const int row = nt * T::BN + wn * T::WTN + n * 32 + col;
+  const int c = mt * kLossM + wm * T::WTM + m * 32 + 8 * grp + 4 * half;
+  if (row >= rows) return;
+  D* to = out + (size_t)(a.is_dh ? a.map[row] : row) * a.ld + c;
+  typedef D D4 __attribute__((ext_vector_type(4)));
+  if (c + 4 <= a.cols && (uintptr_t)to % sizeof(D4) == 0) {
+    *reinterpret_cast<D4*>(to) = D4{(D)r.x, (D)r.y, (D)r.z, (D)r.w};
+  } else {
+    const float v[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (c0 + 8 * q + j < a.cols) to[c0 + 8 * q + j] = (D)s[4 * q + j];
+      if (c + j < a.cols) to[j] = (D)v[j];
+  }
 }
 
 }  // namespace kb

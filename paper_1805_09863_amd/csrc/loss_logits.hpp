@@ -9,14 +9,16 @@
 //
 // Words are the M side: a lane has 64 (small tiles: 32) words of each of its rows, so statistics need no exchange
 // until the end.  The accumulators start at the bias; words that only fill the last tile up start at -inf.
-// Entries were sorted into a list for each wave's part of each tile: the wave goes through its few, reading them with
-// scalar loads (about 21 for 256 x 256 at 16 entries a row and 50,000 words), and picks the register by a branch.
+// Entries were sorted into a list for each wave's part of each tile.  A wave takes one to four one by one, with scalar
+// loads, and picks the register by a branch; more go through LDS, a lane each (a teacher's words cluster where the
+// vocabulary's frequent words are: half of 64 a row in one tile of 256 words).
 #pragma once
 
 #include "loss_mm.hpp"
 
 namespace kb {
 
+typedef float f32x4v __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 #define KB_CONST __attribute__((address_space(4)))
 
@@ -89,6 +91,9 @@ __device__ __forceinline__ void store_bf16(f32x16 (&acc)[T::MB][T::NB], int plan
   }
 }
 
+// Entries of a wave's part of a tile that are taken one by one; more go through LDS.
+constexpr int kFewEntries = 4;
+
 template <class T, int PASSES>
 struct LossOcc {  // workgroups that fit on a CU
   static constexpr int STAGE = MmGeom<T::BM>::BYTES + MmGeom<T::BN>::BYTES;
@@ -98,11 +103,14 @@ struct LossOcc {  // workgroups that fit on a CU
 template <class T, int PASSES, bool GRAD>
 __global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_logits(LossLogitsArgs a) {
   constexpr int MB = T::MB, NB = T::NB, BN = T::BN;
-  constexpr int PLANES = PASSES > 1 ? 3 : 1;
+  constexpr int PLANES = PASSES > 1 ? 3 : 1, NBLK = MB * NB;
   __shared__ __attribute__((aligned(1024))) uint8_t ring[4 * LossOcc<T, PASSES>::STAGE];
   __shared__ __attribute__((aligned(16))) float bias[4][kLossM];
   __shared__ __attribute__((aligned(16))) float2 rowp[GRAD ? BN : 1];
   __shared__ __attribute__((aligned(16))) float red[GRAD ? 1 : BN][T::WM][3];
+  // the gradient's entries have LDS of their own, but for the tile of which two workgroups then fit no more
+  constexpr bool APART = GRAD && LossOcc<T, PASSES>::N == 1;
+  __shared__ __attribute__((aligned(16))) uint8_t apart[APART ? 4 * 32 * 36 * 4 : 16];
 
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -118,7 +126,7 @@ __global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_logits(Loss
     for (int r = tid; r < BN; r += 256) rowp[r] = a.rowp[rt * BN + r];
     __syncthreads();
   }
-  const int32_t* offs = a.offs + (size_t)rt * (a.nb + 1) + wn * a.words0 + a.wt0 + wm;
+  const uint16_t* offs = a.offs + (size_t)rt * (a.nb + 2) + (size_t)(wn * a.words0 + a.wt0 + wm) * NBLK;
   const LossItem* items = a.items + (size_t)rt * BN * a.K;
 
   auto tile = [&](int t, MmSide& A, MmSide& B) {
@@ -146,13 +154,61 @@ __global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_logits(Loss
       }
     }
   };
-  // the wave's entries of tile t: each(block, register, lane, item)
-  auto entries = [&](int t, auto each) {
-    const int32_t* o = offs + (sp + t * P) * (kLossM / T::WTM);
-    const int lo = const_int(o), hi = const_int(o + 1);
-    for (int e = lo; e < hi; ++e) {
-      const i32x4 it = const_int4(items + e);
-      each(it[0] >> 16, (it[0] >> 8) & 255, it[0] & 255, it);
+  // The wave's entries of a tile, block by block (m, n).  The first 256 are held four a lane, loaded as the epilogue
+  // begins (a few: by scalar loads, which do not wait for the DMA); those of a block move between the accumulators and
+  // their lanes through LDS of the wave's own, the block's 32 rows 36 floats apart.
+  struct Entries {
+    uint32_t offs[NBLK / 2 + 1];  // two a word: first entries of the blocks, the end of the last one
+    int lo, n;
+    int payload[4];
+    uint32_t at[4];
+  };
+  auto entry_at = [&](uint32_t mine, int code) {
+    const int r = code >> 8, l = code & 255;
+    return mine + (uint32_t)((l & 31) * 36 + 8 * (r >> 2) + 4 * (l >> 5) + (r & 3)) * 4u;
+  };
+  auto load_entries = [&](int t, uint32_t mine, Entries& e) {
+    const uint16_t* o = offs + (size_t)(sp + t * P) * (kLossM / T::WTM) * NBLK;
+#pragma unroll
+    for (int i = 0; i <= NBLK / 2; ++i) e.offs[i] = (uint32_t)const_int(reinterpret_cast<const int32_t*>(o) + i);
+    e.lo = e.offs[0] & 0xffffu;
+    e.n = (int)(e.offs[NBLK / 2] & 0xffffu) - e.lo;
+    if (e.n <= 0) return;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      e.payload[u] = 0;
+      e.at[u] = mine;
+    }
+    if (e.n <= kFewEntries) {
+      for (int i = 0; i < e.n; ++i) {
+        const int code = const_int(&items[e.lo + i].code), payload = const_int(&items[e.lo + i].payload);
+        if (lane == i) {
+          e.at[0] = entry_at(mine, code);
+          e.payload[0] = payload;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (u * 64 + lane < e.n) {
+          const LossItem it = items[e.lo + u * 64 + lane];
+          e.at[u] = entry_at(mine, it.code);
+          e.payload[u] = it.payload;
+        }
+    }
+  };
+  auto block_has = [&](const Entries& e, int b, int& lo, int& hi) {  // first and end within the list
+    lo = (int)((b & 1 ? e.offs[b / 2] >> 16 : e.offs[b / 2] & 0xffffu)) - e.lo;
+    hi = (int)(((b + 1) & 1 ? e.offs[(b + 1) / 2] >> 16 : e.offs[(b + 1) / 2] & 0xffffu)) - e.lo;
+    return hi > lo;
+  };
+  auto each_entry = [&](const Entries& e, uint32_t mine, int lo, int hi, auto use) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (u * 64 + lane >= lo && u * 64 + lane < hi) use(e.at[u], e.payload[u]);
+    for (int i = max(lo, 256) + lane; i < hi; i += 64) {
+      const LossItem it = items[e.lo + i];
+      use(entry_at(mine, it.code), it.payload);
     }
   };
 
@@ -164,8 +220,11 @@ __global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_logits(Loss
       st_s[n] = st_x[n] = 0.f;
     }
   }
-  auto epi_stats = [&](int t, f32x16 (&acc)[MB][NB]) {
+  auto epi_stats = [&](int t, f32x16 (&acc)[MB][NB], uint32_t lds) {
     const int left = a.words - (sp + t * P) * kLossM - wm * T::WTM - 4 * half;  // words from the lane's first on
+    const uint32_t mine = lds + wave * (32 * 36 * 4), words = mine + (uint32_t)(col * 36 + 4 * half) * 4u;
+    Entries e;
+    load_entries(t, mine, e);
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
 #pragma unroll
@@ -198,78 +257,88 @@ __global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_logits(Loss
           for (int r = 0; r < 16; ++r) x0 += m * 32 + 8 * (r >> 2) + (r & 3) < left ? acc[m][n][r] : 0.f;
         st_x[n] += x0;
       }
+      if (e.n > 0) {
+#pragma unroll
+        for (int m = 0; m < MB; ++m) {
+          int lo, hi;
+          if (!block_has(e, m * NB + n, lo, hi)) continue;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            *(KB_LDS f32x4v*)(uintptr_t)(words + i * 32u) =
+                f32x4v{acc[m][n][4 * i], acc[m][n][4 * i + 1], acc[m][n][4 * i + 2], acc[m][n][4 * i + 3]};
+          each_entry(e, mine, lo, hi, [&](uint32_t at, int slot) { a.xt[slot] = *(const KB_LDS float*)(uintptr_t)at; });
+        }
+      }
       asm volatile("" ::"v"(st_s[n]));  // one row's 64 logits in VGPRs at a time
     }
-    entries(t, [&](int blk, int r, int l, const i32x4& it) {
-      float x = 0.f;
-#pragma unroll
-      for (int m = 0; m < MB; ++m)
-#pragma unroll
-        for (int n = 0; n < NB; ++n)
-          if (blk == m * NB + n) {
-            in_acc(acc[m][n]);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x = r == i ? acc[m][n][i] : x;
-          }
-      if (lane == l) a.xt[it[1]] = x;
-    });
   };
+  // dlogits, 32 words of every wave at a time: from the accumulators through the entries, the bias' sums and the
+  // rounding to LDS, and from there to memory in rows (64 bytes in one piece, where the accumulators alone would give 8)
   auto epi_grad = [&](int t, f32x16 (&acc)[MB][NB], uint32_t lds) {
     const int v0 = (sp + t * P) * kLossM;
     const int left = a.words - v0 - wm * T::WTM - 4 * half;
     const bool ragged = v0 + kLossM > a.words && a.rest != 0.f;
+    constexpr int CH = T::WM * 4;  // 16-byte chunks of a row of the tile's 32 words a wave
+    static_assert(BN * CH * 16 <= LossOcc<T, PASSES>::STAGE && 4 * 32 * 36 * 4 <= LossOcc<T, PASSES>::STAGE, "fit in a stage");
+    const uint32_t mine = (APART ? lds_addr(apart) : lds) + wave * (32 * 36 * 4);
+    const uint32_t words = mine + (uint32_t)(col * 36 + 4 * half) * 4u;
+    Entries e;
+    load_entries(t, mine, e);
+    float off[NB], g[NB];
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
       const float2 rp = rowp[wn * T::WTN + n * 32 + col];  // (lse, g)
-      const float off = PASSES > 1 ? rp.x : rp.x * kL2E;
-      const float gr = rp.y * a.rest;
+      off[n] = PASSES > 1 ? rp.x : rp.x * kL2E;
+      g[n] = rp.y;
+    }
 #pragma unroll
-      for (int m = 0; m < MB; ++m) {
+    for (int m = 0; m < MB; ++m) {
+      if constexpr (!APART)
+        if (m > 0) lds_barrier();  // the entries' LDS is that of the rows before
+      float x[NB][16];
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
         in_acc(acc[m][n]);
+        const float gr = g[n] * a.rest;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           // float32: the difference first, so that its rounding and not that of lse * log2(e) is what p sees
-          const float e = PASSES > 1 ? fmaf(acc[m][n][r], a.scale, -off) * kL2E : fmaf(acc[m][n][r], a.scale, -off);
-          float v = fmaf(rp.y, exp2_fast(e), -gr);
-          if (ragged && m * 32 + 8 * (r >> 2) + (r & 3) >= left) v = 0.f;
-          acc[m][n][r] = v;
+          const float y = PASSES > 1 ? fmaf(acc[m][n][r], a.scale, -off[n]) * kL2E : fmaf(acc[m][n][r], a.scale, -off[n]);
+          x[n][r] = fmaf(g[n], exp2_fast(y), -gr);
         }
-        in_acc(acc[m][n]);
-      }
-    }
-    entries(t, [&](int blk, int r, int l, const i32x4& it) {
-      const float q = __int_as_float(it[2]);
+        if (ragged) {
 #pragma unroll
-      for (int m = 0; m < MB; ++m)
+          for (int r = 0; r < 16; ++r)
+            if (m * 32 + 8 * (r >> 2) + (r & 3) >= left) x[n][r] = 0.f;
+        }
+        int lo, hi;
+        if (e.n > 0 && block_has(e, m * NB + n, lo, hi)) {
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
-          if (blk == m * NB + n) {
-            in_acc(acc[m][n]);
-            const float d = lane == l ? q * rowp[wn * T::WTN + n * 32 + col].y : 0.f;
+          for (int i = 0; i < 4; ++i) *(KB_LDS f32x4v*)(uintptr_t)(words + i * 32u) = f32x4v{0.f, 0.f, 0.f, 0.f};
+          each_entry(e, mine, lo, hi, [&](uint32_t at, int q) { *(KB_LDS float*)(uintptr_t)at = __int_as_float(q); });
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[m][n][i] -= r == i ? d : 0.f;
-            in_acc(acc[m][n]);
+          for (int i = 0; i < 4; ++i) {
+            const f32x4v q = *(const KB_LDS f32x4v*)(uintptr_t)(words + i * 32u);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[n][4 * i + j] = fmaf(-g[n], q[j], x[n][4 * i + j]);
           }
-    });
-    if (a.dbp) {
-      // over the wave's rows: its blocks in registers, then the 32 lanes by halving the words a lane keeps
-#pragma unroll
-      for (int m = 0; m < MB; ++m) {
+        }
+      }
+      if (a.dbp) {
+        // over the wave's rows: its blocks in registers, then the 32 lanes by halving the words a lane keeps
         float s[16];
 #pragma unroll
-        for (int n = 0; n < NB; ++n) in_acc(acc[m][n]);
-#pragma unroll
         for (int r = 0; r < 16; ++r) {
-          s[r] = acc[m][0][r];
+          s[r] = x[0][r];
 #pragma unroll
-          for (int n = 1; n < NB; ++n) s[r] += acc[m][n][r];
+          for (int n = 1; n < NB; ++n) s[r] += x[n][r];
         }
 #pragma unroll
         for (int w = 8; w >= 1; w >>= 1) {
-          const bool up = (col & (2 * w)) != 0;
+          const bool upper = (col & (2 * w)) != 0;
 #pragma unroll
           for (int r = 0; r < w; ++r) {
-            const float keep = up ? s[r + w] : s[r], give = up ? s[r] : s[r + w];
+            const float keep = upper ? s[r + w] : s[r], give = upper ? s[r] : s[r + w];
             s[r] = keep + __shfl_xor(give, 2 * w, 64);
           }
         }
@@ -279,20 +348,39 @@ __global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_logits(Loss
           a.dbp[(size_t)(rt * T::WN + wn) * a.db_ld + a.db0 + v0 + wm * T::WTM + m * 32 + 8 * (r >> 2) + 4 * half + (r & 3)] =
               s[0];
       }
-    }
-#pragma unroll 1
-    for (int pl = 0; pl < PLANES; ++pl) {
-      uint16_t* out = a.g + pl * a.g_plane + (size_t)rt * BN * a.gld + v0;
-      store_bf16<T>(acc, pl, lds, [&](int row, int word, const bf16x8& v) {
-        *reinterpret_cast<bf16x8*>(out + (size_t)row * a.gld + word) = v;
-      });
+#pragma unroll
+      for (int pl = 0; pl < PLANES; ++pl) {
+        if (pl > 0 || m > 0 || !APART) lds_barrier();
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+          const int row = wn * T::WTN + n * 32 + col;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            bf16x4 v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              v[j] = (__bf16)x[n][4 * i + j];
+              if (pl + 1 < PLANES) x[n][4 * i + j] -= (float)v[j];
+            }
+            *(KB_LDS bf16x4*)(uintptr_t)(lds + (uint32_t)(row * CH + ((wm * 4 + i) ^ (row & (CH - 1)))) * 16u + half * 8u) = v;
+          }
+        }
+        lds_barrier();
+        uint16_t* out = a.g + pl * a.g_plane + (size_t)rt * BN * a.gld + v0;
+#pragma unroll
+        for (int k = 0; k < BN * CH / 256; ++k) {
+          const int at = k * 256 + tid, row = at / CH, c = at % CH;
+          *reinterpret_cast<bf16x8*>(out + (size_t)row * a.gld + (c >> 2) * T::WTM + m * 32 + (c & 3) * 8) =
+              *(const KB_LDS bf16x8*)(uintptr_t)(lds + (uint32_t)(row * CH + (c ^ (row & (CH - 1)))) * 16u);
+        }
+      }
     }
   };
   auto epi = [&](int t, f32x16 (&acc)[MB][NB], uint32_t lds) {
     if constexpr (GRAD)
       epi_grad(t, acc, lds);
     else
-      epi_stats(t, acc);
+      epi_stats(t, acc, lds);
   };
   mm_run<T, true, false, PASSES == 1, PASSES>(lds_addr(ring), nt, a.Hk / kLossStage, tile, init, epi);
 

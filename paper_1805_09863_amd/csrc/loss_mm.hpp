@@ -98,7 +98,7 @@ __device__ __forceinline__ void mm_run(uint32_t ring, int nt, int nk, TileFn til
       const int slot = q * 64 + lane;
       if constexpr (S) {
         const int r = slot / (R / 8);
-        int c = ((slot % (R / 8)) ^ wswz(r)) * 8;
+        int c = ((slot % (R / 8)) ^ (wswz(r) & (R / 8 - 1))) * 8;
         if constexpr (decltype(clamp)::value) c = min(c, s.lim - 8);
         off[i] = (uint32_t)r * (uint32_t)s.ld * 2u + (uint32_t)c * 2u;
       } else {
@@ -188,7 +188,7 @@ __device__ __forceinline__ void mm_run(uint32_t ring, int nt, int nk, TileFn til
 #pragma unroll
       for (int x = 0; x < nblk; ++x) {
         const int c = w0 + x * 32 + 16 * (g & 1) + 4 * (j & 3);
-        off[x] = base + (uint32_t)(r0 * R + (((c >> 3) ^ wswz(r0)) << 3) + (c & 7)) * 2u;
+        off[x] = base + (uint32_t)(r0 * R + (((c >> 3) ^ (wswz(r0) & (R / 8 - 1))) << 3) + (c & 7)) * 2u;
       }
     } else {
       const int n = w0 + col;

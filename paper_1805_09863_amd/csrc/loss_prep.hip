@@ -1,5 +1,7 @@
 // Around the products of the output layer's losses: which rows count and their entries, operands laid out for the
 // DMA pipeline, and the losses from the parts of all splits.
+#include <algorithm>
+
 #include "k3_scan.hpp"
 #include "loss_common.hpp"
 
@@ -79,18 +81,19 @@ __global__ __launch_bounds__(256) void loss_teacher(LossTeacherArgs a) {
   }
 }
 
+__device__ __forceinline__ bool row_counts(const LossRows& a, int n) {
+  if (a.flag) return a.flag[n] != 0;
+  const int t = a.token[n];
+  return t >= 0 && t < a.V;
+}
+
 // Rows that count, in order (a stable compaction).  One workgroup: 4,096 rows a turn.
 __global__ __launch_bounds__(K3_T) void loss_rows(LossRows a) {
   __shared__ int wsum[K3_W];
-  auto counts = [&](int n) {
-    if (a.flag) return a.flag[n] != 0;
-    const int t = a.token[n];
-    return t >= 0 && t < a.V;
-  };
   for (int n = threadIdx.x; n < a.N; n += K3_T)
-    if (!counts(n)) a.inv[n] = -1;
+    if (!row_counts(a, n)) a.inv[n] = -1;
   const int kept = compact_entries_pass(
-      a.N, counts,
+      a.N, [&](int n) { return row_counts(a, n); },
       [&](int c, int n) {
         a.map[c] = n;
         a.inv[n] = c;
@@ -142,99 +145,11 @@ __device__ __forceinline__ void load8(const S* p, int n, float (&x)[8]) {
   for (int i = 0; i < 8; ++i) x[i] = i < n ? widen(p, i) : 0.f;
 }
 
-// The packed rows' states in bf16 pieces, as whole row tiles with zeros behind them, and the lists of their entries.
-// Workgroups 0 .. tiles - 1 make a row tile's lists (a counting sort by wave tile; the order within a list is free, as
-// every entry of a row is of another word), the others copy states.
 template <class S, int PLANES>
-__global__ __launch_bounds__(256) void loss_pack(LossPackArgs a, int wtm, int wtn) {
-  extern __shared__ int hist[];  // nb + 1
-  __shared__ int wsum[4];
-  const int rows = *a.rows.count, R = loss_row_tiles(rows, a.BN);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  if ((int)blockIdx.x < a.tiles) {
-    const int rt = blockIdx.x, K = a.rows.K;
-    if (rt >= R) return;
-    const int here = min(a.BN, rows - rt * a.BN), n = here * K;
-    for (int i = tid; i <= a.nb; i += 256) hist[i] = 0;
-    if (a.rowp)
-      for (int r = tid; r < a.BN; r += 256) {
-        const int c = rt * a.BN + r;
-        float2 v = make_float2(INFINITY, 0.f);  // no row: probabilities of zero
-        if (r < here) {
-          const int row = a.rows.map[c];
-          v = make_float2(a.lse[row], a.grad[row] * a.grad_scale);
-        }
-        a.rowp[c] = v;
-      }
-    __syncthreads();
-    auto word = [&](int e) { return a.rows.token[(size_t)a.rows.map[rt * a.BN + e / K] * K + e % K]; };
-    auto list = [&](int e, int t) { return (e / K) / wtn * a.words0 + t / wtm; };
-    for (int e = tid; e < n; e += 256) {
-      const int t = word(e);
-      if (t >= 0 && t < a.rows.V) atomicAdd(&hist[list(e, t) + 1], 1);
-    }
-    __syncthreads();
-    // inclusive scan of hist[1 ..]: hist[i] becomes the first item of list i
-    int carry = 0;
-    for (int i0 = 0; i0 < a.nb; i0 += 256) {
-      const int i = i0 + tid;
-      int x = i < a.nb ? hist[i + 1] : 0;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const int y = __shfl_up(x, d, 64);
-        if (lane >= d) x += y;
-      }
-      if (lane == 63) wsum[wave] = x;
-      __syncthreads();
-      int before = carry;
-      for (int w = 0; w < wave; ++w) before += wsum[w];
-      carry += wsum[0] + wsum[1] + wsum[2] + wsum[3];
-      if (i < a.nb) hist[i + 1] = before + x;
-      __syncthreads();
-    }
-    int32_t* offs = a.offs + (size_t)rt * (a.nb + 1);
-    for (int i = tid; i <= a.nb; i += 256) offs[i] = hist[i];
-    __syncthreads();
-    LossItem* items = a.items + (size_t)rt * a.BN * K;
-    const int NB = wtn / 32;
-    for (int e = tid; e < n; e += 256) {
-      const int t = word(e);
-      if (t < 0 || t >= a.rows.V) continue;
-      const int at = atomicAdd(&hist[list(e, t)], 1);
-      const int r = (e / K) % wtn, w = t % wtm;
-      const int blk = (w >> 5) * NB + (r >> 5);
-      const int reg = 4 * ((w >> 3) & 3) + (w & 3), l = 32 * ((w >> 2) & 1) + (r & 31);
-      const int row = a.rows.map[rt * a.BN + e / K];
-      LossItem it;
-      it.code = blk << 16 | reg << 8 | l;
-      it.slot = rt * a.BN * K + e;
-      it.part = a.rows.part ? a.rows.part[(size_t)row * K + e % K] : a.rows.target_part;
-      it.unused = 0;
-      items[at] = it;
-    }
-    return;
-  }
-  const int chunks = a.Hp / 8, H = a.rows.H;
-  const long long total = (long long)R * a.BN * chunks;
-  for (long long i = (long long)(blockIdx.x - a.tiles) * 256 + tid; i < total; i += (long long)(gridDim.x - a.tiles) * 256) {
-    const int c = (int)(i / chunks), h0 = (int)(i % chunks) * 8;
-    float x[8];
-    if (c < rows && h0 < H) {
-      load8(static_cast<const S*>(a.h) + (size_t)a.rows.map[c] * H + h0, H - h0, x);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = 0.f;
-    }
-    write_pieces<PLANES>(x, a.ph + (size_t)c * a.Hp + h0, a.ph_plane);
-  }
-}
-
-// A piece of W in bf16 pieces, filled up with zeros.
-template <class S, int PLANES>
-__global__ __launch_bounds__(256) void loss_pack_w(LossPackWArgs a) {
+__device__ __forceinline__ void pack_w(const LossPackWArgs& a, long long first, long long step) {
   const int chunks = a.Vc / 8;
   const long long total = (long long)a.Hk * chunks;
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
+  for (long long i = first; i < total; i += step) {
     const int r = (int)(i / chunks), w = (int)(i % chunks) * 8;
     float x[8];
     const int n = a.V - a.v0 - w;
@@ -248,9 +163,139 @@ __global__ __launch_bounds__(256) void loss_pack_w(LossPackWArgs a) {
   }
 }
 
-__global__ __launch_bounds__(256) void loss_pack_b(const float* b, int V, int Vp, float* out) {
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i < Vp) out[i] = i < V ? b[i] : -INFINITY;
+template <class S, int PLANES>
+__global__ __launch_bounds__(256) void loss_pack_w(LossPackWArgs a) {
+  pack_w<S, PLANES>(a, (long long)blockIdx.x * 256 + threadIdx.x, (long long)gridDim.x * 256);
+}
+
+// What a loss lays out before its products, by workgroup:
+//   lists   of a row tile's entries, sorted by the block of 32 x 32 that will hold them (a counting sort in LDS, two
+//           16-bit counters a word: a block has at most 1,024 entries, as every entry of a row is of another word, and
+//           a tile 32,768; the order within a block is free, each entry's result being a value of its own);
+//   states  of the rows that count, in bf16 pieces, as whole row tiles with zeros behind them;
+//   bias    filled up with -inf;
+//   W       its first piece, where it is not read where it lies.
+// Where there are few rows and entries' blocks, every workgroup finds the rows that count by itself, in LDS: a launch
+// and its gap less (about 4 us) for about 2 us.
+constexpr int kFindRows = 8192;
+constexpr int kPackT = 1024;
+
+template <class S, int PLANES>
+__global__ __launch_bounds__(kPackT) void loss_pack(LossPackArgs a) {
+  extern __shared__ uint32_t dyn[];
+  __shared__ int wsum[K3_W];
+  const int tid = threadIdx.x;
+  int wg = blockIdx.x;
+  if (wg >= a.tiles + a.states_wg) {
+    wg -= a.tiles + a.states_wg;
+    if (wg < a.bias_wg) {
+      const int i = wg * kPackT + tid;
+      if (i < a.Vp) a.bp[i] = i < a.rows.V ? a.b[i] : -INFINITY;
+    } else {
+      pack_w<S, PLANES>(a.w, (long long)(wg - a.bias_wg) * kPackT + tid, (long long)a.w_wg * kPackT);
+    }
+    return;
+  }
+  const int32_t* map = a.rows.map;
+  int rows;
+  if (a.find_rows) {
+    int* own = reinterpret_cast<int*>(dyn);
+    const bool tell = wg == 0;
+    if (tell)
+      for (int n = tid; n < a.rows.N; n += kPackT)
+        if (!row_counts(a.rows, n)) a.rows.inv[n] = -1;
+    rows = compact_entries_pass(
+        a.rows.N, [&](int n) { return row_counts(a.rows, n); },
+        [&](int c, int n) {
+          own[c] = n;
+          if (tell) {
+            a.rows.map[c] = n;
+            a.rows.inv[n] = c;
+          }
+        },
+        wsum);
+    if (tell && tid == 0) *a.rows.count = rows;
+    map = own;
+    __syncthreads();
+  } else {
+    rows = *a.rows.count;
+  }
+  const int R = loss_row_tiles(rows, a.BN);
+  if (wg < a.tiles) {
+    const int rt = wg, K = a.rows.K;
+    if (rt >= R) return;
+    const int here = min(a.BN, rows - rt * a.BN);
+    if (a.rowp)
+      for (int r = tid; r < a.BN; r += kPackT) {
+        float2 v = make_float2(INFINITY, 0.f);  // no row: probabilities of zero
+        if (r < here) {
+          const int row = map[rt * a.BN + r];
+          v = make_float2(a.lse[row], a.grad[row] * a.grad_scale);
+        }
+        a.rowp[rt * a.BN + r] = v;
+      }
+    // counter i (list i - 1) in the halves of hist[i / 2]
+    uint32_t* hist = dyn + (a.find_rows ? (a.rows.N + 1) / 2 * 2 : 0);
+    const int words = a.nb / 2 + 1;  // nb is even
+    for (int i = tid; i < words; i += kPackT) hist[i] = 0;
+    __syncthreads();
+    const int wtm = loss_wtm(a.BN), wtn = loss_wtn(a.BN), NB = wtn / 32, blocks = loss_blocks(a.BN);
+    // a thread's entries: j of rows r0, r0 + step, ...
+    const int kp = K <= 1 ? 1 : 1 << (32 - __builtin_clz(K - 1));
+    const int j = tid & (kp - 1), r0 = tid / kp, step = kPackT / kp;
+    auto each = [&](auto use) {
+      if (j < K)
+        for (int r = r0; r < here; r += step) {
+          const int row = map[rt * a.BN + r];
+          const int t = a.rows.token[(size_t)row * K + j];
+          if (t >= 0 && t < a.rows.V) {
+            const int blk = ((t % wtm) >> 5) * NB + ((r % wtn) >> 5);
+            use(r, row, t, (r / wtn * a.words0 + t / wtm) * blocks + blk);
+          }
+        }
+    };
+    each([&](int, int, int, int list) { atomicAdd(&hist[(list + 1) >> 1], ((list + 1) & 1) ? 1u << 16 : 1u); });
+    __syncthreads();
+    // counters to first items: hist[i] becomes the sum of the counters up to i
+    {
+      const int per = (words + kPackT - 1) / kPackT, i0 = min(words, tid * per), i1 = min(words, i0 + per);
+      int sum = 0;
+      for (int i = i0; i < i1; ++i) sum += (hist[i] & 0xffffu) + (hist[i] >> 16);
+      int total;
+      int at = block_excl_scan(sum, wsum, &total);
+      for (int i = i0; i < i1; ++i) {
+        const int lo = at + (hist[i] & 0xffffu), hi = lo + (hist[i] >> 16);
+        hist[i] = (uint32_t)lo | (uint32_t)hi << 16;
+        at = hi;
+      }
+    }
+    __syncthreads();
+    uint32_t* offs = reinterpret_cast<uint32_t*>(a.offs + (size_t)rt * (a.nb + 2));
+    for (int i = tid; i < words; i += kPackT) offs[i] = hist[i];
+    __syncthreads();
+    LossItem* items = a.items + (size_t)rt * a.BN * K;
+    each([&](int r, int row, int t, int list) {
+      const uint32_t before = atomicAdd(&hist[list >> 1], (list & 1) ? 1u << 16 : 1u);
+      const int at = (list & 1) ? before >> 16 : before & 0xffffu;
+      const int reg = 4 * ((t >> 3) & 3) + (t & 3), l = 32 * ((t >> 2) & 1) + (r & 31);
+      const float part = a.rows.part ? a.rows.part[(size_t)row * K + j] : a.rows.target_part;
+      items[at] = {reg << 8 | l, a.rowp ? __float_as_int(part) : (rt * a.BN + r) * K + j};
+    });
+    return;
+  }
+  const int chunks = a.Hp / 8, H = a.rows.H;
+  const long long total = (long long)R * a.BN * chunks;
+  for (long long i = (long long)(wg - a.tiles) * kPackT + tid; i < total; i += (long long)a.states_wg * kPackT) {
+    const int c = (int)(i / chunks), h0 = (int)(i % chunks) * 8;
+    float x[8];
+    if (c < rows && h0 < H) {
+      load8(static_cast<const S*>(a.h) + (size_t)map[c] * H + h0, H - h0, x);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = 0.f;
+    }
+    write_pieces<PLANES>(x, a.ph + (size_t)c * a.Hp + h0, a.ph_plane);
+  }
 }
 
 // loss and log-sum-exp of every row, a wave each: M = max m, S = sum s e^((m - M) / T) over all splits, lse = M / T + ln S.
@@ -331,16 +376,24 @@ hipError_t launch_loss_rows(const LossRows& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-hipError_t launch_loss_pack(bool bf16, const LossPackArgs& a, hipStream_t st) {
-  const long long most = (long long)loss_row_tiles(a.rows.N, a.BN) * a.BN * (a.Hp / 8);
-  const int copies = (int)((most + 255) / 256 < 4096 ? (most + 255) / 256 : 4096);
-  const dim3 gr(a.tiles + copies);
-  const size_t lds = ((size_t)a.nb + 1) * sizeof(int);
-  const int wtm = loss_wtm(a.BN), wtn = loss_wtn(a.BN);
+bool loss_finds_rows(int N, int nb) { return N <= kFindRows && (size_t)N * 4 + (size_t)nb * 2 <= 60 * 1024; }
+
+hipError_t launch_loss_pack(bool bf16, LossPackArgs a, hipStream_t st) {
+  const long long copies = (long long)loss_row_tiles(a.rows.N, a.BN) * a.BN * (a.Hp / 8);
+  a.states_wg = (int)std::min<long long>((copies + kPackT - 1) / kPackT, 512);
+  a.bias_wg = (a.Vp + kPackT - 1) / kPackT;
+  a.w_wg = a.w.out ? (int)std::min<long long>(((long long)a.w.Hk * (a.w.Vc / 8) + kPackT - 1) / kPackT, 2048) : 0;
+  const dim3 gr(a.tiles + a.states_wg + a.bias_wg + a.w_wg), th(kPackT);
+  const size_t lds = ((size_t)(a.find_rows ? (a.rows.N + 1) / 2 * 2 : 0) + a.nb / 2 + 1) * 4;
+  const void* f = bf16 ? reinterpret_cast<const void*>(loss_pack<uint16_t, 1>) : reinterpret_cast<const void*>(loss_pack<float, 3>);
+  if (lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
   if (bf16)
-    loss_pack<uint16_t, 1><<<gr, dim3(256), lds, st>>>(a, wtm, wtn);
+    loss_pack<uint16_t, 1><<<gr, th, lds, st>>>(a);
   else
-    loss_pack<float, 3><<<gr, dim3(256), lds, st>>>(a, wtm, wtn);
+    loss_pack<float, 3><<<gr, th, lds, st>>>(a);
   return hipGetLastError();
 }
 
@@ -351,11 +404,6 @@ hipError_t launch_loss_pack_w(bool bf16, const LossPackWArgs& a, hipStream_t st)
     loss_pack_w<uint16_t, 1><<<gr, dim3(256), 0, st>>>(a);
   else
     loss_pack_w<float, 3><<<gr, dim3(256), 0, st>>>(a);
-  return hipGetLastError();
-}
-
-hipError_t launch_loss_pack_b(const float* b, int V, int Vp, float* out, hipStream_t st) {
-  loss_pack_b<<<dim3((Vp + 255) / 256), dim3(256), 0, st>>>(b, V, Vp, out);
   return hipGetLastError();
 }
 
