@@ -365,6 +365,7 @@ kb_status gradient(const Call& c) {
     g.g = a.g;
     g.g_plane = a.g_plane;
     g.gld = Vc;
+    g.vt = tiles;
     g.N = c.N;
     g.BN = p.BN;
     g.count = w.rows.count;

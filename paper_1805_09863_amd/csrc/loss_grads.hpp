@@ -34,7 +34,7 @@ template <class T, int PASSES>
 __device__ __forceinline__ void dh_tile(const LossGradArgs& a, uint32_t ring, int R, int c) {
   const int split = c / (R * a.mt), at = c - split * (R * a.mt), rt = at / a.mt, mt = at - rt * a.mt;
   // stages of 32 words, the splits' shares of them alike
-  const int stages = a.gld / kLossStage;
+  const int stages = a.vt * (kLossM / kLossStage);
   const int s0 = (int)((long long)stages * split / a.splits), s1 = (int)((long long)stages * (split + 1) / a.splits);
   const int k0 = s0 * kLossStage, m0 = mt * kLossM;
   auto tile = [&](int, MmSide& A, MmSide& B) {

@@ -121,15 +121,15 @@ __global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_logits(Loss
   int rt, sp;
   loss_cell(R, P, blockIdx.x, rt, sp);
   const int nt = (a.vt - sp + P - 1) / P;
+  using Args = LossLogitsArgs;
 
   if constexpr (GRAD) {
     for (int r = tid; r < BN; r += 256) rowp[r] = a.rowp[rt * BN + r];
     __syncthreads();
   }
-  const uint16_t* offs = a.offs + (size_t)rt * (a.nb + 2) + (size_t)(wn * a.words0 + a.wt0 + wm) * NBLK;
-  const LossItem* items = a.items + (size_t)rt * BN * a.K;
 
   auto tile = [&](int t, MmSide& A, MmSide& B) {
+    const auto& a = *args_again<Args>();
     const int v0 = (sp + t * P) * kLossM;
     A = {a.A + v0, a.lda, a.a_plane, a.a_cols - v0, 0};
     B = {a.ph + (size_t)rt * BN * a.Hp, a.Hp, a.ph_plane, 0, 0};
@@ -158,6 +158,7 @@ __global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_logits(Loss
   // begins (a few: by scalar loads, which do not wait for the DMA); those of a block move between the accumulators and
   // their lanes through LDS of the wave's own, the block's 32 rows 36 floats apart.
   struct Entries {
+    const LossItem* items;
     uint32_t offs[NBLK / 2 + 1];  // two a word: first entries of the blocks, the end of the last one
     int lo, n;
     int payload[4];
@@ -168,7 +169,10 @@ __global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_logits(Loss
     return mine + (uint32_t)((l & 31) * 36 + 8 * (r >> 2) + 4 * (l >> 5) + (r & 3)) * 4u;
   };
   auto load_entries = [&](int t, uint32_t mine, Entries& e) {
-    const uint16_t* o = offs + (size_t)(sp + t * P) * (kLossM / T::WTM) * NBLK;
+    const auto& a = *args_again<Args>();
+    const int list = wn * a.words0 + a.wt0 + wm + (sp + t * P) * (kLossM / T::WTM);
+    const uint16_t* o = a.offs + (size_t)rt * (a.nb + 2) + (size_t)list * NBLK;
+    e.items = a.items + (size_t)rt * BN * a.K;
 #pragma unroll
     for (int i = 0; i <= NBLK / 2; ++i) e.offs[i] = (uint32_t)const_int(reinterpret_cast<const int32_t*>(o) + i);
     e.lo = e.offs[0] & 0xffffu;
@@ -181,7 +185,7 @@ __global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_logits(Loss
     }
     if (e.n <= kFewEntries) {
       for (int i = 0; i < e.n; ++i) {
-        const int code = const_int(&items[e.lo + i].code), payload = const_int(&items[e.lo + i].payload);
+        const int code = const_int(&e.items[e.lo + i].code), payload = const_int(&e.items[e.lo + i].payload);
         if (lane == i) {
           e.at[0] = entry_at(mine, code);
           e.payload[0] = payload;
@@ -191,7 +195,7 @@ __global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_logits(Loss
 #pragma unroll
       for (int u = 0; u < 4; ++u)
         if (u * 64 + lane < e.n) {
-          const LossItem it = items[e.lo + u * 64 + lane];
+          const LossItem it = e.items[e.lo + u * 64 + lane];
           e.at[u] = entry_at(mine, it.code);
           e.payload[u] = it.payload;
         }
@@ -207,7 +211,7 @@ __global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_logits(Loss
     for (int u = 0; u < 4; ++u)
       if (u * 64 + lane >= lo && u * 64 + lane < hi) use(e.at[u], e.payload[u]);
     for (int i = max(lo, 256) + lane; i < hi; i += 64) {
-      const LossItem it = items[e.lo + i];
+      const LossItem it = e.items[e.lo + i];
       use(entry_at(mine, it.code), it.payload);
     }
   };
@@ -221,7 +225,9 @@ __global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_logits(Loss
     }
   }
   auto epi_stats = [&](int t, f32x16 (&acc)[MB][NB], uint32_t lds) {
+    const auto& a = *args_again<Args>();
     const int left = a.words - (sp + t * P) * kLossM - wm * T::WTM - 4 * half;  // words from the lane's first on
+    const bool ragged = (sp + t * P + 1) * kLossM > a.words;
     const uint32_t mine = lds + wave * (32 * 36 * 4), words = mine + (uint32_t)(col * 36 + 4 * half) * 4u;
     Entries e;
     load_entries(t, mine, e);
@@ -251,10 +257,19 @@ __global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_logits(Loss
       st_m[n] = mnew;
       if (a.sumx) {
         float x0 = 0.f;
+        if (ragged) {
+          int l = left;
+          asm volatile("" : "+v"(l));  // the comparisons of every row anew, not kept in 128 scalar registers
 #pragma unroll
-        for (int m = 0; m < MB; ++m)
+          for (int m = 0; m < MB; ++m)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) x0 += m * 32 + 8 * (r >> 2) + (r & 3) < left ? acc[m][n][r] : 0.f;
+            for (int r = 0; r < 16; ++r) x0 += m * 32 + 8 * (r >> 2) + (r & 3) < l ? acc[m][n][r] : 0.f;
+        } else {
+#pragma unroll
+          for (int m = 0; m < MB; ++m)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x0 += acc[m][n][r];
+        }
         st_x[n] += x0;
       }
       if (e.n > 0) {
@@ -275,6 +290,7 @@ __global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_logits(Loss
   // dlogits, 32 words of every wave at a time: from the accumulators through the entries, the bias' sums and the
   // rounding to LDS, and from there to memory in rows (64 bytes in one piece, where the accumulators alone would give 8)
   auto epi_grad = [&](int t, f32x16 (&acc)[MB][NB], uint32_t lds) {
+    const auto& a = *args_again<Args>();
     const int v0 = (sp + t * P) * kLossM;
     const int left = a.words - v0 - wm * T::WTM - 4 * half;
     const bool ragged = v0 + kLossM > a.words && a.rest != 0.f;
@@ -307,9 +323,11 @@ __global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_logits(Loss
           x[n][r] = fmaf(g[n], exp2_fast(y), -gr);
         }
         if (ragged) {
+          int l = left;
+          asm volatile("" : "+v"(l));
 #pragma unroll
           for (int r = 0; r < 16; ++r)
-            if (m * 32 + 8 * (r >> 2) + (r & 3) >= left) x[n][r] = 0.f;
+            if (m * 32 + 8 * (r >> 2) + (r & 3) >= l) x[n][r] = 0.f;
         }
         int lo, hi;
         if (e.n > 0 && block_has(e, m * NB + n, lo, hi)) {

@@ -44,11 +44,22 @@ __device__ __forceinline__ const void* uniform_ptr(const void* x) {
                                        (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)p));
 }
 
-// One DMA instruction: lane i's 16 bytes from base + voff to LDS byte lds + 16 i.
+// One DMA instruction: lane i's 16 bytes from base + voff to LDS byte lds + PLUS + 16 i.  (The build checks that the
+// base was not written by a VALU instruction within the five wait states that the load needs; isa_check.py.)
+template <int PLUS>
 __device__ __forceinline__ void dma16_at(uint32_t voff, const void* sbase, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(uniform_ptr(sbase)),
-               "s"(__builtin_amdgcn_readfirstlane(lds))
-               : "m0");
+  asm volatile("s_add_i32 m0, %2, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff),
+               "s"(uniform_ptr(sbase)), "s"(__builtin_amdgcn_readfirstlane(lds)), "i"(PLUS)
+               : "m0", "scc");
+}
+
+// A kernel's arguments, read anew wherever this is called: what only a tile's start or end needs does not take scalar
+// registers in the main loop (which otherwise spills the DMA's addresses).
+template <class Args>
+__device__ __forceinline__ const __attribute__((address_space(4))) Args* args_again() {
+  auto p = (const __attribute__((address_space(4))) Args*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return p;
 }
 
 __device__ __forceinline__ void in_acc(f32x16& x) { asm volatile("" : "+a"(x)); }
@@ -63,6 +74,16 @@ struct MmGeom {
 // Planes of the six products of float32 operands, two bits a pass: (0,0) (0,1) (1,0) (1,1) (0,2) (2,0).
 constexpr uint32_t kPassA = 0u | 0u << 2 | 1u << 4 | 1u << 6 | 0u << 8 | 2u << 10;
 constexpr uint32_t kPassB = 0u | 1u << 2 | 0u << 4 | 1u << 6 | 2u << 8 | 0u << 10;
+
+template <int BASE>
+__device__ __forceinline__ void dma_i(const uint32_t* off, int i, const void* src, uint32_t lds) {
+  switch (i) {
+    case 0: dma16_at<BASE>(off[0], src, lds); break;
+    case 1: dma16_at<BASE + 1024>(off[1], src, lds); break;
+    case 2: dma16_at<BASE + 2048>(off[2], src, lds); break;
+    default: dma16_at<BASE + 3072>(off[3], src, lds); break;
+  }
+}
 
 // T: tile; AS, BS: the side is strided; AC: side A is clamped to its limits; PASSES: 1 or 6.
 // nt tiles of nk stages a pass.  tile(t, A, B): the sides of tile t; init(t, acc); epi(t, acc, lds): lds is a stage's
@@ -127,6 +148,9 @@ __device__ __forceinline__ void mm_run(uint32_t ring, int nt, int nk, TileFn til
       asrc += (size_t)((kPassA >> (2 * pass)) & 3u) * A.plane * 2;
       bsrc += (size_t)((kPassB >> (2 * pass)) & 3u) * B.plane * 2;
     }
+    asrc = static_cast<const char*>(uniform_ptr(asrc));
+    bsrc = static_cast<const char*>(uniform_ptr(bsrc));
+    asm volatile("s_nop 4");  // whatever VALU instruction wrote these registers last: five states before the DMA
   };
   auto tile_sources = [&]() {
     tile(t_issue, A, B);
@@ -136,17 +160,18 @@ __device__ __forceinline__ void mm_run(uint32_t ring, int nt, int nk, TileFn til
     offsets(SB{}, RB{}, CB{}, B, 0, bload);
     sources();
   };
+  // a wave's first DMA instruction of each side
+  const uint32_t wave_a = (GA::ALL >= 4 ? wave * GA::OPS : (wave & (GA::ALL - 1))) * 1024;
+  const uint32_t wave_b = (GB::ALL >= 4 ? wave * GB::OPS : (wave & (GB::ALL - 1))) * 1024;
   auto issue_a = [&](uint32_t buf, int i) {
     if (i == 0 && AC && !AS) {
       // the stage that reaches the end of k has offsets of its own
       if ((k_issue + 1) * kLossStage > A.klim) offsets(SA{}, RA{}, CA{}, A, k_issue * kLossStage, aload);
     }
-    const int q = GA::ALL >= 4 ? wave * GA::OPS + i : (wave & (GA::ALL - 1));
-    dma16_at(aload[i], asrc - kBack * 2, buf + q * 1024);
+    dma_i<0>(aload, i, asrc - kBack * 2, buf + wave_a);
   };
   auto issue_b = [&](uint32_t buf, int i) {
-    const int q = GB::ALL >= 4 ? wave * GB::OPS + i : (wave & (GB::ALL - 1));
-    dma16_at(bload[i], bsrc, buf + GA::BYTES + q * 1024);
+    dma_i<GA::BYTES>(bload, i, bsrc, buf + wave_b);
   };
   auto issue_done = [&]() {
     ++issued;
@@ -226,8 +251,10 @@ __device__ __forceinline__ void mm_run(uint32_t ring, int nt, int nk, TileFn til
     acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.a[m], f.b[n], acc[m][n], 0, 0, 0);
   };
   constexpr int NM = MB * NB;
-  constexpr int FPM = NF / NM >= 1 ? (NF + NM - 1) / NM : 1;  // fragments read after each of the first products
-  auto slot_of = [](int i, int n) { return NM >= 8 ? NM / 2 + i : (i < NM ? i : NM - 1); };  // product after which DMA i goes
+  // the product after which fragment u of the next half is read (in eighths of a product), and DMA i issued
+  auto frag_slot = [](int u, int eighths) { return u * eighths * NM / (8 * 16) < NM ? u * eighths * NM / (8 * 16) : NM - 1; };
+  auto slot_of = [](int i, int n) { return NM >= 8 ? NM / n * i + NM / n - 1 : (i < NM ? i : NM - 1); };
+  constexpr int SP1 = 12 * 8 / NF, SP0 = 16 * 8 / NF;
 
   Frag F0, F1;
   if (total > 0) {
@@ -255,7 +282,8 @@ __device__ __forceinline__ void mm_run(uint32_t ring, int nt, int nk, TileFn til
     for (int i = 0; i < NM; ++i) {
       mf(F0, i);
 #pragma unroll
-      for (int u = i * FPM; u < (i + 1) * FPM && u < NF; ++u) rd(cur, 1, u, F1);
+      for (int u = 0; u < NF; ++u)
+        if (frag_slot(u, SP1) == i) rd(cur, 1, u, F1);
       if (more) {
 #pragma unroll
         for (int o = 0; o < GA::OPS; ++o)
@@ -277,7 +305,8 @@ __device__ __forceinline__ void mm_run(uint32_t ring, int nt, int nk, TileFn til
       mf(F1, i);
       if constexpr (read_next) {
 #pragma unroll
-        for (int u = i * FPM; u < (i + 1) * FPM && u < NF; ++u) rd(nxt, 0, u, F0);
+        for (int u = 0; u < NF; ++u)
+          if (frag_slot(u, SP0) == i) rd(nxt, 0, u, F0);
       }
       if (more) {
 #pragma unroll
