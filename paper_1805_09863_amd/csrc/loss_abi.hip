@@ -40,7 +40,7 @@ struct Space {
 };
 
 struct Plan {
-  bool bf16, direct;
+  bool bf16, few, direct;  // few: the few rows' kernels
   int planes, z;
   int N, H, V, K;
   int BN, R, WN, WTM, WTN;  // row tile, how many, and the wave's part
@@ -64,6 +64,20 @@ Plan make_plan(int dtype, int N, int H, int V, int K, bool teacher, bool grad, b
   p.planes = p.bf16 ? 1 : 3;
   p.z = p.bf16 ? 2 : 4;
   p.N = N, p.H = H, p.V = V, p.K = K;
+  p.few = kb::few_fits(N, H);
+  if (p.few) {
+    Space s;
+    p.grid = kb::few_grid(p.bf16, V);
+    if (grad) {
+      p.dh_part = s.take((size_t)p.grid * H * kb::few_held(N) * 4);
+    } else {
+      p.stat = s.take((size_t)N * p.grid * sizeof(float2));
+      p.sumx = s.take((size_t)N * p.grid * 4);
+      p.xt = s.take((size_t)N * K * 4);
+    }
+    p.bytes = s.at;
+    return p;
+  }
   p.BN = N <= 32 ? 32 : N <= 64 ? 64 : N <= 128 ? 128 : 256;
   p.R = kb::loss_row_tiles(N, p.BN);
   p.WN = p.BN >= 128 ? 2 : 1;
@@ -285,12 +299,53 @@ kb::LossLogitsArgs logits_args(const Call& c, const Plan& p, const Work& w, cons
   return a;
 }
 
+kb::LossFewArgs few_args(const Call& c, const Plan& p) {
+  kb::LossFewArgs a{};
+  a.N = c.N, a.H = c.H, a.V = c.V, a.K = c.K;
+  a.h = c.h, a.W = c.W, a.b = c.b;
+  a.token = c.token, a.logit = c.logit;
+  a.inv_t = 1.f / c.temperature;
+  a.t2 = c.temperature * c.temperature;
+  a.target_part = 1.f - c.smoothing;
+  a.rest = c.smoothing / (float)c.V;
+  a.grid = p.grid;
+  return a;
+}
+
+kb_status few_forward(const Call& c, const Plan& p) {
+  char* ws = static_cast<char*>(c.ws);
+  kb::LossFewArgs a = few_args(c, p);
+  a.stat = reinterpret_cast<float2*>(ws + p.stat);
+  a.sumx = reinterpret_cast<float*>(ws + p.sumx);
+  a.xt = reinterpret_cast<float*>(ws + p.xt);
+  a.loss = c.loss;
+  a.lse_out = c.lse;
+  KB_LAUNCH("logits of a loss", kb::launch_loss_few(p.bf16, false, a, c.st));
+  KB_LAUNCH("losses", kb::launch_loss_few_finish(a, c.st));
+  return ok();
+}
+
+kb_status few_gradient(const Call& c, const Plan& p) {
+  kb::LossFewArgs a = few_args(c, p);
+  a.lse = c.lse_in;
+  a.grad = c.grad;
+  a.grad_scale = c.temperature;
+  a.dh_part = c.dh ? reinterpret_cast<float*>(static_cast<char*>(c.ws) + p.dh_part) : nullptr;
+  a.dh = c.dh;
+  a.dW = c.dW;
+  a.db = c.db;
+  KB_LAUNCH("gradients of a loss", kb::launch_loss_few(p.bf16, true, a, c.st));
+  if (c.dh) KB_LAUNCH("gradient of the states", kb::launch_loss_few_join(p.bf16, a, c.st));
+  return ok();
+}
+
 kb_status forward(const Call& c) {
   const Plan p = make_plan(c.dtype, c.N, c.H, c.V, c.K, c.logit != nullptr, false, aligned(c.W, 16));
   kb_status s = check_call(c, p);
   if (s != KB_OK) return s;
   if (!c.loss || !c.lse) return fail(KB_ERR_INVALID_ARG, "null loss or lse");
   if (!aligned(c.loss, 4) || !aligned(c.lse, 4)) return fail(KB_ERR_INVALID_ARG, "loss or lse not aligned to their type");
+  if (p.few) return few_forward(c, p);
   Work w;
   if ((s = prepare(c, p, w, false)) != KB_OK) return s;
   const bool smooth = c.smoothing > 0.f;
@@ -334,6 +389,7 @@ kb_status gradient(const Call& c) {
   if (!c.lse_in || !c.grad) return fail(KB_ERR_INVALID_ARG, "null lse or grad");
   if (!aligned(c.lse_in, 4) || !aligned(c.grad, 4))
     return fail(KB_ERR_INVALID_ARG, "lse or grad not aligned to their type");
+  if (p.few) return few_gradient(c, p);
   Work w;
   if ((s = prepare(c, p, w, true)) != KB_OK) return s;
   const size_t rows = (size_t)p.R * p.BN;

@@ -173,6 +173,43 @@ struct LossFinishArgs {
   float* lse;
 };
 
+// A few rows (loss_few.hip).
+constexpr int kFewRows = 8;
+constexpr int kFewGrid = 512;   // workgroups at most
+
+struct LossFewArgs {
+  int N, H, V, K;
+  const void* h;
+  const void* W;
+  const float* b;
+  const int32_t* token;   // N x K: targets (K = 1) or the teacher's words
+  const float* logit;     // the teacher's logits; null: targets
+  float inv_t, t2;        // 1 / T, T^2
+  float target_part;      // 1 - smoothing
+  float rest;             // smoothing / V
+  int grid;
+  // forward
+  float2* stat;           // row x grid: (max, sum)
+  float* sumx;            // row x grid
+  float* xt;              // row x K: the entries' logits
+  float* loss;
+  float* lse_out;
+  // gradient
+  const float* lse;
+  const float* grad;
+  float grad_scale;
+  float* dh_part;         // grid x H x rows held; null: not wanted
+  void* dh;
+  void* dW;
+  float* db;
+};
+int few_held(int N);                       // rows that a workgroup holds for N
+bool few_fits(int N, int H);               // the few rows' kernels take this size
+int few_grid(bool bf16, int V);
+hipError_t launch_loss_few(bool bf16, bool grad, const LossFewArgs& a, hipStream_t st);
+hipError_t launch_loss_few_finish(const LossFewArgs& a, hipStream_t st);
+hipError_t launch_loss_few_join(bool bf16, const LossFewArgs& a, hipStream_t st);
+
 hipError_t launch_loss_teacher(const LossTeacherArgs& a, hipStream_t st);
 hipError_t launch_loss_rows(const LossRows& a, hipStream_t st);
 bool loss_finds_rows(int N, int nb);  // launch_loss_pack can do without launch_loss_rows

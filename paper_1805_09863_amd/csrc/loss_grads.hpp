@@ -166,12 +166,12 @@ __global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_both(LossGr
     dw_tile<T, PASSES>(w, lds_addr(ring), rows, xcd_cell(cw, blockIdx.x - ch));
 }
 
-// The parts of a result added up in order and rounded once.  A workgroup takes one block of 32 x 32 of every wave of a
-// tile, in the order of the registers: four groups of 256 threads add up every fourth part each, then the four sums.
+// The parts of a result added up in order and rounded once.  A workgroup takes a quarter of the registers of one block of
+// 32 x 32 of every wave of a tile: four groups of 256 threads add up every fourth part each, then the four sums.
 // (dh of rows that do not count: zeros, by the last workgroups.)
 template <class T, class D>
 __global__ __launch_bounds__(1024) void loss_join(LossJoinArgs a, const int32_t* inv, int N, int zero_blocks) {
-  __shared__ float4 sums[4][4][256];
+  __shared__ float4 sums[4][256];
   const int tid = threadIdx.x & 255, grp = threadIdx.x >> 8, lane = tid & 63, half = lane >> 5, col = lane & 31;
   const int wave = tid >> 6, wm = wave % T::WM, wn = wave / T::WM;
   D* out = static_cast<D*>(a.out);
@@ -184,35 +184,30 @@ __global__ __launch_bounds__(1024) void loss_join(LossJoinArgs a, const int32_t*
   }
   const int rows = a.is_dh ? *a.count : a.rows;
   const int tiles = a.mt * a.ntn;  // dh: by rows, then states; dW: by words, then states
-  const int tile = blockIdx.x / (T::MB * T::NB), blk = blockIdx.x % (T::MB * T::NB);
+  const int q = blockIdx.x & 3, unit = blockIdx.x >> 2;
+  const int tile = unit / (T::MB * T::NB), blk = unit % (T::MB * T::NB);
   const int m = blk / T::NB, n = blk % T::NB;
   const int mt = a.is_dh ? tile % a.mt : tile / a.ntn, nt = a.is_dh ? tile / a.mt : tile % a.ntn;
   if (nt * T::BN >= rows) return;
-  float4 s[4];
-#pragma unroll
-  for (int q = 0; q < 4; ++q) s[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+  float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
   const size_t step = (size_t)tiles * (T::MB * T::NB) * 4 * 256;
-  const float4* p = reinterpret_cast<const float4*>(a.part) + ((size_t)tile * (T::MB * T::NB) + blk) * 4 * 256 + tid;
-#pragma unroll 4
+  const float4* p = reinterpret_cast<const float4*>(a.part) + ((size_t)unit * 4 + q) * 256 + tid;
+#pragma unroll 8
   for (int k = grp; k < a.splits; k += 4) {
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const float4 v = p[k * step + q * 256];
-      s[q].x += v.x, s[q].y += v.y, s[q].z += v.z, s[q].w += v.w;
-    }
+    const float4 v = p[k * step];
+    r.x += v.x, r.y += v.y, r.z += v.z, r.w += v.w;
   }
-#pragma unroll
-  for (int q = 0; q < 4; ++q) sums[grp][q][tid] = s[q];
-  __syncthreads();
-  // group q finishes the register's quarter q: words (states) 8 q + 4 half .. + 3 of the block
-  float4 r = sums[0][grp][tid];
-#pragma unroll
-  for (int k = 1; k < 4; ++k) {
-    const float4 v = sums[k][grp][tid];
+  if (a.splits > 1) {
+    sums[grp][tid] = r;
+    __syncthreads();
+  }
+  if (grp > 0) return;
+  for (int k = 1; k < min(4, a.splits); ++k) {
+    const float4 v = sums[k][tid];
     r.x += v.x, r.y += v.y, r.z += v.z, r.w += v.w;
   }
   const int row = nt * T::BN + wn * T::WTN + n * 32 + col;
-  const int c = mt * kLossM + wm * T::WTM + m * 32 + 8 * grp + 4 * half;
+  const int c = mt * kLossM + wm * T::WTM + m * 32 + 8 * q + 4 * half;
   if (row >= rows) return;
   D* to = out + (size_t)(a.is_dh ? a.map[row] : row) * a.ld + c;
   typedef D D4 __attribute__((ext_vector_type(4)));

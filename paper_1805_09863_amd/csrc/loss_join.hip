@@ -6,7 +6,7 @@ namespace kb {
 template <class T>
 void join(bool bf16, const LossJoinArgs& a, const int32_t* inv, int N, hipStream_t st) {
   const int zero = inv ? (N < 256 ? N : 256) : 0;
-  const dim3 gr(a.mt * a.ntn * T::MB * T::NB + zero), th(1024);
+  const dim3 gr(a.mt * a.ntn * T::MB * T::NB * 4 + zero), th(1024);
   if (bf16)
     loss_join<T, __bf16><<<gr, th, 0, st>>>(a, inv, N, zero);
   else

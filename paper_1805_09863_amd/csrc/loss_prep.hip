@@ -4,80 +4,28 @@
 
 #include "k3_scan.hpp"
 #include "loss_common.hpp"
+#include "loss_teacher.hpp"
 
 namespace kb {
 
 typedef __bf16 bf16x8v __attribute__((ext_vector_type(8)));
 
-// A teacher's row: the softmax over its entries' words of logit / T (an entry whose word is outside the vocabulary or
-// whose logit is -inf is none; entries of the same word are one, the first, with their probabilities' sum), and
-// sum q ln q.  One wave a row, up to two entries a lane.
+// Teachers' rows, a wave each.
 __global__ __launch_bounds__(256) void loss_teacher(LossTeacherArgs a) {
   const int lane = threadIdx.x & 63;
   const int row = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (row >= a.N) return;
-  int tok[2];
-  float y[2];
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const int j = lane + 64 * u;
-    tok[u] = -1;
-    y[u] = -INFINITY;
-    if (j < a.K) {
-      const size_t at = (size_t)row * a.K + j;
-      const int t = a.token[at];
-      const float x = a.logit[at] * a.inv_t;
-      if (t >= 0 && t < a.V && !(x == -INFINITY)) {
-        tok[u] = t;
-        y[u] = x;
-      }
-    }
-  }
-  const bool any = __builtin_amdgcn_ballot_w64(tok[0] >= 0 || tok[1] >= 0) != 0ull;
-  float top = fmaxf(y[0], y[1]);
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-  float e[2], merged[2], total = 0.f;
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    e[u] = tok[u] >= 0 ? expf(y[u] - top) : 0.f;
-    merged[u] = 0.f;
-    total += e[u];
-  }
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d, 64);
-  // entry i goes to the first entry of its word
-  bool first[2] = {tok[0] >= 0, tok[1] >= 0};
+  const TeacherRow r = teacher_row(a.token + (size_t)row * a.K, a.logit + (size_t)row * a.K, a.K, a.V, a.inv_t);
 #pragma unroll
   for (int u = 0; u < 2; ++u)
-    for (int i = 0; i < 64 && i + 64 * u < a.K; ++i) {
-      const int t = __shfl(tok[u], i, 64);
-      const float x = __shfl(e[u], i, 64);
-#pragma unroll
-      for (int w = 0; w < 2; ++w)
-        if (t >= 0 && t == tok[w]) {
-          merged[w] += x;
-          if (i + 64 * u < lane + 64 * w) first[w] = false;
-        }
+    if (lane + 64 * u < a.K) {
+      const size_t at = (size_t)row * a.K + lane + 64 * u;
+      a.out_token[at] = r.token[u];
+      a.part[at] = r.part[u];
     }
-  float known = 0.f;
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const int j = lane + 64 * u;
-    const float q = first[u] ? merged[u] / total : 0.f;
-    if (q > 0.f) known += q * (logf(merged[u]) - logf(total));
-    if (first[u] && !(q >= 0.f)) known = q;  // NaN stays NaN
-    if (j < a.K) {
-      const size_t at = (size_t)row * a.K + j;
-      a.out_token[at] = first[u] ? tok[u] : -1;
-      a.part[at] = q;
-    }
-  }
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) known += __shfl_xor(known, d, 64);
   if (lane == 0) {
-    a.known[row] = known;
-    a.flag[row] = any;
+    a.known[row] = r.known;
+    a.flag[row] = r.any;
   }
 }
 

@@ -125,7 +125,7 @@ def check_kd(kb, dtype, N, H, V, K, T=1.0, seed=1, pad=0.2, edit=None):
 
 
 # one tile and less, every row tile, several row and word tiles, ragged in every direction
-SHAPES = [(1, 32, 256), (1, 64, 1000), (5, 256, 2000), (33, 96, 1024), (64, 128, 512), (100, 160, 777), (128, 512, 1536),
+SHAPES = [(2, 300, 515), (8, 1024, 640), (4, 17, 130), (3, 2500, 300), (9, 64, 384), (1, 32, 256), (1, 64, 1000), (5, 256, 2000), (33, 96, 1024), (64, 128, 512), (100, 160, 777), (128, 512, 1536),
           (200, 64, 300), (257, 320, 2304), (600, 128, 4000)]
 
 
