@@ -97,7 +97,7 @@ Plan make_plan(int dtype, int N, int H, int V, int K, bool teacher, bool grad, b
   // (8,192 x 1,024 x 90,000, a training pass: 5.87 ms; at 64 MB 6.37, 256 MB 6.12, 1 GB 6.29).
   // (W at an odd address where its shape needs no laying out: small pieces, so that the workspace need not grow.)
   const size_t most = (size_t)128 << 20;
-  const size_t w_tile = (size_t)p.Hk * kb::kLossM * 2 * p.planes, g_tile = (size_t)p.R * p.BN * kb::kLossM * 2 * p.planes;
+  const size_t w_tile = (size_t)p.Hk * kb::kLossM * 2 * p.planes, g_tile = (size_t)p.R * p.BN * kb::kLossM * 2 * kb::loss_g_planes(p.bf16, p.BN);
   size_t tiles = p.vt;
   if (!p.direct) tiles = std::min(tiles, std::max<size_t>(1, (shape ? most / 16 : most) / w_tile));
   if (grad) tiles = std::min(tiles, std::max<size_t>(1, most / g_tile));

@@ -31,6 +31,9 @@ __host__ __device__ inline int loss_wtm(int BN) { return BN >= 128 ? 128 : 64; }
 __host__ __device__ inline int loss_wtn(int BN) { return BN >= 128 ? BN / 2 : BN; }
 __host__ __device__ inline int loss_blocks(int BN) { return loss_wtm(BN) / 32 * (loss_wtn(BN) / 32); }
 
+// bf16 pieces of the dlogits.
+inline int loss_g_planes(bool bf16, int BN) { return !bf16 ? 3 : BN <= 128 ? 2 : 1; }
+
 // Rows that count lie packed: `map` has the original row of each packed one, `inv` the packed row of each
 // original one or -1, *count how many there are.
 struct LossRows {

@@ -29,6 +29,8 @@ __device__ __forceinline__ int xcd_cell(int cells, int b) {
   return x * (cells >> 3) + min(x, cells & 7) + j;
 }
 
+// PASSES: 1 (bf16 operands), 2 (the dlogits in two bf16 pieces) or 6 (float32).
+
 // Tile c of the `cells` of dh.
 template <class T, int PASSES>
 __device__ __forceinline__ void dh_tile(const LossGradArgs& a, uint32_t ring, int R, int c) {
@@ -62,7 +64,7 @@ __device__ __forceinline__ void dh_tile(const LossGradArgs& a, uint32_t ring, in
       part_of<T>(a.part, part, i, acc[i / T::NB][i % T::NB], false);
     }
   };
-  mm_run<T, false, false, true, PASSES>(ring, 1, s1 - s0, tile, init, epi);
+  mm_run<T, false, false, true, std::conditional_t<PASSES == 1, MmOne, std::conditional_t<PASSES == 2, MmTwoB, MmSix>>>(ring, 1, s1 - s0, tile, init, epi);
 }
 
 // 8 bf16 values to out, `left` of which exist.
@@ -109,7 +111,7 @@ __device__ __forceinline__ void dw_tile(const LossGradArgs& a, uint32_t ring, in
       }
       return;
     }
-    if constexpr (PASSES == 1) {
+    if constexpr (PASSES <= 2) {
       store_bf16<T>(acc, 0, lds, [&](int row, int word, const bf16x8& v) {
         if (n0 + row < a.H && m0 + word < a.words)
           write8(static_cast<uint16_t*>(a.out) + (size_t)(n0 + row) * a.V + m0 + word, v, a.words - m0 - word);
@@ -138,26 +140,26 @@ __device__ __forceinline__ void dw_tile(const LossGradArgs& a, uint32_t ring, in
         }
     }
   };
-  mm_run<T, true, true, false, PASSES>(ring, 1, s1 - s0, tile, init, epi);
+  mm_run<T, true, true, false, std::conditional_t<PASSES == 1, MmOne, std::conditional_t<PASSES == 2, MmTwoA, MmSix>>>(ring, 1, s1 - s0, tile, init, epi);
 }
 
 template <class T, int PASSES>
-__global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_dh(LossGradArgs a) {
-  __shared__ __attribute__((aligned(1024))) uint8_t ring[4 * LossOcc<T, PASSES>::STAGE];
+__global__ __launch_bounds__(256, (LossOcc<T>::N)) void loss_dh(LossGradArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t ring[4 * LossOcc<T>::STAGE];
   const int R = loss_row_tiles(const_int(a.count), T::BN), cells = a.splits * R * a.mt;
   if ((int)blockIdx.x < cells) dh_tile<T, PASSES>(a, lds_addr(ring), R, xcd_cell(cells, blockIdx.x));
 }
 
 template <class T, int PASSES>
-__global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_dw(LossGradArgs a) {
-  __shared__ __attribute__((aligned(1024))) uint8_t ring[4 * LossOcc<T, PASSES>::STAGE];
+__global__ __launch_bounds__(256, (LossOcc<T>::N)) void loss_dw(LossGradArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t ring[4 * LossOcc<T>::STAGE];
   dw_tile<T, PASSES>(a, lds_addr(ring), const_int(a.count), xcd_cell(gridDim.x, blockIdx.x));
 }
 
 // Both in one launch, the longer tiles of dh first: neither has to fill the card by itself.
 template <class T, int PASSES>
-__global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_both(LossGradArgs h, LossGradArgs w) {
-  __shared__ __attribute__((aligned(1024))) uint8_t ring[4 * LossOcc<T, PASSES>::STAGE];
+__global__ __launch_bounds__(256, (LossOcc<T>::N)) void loss_both(LossGradArgs h, LossGradArgs w) {
+  __shared__ __attribute__((aligned(1024))) uint8_t ring[4 * LossOcc<T>::STAGE];
   const int rows = const_int(h.count), R = loss_row_tiles(rows, T::BN);
   const int ch = h.splits * R * h.mt, cw = w.splits * w.mt * w.ntn;
   if ((int)blockIdx.x < ch)

@@ -7,9 +7,9 @@ hipError_t launch_loss_dh_bf16(int BN, const LossGradArgs& a, hipStream_t st) {
   const dim3 gr(a.splits * loss_row_tiles(a.N, BN) * a.mt), th(256);
   switch (BN) {
     case 256: loss_dh<LossT256, 1><<<gr, th, 0, st>>>(a); break;
-    case 128: loss_dh<LossT128, 1><<<gr, th, 0, st>>>(a); break;
-    case 64: loss_dh<LossT64, 1><<<gr, th, 0, st>>>(a); break;
-    default: loss_dh<LossT32, 1><<<gr, th, 0, st>>>(a); break;
+    case 128: loss_dh<LossT128, 2><<<gr, th, 0, st>>>(a); break;
+    case 64: loss_dh<LossT64, 2><<<gr, th, 0, st>>>(a); break;
+    default: loss_dh<LossT32, 2><<<gr, th, 0, st>>>(a); break;
   }
   return hipGetLastError();
 }
@@ -19,7 +19,7 @@ hipError_t launch_loss_dw_bf16(int BNh, const LossGradArgs& a, hipStream_t st) {
   switch (BNh) {
     case 256: loss_dw<LossT256, 1><<<gr, th, 0, st>>>(a); break;
     case 128: loss_dw<LossT128, 1><<<gr, th, 0, st>>>(a); break;
-    default: loss_dw<LossT64, 1><<<gr, th, 0, st>>>(a); break;
+    default: loss_dw<LossT64, 2><<<gr, th, 0, st>>>(a); break;
   }
   return hipGetLastError();
 }

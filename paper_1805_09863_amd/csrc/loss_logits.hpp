@@ -3,9 +3,11 @@
 // forward: Algorithm 4's running (max, sum of exp) of every row over the workgroup's words, the sum of the logits
 // where labels are smoothed, and the logits of the rows' entries (their targets, or the teacher's words).
 //
-// gradient: dx = g (p - rest - part), p = exp(x / T - lse) from the log-sum-exp that the forward pass left; rounded to
-// bf16 once, as the operand of the two products that follow (float32: three bf16 pieces, to 2^-24), and before that
-// summed over the rows for the bias.
+// gradient: dx = g (p - rest - part), p = exp(x / T - lse) from the log-sum-exp that the forward pass left; summed over the
+// rows in float32 for the bias, and then rounded to bf16 as the operand of the two products that follow, a rounding as
+// large as the one of their bf16 results.  Of at most 128 rows, whose gradients a few dlogits dominate (and whose
+// time the reading of W and the writing of dW do), it is kept in two bf16 pieces, to 2^-17; of float32 operands in
+// three, to 2^-24.
 //
 // Words are the M side: a lane has 64 (small tiles: 32) words of each of its rows, so statistics need no exchange
 // until the end.  The accumulators start at the bias; words that only fill the last tile up start at -inf.
@@ -94,22 +96,24 @@ __device__ __forceinline__ void store_bf16(f32x16 (&acc)[T::MB][T::NB], int plan
 // Entries of a wave's part of a tile that are taken one by one; more go through LDS.
 constexpr int kFewEntries = 4;
 
-template <class T, int PASSES>
+template <class T>
 struct LossOcc {  // workgroups that fit on a CU
   static constexpr int STAGE = MmGeom<T::BM>::BYTES + MmGeom<T::BN>::BYTES;
   static constexpr int N = 4 * STAGE <= 76 * 1024 ? 2 : 1;
 };
 
-template <class T, int PASSES, bool GRAD>
-__global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_logits(LossLogitsArgs a) {
+// PASSES: 1 (bf16 operands) or 6 (float32); PLANES: bf16 pieces of the dlogits, 0 for the forward pass.
+template <class T, int PASSES, int PLANES>
+__global__ __launch_bounds__(256, (LossOcc<T>::N)) void loss_logits(LossLogitsArgs a) {
   constexpr int MB = T::MB, NB = T::NB, BN = T::BN;
-  constexpr int PLANES = PASSES > 1 ? 3 : 1, NBLK = MB * NB;
-  __shared__ __attribute__((aligned(1024))) uint8_t ring[4 * LossOcc<T, PASSES>::STAGE];
+  constexpr bool GRAD = PLANES > 0;
+  constexpr int NBLK = MB * NB;
+  __shared__ __attribute__((aligned(1024))) uint8_t ring[4 * LossOcc<T>::STAGE];
   __shared__ __attribute__((aligned(16))) float bias[4][kLossM];
   __shared__ __attribute__((aligned(16))) float2 rowp[GRAD ? BN : 1];
   __shared__ __attribute__((aligned(16))) float red[GRAD ? 1 : BN][T::WM][3];
   // the gradient's entries have LDS of their own, but for the tile of which two workgroups then fit no more
-  constexpr bool APART = GRAD && LossOcc<T, PASSES>::N == 1;
+  constexpr bool APART = GRAD && LossOcc<T>::N == 1;
   __shared__ __attribute__((aligned(16))) uint8_t apart[APART ? 4 * 32 * 36 * 4 : 16];
 
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
@@ -295,7 +299,7 @@ __global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_logits(Loss
     const int left = a.words - v0 - wm * T::WTM - 4 * half;
     const bool ragged = v0 + kLossM > a.words && a.rest != 0.f;
     constexpr int CH = T::WM * 4;  // 16-byte chunks of a row of the tile's 32 words a wave
-    static_assert(BN * CH * 16 <= LossOcc<T, PASSES>::STAGE && 4 * 32 * 36 * 4 <= LossOcc<T, PASSES>::STAGE, "fit in a stage");
+    static_assert(BN * CH * 16 <= LossOcc<T>::STAGE && 4 * 32 * 36 * 4 <= LossOcc<T>::STAGE, "fit in a stage");
     const uint32_t mine = (APART ? lds_addr(apart) : lds) + wave * (32 * 36 * 4);
     const uint32_t words = mine + (uint32_t)(col * 36 + 4 * half) * 4u;
     Entries e;
@@ -400,7 +404,7 @@ __global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_logits(Loss
     else
       epi_stats(t, acc, lds);
   };
-  mm_run<T, true, false, PASSES == 1, PASSES>(lds_addr(ring), nt, a.Hk / kLossStage, tile, init, epi);
+  mm_run<T, true, false, PASSES == 1, std::conditional_t<PASSES == 1, MmOne, MmSix>>(lds_addr(ring), nt, a.Hk / kLossStage, tile, init, epi);
 
   if constexpr (!GRAD) {
     // the row's holders: two lane halves, and the waves along the words
@@ -439,19 +443,20 @@ __global__ __launch_bounds__(256, (LossOcc<T, PASSES>::N)) void loss_logits(Loss
 template <int PASSES>
 hipError_t launch_loss_logits_t(bool grad, int BN, const LossLogitsArgs& a, int blocks, hipStream_t st) {
   const dim3 gr(blocks), th(256);
+  constexpr int BIG = PASSES > 1 ? 3 : 1, SMALL = PASSES > 1 ? 3 : 2;  // loss_g_planes
   if (grad) {
     switch (BN) {
-      case 256: loss_logits<LossT256, PASSES, true><<<gr, th, 0, st>>>(a); break;
-      case 128: loss_logits<LossT128, PASSES, true><<<gr, th, 0, st>>>(a); break;
-      case 64: loss_logits<LossT64, PASSES, true><<<gr, th, 0, st>>>(a); break;
-      default: loss_logits<LossT32, PASSES, true><<<gr, th, 0, st>>>(a); break;
+      case 256: loss_logits<LossT256, PASSES, BIG><<<gr, th, 0, st>>>(a); break;
+      case 128: loss_logits<LossT128, PASSES, SMALL><<<gr, th, 0, st>>>(a); break;
+      case 64: loss_logits<LossT64, PASSES, SMALL><<<gr, th, 0, st>>>(a); break;
+      default: loss_logits<LossT32, PASSES, SMALL><<<gr, th, 0, st>>>(a); break;
     }
   } else {
     switch (BN) {
-      case 256: loss_logits<LossT256, PASSES, false><<<gr, th, 0, st>>>(a); break;
-      case 128: loss_logits<LossT128, PASSES, false><<<gr, th, 0, st>>>(a); break;
-      case 64: loss_logits<LossT64, PASSES, false><<<gr, th, 0, st>>>(a); break;
-      default: loss_logits<LossT32, PASSES, false><<<gr, th, 0, st>>>(a); break;
+      case 256: loss_logits<LossT256, PASSES, 0><<<gr, th, 0, st>>>(a); break;
+      case 128: loss_logits<LossT128, PASSES, 0><<<gr, th, 0, st>>>(a); break;
+      case 64: loss_logits<LossT64, PASSES, 0><<<gr, th, 0, st>>>(a); break;
+      default: loss_logits<LossT32, PASSES, 0><<<gr, th, 0, st>>>(a); break;
     }
   }
   return hipGetLastError();

@@ -71,9 +71,18 @@ struct MmGeom {
   static constexpr int OPS = ALL >= 4 ? ALL / 4 : 1;   // of each wave (fewer than four: some do the same one)
 };
 
-// Planes of the six products of float32 operands, two bits a pass: (0,0) (0,1) (1,0) (1,1) (0,2) (2,0).
-constexpr uint32_t kPassA = 0u | 0u << 2 | 1u << 4 | 1u << 6 | 0u << 8 | 2u << 10;
-constexpr uint32_t kPassB = 0u | 1u << 2 | 0u << 4 | 1u << 6 | 2u << 8 | 0u << 10;
+// Which pieces of A and B a pass multiplies, two bits a pass.
+template <int PASSES_, uint32_t A_, uint32_t B_>
+struct MmPasses {
+  static constexpr int N = PASSES_;
+  static constexpr uint32_t A = A_, B = B_;
+};
+using MmOne = MmPasses<1, 0, 0>;
+using MmTwoA = MmPasses<2, 0u | 1u << 2, 0>;  // A in two pieces
+using MmTwoB = MmPasses<2, 0, 0u | 1u << 2>;
+// float32: (0,0) (0,1) (1,0) (1,1) (0,2) (2,0)
+using MmSix = MmPasses<6, 0u | 0u << 2 | 1u << 4 | 1u << 6 | 0u << 8 | 2u << 10,
+                       0u | 1u << 2 | 0u << 4 | 1u << 6 | 2u << 8 | 0u << 10>;
 
 template <int BASE>
 __device__ __forceinline__ void dma_i(const uint32_t* off, int i, const void* src, uint32_t lds) {
@@ -85,12 +94,12 @@ __device__ __forceinline__ void dma_i(const uint32_t* off, int i, const void* sr
   }
 }
 
-// T: tile; AS, BS: the side is strided; AC: side A is clamped to its limits; PASSES: 1 or 6.
+// T: tile; AS, BS: the side is strided; AC: side A is clamped to its limits; PS: MmPasses.
 // nt tiles of nk stages a pass.  tile(t, A, B): the sides of tile t; init(t, acc); epi(t, acc, lds): lds is a stage's
 // buffer that is free until epi returns.
-template <class T, bool AS, bool BS, bool AC, int PASSES, class TileFn, class InitFn, class EpiFn>
+template <class T, bool AS, bool BS, bool AC, class PS, class TileFn, class InitFn, class EpiFn>
 __device__ __forceinline__ void mm_run(uint32_t ring, int nt, int nk, TileFn tile, InitFn init, EpiFn epi) {
-  constexpr int MB = T::MB, NB = T::NB, BM = T::BM, BN = T::BN;
+  constexpr int MB = T::MB, NB = T::NB, BM = T::BM, BN = T::BN, PASSES = PS::N;
   using GA = MmGeom<BM>;
   using GB = MmGeom<BN>;
   constexpr int STAGE = GA::BYTES + GB::BYTES;
@@ -145,8 +154,8 @@ __device__ __forceinline__ void mm_run(uint32_t ring, int nt, int nk, TileFn til
     asrc = reinterpret_cast<const char*>(A.p);
     bsrc = reinterpret_cast<const char*>(B.p);
     if constexpr (PASSES > 1) {
-      asrc += (size_t)((kPassA >> (2 * pass)) & 3u) * A.plane * 2;
-      bsrc += (size_t)((kPassB >> (2 * pass)) & 3u) * B.plane * 2;
+      asrc += (size_t)((PS::A >> (2 * pass)) & 3u) * A.plane * 2;
+      bsrc += (size_t)((PS::B >> (2 * pass)) & 3u) * B.plane * 2;
     }
     asrc = static_cast<const char*>(uniform_ptr(asrc));
     bsrc = static_cast<const char*>(uniform_ptr(bsrc));
@@ -328,6 +337,7 @@ __device__ __forceinline__ void mm_run(uint32_t ring, int nt, int nk, TileFn til
       body(std::false_type{});
     }
     epi(t, acc, ring + (uint32_t)((g + 3) & 3) * STAGE);
+    if (t + 1 < nt) lds_barrier();  // the next stage's DMA goes into the buffer that the epilogue had
   }
 }
 

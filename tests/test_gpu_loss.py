@@ -136,6 +136,13 @@ def test_cross_entropy(kb, dtype, N, H, V):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,H,V", [(2900, 32, 14000), (1300, 64, 20001), (100, 32, 70000), (20, 64, 140001), (60, 32, 140000)])
+def test_tiles_in_turn(kb, dtype, N, H, V):
+    # a workgroup takes several word tiles, the next one's stages under way while a tile's logits are worked on
+    check_ce(kb, dtype, N, H, V, pad=0.0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("N,H,V", [(7, 1, 1), (3, 5, 2), (9, 31, 255), (40, 33, 257), (70, 200, 1001), (300, 130, 8), (1, 7, 3000)])
 def test_odd_sizes(kb, dtype, N, H, V):
     check_ce(kb, dtype, N, H, V)
