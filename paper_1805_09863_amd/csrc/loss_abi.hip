@@ -1,5 +1,6 @@
 // Host side of the output layer's losses: argument validation, the plan of a
 // call and the entry points declared in include/kbest_loss.h.
+#include <limits.h>
 #include <math.h>
 
 #include <algorithm>
@@ -9,12 +10,12 @@
 #include "loss_common.hpp"
 
 namespace kb {
-hipError_t launch_loss_logits_bf16(bool grad, int BN, const LossLogitsArgs& a, int blocks, hipStream_t st);
-hipError_t launch_loss_logits_f32(bool grad, int BN, const LossLogitsArgs& a, int blocks, hipStream_t st);
-hipError_t launch_loss_dh_bf16(int BN, const LossGradArgs& a, hipStream_t st);
-hipError_t launch_loss_dh_f32(int BN, const LossGradArgs& a, hipStream_t st);
-hipError_t launch_loss_dw_bf16(int BNh, const LossGradArgs& a, hipStream_t st);
-hipError_t launch_loss_dw_f32(int BNh, const LossGradArgs& a, hipStream_t st);
+hipError_t launch_loss_logits_bf16(int planes, int BN, const LossLogitsArgs& a, int blocks, hipStream_t st);
+hipError_t launch_loss_logits_f32(int planes, int BN, const LossLogitsArgs& a, int blocks, hipStream_t st);
+hipError_t launch_loss_dh_bf16(int planes, int BN, const LossGradArgs& a, hipStream_t st);
+hipError_t launch_loss_dh_f32(int planes, int BN, const LossGradArgs& a, hipStream_t st);
+hipError_t launch_loss_dw_bf16(int planes, int BNh, const LossGradArgs& a, hipStream_t st);
+hipError_t launch_loss_dw_f32(int planes, int BNh, const LossGradArgs& a, hipStream_t st);
 hipError_t launch_loss_both_bf16(const LossGradArgs& h, const LossGradArgs& w, hipStream_t st);
 hipError_t launch_loss_both_f32(const LossGradArgs& h, const LossGradArgs& w, hipStream_t st);
 }  // namespace kb
@@ -41,7 +42,7 @@ struct Space {
 
 struct Plan {
   bool bf16, few, direct;  // few: the few rows' kernels
-  int planes, z;
+  int planes, g_planes, z;  // bf16 pieces of the operands and of the dlogits, bytes of a value
   int N, H, V, K;
   int BN, R, WN, WTM, WTN;  // row tile, how many, and the wave's part
   int Hp, Hk, BNh;
@@ -56,12 +57,32 @@ struct Plan {
   bool both() const { return BN == 256 && BNh == 256; }  // dh and dW in one launch
 };
 
+// The row tile with the least time for the logits: rounds of the card's workgroups times a tile's time, which is that of
+// its stages (96 of float32, 512 states: 73 us for 256 rows, 50 for 128, 38 for 64, 32 for 32; two workgroups of the
+// last on a CU 44), so small problems take small tiles (a training pass of 163 x 512 x 4,384 in float32: 124 us in tiles
+// of 32 rows, 251 in tiles of 256; 378 x 512 x 72,256: 1,005 in tiles of 128, 1,307 and 1,221 in tiles of 256 and 64;
+// bf16 6,852 x 512 x 2,000: 156 in tiles of 256, 179 in tiles of 128).
+int row_tile(int N, int vt) {
+  int best = 32;
+  long long least = LLONG_MAX;
+  for (int BN : {32, 64, 128, 256}) {
+    const long long cells = (long long)kb::loss_row_tiles(N, BN) * vt;
+    const int slots = BN == 32 ? 512 : 256;
+    const int time = BN == 256 ? 73 : BN == 128 ? 50 : BN == 64 ? 38 : cells <= 256 ? 32 : 44;
+    const long long all = (cells + slots - 1) / slots * time;
+    if (all < least) best = BN, least = all;
+    if (BN >= N) break;
+  }
+  return best;
+}
+
 // The plan of a call. `direct`: W is read where it lies; else its pieces are laid out first (float32 in bf16 pieces, odd
 // sizes and addresses with zeros filled up).
 Plan make_plan(int dtype, int N, int H, int V, int K, bool teacher, bool grad, bool w_aligned) {
   Plan p{};
   p.bf16 = dtype == KB_BF16;
   p.planes = p.bf16 ? 1 : 3;
+  p.g_planes = !p.bf16 ? 3 : N <= 128 ? 2 : 1;
   p.z = p.bf16 ? 2 : 4;
   p.N = N, p.H = H, p.V = V, p.K = K;
   p.few = kb::few_fits(N, H);
@@ -78,7 +99,8 @@ Plan make_plan(int dtype, int N, int H, int V, int K, bool teacher, bool grad, b
     p.bytes = s.at;
     return p;
   }
-  p.BN = N <= 32 ? 32 : N <= 64 ? 64 : N <= 128 ? 128 : 256;
+  p.vt = (V + kb::kLossM - 1) / kb::kLossM;
+  p.BN = row_tile(N, p.vt);
   p.R = kb::loss_row_tiles(N, p.BN);
   p.WN = p.BN >= 128 ? 2 : 1;
   p.WTM = kb::loss_wtm(p.BN);
@@ -86,7 +108,6 @@ Plan make_plan(int dtype, int N, int H, int V, int K, bool teacher, bool grad, b
   p.BNh = p.BN <= 128 ? 64 : H > 128 ? 256 : 128;
   p.Hp = up(H, H > 128 ? 256 : 128);
   p.Hk = up(H, kb::kLossStage);
-  p.vt = (V + kb::kLossM - 1) / kb::kLossM;
   p.words0 = p.vt * (kb::kLossM / p.WTM);
   p.nb = p.BN / p.WTN * p.words0 * kb::loss_blocks(p.BN);
   p.grid = std::max(p.BN == 32 ? 512 : 256, p.R);
@@ -97,7 +118,7 @@ Plan make_plan(int dtype, int N, int H, int V, int K, bool teacher, bool grad, b
   // (8,192 x 1,024 x 90,000, a training pass: 5.87 ms; at 64 MB 6.37, 256 MB 6.12, 1 GB 6.29).
   // (W at an odd address where its shape needs no laying out: small pieces, so that the workspace need not grow.)
   const size_t most = (size_t)128 << 20;
-  const size_t w_tile = (size_t)p.Hk * kb::kLossM * 2 * p.planes, g_tile = (size_t)p.R * p.BN * kb::kLossM * 2 * kb::loss_g_planes(p.bf16, p.BN);
+  const size_t w_tile = (size_t)p.Hk * kb::kLossM * 2 * p.planes, g_tile = (size_t)p.R * p.BN * kb::kLossM * 2 * p.g_planes;
   size_t tiles = p.vt;
   if (!p.direct) tiles = std::min(tiles, std::max<size_t>(1, (shape ? most / 16 : most) / w_tile));
   if (grad) tiles = std::min(tiles, std::max<size_t>(1, most / g_tile));
@@ -357,8 +378,8 @@ kb_status forward(const Call& c) {
     a.stat = w.at<float2>(p.stat) + i * p.stat_piece;
     a.sumx = smooth ? w.at<float>(p.sumx) + i * p.stat_piece : nullptr;
     a.xt = w.at<float>(p.xt);
-    KB_LAUNCH("logits of a loss", p.bf16 ? kb::launch_loss_logits_bf16(false, p.BN, a, p.grid, c.st)
-                                         : kb::launch_loss_logits_f32(false, p.BN, a, p.grid, c.st));
+    KB_LAUNCH("logits of a loss", p.bf16 ? kb::launch_loss_logits_bf16(0, p.BN, a, p.grid, c.st)
+                                         : kb::launch_loss_logits_f32(0, p.BN, a, p.grid, c.st));
   }
   kb::LossFinishArgs f{};
   f.rows = w.rows;
@@ -407,8 +428,8 @@ kb_status gradient(const Call& c) {
     a.dbp = c.db ? w.at<float>(p.dbp) : nullptr;
     a.db_ld = Vp;
     a.db0 = t0 * kb::kLossM;
-    KB_LAUNCH("logits of a loss", p.bf16 ? kb::launch_loss_logits_bf16(true, p.BN, a, p.grid, c.st)
-                                         : kb::launch_loss_logits_f32(true, p.BN, a, p.grid, c.st));
+    KB_LAUNCH("logits of a loss", p.bf16 ? kb::launch_loss_logits_bf16(p.g_planes, p.BN, a, p.grid, c.st)
+                                         : kb::launch_loss_logits_f32(p.g_planes, p.BN, a, p.grid, c.st));
     kb::LossGradArgs g{};
     g.W = pw.p;
     g.w_plane = pw.plane;
@@ -444,10 +465,10 @@ kb_status gradient(const Call& c) {
     } else {
       if (c.dh)
         KB_LAUNCH("gradient of the states",
-                  p.bf16 ? kb::launch_loss_dh_bf16(p.BN, gh, c.st) : kb::launch_loss_dh_f32(p.BN, gh, c.st));
+                  p.bf16 ? kb::launch_loss_dh_bf16(p.g_planes, p.BN, gh, c.st) : kb::launch_loss_dh_f32(p.g_planes, p.BN, gh, c.st));
       if (c.dW)
         KB_LAUNCH("gradient of the weights",
-                  p.bf16 ? kb::launch_loss_dw_bf16(p.BNh, gw, c.st) : kb::launch_loss_dw_f32(p.BNh, gw, c.st));
+                  p.bf16 ? kb::launch_loss_dw_bf16(p.g_planes, p.BNh, gw, c.st) : kb::launch_loss_dw_f32(p.g_planes, p.BNh, gw, c.st));
     }
     if (c.dW && gw.part) {
       const kb::LossJoinArgs j{gw.part, p.dw_splits, tiles, p.dw_ntn, p.BNh, c.H, std::min(gw.words, Vc), 0, nullptr,

@@ -31,9 +31,6 @@ __host__ __device__ inline int loss_wtm(int BN) { return BN >= 128 ? 128 : 64; }
 __host__ __device__ inline int loss_wtn(int BN) { return BN >= 128 ? BN / 2 : BN; }
 __host__ __device__ inline int loss_blocks(int BN) { return loss_wtm(BN) / 32 * (loss_wtn(BN) / 32); }
 
-// bf16 pieces of the dlogits.
-inline int loss_g_planes(bool bf16, int BN) { return !bf16 ? 3 : BN <= 128 ? 2 : 1; }
-
 // Rows that count lie packed: `map` has the original row of each packed one, `inv` the packed row of each
 // original one or -1, *count how many there are.
 struct LossRows {
@@ -222,6 +219,7 @@ hipError_t launch_loss_finish(const LossFinishArgs& a, hipStream_t st);
 // inv, N: rows of dh that do not count, filled with zeros (null: none)
 hipError_t launch_loss_join(bool bf16, const LossJoinArgs& a, const int32_t* inv, int N, hipStream_t st);
 hipError_t launch_loss_zero(void* p, size_t bytes, hipStream_t st);
+// wave_rows: rows of dbp for each row tile
 hipError_t launch_loss_db(const float* dbp, int wave_rows, int BN, int db_ld, const int32_t* count, int V, float* db,
                           hipStream_t st);
 

@@ -223,4 +223,35 @@ __global__ __launch_bounds__(1024) void loss_join(LossJoinArgs a, const int32_t*
   }
 }
 
+template <int PASSES>
+hipError_t launch_loss_dh_p(int BN, const LossGradArgs& a, hipStream_t st) {
+  const dim3 gr(a.splits * loss_row_tiles(a.N, BN) * a.mt), th(256);
+  switch (BN) {
+    case 256: loss_dh<LossT256, PASSES><<<gr, th, 0, st>>>(a); break;
+    case 128: loss_dh<LossT128, PASSES><<<gr, th, 0, st>>>(a); break;
+    case 64: loss_dh<LossT64, PASSES><<<gr, th, 0, st>>>(a); break;
+    default: loss_dh<LossT32, PASSES><<<gr, th, 0, st>>>(a); break;
+  }
+  return hipGetLastError();
+}
+
+template <int PASSES>
+hipError_t launch_loss_dw_p(int BNh, const LossGradArgs& a, hipStream_t st) {
+  const dim3 gr(a.splits * a.mt * a.ntn), th(256);
+  switch (BNh) {
+    case 256: loss_dw<LossT256, PASSES><<<gr, th, 0, st>>>(a); break;
+    case 128: loss_dw<LossT128, PASSES><<<gr, th, 0, st>>>(a); break;
+    default: loss_dw<LossT64, PASSES><<<gr, th, 0, st>>>(a); break;
+  }
+  return hipGetLastError();
+}
+
+// row tiles and state tiles of 256
+template <int PASSES>
+hipError_t launch_loss_both_p(const LossGradArgs& h, const LossGradArgs& w, hipStream_t st) {
+  const dim3 gr(h.splits * loss_row_tiles(h.N, 256) * h.mt + w.splits * w.mt * w.ntn), th(256);
+  loss_both<LossT256, PASSES><<<gr, th, 0, st>>>(h, w);
+  return hipGetLastError();
+}
+
 }  // namespace kb

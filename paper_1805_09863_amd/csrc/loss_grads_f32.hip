@@ -2,33 +2,9 @@
 #include "loss_grads.hpp"
 
 namespace kb {
-
-hipError_t launch_loss_dh_f32(int BN, const LossGradArgs& a, hipStream_t st) {
-  const dim3 gr(a.splits * loss_row_tiles(a.N, BN) * a.mt), th(256);
-  switch (BN) {
-    case 256: loss_dh<LossT256, 6><<<gr, th, 0, st>>>(a); break;
-    case 128: loss_dh<LossT128, 6><<<gr, th, 0, st>>>(a); break;
-    case 64: loss_dh<LossT64, 6><<<gr, th, 0, st>>>(a); break;
-    default: loss_dh<LossT32, 6><<<gr, th, 0, st>>>(a); break;
-  }
-  return hipGetLastError();
-}
-
-hipError_t launch_loss_dw_f32(int BNh, const LossGradArgs& a, hipStream_t st) {
-  const dim3 gr(a.splits * a.mt * a.ntn), th(256);
-  switch (BNh) {
-    case 256: loss_dw<LossT256, 6><<<gr, th, 0, st>>>(a); break;
-    case 128: loss_dw<LossT128, 6><<<gr, th, 0, st>>>(a); break;
-    default: loss_dw<LossT64, 6><<<gr, th, 0, st>>>(a); break;
-  }
-  return hipGetLastError();
-}
-
-// row tiles and state tiles of 256
+hipError_t launch_loss_dh_f32(int, int BN, const LossGradArgs& a, hipStream_t st) { return launch_loss_dh_p<6>(BN, a, st); }
+hipError_t launch_loss_dw_f32(int, int BNh, const LossGradArgs& a, hipStream_t st) { return launch_loss_dw_p<6>(BNh, a, st); }
 hipError_t launch_loss_both_f32(const LossGradArgs& h, const LossGradArgs& w, hipStream_t st) {
-  const dim3 gr(h.splits * loss_row_tiles(h.N, 256) * h.mt + w.splits * w.mt * w.ntn), th(256);
-  loss_both<LossT256, 6><<<gr, th, 0, st>>>(h, w);
-  return hipGetLastError();
+  return launch_loss_both_p<6>(h, w, st);
 }
-
 }  // namespace kb

@@ -440,24 +440,20 @@ __global__ __launch_bounds__(256, (LossOcc<T>::N)) void loss_logits(LossLogitsAr
   }
 }
 
-template <int PASSES>
-hipError_t launch_loss_logits_t(bool grad, int BN, const LossLogitsArgs& a, int blocks, hipStream_t st) {
+// planes: of the dlogits (1 or 2 for bf16 operands, 3 for float32); 0: forward.
+template <int PASSES, int PLANES>
+hipError_t launch_loss_logits_p(int BN, const LossLogitsArgs& a, int blocks, hipStream_t st) {
   const dim3 gr(blocks), th(256);
-  constexpr int BIG = PASSES > 1 ? 3 : 1, SMALL = PASSES > 1 ? 3 : 2;  // loss_g_planes
-  if (grad) {
-    switch (BN) {
-      case 256: loss_logits<LossT256, PASSES, BIG><<<gr, th, 0, st>>>(a); break;
-      case 128: loss_logits<LossT128, PASSES, SMALL><<<gr, th, 0, st>>>(a); break;
-      case 64: loss_logits<LossT64, PASSES, SMALL><<<gr, th, 0, st>>>(a); break;
-      default: loss_logits<LossT32, PASSES, SMALL><<<gr, th, 0, st>>>(a); break;
-    }
-  } else {
-    switch (BN) {
-      case 256: loss_logits<LossT256, PASSES, 0><<<gr, th, 0, st>>>(a); break;
-      case 128: loss_logits<LossT128, PASSES, 0><<<gr, th, 0, st>>>(a); break;
-      case 64: loss_logits<LossT64, PASSES, 0><<<gr, th, 0, st>>>(a); break;
-      default: loss_logits<LossT32, PASSES, 0><<<gr, th, 0, st>>>(a); break;
-    }
+  switch (BN) {
+    case 256:
+      if constexpr (PLANES != 2) {  // at most 128 rows have two
+        loss_logits<LossT256, PASSES, PLANES><<<gr, th, 0, st>>>(a);
+        break;
+      }
+      return hipErrorInvalidValue;
+    case 128: loss_logits<LossT128, PASSES, PLANES><<<gr, th, 0, st>>>(a); break;
+    case 64: loss_logits<LossT64, PASSES, PLANES><<<gr, th, 0, st>>>(a); break;
+    default: loss_logits<LossT32, PASSES, PLANES><<<gr, th, 0, st>>>(a); break;
   }
   return hipGetLastError();
 }

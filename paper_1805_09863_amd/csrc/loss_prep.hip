@@ -193,13 +193,19 @@ __global__ __launch_bounds__(kPackT) void loss_pack(LossPackArgs a) {
     const int j = tid & (kp - 1), r0 = tid / kp, step = kPackT / kp;
     auto each = [&](auto use) {
       if (j < K)
-        for (int r = r0; r < here; r += step) {
-          const int row = map[rt * a.BN + r];
-          const int t = a.rows.token[(size_t)row * K + j];
-          if (t >= 0 && t < a.rows.V) {
-            const int blk = ((t % wtm) >> 5) * NB + ((r % wtn) >> 5);
-            use(r, row, t, (r / wtn * a.words0 + t / wtm) * blocks + blk);
+        for (int r = r0; r < here; r += 4 * step) {
+          int row[4], t[4];  // four loads under way
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            row[u] = r + u * step < here ? map[rt * a.BN + r + u * step] : -1;
+            t[u] = row[u] >= 0 ? a.rows.token[(size_t)row[u] * K + j] : -1;
           }
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            if (t[u] >= 0 && t[u] < a.rows.V) {
+              const int ru = r + u * step, blk = ((t[u] & (wtm - 1)) >> 5) * NB + ((ru & (wtn - 1)) >> 5);
+              use(ru, row[u], t[u], ((ru >= wtn ? a.words0 : 0) + t[u] / wtm) * blocks + blk);
+            }
         }
     };
     each([&](int, int, int, int list) { atomicAdd(&hist[(list + 1) >> 1], ((list + 1) & 1) ? 1u << 16 : 1u); });
@@ -294,14 +300,22 @@ __global__ __launch_bounds__(256) void loss_finish(LossFinishArgs a) {
   }
 }
 
-// db: the row tiles' sums, in order.
-__global__ __launch_bounds__(256) void loss_db(const float* dbp, int wave_rows, int BN, int db_ld, const int32_t* count,
-                                               int V, float* db) {
-  const int v = blockIdx.x * 256 + threadIdx.x;
-  if (v >= V) return;
+// db: the row tiles' sums; 16 groups of 64 threads add up every 16th, then the groups' sums.
+__global__ __launch_bounds__(1024) void loss_db(const float* dbp, int wave_rows, int BN, int db_ld, const int32_t* count,
+                                                int V, float* db) {
+  __shared__ float sums[16][64];
+  const int x = threadIdx.x & 63, grp = threadIdx.x >> 6, v = blockIdx.x * 64 + x;
   const int n = loss_row_tiles(*count, BN) * wave_rows;
   float s = 0.f;
-  for (int i = 0; i < n; ++i) s += dbp[(size_t)i * db_ld + v];
+  if (v < V) {
+#pragma unroll 4
+    for (int i = grp; i < n; i += 16) s += dbp[(size_t)i * db_ld + v];
+  }
+  sums[grp][x] = s;
+  __syncthreads();
+  if (grp > 0 || v >= V) return;
+#pragma unroll
+  for (int g = 1; g < 16; ++g) s += sums[g][x];
   db[v] = s;
 }
 
@@ -362,7 +376,7 @@ hipError_t launch_loss_finish(const LossFinishArgs& a, hipStream_t st) {
 
 hipError_t launch_loss_db(const float* dbp, int wave_rows, int BN, int db_ld, const int32_t* count, int V, float* db,
                           hipStream_t st) {
-  loss_db<<<dim3((V + 255) / 256), dim3(256), 0, st>>>(dbp, wave_rows, BN, db_ld, count, V, db);
+  loss_db<<<dim3((V + 63) / 64), dim3(1024), 0, st>>>(dbp, wave_rows, BN, db_ld, count, V, db);
   return hipGetLastError();
 }
 

@@ -50,15 +50,17 @@ __device__ __forceinline__ TeacherRow teacher_row(const int32_t* token, const fl
   for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d, 64);
 #pragma unroll
   for (int u = 0; u < 2; ++u)
-    for (int i = 0; i < 64 && i + 64 * u < K; ++i) {
-      const int t = __shfl(tok[u], i, 64);
-      const float x = __shfl(e[u], i, 64);
-#pragma unroll
-      for (int w = 0; w < 2; ++w)
+    for (int i = 0; i < min(64, K - 64 * u); ++i) {
+      const int t = __builtin_amdgcn_readlane(tok[u], i);
+      const float x = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(e[u]), i));
+      const auto same = [&](int w) {
         if (t >= 0 && t == tok[w]) {
           merged[w] += x;
           if (i + 64 * u < lane + 64 * w) first[w] = false;
         }
+      };
+      same(0);
+      if (K > 64) same(1);
     }
   r.known = 0.f;
 #pragma unroll
