@@ -12,8 +12,8 @@
 namespace kb {
 hipError_t launch_loss_logits_bf16(int planes, int BN, const LossLogitsArgs& a, int blocks, hipStream_t st);
 hipError_t launch_loss_logits_f32(int planes, int BN, const LossLogitsArgs& a, int blocks, hipStream_t st);
-hipError_t launch_loss_dh_bf16(int planes, int BN, const LossGradArgs& a, hipStream_t st);
-hipError_t launch_loss_dh_f32(int planes, int BN, const LossGradArgs& a, hipStream_t st);
+hipError_t launch_loss_dh_bf16(int BN, const LossGradArgs& a, hipStream_t st);
+hipError_t launch_loss_dh_f32(int BN, const LossGradArgs& a, hipStream_t st);
 hipError_t launch_loss_dw_bf16(int planes, int BNh, const LossGradArgs& a, hipStream_t st);
 hipError_t launch_loss_dw_f32(int planes, int BNh, const LossGradArgs& a, hipStream_t st);
 hipError_t launch_loss_both_bf16(const LossGradArgs& h, const LossGradArgs& w, hipStream_t st);
@@ -46,6 +46,8 @@ struct Plan {
   int N, H, V, K;
   int BN, R, WN, WTM, WTN;  // row tile, how many, and the wave's part
   int Hp, Hk, BNh;
+  int BNd, Rd, two;         // dh: its row tile and how many; where second pieces of the dlogits lie (0: none)
+  int dw_grid;
   int vt, words0, nb, grid;
   int piece;                // word tiles of a piece of the vocabulary
   int pieces;
@@ -148,23 +150,30 @@ Plan make_plan(int dtype, int N, int H, int V, int K, bool teacher, bool grad, b
     p.xt = s.take((size_t)p.R * p.BN * K * 4);
   } else {
     p.rowp = s.take((size_t)p.R * p.BN * sizeof(float2));
-    p.g = s.take(p.piece * g_tile);
+    // two pieces: rows of one tile of dh, the second ones behind all of the first
+    p.two = p.g_planes == 2 ? p.R * p.BN : 0;
+    p.BNd = p.two == 0 ? p.BN : p.two <= 32 ? 64 : p.two <= 64 ? 128 : 256;
+    p.Rd = p.two == 0 ? p.R : 1;
+    p.g = s.take(p.two == 0 ? p.piece * g_tile : (size_t)p.piece * kb::kLossM * 2 * p.BNd);
     p.dbp = s.take((size_t)p.R * p.WN * p.vt * kb::kLossM * 4);
     p.dh_mt = (H + kb::kLossM - 1) / kb::kLossM;
     p.dw_ntn = (H + p.BNh - 1) / p.BNh;
     // Stages of 32 steps: of dh along the piece's words, of dW along the rows.
     const long long st_h = (long long)p.piece * (kb::kLossM / kb::kLossStage), st_w = p.R * p.BN / kb::kLossStage;
-    const long long n_h = (long long)p.R * p.dh_mt, n_w = (long long)p.piece * p.dw_ntn;
+    const long long n_h = (long long)p.Rd * p.dh_mt, n_w = (long long)p.piece * p.dw_ntn;
     if (p.both()) {
       // one launch: every workgroup about its share of all stages, and none of less than 16
       const long long share = std::max<long long>(16, (n_h * st_h + n_w * st_w) / 256);
       p.dh_splits = (int)std::max<long long>(1, std::min<long long>((st_h + share / 2) / share, p.piece));
       p.dw_splits = (int)std::max<long long>(1, (st_w + share / 2) / share);
     } else {
-      p.dh_splits = (int)std::max<long long>(1, std::min<long long>((p.BN == 32 ? 512 : 256) / n_h, p.piece));
+      p.dh_splits = (int)std::max<long long>(1, std::min<long long>((p.BNd == 32 ? 512 : 256) / n_h, p.piece));
       p.dw_splits = (int)std::max<long long>(1, std::min<long long>(256 / n_w, st_w / 8));
     }
-    p.dh_part = s.take((size_t)p.dh_splits * n_h * kb::kLossM * p.BN * 4);
+    // few stages a tile: a workgroup takes several tiles, the next one's loads under way while it writes one
+    p.dw_grid = (int)(n_w * p.dw_splits);
+    if (p.dw_splits == 1 && st_w * p.g_planes <= 16) p.dw_grid = std::min(p.dw_grid, p.BNh == 64 ? 512 : 256);
+    p.dh_part = s.take((size_t)p.dh_splits * n_h * kb::kLossM * p.BNd * 4);
     if (p.dw_splits > 1) p.dw_part = s.take((size_t)p.dw_splits * n_w * kb::kLossM * p.BNh * 4);
   }
   p.bytes = s.at;
@@ -451,12 +460,14 @@ kb_status gradient(const Call& c) {
     gh.words = pw.cols;
     gh.splits = p.dh_splits;
     gh.mt = p.dh_mt;
+    gh.two = p.two;
     gh.part = w.at<float>(p.dh_part);
     gh.add = i > 0;
     gw.words = c.V - t0 * kb::kLossM;
     gw.splits = p.dw_splits;
     gw.mt = tiles;
     gw.ntn = p.dw_ntn;
+    gw.grid = std::min(p.dw_grid, gw.splits * gw.mt * gw.ntn);
     gw.part = p.dw_splits > 1 ? w.at<float>(p.dw_part) : nullptr;
     gw.out = static_cast<char*>(c.dW) + (size_t)t0 * kb::kLossM * p.z;
     if (c.dh && c.dW && p.both()) {
@@ -465,23 +476,25 @@ kb_status gradient(const Call& c) {
     } else {
       if (c.dh)
         KB_LAUNCH("gradient of the states",
-                  p.bf16 ? kb::launch_loss_dh_bf16(p.g_planes, p.BN, gh, c.st) : kb::launch_loss_dh_f32(p.g_planes, p.BN, gh, c.st));
+                  p.bf16 ? kb::launch_loss_dh_bf16(p.BNd, gh, c.st) : kb::launch_loss_dh_f32(p.BNd, gh, c.st));
       if (c.dW)
         KB_LAUNCH("gradient of the weights",
                   p.bf16 ? kb::launch_loss_dw_bf16(p.g_planes, p.BNh, gw, c.st) : kb::launch_loss_dw_f32(p.g_planes, p.BNh, gw, c.st));
     }
     if (c.dW && gw.part) {
       const kb::LossJoinArgs j{gw.part, p.dw_splits, tiles, p.dw_ntn, p.BNh, c.H, std::min(gw.words, Vc), 0, nullptr,
-                               nullptr, gw.out, c.V};
-      KB_LAUNCH("gradient of the weights", kb::launch_loss_join(p.bf16, j, nullptr, 0, c.st));
+                               nullptr, gw.out, c.V, 0};
+      KB_LAUNCH("gradient of the weights", kb::launch_loss_join(p.bf16, j, kb::LossJoinMore{}, c.st));
     }
   }
+  const kb::LossBiasArgs db{w.at<float>(p.dbp), p.WN, p.BN, Vp, w.rows.count, c.V, c.db};
   if (c.dh) {
-    kb::LossJoinArgs j{w.at<float>(p.dh_part), p.dh_splits, p.dh_mt, p.R, p.BN, c.N, c.H, 1, w.rows.map, w.rows.count,
-                       c.dh, c.H};
-    KB_LAUNCH("gradient of the states", kb::launch_loss_join(p.bf16, j, w.rows.inv, c.N, c.st));
+    const kb::LossJoinArgs j{w.at<float>(p.dh_part), p.dh_splits, p.dh_mt, p.Rd, p.BNd, c.N, c.H, 1, w.rows.map,
+                             w.rows.count, c.dh, c.H, p.two};
+    KB_LAUNCH("gradient of the states", kb::launch_loss_join(p.bf16, j, kb::LossJoinMore{w.rows.inv, c.N, db, 0, 0}, c.st));
+  } else if (c.db) {
+    KB_LAUNCH("gradient of the bias", kb::launch_loss_db(db, c.st));
   }
-  if (c.db) KB_LAUNCH("gradient of the bias", kb::launch_loss_db(w.at<float>(p.dbp), p.WN, p.BN, Vp, w.rows.count, c.V, c.db, c.st));
   return ok();
 }
 

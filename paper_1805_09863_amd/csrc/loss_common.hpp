@@ -141,6 +141,8 @@ struct LossGradArgs {
   const int32_t* count;
   int splits;            // of the long axis
   int mt, ntn;           // tiles along M and N (dh: states, rows; dW: words, states)
+  int two;               // dh: the dlogits' second pieces are rows this far behind the first, all in one row tile; 0: none
+  int grid;              // dW: workgroups
   float* part;           // [split][tile] in the order of the registers; null (dW): written to out
   int add;               // dh: added to what the pieces before have left
   void* out;             // dW
@@ -156,6 +158,24 @@ struct LossJoinArgs {
   const int32_t* count;
   void* out;
   int ld;
+  int two;                    // dh: a row's second piece lies this many rows behind it; 0: there is one piece
+};
+
+// The bias' gradient from dbp (wave_rows rows for each row tile of BN).
+struct LossBiasArgs {
+  const float* dbp;
+  int wave_rows, BN, ld;
+  const int32_t* count;
+  int V;
+  float* db;                  // null: not wanted
+};
+
+// What the join of dh does besides: rows that do not count (of N; inv < 0), and the bias.
+struct LossJoinMore {
+  const int32_t* inv;         // null: none
+  int N;
+  LossBiasArgs db;
+  int zero_wg, db_wg;         // workgroups (set by the launch)
 };
 
 struct LossFinishArgs {
@@ -216,12 +236,9 @@ bool loss_finds_rows(int N, int nb);  // launch_loss_pack can do without launch_
 hipError_t launch_loss_pack(bool bf16, LossPackArgs a, hipStream_t st);
 hipError_t launch_loss_pack_w(bool bf16, const LossPackWArgs& a, hipStream_t st);
 hipError_t launch_loss_finish(const LossFinishArgs& a, hipStream_t st);
-// inv, N: rows of dh that do not count, filled with zeros (null: none)
-hipError_t launch_loss_join(bool bf16, const LossJoinArgs& a, const int32_t* inv, int N, hipStream_t st);
+hipError_t launch_loss_join(bool bf16, const LossJoinArgs& a, LossJoinMore more, hipStream_t st);
 hipError_t launch_loss_zero(void* p, size_t bytes, hipStream_t st);
-// wave_rows: rows of dbp for each row tile
-hipError_t launch_loss_db(const float* dbp, int wave_rows, int BN, int db_ld, const int32_t* count, int V, float* db,
-                          hipStream_t st);
+hipError_t launch_loss_db(const LossBiasArgs& a, hipStream_t st);
 
 // How the row tiles that exist share the workgroups: the same on the host's sizes, in the kernels and in the join.
 __host__ __device__ inline int loss_row_tiles(int rows, int BN) { return (rows + BN - 1) / BN; }

@@ -5,6 +5,7 @@
 // bytes a lane, and a join adds them up in order.  dh takes the words piece by piece and adds to its parts.
 #pragma once
 
+#include "loss_bias.hpp"
 #include "loss_logits.hpp"
 
 namespace kb {
@@ -29,9 +30,8 @@ __device__ __forceinline__ int xcd_cell(int cells, int b) {
   return x * (cells >> 3) + min(x, cells & 7) + j;
 }
 
-// PASSES: 1 (bf16 operands), 2 (the dlogits in two bf16 pieces) or 6 (float32).
-
-// Tile c of the `cells` of dh.
+// Tile c of the `cells` of dh; PASSES: 1 (bf16 operands) or 6 (float32).  Dlogits in two bf16 pieces are rows of
+// their own, behind all of the first pieces', and the join adds the two rows' results.
 template <class T, int PASSES>
 __device__ __forceinline__ void dh_tile(const LossGradArgs& a, uint32_t ring, int R, int c) {
   const int split = c / (R * a.mt), at = c - split * (R * a.mt), rt = at / a.mt, mt = at - rt * a.mt;
@@ -43,7 +43,7 @@ __device__ __forceinline__ void dh_tile(const LossGradArgs& a, uint32_t ring, in
     A = {a.W + (size_t)m0 * a.ldw + k0, a.ldw, a.w_plane, a.w_rows - m0, a.words - k0};
     B = {a.g + (size_t)rt * T::BN * a.gld + k0, a.gld, a.g_plane, 0, 0};
   };
-  const size_t part = (size_t)split * (loss_row_tiles(a.N, T::BN) * a.mt) + at;
+  const size_t part = (size_t)split * ((a.two > 0 ? 1 : loss_row_tiles(a.N, T::BN)) * a.mt) + at;
   auto init = [&](int, f32x16 (&acc)[T::MB][T::NB]) {
 #pragma unroll
     for (int i = 0; i < T::MB * T::NB; ++i) {
@@ -64,7 +64,7 @@ __device__ __forceinline__ void dh_tile(const LossGradArgs& a, uint32_t ring, in
       part_of<T>(a.part, part, i, acc[i / T::NB][i % T::NB], false);
     }
   };
-  mm_run<T, false, false, true, std::conditional_t<PASSES == 1, MmOne, std::conditional_t<PASSES == 2, MmTwoB, MmSix>>>(ring, 1, s1 - s0, tile, init, epi);
+  mm_run<T, false, false, true, std::conditional_t<PASSES == 1, MmOne, MmSix>, 0>(ring, 1, s1 - s0, tile, init, epi);
 }
 
 // 8 bf16 values to out, `left` of which exist.
@@ -78,20 +78,32 @@ __device__ __forceinline__ void write8(uint16_t* out, const bf16x8& v, int left)
     if (i < left) reinterpret_cast<__bf16*>(out)[i] = v[i];
 }
 
-// Tile c of the tiles and splits of dW.
+// Tiles c, c + step, ... below `cells` of the tiles and splits of dW (all the splits of a workgroup's tiles have the
+// same stages: it takes several only where there is one split); PASSES: 1 (bf16 operands), 2 (the dlogits in two bf16
+// pieces) or 6 (float32).
 template <class T, int PASSES>
-__device__ __forceinline__ void dw_tile(const LossGradArgs& a, uint32_t ring, int rows, int c) {
+__device__ __forceinline__ void dw_tile(const LossGradArgs& a, uint32_t ring, int rows, int first, int step, int cells) {
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave % T::WM, wn = wave / T::WM;
   const int stages = loss_row_tiles(rows, a.BN) * a.BN / kLossStage;
+  const int tiles = a.mt * a.ntn, nt = (cells - first + step - 1) / step;
+  // (a division leaves its quotient in a vector register)
+  auto stage0 = [&](int split) { return __builtin_amdgcn_readfirstlane((int)((long long)stages * split / a.splits)); };
+  auto stages_of = [&](int c) { return stage0(c / tiles + 1) - stage0(c / tiles); };
   // the state tiles of the same words next to each other: they read the same dlogits
-  const int split = c / (a.mt * a.ntn), at = c - split * (a.mt * a.ntn), mt = at / a.ntn, ht = at - mt * a.ntn;
-  const int s0 = (int)((long long)stages * split / a.splits), s1 = (int)((long long)stages * (split + 1) / a.splits);
-  const int m0 = mt * kLossM, n0 = ht * T::BN;
-  auto tile = [&](int, MmSide& A, MmSide& B) {
-    A = {a.g + (size_t)s0 * kLossStage * a.gld + m0, a.gld, a.g_plane, 0, 0};
-    B = {a.ph + (size_t)s0 * kLossStage * a.Hp + n0, a.Hp, a.ph_plane, 0, 0};
+  auto place = [&](int t, int& m0, int& n0) {
+    const int at = __builtin_amdgcn_readfirstlane((first + t * step) % tiles);
+    const int mt = __builtin_amdgcn_readfirstlane(at / a.ntn);
+    m0 = mt * kLossM;
+    n0 = (at - mt * a.ntn) * T::BN;
+  };
+  auto tile = [&](int t, MmSide& A, MmSide& B) {
+    int m0, n0;
+    place(t, m0, n0);
+    const size_t k0 = (size_t)stage0((first + t * step) / tiles) * kLossStage;
+    A = {a.g + k0 * a.gld + m0, a.gld, a.g_plane, 0, 0};
+    B = {a.ph + k0 * a.Hp + n0, a.Hp, a.ph_plane, 0, 0};
   };
   auto init = [&](int, f32x16 (&acc)[T::MB][T::NB]) {
 #pragma unroll
@@ -102,12 +114,14 @@ __device__ __forceinline__ void dw_tile(const LossGradArgs& a, uint32_t ring, in
       in_acc(x);
     }
   };
-  auto epi = [&](int, f32x16 (&acc)[T::MB][T::NB], uint32_t lds) {
+  auto epi = [&](int t, f32x16 (&acc)[T::MB][T::NB], uint32_t lds) {
+    int m0, n0;
+    place(t, m0, n0);
     if (a.part) {
 #pragma unroll
       for (int i = 0; i < T::MB * T::NB; ++i) {
         in_acc(acc[i / T::NB][i % T::NB]);
-        part_of<T>(a.part, c, i, acc[i / T::NB][i % T::NB], false);
+        part_of<T>(a.part, first + t * step, i, acc[i / T::NB][i % T::NB], false);
       }
       return;
     }
@@ -140,20 +154,22 @@ __device__ __forceinline__ void dw_tile(const LossGradArgs& a, uint32_t ring, in
         }
     }
   };
-  mm_run<T, true, true, false, std::conditional_t<PASSES == 1, MmOne, std::conditional_t<PASSES == 2, MmTwoA, MmSix>>>(ring, 1, s1 - s0, tile, init, epi);
+  mm_run<T, true, true, false, std::conditional_t<PASSES == 1, MmOne, std::conditional_t<PASSES == 2, MmTwoA, MmSix>>, 0>(
+      ring, nt, stages_of(first), tile, init, epi);
 }
 
 template <class T, int PASSES>
 __global__ __launch_bounds__(256, (LossOcc<T>::N)) void loss_dh(LossGradArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t ring[4 * LossOcc<T>::STAGE];
-  const int R = loss_row_tiles(const_int(a.count), T::BN), cells = a.splits * R * a.mt;
+  const int R = a.two > 0 ? 1 : loss_row_tiles(const_int(a.count), T::BN), cells = a.splits * R * a.mt;
   if ((int)blockIdx.x < cells) dh_tile<T, PASSES>(a, lds_addr(ring), R, xcd_cell(cells, blockIdx.x));
 }
 
 template <class T, int PASSES>
 __global__ __launch_bounds__(256, (LossOcc<T>::N)) void loss_dw(LossGradArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t ring[4 * LossOcc<T>::STAGE];
-  dw_tile<T, PASSES>(a, lds_addr(ring), const_int(a.count), xcd_cell(gridDim.x, blockIdx.x));
+  dw_tile<T, PASSES>(a, lds_addr(ring), const_int(a.count), xcd_cell(gridDim.x, blockIdx.x), gridDim.x,
+                     a.splits * a.mt * a.ntn);
 }
 
 // Both in one launch, the longer tiles of dh first: neither has to fill the card by itself.
@@ -165,22 +181,26 @@ __global__ __launch_bounds__(256, (LossOcc<T>::N)) void loss_both(LossGradArgs h
   if ((int)blockIdx.x < ch)
     dh_tile<T, PASSES>(h, lds_addr(ring), R, xcd_cell(ch, blockIdx.x));
   else if ((int)blockIdx.x < ch + cw)
-    dw_tile<T, PASSES>(w, lds_addr(ring), rows, xcd_cell(cw, blockIdx.x - ch));
+    dw_tile<T, PASSES>(w, lds_addr(ring), rows, xcd_cell(cw, blockIdx.x - ch), cw, cw);
 }
 
 // The parts of a result added up in order and rounded once.  A workgroup takes a quarter of the registers of one block of
 // 32 x 32 of every wave of a tile: four groups of 256 threads add up every fourth part each, then the four sums.
-// (dh of rows that do not count: zeros, by the last workgroups.)
+// Behind them, workgroups that fill the rows of dh that do not count with zeros, and some that add up the bias' sums.
 template <class T, class D>
-__global__ __launch_bounds__(1024) void loss_join(LossJoinArgs a, const int32_t* inv, int N, int zero_blocks) {
+__global__ __launch_bounds__(1024) void loss_join(LossJoinArgs a, LossJoinMore more) {
   __shared__ float4 sums[4][256];
   const int tid = threadIdx.x & 255, grp = threadIdx.x >> 8, lane = tid & 63, half = lane >> 5, col = lane & 31;
   const int wave = tid >> 6, wm = wave % T::WM, wn = wave / T::WM;
   D* out = static_cast<D*>(a.out);
-  const int work = gridDim.x - zero_blocks;
+  const int work = gridDim.x - more.zero_wg - more.db_wg;
+  if ((int)blockIdx.x >= work + more.zero_wg) {
+    sum_bias(more.db, blockIdx.x - work - more.zero_wg, reinterpret_cast<float*>(sums));
+    return;
+  }
   if ((int)blockIdx.x >= work) {
-    for (int n = blockIdx.x - work; n < N; n += zero_blocks)
-      if (inv[n] < 0)
+    for (int n = blockIdx.x - work; n < more.N; n += more.zero_wg)
+      if (more.inv[n] < 0)
         for (int i = threadIdx.x; i < a.cols; i += 1024) out[(size_t)n * a.ld + i] = (D)0.f;
     return;
   }
@@ -191,13 +211,24 @@ __global__ __launch_bounds__(1024) void loss_join(LossJoinArgs a, const int32_t*
   const int m = blk / T::NB, n = blk % T::NB;
   const int mt = a.is_dh ? tile % a.mt : tile / a.ntn, nt = a.is_dh ? tile / a.mt : tile % a.ntn;
   if (nt * T::BN >= rows) return;
-  float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int row = nt * T::BN + wn * T::WTN + n * 32 + col;
   const size_t step = (size_t)tiles * (T::MB * T::NB) * 4 * 256;
   const float4* p = reinterpret_cast<const float4*>(a.part) + ((size_t)unit * 4 + q) * 256 + tid;
+  float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](const float4* from) {
 #pragma unroll 8
-  for (int k = grp; k < a.splits; k += 4) {
-    const float4 v = p[k * step];
-    r.x += v.x, r.y += v.y, r.z += v.z, r.w += v.w;
+    for (int k = grp; k < a.splits; k += 4) {
+      const float4 v = from[k * step];
+      r.x += v.x, r.y += v.y, r.z += v.z, r.w += v.w;
+    }
+  };
+  if (row < rows) {
+    add(p);
+    if (a.two > 0) {  // the row's second pieces: row + two, in the same tile
+      const int r2 = row + a.two, wn2 = r2 / T::WTN, n2 = r2 % T::WTN / 32;
+      add(reinterpret_cast<const float4*>(a.part) + ((size_t)(tile * T::MB * T::NB + m * T::NB + n2) * 4 + q) * 256 +
+          (wm + T::WM * wn2) * 64 + half * 32 + r2 % 32);
+    }
   }
   if (a.splits > 1) {
     sums[grp][tid] = r;
@@ -208,7 +239,6 @@ __global__ __launch_bounds__(1024) void loss_join(LossJoinArgs a, const int32_t*
     const float4 v = sums[k][tid];
     r.x += v.x, r.y += v.y, r.z += v.z, r.w += v.w;
   }
-  const int row = nt * T::BN + wn * T::WTN + n * 32 + col;
   const int c = mt * kLossM + wm * T::WTM + m * 32 + 8 * q + 4 * half;
   if (row >= rows) return;
   D* to = out + (size_t)(a.is_dh ? a.map[row] : row) * a.ld + c;
@@ -225,7 +255,7 @@ __global__ __launch_bounds__(1024) void loss_join(LossJoinArgs a, const int32_t*
 
 template <int PASSES>
 hipError_t launch_loss_dh_p(int BN, const LossGradArgs& a, hipStream_t st) {
-  const dim3 gr(a.splits * loss_row_tiles(a.N, BN) * a.mt), th(256);
+  const dim3 gr(a.splits * (a.two > 0 ? 1 : loss_row_tiles(a.N, BN)) * a.mt), th(256);
   switch (BN) {
     case 256: loss_dh<LossT256, PASSES><<<gr, th, 0, st>>>(a); break;
     case 128: loss_dh<LossT128, PASSES><<<gr, th, 0, st>>>(a); break;
@@ -237,7 +267,7 @@ hipError_t launch_loss_dh_p(int BN, const LossGradArgs& a, hipStream_t st) {
 
 template <int PASSES>
 hipError_t launch_loss_dw_p(int BNh, const LossGradArgs& a, hipStream_t st) {
-  const dim3 gr(a.splits * a.mt * a.ntn), th(256);
+  const dim3 gr(a.grid), th(256);
   switch (BNh) {
     case 256: loss_dw<LossT256, PASSES><<<gr, th, 0, st>>>(a); break;
     case 128: loss_dw<LossT128, PASSES><<<gr, th, 0, st>>>(a); break;

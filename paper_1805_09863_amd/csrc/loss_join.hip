@@ -4,21 +4,22 @@
 namespace kb {
 
 template <class T>
-void join(bool bf16, const LossJoinArgs& a, const int32_t* inv, int N, hipStream_t st) {
-  const int zero = inv ? (N < 256 ? N : 256) : 0;
-  const dim3 gr(a.mt * a.ntn * T::MB * T::NB * 4 + zero), th(1024);
+void join(bool bf16, const LossJoinArgs& a, const LossJoinMore& more, hipStream_t st) {
+  const dim3 gr(a.mt * a.ntn * T::MB * T::NB * 4 + more.zero_wg + more.db_wg), th(1024);
   if (bf16)
-    loss_join<T, __bf16><<<gr, th, 0, st>>>(a, inv, N, zero);
+    loss_join<T, __bf16><<<gr, th, 0, st>>>(a, more);
   else
-    loss_join<T, float><<<gr, th, 0, st>>>(a, inv, N, zero);
+    loss_join<T, float><<<gr, th, 0, st>>>(a, more);
 }
 
-hipError_t launch_loss_join(bool bf16, const LossJoinArgs& a, const int32_t* inv, int N, hipStream_t st) {
+hipError_t launch_loss_join(bool bf16, const LossJoinArgs& a, LossJoinMore more, hipStream_t st) {
+  more.zero_wg = more.inv ? (more.N < 256 ? more.N : 256) : 0;
+  more.db_wg = more.db.db ? (more.db.V + 63) / 64 : 0;
   switch (a.BNt) {
-    case 256: join<LossT256>(bf16, a, inv, N, st); break;
-    case 128: join<LossT128>(bf16, a, inv, N, st); break;
-    case 64: join<LossT64>(bf16, a, inv, N, st); break;
-    default: join<LossT32>(bf16, a, inv, N, st); break;
+    case 256: join<LossT256>(bf16, a, more, st); break;
+    case 128: join<LossT128>(bf16, a, more, st); break;
+    case 64: join<LossT64>(bf16, a, more, st); break;
+    default: join<LossT32>(bf16, a, more, st); break;
   }
   return hipGetLastError();
 }

@@ -347,28 +347,25 @@ __global__ __launch_bounds__(256, (LossOcc<T>::N)) void loss_logits(LossLogitsAr
         }
       }
       if (a.dbp) {
-        // over the wave's rows: its blocks in registers, then the 32 lanes by halving the words a lane keeps
-        float s[16];
+        // over the wave's rows: its blocks in registers, the 32 lanes through LDS (a word's 32 sums 36 floats apart), a
+        // lane half a word's
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          s[r] = x[0][r];
+          float s = x[0][r];
 #pragma unroll
-          for (int n = 1; n < NB; ++n) s[r] += x[n][r];
+          for (int n = 1; n < NB; ++n) s += x[n][r];
+          *(KB_LDS float*)(uintptr_t)(mine + (uint32_t)((8 * (r >> 2) + 4 * half + (r & 3)) * 36 + col) * 4u) = s;
         }
+        const uint32_t from = mine + (uint32_t)((lane >> 1) * 36 + (lane & 1) * 16) * 4u;
+        float s = 0.f;
 #pragma unroll
-        for (int w = 8; w >= 1; w >>= 1) {
-          const bool upper = (col & (2 * w)) != 0;
-#pragma unroll
-          for (int r = 0; r < w; ++r) {
-            const float keep = upper ? s[r + w] : s[r], give = upper ? s[r] : s[r + w];
-            s[r] = keep + __shfl_xor(give, 2 * w, 64);
-          }
+        for (int i = 0; i < 4; ++i) {
+          const f32x4v v = *(const KB_LDS f32x4v*)(uintptr_t)(from + i * 16u);
+          s += (v[0] + v[1]) + (v[2] + v[3]);
         }
-        s[0] += __shfl_xor(s[0], 1, 64);
-        const int r = col >> 1;  // bits 4..1 of the lane chose the word's bits 3..0
-        if ((col & 1) == 0)
-          a.dbp[(size_t)(rt * T::WN + wn) * a.db_ld + a.db0 + v0 + wm * T::WTM + m * 32 + 8 * (r >> 2) + 4 * half + (r & 3)] =
-              s[0];
+        s += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(s), 0xb1, 0xf, 0xf, true));  // its neighbour's
+        if ((lane & 1) == 0)
+          a.dbp[(size_t)(rt * T::WN + wn) * a.db_ld + a.db0 + v0 + wm * T::WTM + m * 32 + (lane >> 1)] = s;
       }
 #pragma unroll
       for (int pl = 0; pl < PLANES; ++pl) {
@@ -398,13 +395,14 @@ __global__ __launch_bounds__(256, (LossOcc<T>::N)) void loss_logits(LossLogitsAr
       }
     }
   };
+  constexpr int STORES = MB * PLANES * (BN * T::WM * 4 / 256);
   auto epi = [&](int t, f32x16 (&acc)[MB][NB], uint32_t lds) {
     if constexpr (GRAD)
       epi_grad(t, acc, lds);
     else
       epi_stats(t, acc, lds);
   };
-  mm_run<T, true, false, PASSES == 1, std::conditional_t<PASSES == 1, MmOne, MmSix>>(lds_addr(ring), nt, a.Hk / kLossStage, tile, init, epi);
+  mm_run<T, true, false, PASSES == 1, std::conditional_t<PASSES == 1, MmOne, MmSix>, STORES>(lds_addr(ring), nt, a.Hk / kLossStage, tile, init, epi);
 
   if constexpr (!GRAD) {
     // the row's holders: two lane halves, and the waves along the words

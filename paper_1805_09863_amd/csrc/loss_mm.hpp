@@ -44,12 +44,13 @@ __device__ __forceinline__ const void* uniform_ptr(const void* x) {
                                        (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)p));
 }
 
-// One DMA instruction: lane i's 16 bytes from base + voff to LDS byte lds + PLUS + 16 i.  (The build checks that the
-// base was not written by a VALU instruction within the five wait states that the load needs; isa_check.py.)
-template <int PLUS>
+// One DMA instruction: lane i's 16 bytes from base + voff to LDS byte lds + PLUS + 16 i.  The load needs five wait
+// states after a VALU instruction that wrote its base: NOP 0 where the compiler keeps the base in scalar registers (the
+// build checks that; isa_check.py), 4 where it may come from a vector register.
+template <int PLUS, int NOP>
 __device__ __forceinline__ void dma16_at(uint32_t voff, const void* sbase, uint32_t lds) {
-  asm volatile("s_add_i32 m0, %2, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff),
-               "s"(uniform_ptr(sbase)), "s"(__builtin_amdgcn_readfirstlane(lds)), "i"(PLUS)
+  asm volatile("s_add_i32 m0, %2, %3\n\ts_nop %4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff),
+               "s"(uniform_ptr(sbase)), "s"(__builtin_amdgcn_readfirstlane(lds)), "i"(PLUS), "i"(NOP)
                : "m0", "scc");
 }
 
@@ -84,22 +85,26 @@ using MmTwoB = MmPasses<2, 0, 0u | 1u << 2>;
 using MmSix = MmPasses<6, 0u | 0u << 2 | 1u << 4 | 1u << 6 | 0u << 8 | 2u << 10,
                        0u | 1u << 2 | 0u << 4 | 1u << 6 | 2u << 8 | 0u << 10>;
 
-template <int BASE>
+template <int BASE, int NOP>
 __device__ __forceinline__ void dma_i(const uint32_t* off, int i, const void* src, uint32_t lds) {
   switch (i) {
-    case 0: dma16_at<BASE>(off[0], src, lds); break;
-    case 1: dma16_at<BASE + 1024>(off[1], src, lds); break;
-    case 2: dma16_at<BASE + 2048>(off[2], src, lds); break;
-    default: dma16_at<BASE + 3072>(off[3], src, lds); break;
+    case 0: dma16_at<BASE, NOP>(off[0], src, lds); break;
+    case 1: dma16_at<BASE + 1024, NOP>(off[1], src, lds); break;
+    case 2: dma16_at<BASE + 2048, NOP>(off[2], src, lds); break;
+    default: dma16_at<BASE + 3072, NOP>(off[3], src, lds); break;
   }
 }
 
 // T: tile; AS, BS: the side is strided; AC: side A is clamped to its limits; PS: MmPasses.
+// STORES: vector memory instructions that every wave issues in each epilogue, at least: the loads of the two stages
+// after it were issued before them, and are not waited for as if they came after (the counter is in order).
 // nt tiles of nk stages a pass.  tile(t, A, B): the sides of tile t; init(t, acc); epi(t, acc, lds): lds is a stage's
 // buffer that is free until epi returns.
-template <class T, bool AS, bool BS, bool AC, class PS, class TileFn, class InitFn, class EpiFn>
-__device__ __forceinline__ void mm_run(uint32_t ring, int nt, int nk, TileFn tile, InitFn init, EpiFn epi) {
+template <class T, bool AS, bool BS, bool AC, class PS, int STORES, class TileFn, class InitFn, class EpiFn>
+__device__ __forceinline__ void mm_run(uint32_t ring, int nt_, int nk_, TileFn tile, InitFn init, EpiFn epi) {
+  const int nt = __builtin_amdgcn_readfirstlane(nt_), nk = __builtin_amdgcn_readfirstlane(nk_);
   constexpr int MB = T::MB, NB = T::NB, BM = T::BM, BN = T::BN, PASSES = PS::N;
+  constexpr int NOP = PASSES > 1 ? 4 : 0;  // several passes: the compiler selects the bases in vector registers
   using GA = MmGeom<BM>;
   using GB = MmGeom<BN>;
   constexpr int STAGE = GA::BYTES + GB::BYTES;
@@ -113,7 +118,7 @@ __device__ __forceinline__ void mm_run(uint32_t ring, int nt, int nk, TileFn til
   MmSide A, B;
   uint32_t aload[GA::OPS], bload[GB::OPS];  // byte offsets from the stage's first element
   const char *asrc = nullptr, *bsrc = nullptr;
-  size_t astep = 0, bstep = 0;
+  uint32_t astep = 0, bstep = 0;  // bytes from a stage to the next
   int t_issue = 0, k_issue = 0, pass = 0, issued = 0;
 
   // offsets of a clamped side along k count from this many steps before the stage: they are never negative
@@ -163,8 +168,8 @@ __device__ __forceinline__ void mm_run(uint32_t ring, int nt, int nk, TileFn til
   };
   auto tile_sources = [&]() {
     tile(t_issue, A, B);
-    astep = AS ? (size_t)kLossStage * A.ld * 2 : kLossStage * 2;
-    bstep = BS ? (size_t)kLossStage * B.ld * 2 : kLossStage * 2;
+    astep = AS ? (uint32_t)__builtin_amdgcn_readfirstlane(kLossStage * 2 * A.ld) : kLossStage * 2;
+    bstep = BS ? (uint32_t)__builtin_amdgcn_readfirstlane(kLossStage * 2 * B.ld) : kLossStage * 2;
     offsets(SA{}, RA{}, CA{}, A, 0, aload);
     offsets(SB{}, RB{}, CB{}, B, 0, bload);
     sources();
@@ -177,10 +182,10 @@ __device__ __forceinline__ void mm_run(uint32_t ring, int nt, int nk, TileFn til
       // the stage that reaches the end of k has offsets of its own
       if ((k_issue + 1) * kLossStage > A.klim) offsets(SA{}, RA{}, CA{}, A, k_issue * kLossStage, aload);
     }
-    dma_i<0>(aload, i, asrc - kBack * 2, buf + wave_a);
+    dma_i<0, NOP>(aload, i, asrc - kBack * 2, buf + wave_a);
   };
   auto issue_b = [&](uint32_t buf, int i) {
-    dma_i<GA::BYTES>(bload, i, bsrc, buf + wave_b);
+    dma_i<GA::BYTES, NOP>(bload, i, bsrc, buf + wave_b);
   };
   auto issue_done = [&]() {
     ++issued;
@@ -280,7 +285,7 @@ __device__ __forceinline__ void mm_run(uint32_t ring, int nt, int nk, TileFn til
     lds_barrier();
   }
 
-  int g = 0;
+  int g = 0, after_epi = 0;
   auto body = [&](auto rc) {
     constexpr bool read_next = decltype(rc)::value;
     const uint32_t cur = ring + (uint32_t)(g & 3) * STAGE;
@@ -301,7 +306,10 @@ __device__ __forceinline__ void mm_run(uint32_t ring, int nt, int nk, TileFn til
       __builtin_amdgcn_sched_barrier(0);
     }
     // stage g + 1 has landed when no more than what was issued after it is under way
-    if (g + 3 < total)
+    constexpr int LATER = OPS + GA::OPS + STORES < 63 ? STORES : 63 - OPS - GA::OPS;
+    if (g + 3 < total && STORES > 0 && after_epi > 0)
+      wait_vm<OPS + GA::OPS + LATER>();
+    else if (g + 3 < total)
       wait_vm<OPS + GA::OPS>();
     else if (g + 2 < total)
       wait_vm<OPS>();
@@ -326,6 +334,7 @@ __device__ __forceinline__ void mm_run(uint32_t ring, int nt, int nk, TileFn til
     }
     if (more) issue_done();
     ++g;
+    --after_epi;
   };
   for (int t = 0; t < nt; ++t) {
     init(t, acc);
@@ -337,6 +346,7 @@ __device__ __forceinline__ void mm_run(uint32_t ring, int nt, int nk, TileFn til
       body(std::false_type{});
     }
     epi(t, acc, ring + (uint32_t)((g + 3) & 3) * STAGE);
+    after_epi = 2;
     if (t + 1 < nt) lds_barrier();  // the next stage's DMA goes into the buffer that the epilogue had
   }
 }

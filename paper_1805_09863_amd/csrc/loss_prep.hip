@@ -3,6 +3,7 @@
 #include <algorithm>
 
 #include "k3_scan.hpp"
+#include "loss_bias.hpp"
 #include "loss_common.hpp"
 #include "loss_teacher.hpp"
 
@@ -300,23 +301,9 @@ __global__ __launch_bounds__(256) void loss_finish(LossFinishArgs a) {
   }
 }
 
-// db: the row tiles' sums; 16 groups of 64 threads add up every 16th, then the groups' sums.
-__global__ __launch_bounds__(1024) void loss_db(const float* dbp, int wave_rows, int BN, int db_ld, const int32_t* count,
-                                                int V, float* db) {
-  __shared__ float sums[16][64];
-  const int x = threadIdx.x & 63, grp = threadIdx.x >> 6, v = blockIdx.x * 64 + x;
-  const int n = loss_row_tiles(*count, BN) * wave_rows;
-  float s = 0.f;
-  if (v < V) {
-#pragma unroll 4
-    for (int i = grp; i < n; i += 16) s += dbp[(size_t)i * db_ld + v];
-  }
-  sums[grp][x] = s;
-  __syncthreads();
-  if (grp > 0 || v >= V) return;
-#pragma unroll
-  for (int g = 1; g < 16; ++g) s += sums[g][x];
-  db[v] = s;
+__global__ __launch_bounds__(1024) void loss_db(LossBiasArgs a) {
+  __shared__ float sums[1024];
+  sum_bias(a, blockIdx.x, sums);
 }
 
 __global__ __launch_bounds__(256) void loss_zero(uint16_t* p, size_t n) {
@@ -374,9 +361,8 @@ hipError_t launch_loss_finish(const LossFinishArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-hipError_t launch_loss_db(const float* dbp, int wave_rows, int BN, int db_ld, const int32_t* count, int V, float* db,
-                          hipStream_t st) {
-  loss_db<<<dim3((V + 63) / 64), dim3(1024), 0, st>>>(dbp, wave_rows, BN, db_ld, count, V, db);
+hipError_t launch_loss_db(const LossBiasArgs& a, hipStream_t st) {
+  loss_db<<<dim3((a.V + 63) / 64), dim3(1024), 0, st>>>(a);
   return hipGetLastError();
 }
 
