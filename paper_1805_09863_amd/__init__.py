@@ -13,4 +13,5 @@ from .binding import (KB_BF16, KB_F32, KB_MAX_K, KBestError, abi_version, argmax
                       compact_batch, compact_beams, compact_workspace_bytes, cross_entropy, cross_entropy_grad,
                       distill, distill_grad, gather_rows, kbest_step, kbest_step_unfused, kbest_plan,
                       kbest_step_noalloc, kbest_workspace_bytes, lib, loss_grad_workspace_bytes,
-                      loss_workspace_bytes, merge_partials, rotary_frequencies, shard_partials, shard_splits, unfused_workspace_bytes, workspace)
+                      loss_workspace_bytes, merge_partials, rotary_frequencies, shard_partials, shard_splits,
+                      unfused_workspace_bytes, workspace)

@@ -938,139 +938,154 @@ def rotary_frequencies(rot_dim: int, *, base: float = 10000.0, factor: float = 1
 
 
 # ---------------------------------------------------------------- losses of the output layer
+def _loss_bytes(name: str, *shape: int) -> int:
+    # a pure function of the shape, asked once
+    key = (id(lib()), name) + shape
+    n = _ws_bytes_cache.get(key)
+    if n is None:
+        n = _ws_bytes_cache[key] = int(getattr(lib(), name)(*shape))
+    return n
+
+
 def loss_workspace_bytes(dtype: int, N: int, H: int, V: int, K: int = 1) -> int:
     """Workspace of ``cross_entropy`` (K = 1) and ``distill``."""
-    return int(lib().kb_loss_workspace_bytes(dtype, N, H, V, K))
+    return _loss_bytes("kb_loss_workspace_bytes", dtype, N, H, V, K)
 
 
 def loss_grad_workspace_bytes(dtype: int, N: int, H: int, V: int, K: int = 1) -> int:
     """Workspace of ``cross_entropy_grad`` (K = 1) and ``distill_grad``."""
-    return int(lib().kb_loss_grad_workspace_bytes(dtype, N, H, V, K))
+    return _loss_bytes("kb_loss_grad_workspace_bytes", dtype, N, H, V, K)
 
 
-def _loss_layer(h, W, b, rows):
-    """Checks the layer and the tensors of one value a row, all on one device; returns (dtype, N, H, V)."""
+def _loss_need(t, name: str, dtype, shape: tuple, dev: int) -> int:
+    """Address of a contiguous tensor of exactly ``shape`` and ``dtype`` on GPU ``dev``."""
+    try:
+        if t.shape == shape and t.dtype is dtype and t.get_device() == dev and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _need(t, name, dtype=dtype)
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {' x '.join(map(str, shape))}, got {tuple(t.shape)}")
+    raise ValueError(f"{name} is on {t.device}, h on cuda:{dev}")
+
+
+def _loss_layer(h, W, b):
+    """(device, type, dtype code, N, H, V, addresses of h, W and b) of the output layer."""
     _need(h, "h", dim=2)
-    _need(W, "W", dtype=h.dtype, dim=2)
-    _need(b, "b", dtype=torch.float32, dim=1)
-    dt = _dtype_code(h)
-    N, H = h.shape
-    V = W.shape[1]
-    if W.shape[0] != H or b.shape[0] != V:
-        raise ValueError("shape mismatch among h, W, b")
-    for name, t, dtype, shape in rows:
-        _need(t, name, dtype=dtype)
-        if t.shape != shape:
-            raise ValueError(f"{name} must be {' x '.join(str(n) for n in shape)}, got {tuple(t.shape)}")
-        if t.device != h.device:
-            raise ValueError(f"{name} must be on {h.device}, as h is")
-    if W.device != h.device or b.device != h.device:
-        raise ValueError(f"W and b must be on {h.device}, as h is")
-    return dt, N, H, V
+    code, dtype, dev = _dtype_code(h), h.dtype, h.get_device()
+    _need(W, "W", dtype=dtype, dim=2)
+    (N, H), V = h.shape, W.shape[1]
+    if max(N, H, V) > _INT_MAX:
+        _refuse_sizes(N=N, H=H, V=V)
+    return (dev, dtype, code, N, H, V, _loss_need(h, "h", dtype, (N, H), dev), _loss_need(W, "W", dtype, (H, V), dev),
+            _loss_need(b, "b", _F32, (V,), dev))
 
 
-def _loss_out(h, N, out, stream):
-    if out is None:
-        return _empty(h, N, stream, torch.float32), _empty(h, N, stream, torch.float32)
-    _need_outs(out, ("loss", "lse"), (torch.float32, torch.float32), N)
-    return out
+def _loss_teacher(token, logit, N: int, dev: int):
+    """(K, addresses of the teacher's words and logits)."""
+    _need(token, "token", dtype=_I32, dim=2)
+    K = token.shape[1]
+    if K > _INT_MAX:
+        _refuse_sizes(K=K)
+    return K, _loss_need(token, "token", _I32, (N, K), dev), _loss_need(logit, "logit", _F32, (N, K), dev)
 
 
-def _grad_out(h, W, b, out, stream):
-    if out is None:
-        return tuple(_empty(t, t.shape, stream, t.dtype) for t in (h, W, b))
-    if len(out) != 3:
-        raise ValueError("out must hold 3 tensors or Nones (dh, dW, db)")
-    if all(t is None for t in out):
-        raise ValueError("out holds no tensor: no gradient is asked for")
-    for t, name, like in zip(out, ("dh", "dW", "db"), (h, W, b)):
-        if t is None:
-            continue
-        _need(t, name, dtype=like.dtype)
-        if t.shape != like.shape:
-            raise ValueError(f"{name} must be {tuple(like.shape)}, got {tuple(t.shape)}")
-    return out
-
-
-def _loss_ws(h, need, ws, stream):
+def _loss_ws(h, need: int, ws, stream, dev: int):
+    """(address, bytes, tensor) of the workspace."""
     if ws is None:
         ws = _empty(h, max(need, 1), stream, torch.uint8)
-    _need_ws(ws, need)
-    return ws
+    else:
+        _need_ws(ws, need)
+        if ws.get_device() != dev:
+            raise ValueError(f"ws is on {ws.device}, h on cuda:{dev}")
+    return ws.data_ptr(), ws.numel() * ws.element_size(), ws
+
+
+def _loss_out(h, N: int, out, stream, dev: int):
+    """((loss, lse), their addresses)."""
+    if out is None:
+        out = _empty(h, N, stream, _F32), _empty(h, N, stream, _F32)
+    elif len(out) != 2:
+        raise ValueError("out must hold 2 tensors (loss, lse)")
+    return tuple(out), [_loss_need(t, n, _F32, (N,), dev) for t, n in zip(out, ("loss", "lse"))]
+
+
+def _grad_out(h, W, b, out, stream, dev: int):
+    """((dh, dW, db), their addresses), None for what is not wanted."""
+    if out is None:
+        out = tuple(_empty(t, t.shape, stream) for t in (h, W, b))
+    elif len(out) != 3:
+        raise ValueError("out must hold 3 tensors or Nones (dh, dW, db)")
+    elif all(t is None for t in out):
+        raise ValueError("out holds no tensor: no gradient is asked for")
+    return tuple(out), [None if t is None else _loss_need(t, n, x.dtype, tuple(x.shape), dev)
+                        for t, n, x in zip(out, ("dh", "dW", "db"), (h, W, b))]
 
 
 def cross_entropy(h: torch.Tensor, W: torch.Tensor, b: torch.Tensor, target: torch.Tensor, *, smoothing: float = 0.0,
                   out: Optional[tuple] = None, ws: Optional[torch.Tensor] = None, stream=None):
-    """Cross entropy of the output layer: returns (loss, lse), N float32 each, without storing h W + b.
+    """Cross entropy of the output layer (kb_cross_entropy): returns (loss, lse), N float32 each, without
+    storing h W + b.
 
     ``h`` is N x H, ``W`` H x V (float32 or bfloat16, same type), ``b`` V float32 as for ``kbest_step``;
     ``target`` N int32, the word of every row (outside 0 .. V - 1: the row is left out, its loss and lse are
     0).  ``smoothing``: the part of the labels that is spread over all words.  ``out`` may supply (loss, lse),
     ``ws`` a workspace of at least ``loss_workspace_bytes`` bytes.
     """
-    N = h.shape[0] if isinstance(h, torch.Tensor) and h.dim() else 0
-    dt, N, H, V = _loss_layer(h, W, b, (("target", target, torch.int32, (N,)),))
-    loss, lse = _loss_out(h, N, out, stream)
-    ws = _loss_ws(h, loss_workspace_bytes(dt, N, H, V), ws, stream)
-    _check(lib().kb_cross_entropy(dt, N, H, V, _ptr(h), _ptr(W), _ptr(b), _ptr(target), smoothing, _ptr(loss),
-                                  _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream, h.device)))
-    return loss, lse
+    dev, _, code, N, H, V, hp, Wp, bp = _loss_layer(h, W, b)
+    tp = _loss_need(target, "target", _I32, (N,), dev)
+    out, op = _loss_out(h, N, out, stream, dev)
+    wp, nbytes, ws = _loss_ws(h, loss_workspace_bytes(code, N, H, V), ws, stream, dev)
+    _run(lib().kb_cross_entropy, dev, stream, code, N, H, V, hp, Wp, bp, tp, smoothing, *op, wp, nbytes)
+    return out
 
 
 def cross_entropy_grad(h: torch.Tensor, W: torch.Tensor, b: torch.Tensor, target: torch.Tensor, lse: torch.Tensor,
                        grad: torch.Tensor, *, smoothing: float = 0.0, out: Optional[tuple] = None,
                        ws: Optional[torch.Tensor] = None, stream=None):
-    """Gradients of sum(grad * loss) of ``cross_entropy`` with the same h, W, b, target and smoothing: returns
-    (dh, dW, db), of the types and shapes of h, W and b.
+    """Gradients of sum(grad * loss) of ``cross_entropy`` with the same h, W, b, target and smoothing
+    (kb_cross_entropy_grad): returns (dh, dW, db), of the types and shapes of h, W and b.
 
     ``lse`` is what ``cross_entropy`` returned, ``grad`` N float32.  ``out`` may supply (dh, dW, db), with None
     for what is not wanted; ``ws`` a workspace of at least ``loss_grad_workspace_bytes`` bytes.
     """
-    N = h.shape[0] if isinstance(h, torch.Tensor) and h.dim() else 0
-    dt, N, H, V = _loss_layer(h, W, b, (("target", target, torch.int32, (N,)), ("lse", lse, torch.float32, (N,)),
-                                        ("grad", grad, torch.float32, (N,))))
-    out = _grad_out(h, W, b, out, stream)
-    ws = _loss_ws(h, loss_grad_workspace_bytes(dt, N, H, V), ws, stream)
-    _check(lib().kb_cross_entropy_grad(dt, N, H, V, _ptr(h), _ptr(W), _ptr(b), _ptr(target), smoothing, _ptr(lse),
-                                       _ptr(grad), _ptr(out[0]), _ptr(out[1]), _ptr(out[2]), _ptr(ws),
-                                       ws.numel() * ws.element_size(), _stream(stream, h.device)))
-    return tuple(out)
+    dev, _, code, N, H, V, hp, Wp, bp = _loss_layer(h, W, b)
+    tp = _loss_need(target, "target", _I32, (N,), dev)
+    lp, gp = _loss_need(lse, "lse", _F32, (N,), dev), _loss_need(grad, "grad", _F32, (N,), dev)
+    out, op = _grad_out(h, W, b, out, stream, dev)
+    wp, nbytes, ws = _loss_ws(h, loss_grad_workspace_bytes(code, N, H, V), ws, stream, dev)
+    _run(lib().kb_cross_entropy_grad, dev, stream, code, N, H, V, hp, Wp, bp, tp, smoothing, lp, gp, *op, wp, nbytes)
+    return out
 
 
 def distill(h: torch.Tensor, W: torch.Tensor, b: torch.Tensor, token: torch.Tensor, logit: torch.Tensor, *,
             temperature: float = 1.0, out: Optional[tuple] = None, ws: Optional[torch.Tensor] = None, stream=None):
-    """Distillation from a teacher's best words: returns (loss, lse), N float32 each.
+    """Distillation from a teacher's best words (kb_distill): returns (loss, lse), N float32 each.
 
     ``token``, ``logit``: N x K int32 and float32, the teacher's words for every row and their logits (or
-    log-probabilities), in any order; a token outside 0 .. V - 1 or a logit of -inf is no entry, and a row
-    without one is left out.  The loss is temperature^2 times the divergence of softmax(student / temperature)
-    from softmax(logit / temperature); lse is the log-sum-exp of the student's logits / temperature.
+    log-probabilities, as ``kbest_step`` scores them), in any order; a token outside 0 .. V - 1 or a logit of
+    -inf is no entry, and a row without one is left out.  The loss is temperature^2 times the divergence of
+    softmax(student / temperature) from softmax(logit / temperature); lse is the log-sum-exp of the student's
+    logits / temperature.
     """
-    shape = (h.shape[0] if isinstance(h, torch.Tensor) and h.dim() else 0,
-             token.shape[1] if isinstance(token, torch.Tensor) and token.dim() == 2 else 0)
-    dt, N, H, V = _loss_layer(h, W, b, (("token", token, torch.int32, shape), ("logit", logit, torch.float32, shape)))
-    K = shape[1]
-    loss, lse = _loss_out(h, N, out, stream)
-    ws = _loss_ws(h, loss_workspace_bytes(dt, N, H, V, K), ws, stream)
-    _check(lib().kb_distill(dt, N, H, V, K, _ptr(h), _ptr(W), _ptr(b), _ptr(token), _ptr(logit), temperature,
-                            _ptr(loss), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(),
-                            _stream(stream, h.device)))
-    return loss, lse
+    dev, _, code, N, H, V, hp, Wp, bp = _loss_layer(h, W, b)
+    K, tp, yp = _loss_teacher(token, logit, N, dev)
+    out, op = _loss_out(h, N, out, stream, dev)
+    wp, nbytes, ws = _loss_ws(h, loss_workspace_bytes(code, N, H, V, K), ws, stream, dev)
+    _run(lib().kb_distill, dev, stream, code, N, H, V, K, hp, Wp, bp, tp, yp, temperature, *op, wp, nbytes)
+    return out
 
 
 def distill_grad(h: torch.Tensor, W: torch.Tensor, b: torch.Tensor, token: torch.Tensor, logit: torch.Tensor,
                  lse: torch.Tensor, grad: torch.Tensor, *, temperature: float = 1.0, out: Optional[tuple] = None,
                  ws: Optional[torch.Tensor] = None, stream=None):
-    """Gradients of sum(grad * loss) of ``distill`` with the same arguments: returns (dh, dW, db), as
-    ``cross_entropy_grad`` does; the teacher has none."""
-    shape = (h.shape[0] if isinstance(h, torch.Tensor) and h.dim() else 0,
-             token.shape[1] if isinstance(token, torch.Tensor) and token.dim() == 2 else 0)
-    dt, N, H, V = _loss_layer(h, W, b, (("token", token, torch.int32, shape), ("logit", logit, torch.float32, shape),
-                                        ("lse", lse, torch.float32, shape[:1]), ("grad", grad, torch.float32, shape[:1])))
-    K = shape[1]
-    out = _grad_out(h, W, b, out, stream)
-    ws = _loss_ws(h, loss_grad_workspace_bytes(dt, N, H, V, K), ws, stream)
-    _check(lib().kb_distill_grad(dt, N, H, V, K, _ptr(h), _ptr(W), _ptr(b), _ptr(token), _ptr(logit), temperature,
-                                 _ptr(lse), _ptr(grad), _ptr(out[0]), _ptr(out[1]), _ptr(out[2]), _ptr(ws),
-                                 ws.numel() * ws.element_size(), _stream(stream, h.device)))
-    return tuple(out)
+    """Gradients of sum(grad * loss) of ``distill`` with the same arguments (kb_distill_grad): returns
+    (dh, dW, db), as ``cross_entropy_grad`` does; the teacher has none."""
+    dev, _, code, N, H, V, hp, Wp, bp = _loss_layer(h, W, b)
+    K, tp, yp = _loss_teacher(token, logit, N, dev)
+    lp, gp = _loss_need(lse, "lse", _F32, (N,), dev), _loss_need(grad, "grad", _F32, (N,), dev)
+    out, op = _grad_out(h, W, b, out, stream, dev)
+    wp, nbytes, ws = _loss_ws(h, loss_grad_workspace_bytes(code, N, H, V, K), ws, stream, dev)
+    _run(lib().kb_distill_grad, dev, stream, code, N, H, V, K, hp, Wp, bp, tp, yp, temperature, lp, gp, *op, wp, nbytes)
+    return out

@@ -159,3 +159,326 @@ def test_smoothing(kb, dtype, N, H, V):
                                        (300, 64, 1536, 64, 4.0), (60, 96, 400, 128, 1.0)])
 def test_distill(kb, dtype, N, H, V, K, T):
     check_kd(kb, dtype, N, H, V, K, T)
+
+
+def bits(t):
+    return t.detach().cpu().view(torch.int16 if t.dtype == BF16 else torch.int32).numpy()
+
+
+# few rows, small tiles, tiles of 64, 128 and 256 rows
+PATHS = [(6, 96, 700), (40, 96, 2000), (60, 64, 60000), (120, 32, 52000), (700, 64, 26000)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,H,V", PATHS)
+def test_rows_left_out(kb, dtype, N, H, V):
+    def edit(h, W, b, target, grad):
+        target[0] = V                  # one past the vocabulary
+        target[1] = -2 ** 31
+        target[2] = 2 ** 31 - 1
+        target[N - 1] = -100
+        out = (target < 0) | (target >= V)
+        h[out] = math.nan              # whatever they hold
+        h[1] = math.inf
+        grad[out] = math.nan
+    check_ce(kb, dtype, N, H, V, edit=edit)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,H,V", PATHS)
+def test_no_row_counts(kb, dtype, N, H, V):
+    _, h, W, b, _, grad = make(3, dtype, N, H, V)
+    target = torch.full((N,), -1, dtype=torch.int32)
+    hd, Wd, bd, td, gd = dev(h, W, b, target, grad)
+    loss, lse = kb.cross_entropy(hd, Wd, bd, td, smoothing=0.2)
+    for t in (loss, lse, *kb.cross_entropy_grad(hd, Wd, bd, td, lse, gd, smoothing=0.2)):
+        assert (f64(t) == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,H,V", PATHS)
+def test_masked_words(kb, dtype, N, H, V):
+    def edit(h, W, b, target, grad):
+        b[::3] = -math.inf             # a shortlist: two words of three
+        b[V - 1] = -math.inf
+        ok = (target >= 0) & torch.isinf(b[target.clamp_min(0).long()])
+        target[ok] = 1
+    check_ce(kb, dtype, N, H, V, edit=edit)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,H,V", PATHS)
+def test_large_logits(kb, dtype, N, H, V):
+    # a word far above all others, and states of very different sizes
+    def edit(h, W, b, target, grad):
+        h *= torch.logspace(-3, 1.5, N)[:, None].to(dtype)
+        b[V // 2] = 60.0
+        b[V // 3] = -3e4
+    check_ce(kb, dtype, N, H, V, edit=edit)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,H,V", PATHS)
+@pytest.mark.parametrize("T", [1.0, 2.0])
+def test_teachers_entries(kb, dtype, N, H, V, T):
+    def edit(token, logit):
+        token[0] = 5                              # one word again and again
+        token[1, ::2] = token[1, 0]
+        logit[2] = -math.inf                      # a row without an entry
+        logit[3, 1:] = -math.inf                  # one entry
+        token[4] = torch.arange(40)               # neighbours
+        token[5] = torch.tensor([-1, V, 2 ** 31 - 1, -2 ** 31] * 10)
+        logit[:, 7] = -80.0                       # nearly nothing
+    check_kd(kb, dtype, N, H, V, 40, T, edit=edit)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,H,V", [(8, 64, 2000), (30, 64, 2000), (64, 64, 60000), (128, 32, 52000), (600, 32, 30000)])
+def test_all_entries_in_one_place(kb, dtype, N, H, V):
+    # every row's 128 words in the same 128: thousands of entries in one wave's part of a tile, 1,024 in a block
+    def edit(token, logit):
+        token[:] = torch.stack([torch.randperm(128) for _ in range(N)]).to(torch.int32) + 256
+    check_kd(kb, dtype, N, H, V, 128, 2.0, pad=0.0, edit=edit)
+
+
+@pytest.mark.parametrize("N", [8193, 9000])
+def test_many_rows(kb, N):
+    check_ce(kb, BF16, N, 32, 300, pad=0.5)
+    check_kd(kb, BF16, N, 32, 300, 3)
+
+
+@pytest.mark.parametrize("N,H,V", [(5, 32, 262144), (40, 32, 262144), (2000, 32, 262144)])
+def test_largest_vocabulary(kb, N, H, V):
+    _, h, W, b, target, grad = make(5, BF16, N, H, V, pad=0.0)
+    target[:3] = torch.tensor([0, V - 1, V - 2])
+    hd, Wd, bd, td, gd = dev(h, W, b, target, grad)
+    loss, lse = kb.cross_entropy(hd, Wd, bd, td)
+    dh, dW, db = kb.cross_entropy_grad(hd, Wd, bd, td, lse, gd)
+    # the first rows and the last against the oracle; of the sums over rows, the columns of some words
+    rows = np.r_[0:4, N - 1]
+    o = lo.cross_entropy(f64(h)[rows], f64(W), f64(b), target.numpy()[rows])
+    bnd = lo.bounds(o, f64(h)[rows], f64(W), f64(b), False, f64(grad)[rows])
+    check_rows(o, bnd, loss[rows], lse[rows], f"{N} x {H} x {V}")
+    check_grads(o, bnd, h[rows], W, grad[rows], (dh[rows], None, None), BF16, f"{N} x {H} x {V}")
+    words = np.r_[0:8, 100000:100008, V - 8:V]
+    x = f64(h) @ f64(W)[:, words] + f64(b)[words]
+    p = np.exp(x - f64(lse)[:, None])
+    G = f64(grad)[:, None] * (p - (target.numpy()[:, None] == words[None]))
+    # a probability is off by what its exponent is: lse's float32 (3 u of it), the logit's (H + 3) u of sum |h W| + |b| and
+    # their difference's rounding
+    size = np.abs(f64(h)) @ np.abs(f64(W)[:, words]) + np.abs(f64(b)[words])
+    off = 3 * U * np.abs(f64(lse))[:, None] + (H + 5) * U * size + 4 * U * (np.abs(x) + np.abs(f64(lse))[:, None]) + 2.0 ** -22
+    dp = np.abs(f64(grad))[:, None] * p * (np.exp(off) - 1) + 4 * U * np.abs(f64(grad))[:, None] * (p + 1)
+    e = dp + 2.0 ** -8 * np.abs(G) + 2.0 ** -126
+    ah, aG = np.abs(f64(h)), np.abs(G)
+    want, lim = f64(h).T @ G, ah.T @ e + (N + 80) * U * (ah.T @ aG)
+    assert (np.abs(f64(dW)[:, words] - want) <= lim + 2.0 ** -8 * (np.abs(want) + lim)).all()
+    want, lim = G.sum(0), dp.sum(0) + (N + 80) * U * aG.sum(0)
+    assert (np.abs(f64(db)[words] - want) <= lim + U * np.abs(want)).all()
+
+
+def test_logits_beyond_32_bits(kb):
+    # 20,000 x 131,072: 2.6e9 logits; some rows against 64 bits
+    N, H, V = 20000, 32, 131072
+    g = torch.Generator(device="cuda").manual_seed(11)
+    h = torch.randn((N, H), generator=g, device="cuda").to(BF16)
+    W = (torch.randn((H, V), generator=g, device="cuda") / 6).to(BF16)
+    b = torch.randn(V, generator=g, device="cuda")
+    target = torch.randint(0, V, (N,), generator=g, device="cuda", dtype=torch.int32)
+    grad = torch.randn(N, generator=g, device="cuda")
+    loss, lse = kb.cross_entropy(h, W, b, target)
+    dh, dW, db = kb.cross_entropy_grad(h, W, b, target, lse, grad)
+    rows = torch.tensor([0, 255, 256, 16383, 16384, 19998, 19999], device="cuda")
+    hr, tr = h[rows].cpu(), target[rows].cpu().numpy()
+    o = lo.cross_entropy(f64(hr), f64(W), f64(b), tr)
+    bnd = lo.bounds(o, f64(hr), f64(W), f64(b), False, f64(grad[rows]))
+    check_rows(o, bnd, loss[rows], lse[rows], "2.6e9 logits")
+    check_grads(o, bnd, hr, W.cpu(), grad[rows].cpu(), (dh[rows], None, None), BF16, "2.6e9 logits")
+    # every row's dlogits add up to zero, and so does db: to the rounding of N x V float32 terms
+    assert abs(f64(db).sum()) <= 1e-3 * f64(grad.abs()).sum() / math.sqrt(N)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,H,V", PATHS)
+def test_wanted_gradients_only(kb, dtype, N, H, V):
+    _, h, W, b, target, grad = make(7, dtype, N, H, V)
+    hd, Wd, bd, td, gd = dev(h, W, b, target, grad)
+    _, lse = kb.cross_entropy(hd, Wd, bd, td)
+    whole = kb.cross_entropy_grad(hd, Wd, bd, td, lse, gd)
+    for want in range(1, 7):
+        out = tuple(torch.full_like(t, math.nan) if want >> i & 1 else None for i, t in enumerate((hd, Wd, bd)))
+        got = kb.cross_entropy_grad(hd, Wd, bd, td, lse, gd, out=out)
+        for x, y, z in zip(got, out, whole):
+            assert x is y
+            if x is not None:
+                err = (x.double() - z.double()).abs().max()  # dh and dW apart may be split otherwise than together
+                assert err <= 2 * ROUND[x.dtype if x.dim() == 2 else F32] * z.double().abs().max()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,H,V", PATHS)
+def test_same_bits_whatever_the_workspace_held(kb, dtype, N, H, V):
+    g, h, W, b, _, grad = make(9, dtype, N, H, V)
+    token, logit = teacher(g, N, V, 9)
+    hd, Wd, bd, td, yd, gd = dev(h, W, b, token, logit, grad)
+    code = kb.KB_BF16 if dtype == BF16 else kb.KB_F32
+    seen = []
+    for fill in (0, 0xFF, 0x7F):
+        ws = torch.full((kb.loss_workspace_bytes(code, N, H, V, 9),), fill, dtype=torch.uint8, device="cuda")
+        wg = torch.full((kb.loss_grad_workspace_bytes(code, N, H, V, 9),), fill, dtype=torch.uint8, device="cuda")
+        out = tuple(torch.full((N,), math.nan, device="cuda") for _ in range(2))
+        loss, lse = kb.distill(hd, Wd, bd, td, yd, temperature=1.5, ws=ws, out=out)
+        assert loss is out[0] and lse is out[1]
+        seen.append([bits(t) for t in (loss, lse, *kb.distill_grad(hd, Wd, bd, td, yd, lse, gd, temperature=1.5, ws=wg))])
+    for other in seen[1:]:
+        assert all((x == y).all() for x, y in zip(seen[0], other))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,H,V", [(6, 96, 704), (40, 96, 2000), (300, 64, 1536)])
+def test_any_address(kb, dtype, N, H, V):
+    # operands one value past an allocation's start, results as well
+    _, h, W, b, target, grad = make(13, dtype, N, H, V)
+
+    def shifted(t, by=1):
+        buf = torch.zeros(t.numel() + by, dtype=t.dtype, device="cuda")
+        buf[by:] = t.flatten().cuda()
+        return buf[by:].view(t.shape)
+
+    hd, Wd, bd, td, gd = (shifted(t) for t in (h, W, b, target, grad))
+    loss, lse = kb.cross_entropy(hd, Wd, bd, td, out=tuple(shifted(torch.zeros(N)) for _ in range(2)))
+    out = tuple(shifted(torch.zeros_like(t)) for t in (h, W, b))
+    outs = kb.cross_entropy_grad(hd, Wd, bd, td, lse, gd, out=out)
+    o = lo.cross_entropy(f64(h), f64(W), f64(b), target.numpy())
+    bnd = lo.bounds(o, f64(h), f64(W), f64(b), dtype == F32, f64(grad))
+    check_rows(o, bnd, loss, lse, "shifted")
+    check_grads(o, bnd, h, W, grad, outs, dtype, "shifted")
+
+
+def test_no_rows(kb):
+    h, W, b = (torch.zeros(s, device="cuda") for s in ((0, 16), (16, 300), (300,)))
+    target = torch.zeros(0, dtype=torch.int32, device="cuda")
+    loss, lse = kb.cross_entropy(h, W, b, target)
+    assert loss.shape == (0,) and lse.shape == (0,)
+    out = (torch.empty_like(h), torch.full_like(W, math.nan), torch.full_like(b, math.nan))
+    kb.cross_entropy_grad(h, W, b, target, lse, loss, out=out)
+    assert (f64(out[1]) == 0).all() and (f64(out[2]) == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,H,V", [(6, 96, 700), (70, 64, 3000), (300, 64, 3000)])
+def test_captured_and_replayed(kb, dtype, N, H, V):
+    """A training step in a graph, replayed on new inputs between eager calls of the same size."""
+    g, h, W, b, target, grad = make(17, dtype, N, H, V)
+    token, logit = teacher(g, N, V, 6)
+    hd, Wd, bd, td, kd, yd, gd = dev(h, W, b, target, token, logit, grad)
+
+    def step(ws=None):
+        loss, lse = kb.cross_entropy(hd, Wd, bd, td, smoothing=0.1)
+        l2, s2 = kb.distill(hd, Wd, bd, kd, yd, temperature=2.0)
+        return (loss, lse, l2, s2, *kb.cross_entropy_grad(hd, Wd, bd, td, lse, gd, smoothing=0.1),
+                *kb.distill_grad(hd, Wd, bd, kd, yd, s2, gd, temperature=2.0))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step()
+    for turn in range(4):
+        for t, like in ((hd, h), (bd, b), (gd, grad), (yd, logit)):
+            t.copy_(torch.randn(like.shape, generator=g).to(like.dtype))
+        td.copy_(torch.randint(-1, V, (N,), generator=g, dtype=torch.int32))  # other rows left out
+        kd.copy_(torch.randint(-1, V, kd.shape, generator=g, dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = step()
+        torch.cuda.synchronize()
+        for i, (x, y) in enumerate(zip(captured, eager)):
+            assert (bits(x) == bits(y)).all(), f"turn {turn}: result {i}"
+
+
+def test_two_streams_at_once(kb):
+    jobs = []
+    for seed, (dtype, N, H, V) in enumerate([(BF16, 300, 128, 9000), (F32, 200, 64, 5000), (BF16, 7, 64, 3000)]):
+        _, h, W, b, target, grad = make(seed, dtype, N, H, V)
+        jobs.append(dev(h, W, b, target, grad))
+
+    def step(j, stream):
+        h, W, b, target, grad = j
+        loss, lse = kb.cross_entropy(h, W, b, target, stream=stream)
+        return (loss, lse, *kb.cross_entropy_grad(h, W, b, target, lse, grad, stream=stream))
+
+    alone = [[bits(t) for t in step(j, None)] for j in jobs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in jobs]
+    got = [[] for _ in jobs]
+    for _ in range(5):
+        for i, (j, s) in enumerate(zip(jobs, streams)):
+            got[i].append(step(j, s))
+    torch.cuda.synchronize()
+    for want, runs in zip(alone, got):
+        for run in runs:
+            assert all((x == bits(t)).all() for x, t in zip(want, run))
+
+
+@pytest.mark.parametrize("N,H,V", [(4, 24, 90), (20, 24, 400), (140, 32, 600)])
+def test_gradient_is_that_of_the_loss(kb, N, H, V):
+    """Against central differences of the float32 loss along random directions.  A step of e leaves e^2 / 6 of the third
+    derivative, a third central moment of the logits' change over a row: at most its spread cubed; and the rounding of
+    the two losses, 2^-20 of their size and of the log-sum-exp's, at most 8 here, over 2 e."""
+    g, h, W, b, target, grad = make(21, F32, N, H, V)
+    token, logit = teacher(g, N, V, 5)
+    eps = 2.0 ** -6
+    hd, Wd, bd, td, kd, yd, gd = dev(h, W, b, target, token, logit, grad)
+    losses = {
+        "cross entropy": (lambda h_, W_, b_: kb.cross_entropy(h_, W_, b_, td, smoothing=0.1)[0],
+                          lambda: kb.cross_entropy_grad(hd, Wd, bd, td, kb.cross_entropy(hd, Wd, bd, td, smoothing=0.1)[1],
+                                                        gd, smoothing=0.1)),
+        "distillation": (lambda h_, W_, b_: kb.distill(h_, W_, b_, kd, yd, temperature=2.0)[0],
+                         lambda: kb.distill_grad(hd, Wd, bd, kd, yd, kb.distill(hd, Wd, bd, kd, yd, temperature=2.0)[1], gd,
+                                                 temperature=2.0))}
+    for name, (loss, gradient) in losses.items():
+        grads = gradient()
+        for i, t in enumerate((hd, Wd, bd)):
+            v = torch.randn(t.shape, generator=g).cuda()
+            v /= v.norm() / math.sqrt(t.shape[0])
+            args = [hd, Wd, bd]
+            args[i] = t + eps * v
+            up = loss(*args)
+            args[i] = t - eps * v
+            down = loss(*args)
+            size = ((up.abs() + down.abs() + 16) * gd.abs()).double().sum().item()
+            diff = ((up.double() - down.double()) * gd.double()).sum().item() / (2 * eps)
+            want = (grads[i].double() * v.double()).sum().item()
+            dx = {0: lambda: v @ Wd, 1: lambda: hd @ v, 2: lambda: v[None].expand(N, V)}[i]().double()
+            spread = (dx.max(1).values - dx.min(1).values) ** 3
+            lim = eps ** 2 / 6 * (gd.abs().double() * spread).sum().item() + 2.0 ** -20 * size / (2 * eps)
+            assert abs(diff - want) <= lim, f"{name}, argument {i}: {diff} and {want}, {lim}"
+
+
+def test_student_learns_from_a_teacher_through_the_step(kb):
+    """As they are used together: a teacher's step gives every row's best words, the student is distilled from them, and
+    the update goes down the gradient."""
+    N, H, V, k = 96, 64, 3000, 8
+    g = torch.Generator().manual_seed(31)
+    ht, Wt = torch.randn((N, 128), generator=g).to(BF16).cuda(), (torch.randn((128, V), generator=g) / 11).to(BF16).cuda()
+    bt = torch.zeros(V, device="cuda")
+    _, h, W, b, _, _ = make(32, BF16, N, H, V)
+    hd, Wd, bd = dev(h, W, b)
+    off = torch.arange(N + 1, dtype=torch.int32, device="cuda")
+    token, parent, score = kb.kbest_step(ht, Wt, bt, torch.zeros(N, device="cuda"), off, k)
+    assert (parent == off[:N, None]).all()
+    loss, lse = kb.distill(hd, Wd, bd, token, score, temperature=2.0)
+    grad = torch.full((N,), 1.0 / N, device="cuda")
+    dh, dW, db = kb.distill_grad(hd, Wd, bd, token, score, lse, grad, temperature=2.0)
+    o = lo.distill(f64(h), f64(W), f64(b), token.cpu().numpy(), f64(score), 2.0)
+    bnd = lo.bounds(o, f64(h), f64(W), f64(b), False, f64(grad), k)
+    check_rows(o, bnd, loss, lse, "student")
+    check_grads(o, bnd, h, W, grad.cpu(), (dh, dW, db), BF16, "student")
+    # the greedy step's logit less the cross entropy's lse is the best word's log-probability
+    best, x = kb.argmax_step(hd, Wd, bd)
+    ce, lse1 = kb.cross_entropy(hd, Wd, bd, best)
+    assert (ce - (lse1 - x)).abs().max() <= 1e-4
