@@ -126,7 +126,7 @@ __device__ __forceinline__ void dw_tile(const LossGradArgs& a, uint32_t ring, in
       return;
     }
     if constexpr (PASSES <= 2) {
-      store_bf16<T>(acc, 0, lds, [&](int row, int word, const bf16x8& v) {
+      store_bf16<T>(acc, lds, [&](int row, int word, const bf16x8& v) {
         if (n0 + row < a.H && m0 + word < a.words)
           write8(static_cast<uint16_t*>(a.out) + (size_t)(n0 + row) * a.V + m0 + word, v, a.words - m0 - word);
       });

@@ -11,9 +11,10 @@
 //
 // Words are the M side: a lane has 64 (small tiles: 32) words of each of its rows, so statistics need no exchange
 // until the end.  The accumulators start at the bias; words that only fill the last tile up start at -inf.
-// Entries were sorted into a list for each wave's part of each tile.  A wave takes one to four one by one, with scalar
-// loads, and picks the register by a branch; more go through LDS, a lane each (a teacher's words cluster where the
-// vocabulary's frequent words are: half of 64 a row in one tile of 256 words).
+// Entries were sorted into lists by the 32 x 32 block that holds their logits.  A block with entries goes through LDS of
+// the wave's own, from its accumulators to the entries' lanes or the other way: picking registers for one entry after
+// the other took 1.5 ms more for 4,096 rows of 64 words of 60,000, as a teacher's words cluster where the vocabulary's
+// frequent words are (half of the 64 in one tile of 256).
 #pragma once
 
 #include "loss_mm.hpp"
@@ -51,19 +52,11 @@ __device__ __forceinline__ void loss_cell(int R, int P, int b, int& rt, int& sp)
   rt = rg * GR + (q - sp * gr);
 }
 
-// bf16 piece `plane` of x.
-__device__ __forceinline__ float piece(float x, int plane) {
-  const float p0 = (float)(__bf16)x;
-  if (plane == 0) return p0;
-  const float r = x - p0, p1 = (float)(__bf16)r;
-  return plane == 1 ? p1 : r - p1;
-}
-
 // A tile as bf16 to rows of `out` (row n of the tile at out + n * ld, words along it), through the LDS buffer `lds`
 // of one stage, 32 words of every wave at a time: 16 bytes a lane, 64 in a row, where the accumulators alone would
 // give eight.  write(row, word, v): rows and words of the tile, v: 8 values.
 template <class T, class Write>
-__device__ __forceinline__ void store_bf16(f32x16 (&acc)[T::MB][T::NB], int plane, uint32_t lds, Write write) {
+__device__ __forceinline__ void store_bf16(f32x16 (&acc)[T::MB][T::NB], uint32_t lds, Write write) {
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
   const int wave = tid >> 6, wm = wave % T::WM, wn = wave / T::WM;
   constexpr int CH = T::WM * 4;  // 16-byte chunks of a row
@@ -79,7 +72,7 @@ __device__ __forceinline__ void store_bf16(f32x16 (&acc)[T::MB][T::NB], int plan
       for (int i = 0; i < 4; ++i) {
         bf16x4 v;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = (__bf16)piece(acc[m][n][4 * i + j], plane);
+        for (int j = 0; j < 4; ++j) v[j] = (__bf16)acc[m][n][4 * i + j];
         *(KB_LDS bf16x4*)(uintptr_t)(lds + (uint32_t)(row * CH + ((wm * 4 + i) ^ (row & (CH - 1)))) * 16u + half * 8u) = v;
       }
     }
@@ -93,7 +86,7 @@ __device__ __forceinline__ void store_bf16(f32x16 (&acc)[T::MB][T::NB], int plan
   }
 }
 
-// Entries of a wave's part of a tile that are taken one by one; more go through LDS.
+// As many entries of a wave's part of a tile are read by scalar loads.
 constexpr int kFewEntries = 4;
 
 template <class T>
@@ -402,7 +395,8 @@ __global__ __launch_bounds__(256, (LossOcc<T>::N)) void loss_logits(LossLogitsAr
     else
       epi_stats(t, acc, lds);
   };
-  mm_run<T, true, false, PASSES == 1, std::conditional_t<PASSES == 1, MmOne, MmSix>, STORES>(lds_addr(ring), nt, a.Hk / kLossStage, tile, init, epi);
+  using Passes = std::conditional_t<PASSES == 1, MmOne, MmSix>;
+  mm_run<T, true, false, PASSES == 1, Passes, STORES>(lds_addr(ring), nt, a.Hk / kLossStage, tile, init, epi);
 
   if constexpr (!GRAD) {
     // the row's holders: two lane halves, and the waves along the words

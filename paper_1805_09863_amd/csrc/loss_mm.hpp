@@ -80,7 +80,6 @@ struct MmPasses {
 };
 using MmOne = MmPasses<1, 0, 0>;
 using MmTwoA = MmPasses<2, 0u | 1u << 2, 0>;  // A in two pieces
-using MmTwoB = MmPasses<2, 0, 0u | 1u << 2>;
 // float32: (0,0) (0,1) (1,0) (1,1) (0,2) (2,0)
 using MmSix = MmPasses<6, 0u | 0u << 2 | 1u << 4 | 1u << 6 | 0u << 8 | 2u << 10,
                        0u | 1u << 2 | 0u << 4 | 1u << 6 | 2u << 8 | 0u << 10>;
