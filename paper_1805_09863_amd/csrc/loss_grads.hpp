@@ -126,10 +126,18 @@ __device__ __forceinline__ void dw_tile(const LossGradArgs& a, uint32_t ring, in
       return;
     }
     if constexpr (PASSES <= 2) {
-      store_bf16<T>(acc, lds, [&](int row, int word, const bf16x8& v) {
-        if (n0 + row < a.H && m0 + word < a.words)
-          write8(static_cast<uint16_t*>(a.out) + (size_t)(n0 + row) * a.V + m0 + word, v, a.words - m0 - word);
-      });
+#pragma unroll
+      for (int m = 0; m < T::MB; ++m) {
+        const int r0 = n0 + wn * T::WTN, w0 = m0 + wm * T::WTM + m * 32;
+#pragma unroll
+        for (int n = 0; n < T::NB; ++n) in_acc(acc[m][n]);
+        store_rows<T>(lds + wave * (T::WTN * 64), [&](int n, int r) { return (__bf16)acc[m][n][r]; },
+                      [&](int row, int word, const bf16x8& v) {
+                        if (r0 + row < a.H && w0 + word < a.words)
+                          write8(static_cast<uint16_t*>(a.out) + (size_t)(r0 + row) * a.V + w0 + word, v,
+                                 a.words - w0 - word);
+                      });
+      }
     } else {
 #pragma unroll
       for (int m = 0; m < T::MB; ++m)

@@ -52,37 +52,29 @@ __device__ __forceinline__ void loss_cell(int R, int P, int b, int& rt, int& sp)
   rt = rg * GR + (q - sp * gr);
 }
 
-// A tile as bf16 to rows of `out` (row n of the tile at out + n * ld, words along it), through the LDS buffer `lds`
-// of one stage, 32 words of every wave at a time: 16 bytes a lane, 64 in a row, where the accumulators alone would
-// give eight.  write(row, word, v): rows and words of the tile, v: 8 values.
-template <class T, class Write>
-__device__ __forceinline__ void store_bf16(f32x16 (&acc)[T::MB][T::NB], uint32_t lds, Write write) {
-  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
-  const int wave = tid >> 6, wm = wave % T::WM, wn = wave / T::WM;
-  constexpr int CH = T::WM * 4;  // 16-byte chunks of a row
-  static_assert(T::BN * CH * 16 <= MmGeom<T::BM>::BYTES + MmGeom<T::BN>::BYTES, "fits in a stage");
+// 32 words of a wave's rows as bf16, through LDS of the wave's own (64 bytes a row, in 16-byte chunks that are swizzled
+// by the row), to rows of memory: 16 bytes a lane, 64 in one piece, where the accumulators alone would give eight.
+// Waves need not wait for each other: a wave's LDS operations are done in their order.
+// value(n, r): register r of the rows of block n; write(row, word, v): within the wave's part, v: 8 values.
+template <class T, class Value, class Write>
+__device__ __forceinline__ void store_rows(uint32_t mine, Value value, Write write) {
+  const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
 #pragma unroll
-  for (int m = 0; m < T::MB; ++m) {
-    lds_barrier();
+  for (int n = 0; n < T::NB; ++n) {
+    const int row = n * 32 + col;
 #pragma unroll
-    for (int n = 0; n < T::NB; ++n) {
-      in_acc(acc[m][n]);
-      const int row = wn * T::WTN + n * 32 + col;
+    for (int i = 0; i < 4; ++i) {
+      bf16x4 v;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        bf16x4 v;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = (__bf16)acc[m][n][4 * i + j];
-        *(KB_LDS bf16x4*)(uintptr_t)(lds + (uint32_t)(row * CH + ((wm * 4 + i) ^ (row & (CH - 1)))) * 16u + half * 8u) = v;
-      }
+      for (int j = 0; j < 4; ++j) v[j] = value(n, 4 * i + j);
+      *(KB_LDS bf16x4*)(uintptr_t)(mine + (uint32_t)(row * 64 + (i ^ hswz(row)) * 16 + half * 8)) = v;
     }
-    lds_barrier();
+  }
 #pragma unroll
-    for (int k = 0; k < T::BN * CH / 256; ++k) {
-      const int at = k * 256 + tid, row = at / CH, c = at % CH;
-      const bf16x8 v = *(const KB_LDS bf16x8*)(uintptr_t)(lds + (uint32_t)(row * CH + (c ^ (row & (CH - 1)))) * 16u);
-      write(row, (c >> 2) * T::WTM + m * 32 + (c & 3) * 8, v);
-    }
+  for (int k = 0; k < T::WTN / 16; ++k) {
+    const int row = k * 16 + (lane >> 2), c = lane & 3;
+    const bf16x8 v = *(const KB_LDS bf16x8*)(uintptr_t)(mine + (uint32_t)(row * 64 + (c ^ hswz(row)) * 16));
+    write(row, c * 8, v);
   }
 }
 
@@ -284,15 +276,13 @@ __global__ __launch_bounds__(256, (LossOcc<T>::N)) void loss_logits(LossLogitsAr
       asm volatile("" ::"v"(st_s[n]));  // one row's 64 logits in VGPRs at a time
     }
   };
-  // dlogits, 32 words of every wave at a time: from the accumulators through the entries, the bias' sums and the
-  // rounding to LDS, and from there to memory in rows (64 bytes in one piece, where the accumulators alone would give 8)
+  // dlogits, 32 words at a time: from the accumulators through the entries, the bias' sums and the rounding to memory
   auto epi_grad = [&](int t, f32x16 (&acc)[MB][NB], uint32_t lds) {
     const auto& a = *args_again<Args>();
     const int v0 = (sp + t * P) * kLossM;
     const int left = a.words - v0 - wm * T::WTM - 4 * half;
     const bool ragged = v0 + kLossM > a.words && a.rest != 0.f;
-    constexpr int CH = T::WM * 4;  // 16-byte chunks of a row of the tile's 32 words a wave
-    static_assert(BN * CH * 16 <= LossOcc<T>::STAGE && 4 * 32 * 36 * 4 <= LossOcc<T>::STAGE, "fit in a stage");
+    static_assert(4 * T::WTN * 64 <= LossOcc<T>::STAGE && 4 * 32 * 36 * 4 <= LossOcc<T>::STAGE, "fit in a stage");
     const uint32_t mine = (APART ? lds_addr(apart) : lds) + wave * (32 * 36 * 4);
     const uint32_t words = mine + (uint32_t)(col * 36 + 4 * half) * 4u;
     Entries e;
@@ -306,8 +296,6 @@ __global__ __launch_bounds__(256, (LossOcc<T>::N)) void loss_logits(LossLogitsAr
     }
 #pragma unroll
     for (int m = 0; m < MB; ++m) {
-      if constexpr (!APART)
-        if (m > 0) lds_barrier();  // the entries' LDS is that of the rows before
       float x[NB][16];
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
@@ -362,33 +350,18 @@ __global__ __launch_bounds__(256, (LossOcc<T>::N)) void loss_logits(LossLogitsAr
       }
 #pragma unroll
       for (int pl = 0; pl < PLANES; ++pl) {
-        if (pl > 0 || m > 0 || !APART) lds_barrier();
-#pragma unroll
-        for (int n = 0; n < NB; ++n) {
-          const int row = wn * T::WTN + n * 32 + col;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            bf16x4 v;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              v[j] = (__bf16)x[n][4 * i + j];
-              if (pl + 1 < PLANES) x[n][4 * i + j] -= (float)v[j];
-            }
-            *(KB_LDS bf16x4*)(uintptr_t)(lds + (uint32_t)(row * CH + ((wm * 4 + i) ^ (row & (CH - 1)))) * 16u + half * 8u) = v;
-          }
-        }
-        lds_barrier();
-        uint16_t* out = a.g + pl * a.g_plane + (size_t)rt * BN * a.gld + v0;
-#pragma unroll
-        for (int k = 0; k < BN * CH / 256; ++k) {
-          const int at = k * 256 + tid, row = at / CH, c = at % CH;
-          *reinterpret_cast<bf16x8*>(out + (size_t)row * a.gld + (c >> 2) * T::WTM + m * 32 + (c & 3) * 8) =
-              *(const KB_LDS bf16x8*)(uintptr_t)(lds + (uint32_t)(row * CH + (c ^ (row & (CH - 1)))) * 16u);
-        }
+        uint16_t* out = a.g + pl * a.g_plane + (size_t)(rt * BN + wn * T::WTN) * a.gld + v0 + wm * T::WTM + m * 32;
+        store_rows<T>(APART ? lds + wave * (T::WTN * 64) : mine, [&](int n, int r) {
+          const __bf16 v = (__bf16)x[n][r];
+          if (pl + 1 < PLANES) x[n][r] -= (float)v;
+          return v;
+        }, [&](int row, int word, const bf16x8& v) {
+          *reinterpret_cast<bf16x8*>(out + (size_t)row * a.gld + word) = v;
+        });
       }
     }
   };
-  constexpr int STORES = MB * PLANES * (BN * T::WM * 4 / 256);
+  constexpr int STORES = MB * PLANES * (T::WTN / 16);
   auto epi = [&](int t, f32x16 (&acc)[MB][NB], uint32_t lds) {
     if constexpr (GRAD)
       epi_grad(t, acc, lds);
