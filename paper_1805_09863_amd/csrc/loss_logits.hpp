@@ -78,6 +78,28 @@ __device__ __forceinline__ void store_rows(uint32_t mine, Value value, Write wri
   }
 }
 
+template <int CTRL>
+__device__ __forceinline__ float dpp_of(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+
+// s[0 .. 16) summed over each half's 32 lanes: lane i gets value (i & 31) / 2.  Rows of 16 lanes swap halves of the
+// values; within a row, lanes keep half of what is left and take their mirror image's other half.
+__device__ __forceinline__ float sum32(float (&s)[16], int lane) {
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(s[r]), __float_as_uint(s[r + 8]), false, false);
+    s[r] = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  }
+  const bool b3 = (lane & 8) != 0, b2 = (lane & 4) != 0, b1 = (lane & 2) != 0;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) s[r] = (b3 ? s[r + 4] : s[r]) + dpp_of<0x140>(b3 ? s[r] : s[r + 4]);  // row_mirror
+#pragma unroll
+  for (int r = 0; r < 2; ++r) s[r] = (b2 ? s[r + 2] : s[r]) + dpp_of<0x141>(b2 ? s[r] : s[r + 2]);  // row_half_mirror
+  s[0] = (b1 ? s[1] : s[0]) + dpp_of<0x1b>(b1 ? s[0] : s[1]);                                       // quad_perm 3 2 1 0
+  return s[0] + dpp_of<0xb1>(s[0]);                                                                 // quad_perm 1 0 3 2
+}
+
 // As many entries of a wave's part of a tile are read by scalar loads.
 constexpr int kFewEntries = 4;
 
@@ -328,25 +350,19 @@ __global__ __launch_bounds__(256, (LossOcc<T>::N)) void loss_logits(LossLogitsAr
         }
       }
       if (a.dbp) {
-        // over the wave's rows: its blocks in registers, the 32 lanes through LDS (a word's 32 sums 36 floats apart), a
-        // lane half a word's
+        // over the wave's rows: its blocks in registers, then the 32 lanes by halving the words that a lane keeps
+        float s[16];
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          float s = x[0][r];
+          s[r] = x[0][r];
 #pragma unroll
-          for (int n = 1; n < NB; ++n) s += x[n][r];
-          *(KB_LDS float*)(uintptr_t)(mine + (uint32_t)((8 * (r >> 2) + 4 * half + (r & 3)) * 36 + col) * 4u) = s;
+          for (int n = 1; n < NB; ++n) s[r] += x[n][r];
         }
-        const uint32_t from = mine + (uint32_t)((lane >> 1) * 36 + (lane & 1) * 16) * 4u;
-        float s = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x4v v = *(const KB_LDS f32x4v*)(uintptr_t)(from + i * 16u);
-          s += (v[0] + v[1]) + (v[2] + v[3]);
-        }
-        s += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(s), 0xb1, 0xf, 0xf, true));  // its neighbour's
+        const float sum = sum32(s, lane);
+        const int r = col >> 1;  // the word whose sum the lane has: bits 4 .. 1 of the lane
         if ((lane & 1) == 0)
-          a.dbp[(size_t)(rt * T::WN + wn) * a.db_ld + a.db0 + v0 + wm * T::WTM + m * 32 + (lane >> 1)] = s;
+          a.dbp[(size_t)(rt * T::WN + wn) * a.db_ld + a.db0 + v0 + wm * T::WTM + m * 32 + 8 * (r >> 2) + 4 * half + (r & 3)] =
+              sum;
       }
 #pragma unroll
       for (int pl = 0; pl < PLANES; ++pl) {
