@@ -137,7 +137,7 @@ struct LossGradArgs {
   const uint16_t* g;     // packed rows x words of the piece
   size_t g_plane;
   int gld, vt;           // words of the piece with its last tile filled up, word tiles
-  int N, BN;             // BN: the row tile that g was made with
+  int N;
   const int32_t* count;
   int splits;            // of the long axis
   int mt, ntn;           // tiles along M and N (dh: states, rows; dW: words, states)

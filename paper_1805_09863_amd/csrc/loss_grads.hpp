@@ -67,15 +67,56 @@ __device__ __forceinline__ void dh_tile(const LossGradArgs& a, uint32_t ring, in
   mm_run<T, false, false, true, std::conditional_t<PASSES == 1, MmOne, MmSix>, 0>(ring, 1, s1 - s0, tile, init, epi);
 }
 
-// 8 bf16 values to out, `left` of which exist.
-__device__ __forceinline__ void write8(uint16_t* out, const bf16x8& v, int left) {
-  if (left >= 8 && (uintptr_t)out % 16 == 0) {
-    *reinterpret_cast<bf16x8*>(out) = v;
-    return;
-  }
+// A wave's part of a tile to rows of memory, `out` its first element, `left_rows` x `left` of which exist: 32 rows at a
+// time through LDS of the wave's own, 128 or 256 bytes a row in 16-byte chunks that are swizzled by the row, and from
+// there 16 bytes a lane at any element's address (written from the accumulators, 8 or 16 bytes a lane, rows of an odd
+// length by single values: 1,111 x 500 x 32,001 251 us and 214; 4,096 x 1,024 x 50,000 in pieces of 64 bytes 1,475 us
+// and 1,460).
+template <class T, class D>
+__device__ __forceinline__ void store_tile(uint32_t mine, f32x16 (&acc)[T::MB][T::NB], D* out, size_t ld, int left_rows,
+                                           int left) {
+  typedef D Quad __attribute__((ext_vector_type(4)));
+  typedef D Chunk __attribute__((ext_vector_type(16 / sizeof(D))));
+  typedef Chunk AnyChunk __attribute__((aligned(sizeof(D))));
+  constexpr int WORDS = 16 / sizeof(D);                 // of a chunk
+  constexpr int CH = T::BN == 256 ? 16 : 8;             // chunks of a row
+  constexpr int BLK = 32 / WORDS, MG = CH / BLK;        // chunks of a block, blocks of a row
+  static_assert(4 * 32 * CH * 16 <= LossOcc<T>::STAGE && T::MB % MG == 0, "fits in a stage");
+  const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31, c = lane % CH;
+  auto at = [&](int row, int chunk) { return mine + (uint32_t)(row * CH * 16 + (chunk ^ (row & (CH - 1))) * 16); };
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (i < left) reinterpret_cast<__bf16*>(out)[i] = v[i];
+  for (int m = 0; m < T::MB; m += MG) {
+    const int word = m * 32 + c * WORDS;
+#pragma unroll
+    for (int n = 0; n < T::NB; ++n) {
+#pragma unroll
+      for (int u = 0; u < MG; ++u) {
+        const f32x16& x = acc[m + u][n];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          Quad v;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] = (D)x[4 * i + j];
+          const int byte = (8 * i + 4 * half) * sizeof(D);  // within the block's row
+          *(KB_LDS Quad*)(uintptr_t)(at(col, u * BLK + byte / 16) + byte % 16) = v;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < CH / 2; ++k) {
+        const int r = k * (64 / CH) + lane / CH, row = n * 32 + r;
+        const Chunk v = *(const KB_LDS Chunk*)(uintptr_t)at(r, c);
+        D* to = out + (size_t)row * ld + word;
+        if (row >= left_rows) continue;
+        if (left - word >= WORDS) {
+          *reinterpret_cast<AnyChunk*>(to) = v;
+        } else {
+#pragma unroll
+          for (int q = 0; q < WORDS; ++q)
+            if (q < left - word) to[q] = v[q];
+        }
+      }
+    }
+  }
 }
 
 // Tiles c, c + step, ... below `cells` of the tiles and splits of dW (all the splits of a workgroup's tiles have the
@@ -83,10 +124,9 @@ __device__ __forceinline__ void write8(uint16_t* out, const bf16x8& v, int left)
 // pieces) or 6 (float32).
 template <class T, int PASSES>
 __device__ __forceinline__ void dw_tile(const LossGradArgs& a, uint32_t ring, int rows, int first, int step, int cells) {
-  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave % T::WM, wn = wave / T::WM;
-  const int stages = loss_row_tiles(rows, a.BN) * a.BN / kLossStage;
+  const int stages = (rows + kLossStage - 1) / kLossStage;
   const int tiles = a.mt * a.ntn, nt = (cells - first + step - 1) / step;
   // (a division leaves its quotient in a vector register)
   auto stage0 = [&](int split) { return __builtin_amdgcn_readfirstlane((int)((long long)stages * split / a.splits)); };
@@ -125,42 +165,12 @@ __device__ __forceinline__ void dw_tile(const LossGradArgs& a, uint32_t ring, in
       }
       return;
     }
-    if constexpr (PASSES <= 2) {
+    using D = std::conditional_t<PASSES <= 2, __bf16, float>;
 #pragma unroll
-      for (int m = 0; m < T::MB; ++m) {
-        const int r0 = n0 + wn * T::WTN, w0 = m0 + wm * T::WTM + m * 32;
-#pragma unroll
-        for (int n = 0; n < T::NB; ++n) in_acc(acc[m][n]);
-        store_rows<T>(lds + wave * (T::WTN * 64), [&](int n, int r) { return (__bf16)acc[m][n][r]; },
-                      [&](int row, int word, const bf16x8& v) {
-                        if (r0 + row < a.H && w0 + word < a.words)
-                          write8(static_cast<uint16_t*>(a.out) + (size_t)(r0 + row) * a.V + w0 + word, v,
-                                 a.words - w0 - word);
-                      });
-      }
-    } else {
-#pragma unroll
-      for (int m = 0; m < T::MB; ++m)
-#pragma unroll
-        for (int n = 0; n < T::NB; ++n) {
-          in_acc(acc[m][n]);
-          const int row = n0 + wn * T::WTN + n * 32 + col;
-          if (row >= a.H) continue;
-          float* out = static_cast<float*>(a.out) + (size_t)row * a.V;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int w = m0 + wm * T::WTM + m * 32 + 8 * i + 4 * half;
-            if (w + 4 <= a.words && (uintptr_t)(out + w) % 16 == 0) {
-              *reinterpret_cast<float4*>(out + w) =
-                  make_float4(acc[m][n][4 * i], acc[m][n][4 * i + 1], acc[m][n][4 * i + 2], acc[m][n][4 * i + 3]);
-            } else {
-#pragma unroll
-              for (int j = 0; j < 4; ++j)
-                if (w + j < a.words) out[w + j] = acc[m][n][4 * i + j];
-            }
-          }
-        }
-    }
+    for (int i = 0; i < T::MB * T::NB; ++i) in_acc(acc[i / T::NB][i % T::NB]);
+    const int r0 = n0 + wn * T::WTN, w0 = m0 + wm * T::WTM;
+    store_tile<T>(lds + wave * (LossOcc<T>::STAGE / 4 / 16 * 16), acc, static_cast<D*>(a.out) + (size_t)r0 * a.V + w0, a.V,
+                  a.H - r0, a.words - w0);
   };
   mm_run<T, true, true, false, std::conditional_t<PASSES == 1, MmOne, std::conditional_t<PASSES == 2, MmTwoA, MmSix>>, 0>(
       ring, nt, stages_of(first), tile, init, epi);
