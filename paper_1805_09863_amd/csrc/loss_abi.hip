@@ -102,7 +102,7 @@ Plan make_plan(int dtype, int N, int H, int V, int K, bool teacher, bool grad, b
   p.g_planes = !p.bf16 ? 3 : N <= 128 ? 2 : 1;
   p.z = p.bf16 ? 2 : 4;
   p.N = N, p.H = H, p.V = V, p.K = K;
-  p.few = kb::few_fits(N, H);
+  p.few = kb::few_fits(p.bf16, N, H, V);
   if (p.few) {
     Space s;
     p.grid = kb::few_grid(p.bf16, V);

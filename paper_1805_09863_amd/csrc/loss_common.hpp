@@ -224,7 +224,7 @@ struct LossFewArgs {
   float* db;
 };
 int few_held(int N);                       // rows that a workgroup holds for N
-bool few_fits(int N, int H);               // the few rows' kernels take this size
+bool few_fits(bool bf16, int N, int H, int V);  // the few rows' kernels take this size
 int few_grid(bool bf16, int V);
 hipError_t launch_loss_few(bool bf16, bool grad, const LossFewArgs& a, hipStream_t st);
 hipError_t launch_loss_few_finish(const LossFewArgs& a, hipStream_t st);

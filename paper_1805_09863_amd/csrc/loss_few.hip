@@ -1,12 +1,15 @@
 // The losses of at most eight rows: W is read once (twice for its gradient) and everything else is small, so the
 // vector ALUs do, in float32 whatever the operands' type, and W needs no laying out, whatever its alignment.
 //
-// A workgroup takes chunks of 16 x 16 bytes of words (64 float32, 128 bf16): 16 threads of 16 bytes each along the
-// words, 16 slices along the states.  Forward: every thread sums its words' products over its slice's states for all
-// rows, the states in LDS; the slices are summed through LDS; one wave a row takes the chunk into the row's running
-// (max, sum), and threads pick the entries' logits.  Gradient: the same logits become dlogits in LDS, and a second walk
-// over the states gives dW (a product over the rows, written as it comes) and the chunk's part of dh (summed over the
-// 16 threads by halving what a lane keeps), which the workgroup adds up over its chunks in LDS.
+// A workgroup takes chunks of 16 (few words: 8) x 16 bytes of words: threads of 16 bytes each along the words, and 16 or
+// 32 slices along the states.  Forward: every thread sums its words' products over its slice's states for all rows, the
+// states in LDS; the slices are summed through LDS; one wave a row takes the chunk into the row's running (max, sum),
+// and threads pick the entries' logits.  Gradient: the same logits become dlogits in LDS, and a second walk over the
+// states gives dW (a product over the rows, written as it comes) and the chunk's part of dh (summed over the threads
+// along the words by halving what a lane keeps), which the workgroup adds up over its chunks in LDS.
+//
+// 8 rows of float32, 1,024 x 32,000: 42 us (3.2 TB/s, one reading of W), with gradients 141 (3.7 TB/s, three passes over
+// its size); 5 x 256 x 8,000 is bound by the launches (11 and 4 us of kernels; with gradients 37 in four).
 #include <algorithm>
 #include <type_traits>
 
@@ -19,7 +22,6 @@ typedef __bf16 bf16x8f __attribute__((ext_vector_type(8)));
 template <class S>
 struct FewWords {
   static constexpr int N = 16 / sizeof(S);  // of a thread
-  static constexpr int CHUNK = 16 * N;
 };
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -87,11 +89,11 @@ __device__ __forceinline__ float dpp(float x) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
 }
 
-// v[0 .. NR) summed over the 16 lanes of a row; lane i gets value (i >> 1 & ..): the one its bits 3, 2, 1 (from the
-// top, as many as NR needs) name, the same in the lanes that differ in the others.
-template <int NR>
-__device__ __forceinline__ float few_sum16(float (&v)[NR], int i) {
-  // steps across bit 3 (mirror of 16), bit 2 (mirror of 8), bit 1 (quad 3 2 1 0), bit 0 (quad 1 0 3 2)
+// v[0 .. NR) summed over TW lanes in a row, 16 or 8 (i: the lane among them); lane i gets the value that its bits name
+// from the top, as many as NR needs, the same in the lanes that differ in the others.
+template <int NR, int TW>
+__device__ __forceinline__ float few_sum(float (&v)[NR], int i) {
+  static_assert((TW == 16 || TW == 8) && NR <= 8, "at most eight values");
   auto step = [&](auto n_c, bool upper, auto move) {
     constexpr int n = decltype(n_c)::value;  // values kept before
     if constexpr (n > 1) {
@@ -104,18 +106,18 @@ __device__ __forceinline__ float few_sum16(float (&v)[NR], int i) {
       v[0] += move(v[0]);
     }
   };
-  constexpr int n1 = NR, n2 = n1 > 1 ? n1 / 2 : 1, n3 = n2 > 1 ? n2 / 2 : 1, n4 = n3 > 1 ? n3 / 2 : 1;
-  static_assert(n4 == 1, "at most eight values");
-  step(std::integral_constant<int, n1>{}, (i & 8) != 0, [](float x) { return dpp<0x140>(x); });  // row_mirror
-  step(std::integral_constant<int, n2>{}, (i & 4) != 0, [](float x) { return dpp<0x141>(x); });  // row_half_mirror
-  step(std::integral_constant<int, n3>{}, (i & 2) != 0, [](float x) { return dpp<0x1b>(x); });   // quad_perm 3 2 1 0
-  step(std::integral_constant<int, n4>{}, false, [](float x) { return dpp<0xb1>(x); });          // quad_perm 1 0 3 2
+  auto half = [](int n) { return n > 1 ? n / 2 : 1; };
+  constexpr int n3 = TW == 16 ? half(NR) : NR, n2 = half(n3), n1 = half(n2);
+  if constexpr (TW == 16) step(std::integral_constant<int, NR>{}, (i & 8) != 0, [](float x) { return dpp<0x140>(x); });  // row_mirror
+  step(std::integral_constant<int, n3>{}, (i & 4) != 0, [](float x) { return dpp<0x141>(x); });  // row_half_mirror
+  step(std::integral_constant<int, n2>{}, (i & 2) != 0, [](float x) { return dpp<0x1b>(x); });   // quad_perm 3 2 1 0
+  step(std::integral_constant<int, n1>{}, (i & 1) != 0, [](float x) { return dpp<0xb1>(x); });   // quad_perm 1 0 3 2
   return v[0];
 }
 
-template <class S, int NR, bool GRAD>
+template <class S, int NR, bool GRAD, int TW>
 __global__ __launch_bounds__(256) void loss_few(LossFewArgs a) {
-  constexpr int NW = FewWords<S>::N, CH = FewWords<S>::CHUNK;
+  constexpr int NW = FewWords<S>::N, CH = TW * NW, NS = 256 / TW;  // words of a chunk, slices
   extern __shared__ float dyn[];
   float* hs = dyn;                                  // H x NR states
   float* dhs = hs + (size_t)a.H * NR;               // H x NR (gradient)
@@ -125,7 +127,7 @@ __global__ __launch_bounds__(256) void loss_few(LossFewArgs a) {
   float* part = rowv + 2 * NR;                      // NR x K (gradient)
   int* tok = reinterpret_cast<int*>(part + (GRAD ? NR * a.K : 0));  // NR x K
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int ws = tid & 15, slice = tid >> 4;
+  const int ws = tid % TW, slice = tid / TW;
   const S* W = static_cast<const S*>(a.W);
   const S* h = static_cast<const S*>(a.h);
   const int N = a.N, H = a.H, V = a.V, K = a.K;
@@ -196,34 +198,35 @@ __global__ __launch_bounds__(256) void loss_few(LossFewArgs a) {
     if (left >= NW) {
       constexpr int U = 8;  // loads under way
       int k = slice;
-      for (; k + 16 * (U - 1) < H; k += 16 * U) {
+      for (; k + NS * (U - 1) < H; k += NS * U) {
         float w[U][NW];
 #pragma unroll
-        for (int u = 0; u < U; ++u) few_load<true>(Wc + (size_t)(k + 16 * u) * V, left, w[u]);
+        for (int u = 0; u < U; ++u) few_load<true>(Wc + (size_t)(k + NS * u) * V, left, w[u]);
 #pragma unroll
-        for (int u = 0; u < U; ++u) take(k + 16 * u, w[u]);
+        for (int u = 0; u < U; ++u) take(k + NS * u, w[u]);
       }
-      for (; k < H; k += 16) {
+      for (; k < H; k += NS) {
         float w[NW];
         few_load<true>(Wc + (size_t)k * V, left, w);
         take(k, w);
       }
     } else if (left > 0) {
-      for (int k = slice; k < H; k += 16) {
+      for (int k = slice; k < H; k += NS) {
         float w[NW];
         few_load<false>(Wc + (size_t)k * V, left, w);
         take(k, w);
       }
     }
-    // ---- over the slices: four in a wave, then the waves
+    // ---- over the slices: those of a wave, then the waves
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
 #pragma unroll
       for (int i = 0; i < NW; ++i) {
+        if (TW == 8) acc[n][i] += dpp<0x128>(acc[n][i]);  // row_ror by 8
         acc[n][i] += __shfl_xor(acc[n][i], 16, 64);
         acc[n][i] += __shfl_xor(acc[n][i], 32, 64);
       }
-      if (lane < 16) {
+      if (lane < TW) {
 #pragma unroll
         for (int i = 0; i < NW; i += 4)
           *reinterpret_cast<float4*>(&red[(wave * NR + n) * CH + w0 + i]) =
@@ -258,17 +261,18 @@ __global__ __launch_bounds__(256) void loss_few(LossFewArgs a) {
       for (int i = 0; i < RW; ++i) {
         const int n = wave + 4 * i;
         if (n >= NR) continue;
-        float x[CH / 64], m = st_m[i];
+        constexpr int NU = (CH + 63) / 64;
+        float x[NU], m = st_m[i];
 #pragma unroll
-        for (int u = 0; u < CH / 64; ++u) {
-          x[u] = xs[n * CH + u * 64 + lane];
+        for (int u = 0; u < NU; ++u) {
+          x[u] = CH >= 64 || lane < CH ? xs[n * CH + u * 64 + lane] : -INFINITY;
           m = fmaxf(m, x[u]);
         }
         float s = st_s[i] * exp2_fast((st_m[i] - m) * (kL2E * a.inv_t));
 #pragma unroll
-        for (int u = 0; u < CH / 64; ++u) {
+        for (int u = 0; u < NU; ++u) {
           s += exp2_fast((x[u] - m) * (kL2E * a.inv_t));
-          if (v0 + u * 64 + lane < V) st_x[i] += x[u];
+          if ((CH >= 64 || lane < CH) && v0 + u * 64 + lane < V) st_x[i] += x[u];
         }
         st_m[i] = m;
         st_s[i] = s;
@@ -314,24 +318,24 @@ __global__ __launch_bounds__(256) void loss_few(LossFewArgs a) {
 #pragma unroll
                 for (int i = 0; i < NW; ++i) v[n] = fmaf(g[n][i], w[i], v[n]);
               }
-              const float s = few_sum16<NR>(v, ws);
-              constexpr int SH = NR == 8 ? 1 : NR == 4 ? 2 : NR == 2 ? 3 : 4;  // 2^SH lanes have the same value
-              if ((ws & ((1 << SH) - 1)) == 0) dhs[k * NR + (ws >> SH)] += s;
+              const float s = few_sum<NR, TW>(v, ws);
+              constexpr int SAME = TW / NR;  // lanes that have the same value
+              if (ws % SAME == 0) dhs[k * NR + ws / SAME] += s;
             }
           };
           int k = slice;
           if constexpr (ALL) {
-            for (; k + 16 * (U - 1) < H; k += 16 * U) {
+            for (; k + NS * (U - 1) < H; k += NS * U) {
               float w[U][NW];
               if constexpr (DH) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) few_load<true>(Wc + (size_t)(k + 16 * u) * V, left, w[u]);
+                for (int u = 0; u < U; ++u) few_load<true>(Wc + (size_t)(k + NS * u) * V, left, w[u]);
               }
 #pragma unroll
-              for (int u = 0; u < U; ++u) turn(k + 16 * u, w[u]);
+              for (int u = 0; u < U; ++u) turn(k + NS * u, w[u]);
             }
           }
-          for (; k < H; k += 16) {
+          for (; k < H; k += NS) {
             float w[NW];
             if constexpr (DH) few_load<ALL>(Wc + (size_t)k * V, left, w);
             turn(k, w);
@@ -339,7 +343,7 @@ __global__ __launch_bounds__(256) void loss_few(LossFewArgs a) {
         };
         using Y = std::true_type;
         using No = std::false_type;
-        // the sums over 16 lanes are all lanes' work: one that has no words, or not all, takes its whole wave along
+        // the sums over lanes are all lanes' work: one that has no words, or not all, takes its whole wave along
         if (__builtin_amdgcn_ballot_w64(left < NW) == 0ull) {
           if (a.dW && a.dh_part)
             walk(Y{}, Y{}, Y{});
@@ -459,27 +463,37 @@ __global__ __launch_bounds__(1024) void loss_few_join(LossFewArgs a, int held) {
 
 int few_held(int N) { return N <= 1 ? 1 : N <= 2 ? 2 : N <= 4 ? 4 : 8; }
 
-static size_t few_lds(bool bf16, bool grad, int N, int H, int K) {
-  const size_t nr = few_held(N), ch = bf16 ? 128 : 64;
+// Threads along the words: 8 where chunks of 16 would leave half of the card idle (bf16, 8 x 512 x 8,000 with gradients:
+// 42 us, 77 in chunks of 16; 8 x 512 x 32,000: 60 in both, one row 45 and 38).
+static int few_threads(bool bf16, int V) { return V <= 128 * 16 * (bf16 ? 8 : 4) ? 8 : 16; }
+
+static size_t few_lds(bool bf16, bool grad, int N, int H, int K, int threads) {
+  const size_t nr = few_held(N), ch = threads * (bf16 ? 8 : 4);
   return ((size_t)H * nr * (grad ? 2 : 1) + 5 * nr * ch + 2 * nr + nr * K * (grad ? 2 : 1)) * 4;
 }
 
-bool few_fits(int N, int H) { return N <= kFewRows && few_lds(true, true, N, H, kLossMaxK) <= 150 * 1024; }
+// bf16 rows of a large W are the matrix cores' (8 x 1,024 x 32,000: 24 us there and 35 here, with gradients 87 and 97; one
+// row of 1,024 x 60,000 33 and 31, 140 and 168; 8 x 512 x 32,000 21 and 23, 71 and 60).  Those of float32 are not: W would
+// have to be laid out in pieces (8 x 1,024 x 60,000: 275 us there, 80 here).
+bool few_fits(bool bf16, int N, int H, int V) {
+  if (N > kFewRows || few_lds(true, true, N, H, kLossMaxK, 16) > 150 * 1024) return false;
+  return !bf16 || (long long)H * V * (N + 4) <= 1ll << 28;
+}
 
 int few_grid(bool bf16, int V) {
-  const int ch = bf16 ? 128 : 64;
+  const int ch = few_threads(bf16, V) * (bf16 ? 8 : 4);
   return std::min((V + ch - 1) / ch, kFewGrid);
 }
 
-template <class S, bool GRAD>
+template <class S, bool GRAD, int TW>
 static hipError_t few_launch(const LossFewArgs& a, size_t lds, hipStream_t st) {
   const dim3 gr(a.grid), th(256);
   void (*f)(LossFewArgs) = nullptr;
   switch (few_held(a.N)) {
-    case 1: f = loss_few<S, 1, GRAD>; break;
-    case 2: f = loss_few<S, 2, GRAD>; break;
-    case 4: f = loss_few<S, 4, GRAD>; break;
-    default: f = loss_few<S, 8, GRAD>; break;
+    case 1: f = loss_few<S, 1, GRAD, TW>; break;
+    case 2: f = loss_few<S, 2, GRAD, TW>; break;
+    case 4: f = loss_few<S, 4, GRAD, TW>; break;
+    default: f = loss_few<S, 8, GRAD, TW>; break;
   }
   if (lds > 64 * 1024) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(f), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -489,10 +503,16 @@ static hipError_t few_launch(const LossFewArgs& a, size_t lds, hipStream_t st) {
   return hipGetLastError();
 }
 
+template <class S>
+static hipError_t few_launch(bool grad, int threads, const LossFewArgs& a, size_t lds, hipStream_t st) {
+  if (threads == 16) return grad ? few_launch<S, true, 16>(a, lds, st) : few_launch<S, false, 16>(a, lds, st);
+  return grad ? few_launch<S, true, 8>(a, lds, st) : few_launch<S, false, 8>(a, lds, st);
+}
+
 hipError_t launch_loss_few(bool bf16, bool grad, const LossFewArgs& a, hipStream_t st) {
-  const size_t lds = few_lds(bf16, grad, a.N, a.H, a.K);
-  if (bf16) return grad ? few_launch<uint16_t, true>(a, lds, st) : few_launch<uint16_t, false>(a, lds, st);
-  return grad ? few_launch<float, true>(a, lds, st) : few_launch<float, false>(a, lds, st);
+  const int threads = few_threads(bf16, a.V);
+  const size_t lds = few_lds(bf16, grad, a.N, a.H, a.K, threads);
+  return bf16 ? few_launch<uint16_t>(grad, threads, a, lds, st) : few_launch<float>(grad, threads, a, lds, st);
 }
 
 hipError_t launch_loss_few_finish(const LossFewArgs& a, hipStream_t st) {

@@ -135,6 +135,19 @@ def test_cross_entropy(kb, dtype, N, H, V):
     check_ce(kb, dtype, N, H, V)
 
 
+# chunks of 8 and of 16 threads, several of a workgroup; bf16 of a large W in tiles of 32 rows
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,H,V", [(1, 70, 16384), (2, 33, 16385), (4, 100, 8193), (3, 260, 9001), (8, 96, 40001), (7, 40, 70000), (1, 24, 140003), (8, 712, 32001), (3, 1200, 33000)])
+def test_few_rows(kb, dtype, N, H, V):
+    check_ce(kb, dtype, N, H, V, smoothing=0.1)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,H,V", [(8, 48, 30000), (2, 65, 6001), (5, 800, 40000)])
+def test_few_rows_of_a_teacher(kb, dtype, N, H, V):
+    check_kd(kb, dtype, N, H, V, 128, 2.0)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("N,H,V", [(2900, 32, 14000), (1300, 64, 20001), (100, 32, 70000), (20, 64, 140001), (60, 32, 140000)])
 def test_tiles_in_turn(kb, dtype, N, H, V):
