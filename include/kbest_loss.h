@@ -33,7 +33,11 @@
  * do not depend on the order in which workgroups run: the same call gives the
  * same bits.  The states and logits of rows that count, W and the weights of
  * entries must be finite; b may be -inf for words that are to be left out
- * (not all of them).
+ * (not all of them).  The loss of a row whose target or whose smoothed labels
+ * name such a word, or whose teacher gives one a probability above 0, is
+ * +inf; its gradient is as it would be without that.  The gradient works from
+ * x / T - lse in float32, so probabilities are as exact as a float32 lse of
+ * that size is (2^-24 |lse|).
  *
  * Limits (KB_ERR_UNSUPPORTED beyond them): V <= KB_LOSS_MAX_V,
  * H <= KB_LOSS_MAX_H, N <= KB_LOSS_MAX_N, N * K <= 2^30.
@@ -55,7 +59,9 @@ extern "C" {
 /*
  * Workspace bytes of kb_cross_entropy (K = 1) and kb_distill, and of their
  * gradients.  0 for N = 0 and for sizes that the calls refuse.  The gradients'
- * grows with N * H, with H * V only as far as a piece of the vocabulary goes.
+ * grows with N * H and, for db, by N * V / 32 bytes (a row of sums for every
+ * 128 rows); with the logits' N * V and with H * V only as far as a piece of
+ * the vocabulary goes.
  */
 size_t kb_loss_workspace_bytes(int dtype, int N, int H, int V, int K);
 size_t kb_loss_grad_workspace_bytes(int dtype, int N, int H, int V, int K);

@@ -420,7 +420,7 @@ __global__ __launch_bounds__(64) void loss_few_finish(LossFewArgs a) {
   float dot = 0.f;
 #pragma unroll
   for (int u = 0; u < 2; ++u)
-    if (tok[u] >= 0) dot += part[u] * a.xt[n * K + lane + 64 * u];
+    if (tok[u] >= 0 && part[u] != 0.f) dot += part[u] * a.xt[n * K + lane + 64 * u];  // of no weight: also where x = -inf
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) {
     const float mo = __shfl_xor(M, d, 64), so = __shfl_xor(S, d, 64);

@@ -294,7 +294,9 @@ __global__ __launch_bounds__(256) void loss_finish(LossFinishArgs a) {
   float dot = 0.f;
   for (int j = lane; j < K; j += 64) {
     const int t = a.rows.token[(size_t)row * K + j];
-    if (t >= 0 && t < a.rows.V) dot += (a.rows.part ? a.rows.part[(size_t)row * K + j] : a.rows.target_part) * a.xt[(size_t)c * K + j];
+    if (t < 0 || t >= a.rows.V) continue;
+    const float part = a.rows.part ? a.rows.part[(size_t)row * K + j] : a.rows.target_part;
+    if (part != 0.f) dot += part * a.xt[(size_t)c * K + j];  // of no weight: also where x = -inf
   }
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) dot += __shfl_xor(dot, d, 64);

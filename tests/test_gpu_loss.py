@@ -221,6 +221,36 @@ def test_masked_words(kb, dtype, N, H, V):
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("N,H,V", PATHS)
+def test_masked_words_of_a_teacher(kb, dtype, N, H, V):
+    """Teacher and student leave the same words out, the teacher by the lowest finite logit: probabilities of 0 for a
+    word whose logit is -inf.  And a target that is left out: a loss of +inf, with a gradient all the same."""
+    g, h, W, b, target, grad = make(23, dtype, N, H, V)
+    K = 6
+    token = torch.arange(K, dtype=torch.int32).expand(N, K).contiguous()
+    logit = torch.randn((N, K), generator=g)
+    logit[:, 4:] = torch.finfo(F32).min
+    b[4:6] = -math.inf
+    hd, Wd, bd, td, ld, gd = dev(h, W, b, token, logit, grad)
+    loss, lse = kb.distill(hd, Wd, bd, td, ld)
+    o = lo.distill(f64(h), f64(W), f64(b), token.numpy(), f64(logit))
+    bnd = lo.bounds(o, f64(h), f64(W), f64(b), dtype == F32, f64(grad), K)
+    check_rows(o, bnd, loss, lse, "masked by teacher and student")
+    check_grads(o, bnd, h, W, grad, kb.distill_grad(hd, Wd, bd, td, ld, lse, gd), dtype, "masked by teacher and student")
+    target[0] = 5
+    loss, lse = kb.cross_entropy(hd, Wd, bd, target.cuda())
+    o = lo.cross_entropy(f64(h), f64(W), f64(b), target.numpy())
+    assert loss[0].item() == math.inf and np.isposinf(o.loss[0])
+    outs = kb.cross_entropy_grad(hd, Wd, bd, target.cuda(), lse, gd)
+    bnd = lo.bounds(o, f64(h), f64(W), f64(b), dtype == F32, f64(grad))
+    bnd.loss[0] = 1.0  # compared above
+    o.loss[0] = 0.0
+    loss[0] = 0.0
+    check_rows(o, bnd, loss, lse, "a target that is left out")
+    check_grads(o, bnd, h, W, grad, outs, dtype, "a target that is left out")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,H,V", PATHS)
 def test_large_logits(kb, dtype, N, H, V):
     # a word far above all others, and states of very different sizes
     def edit(h, W, b, target, grad):
