@@ -16,8 +16,8 @@ hipError_t launch_loss_dh_bf16(int BN, const LossGradArgs& a, hipStream_t st);
 hipError_t launch_loss_dh_f32(int BN, const LossGradArgs& a, hipStream_t st);
 hipError_t launch_loss_dw_bf16(int planes, int BNh, const LossGradArgs& a, hipStream_t st);
 hipError_t launch_loss_dw_f32(int planes, int BNh, const LossGradArgs& a, hipStream_t st);
-hipError_t launch_loss_both_bf16(const LossGradArgs& h, const LossGradArgs& w, hipStream_t st);
-hipError_t launch_loss_both_f32(const LossGradArgs& h, const LossGradArgs& w, hipStream_t st);
+hipError_t launch_loss_both_bf16(int BN, const LossGradArgs& h, const LossGradArgs& w, hipStream_t st);
+hipError_t launch_loss_both_f32(int BN, const LossGradArgs& h, const LossGradArgs& w, hipStream_t st);
 }  // namespace kb
 
 namespace {
@@ -56,22 +56,30 @@ struct Plan {
   size_t count, map, inv, flag, token, part, known, offs, items, ph, b, wp, stat, sumx, xt, rowp, g, dbp, dh_part, dw_part;
   size_t stat_piece;        // values of one piece's statistics
   size_t bytes;
-  bool both() const { return BN == 256 && BNh == 256; }  // dh and dW in one launch
+  bool both() const { return BN >= 192 && BNh == 256; }  // dh and dW in one launch
 };
 
 // The row tile with the least time for the logits: rounds of the card's workgroups times a tile's time, which is that of
-// its stages (96 of float32, 512 states: 73 us for 256 rows, 50 for 128, 38 for 64, 32 for 32; two workgroups of the
-// last on a CU 44), so small problems take small tiles (a training pass of 163 x 512 x 4,384 in float32: 124 us in tiles
-// of 32 rows, 251 in tiles of 256; 378 x 512 x 72,256: 1,005 in tiles of 128, 1,307 and 1,221 in tiles of 256 and 64;
-// bf16 6,852 x 512 x 2,000: 156 in tiles of 256, 179 in tiles of 128).
+// its stages (96 of float32, 512 states: 73 us for 256 rows, 60 for 192, 50 for 128, 38 for 64, 32 for 32; two workgroups
+// of the last on a CU 44), so small problems take small tiles (a training pass of 163 x 512 x 4,384 in float32: 124 us in
+// tiles of 32 rows, 251 in tiles of 256; bf16 6,852 x 512 x 2,000: 156 in tiles of 256, 179 in tiles of 128), and others
+// those that leave least of the last round and the last tile empty (scored and trained: 640 x 512 x 30,000 in float32
+// 608 in tiles of 192, 663 in tiles of 256; 570 x 1,024 x 50,000 in bf16 334, 372 and, in tiles of 128, 368; 180 x 1,024 x
+// 60,000 175, 196 and 205).  How many of the rows count is not known here: the sum over all, nine tenths and eight tenths
+// of them, as a batch's padding has it (1,111 x 512 x 32,000 in bf16: 226 in tiles of 192, 253 in tiles of 256; of 889
+// rows that count 207 and 200).
 int row_tile(int N, int vt) {
   int best = 32;
   long long least = LLONG_MAX;
-  for (int BN : {32, 64, 128, 256}) {
-    const long long cells = (long long)kb::loss_row_tiles(N, BN) * vt;
-    const int slots = BN == 32 ? 512 : 256;
-    const int time = BN == 256 ? 73 : BN == 128 ? 50 : BN == 64 ? 38 : cells <= 256 ? 32 : 44;
-    const long long all = (cells + slots - 1) / slots * time;
+  for (int BN : {32, 64, 128, 192, 256}) {
+    long long all = 0;
+    for (int tenths : {10, 9, 8}) {
+      const int rows = (int)(((long long)N * tenths + 9) / 10);
+      const long long cells = (long long)kb::loss_row_tiles(rows, BN) * vt;
+      const int slots = BN == 32 ? 512 : 256;
+      const int time = BN == 256 ? 73 : BN == 192 ? 60 : BN == 128 ? 50 : BN == 64 ? 38 : cells <= 256 ? 32 : 44;
+      all += (cells + slots - 1) / slots * time;
+    }
     if (all < least) best = BN, least = all;
     if (BN >= N) break;
   }
@@ -190,7 +198,7 @@ Plan make_plan(int dtype, int N, int H, int V, int K, bool teacher, bool grad, b
       for (int k = 0; k <= 3; ++k) {
         long long sh = k == 0 ? (st_h + share / 2) / share : (256 * k - nw) / n_h;
         sh = std::max<long long>(1, std::min<long long>(std::min(sh, st_h / 16), p.piece));
-        const long long time = all_done(n_h * sh, (st_h + sh - 1) / sh + start, nw, lw) + n_h * sh / (p.bf16 ? 3 : 18);
+        const long long time = all_done(n_h * sh, (st_h + sh - 1) / sh * p.BN / 256 + start, nw, lw) + n_h * sh / (p.bf16 ? 3 : 18);
         if (time < least) least = time, p.dh_splits = (int)sh;
       }
     } else {
@@ -498,7 +506,7 @@ kb_status gradient(const Call& c) {
     gw.out = static_cast<char*>(c.dW) + (size_t)t0 * kb::kLossM * p.z;
     if (c.dh && c.dW && p.both()) {
       KB_LAUNCH("gradients of a loss",
-                p.bf16 ? kb::launch_loss_both_bf16(gh, gw, c.st) : kb::launch_loss_both_f32(gh, gw, c.st));
+                p.bf16 ? kb::launch_loss_both_bf16(p.BN, gh, gw, c.st) : kb::launch_loss_both_f32(p.BN, gh, gw, c.st));
     } else {
       if (c.dh)
         KB_LAUNCH("gradient of the states",

@@ -16,6 +16,7 @@ struct LossTile {
   static_assert(WM * WN == 4 && BM == 256, "four waves, 256 on the M side");
 };
 using LossT256 = LossTile<4, 4, 2, 2>;
+using LossT192 = LossTile<4, 3, 2, 2>;
 using LossT128 = LossTile<4, 2, 2, 2>;
 using LossT64 = LossTile<2, 2, 4, 1>;
 using LossT32 = LossTile<2, 1, 4, 1>;

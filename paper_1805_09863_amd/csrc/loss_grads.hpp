@@ -190,14 +190,14 @@ __global__ __launch_bounds__(256, (LossOcc<T>::N)) void loss_dw(LossGradArgs a) 
                      a.splits * a.mt * a.ntn);
 }
 
-// Both in one launch, the longer tiles of dh first: neither has to fill the card by itself.
-template <class T, int PASSES>
+// Both in one launch, the longer tiles of dh (TH) first: neither has to fill the card by itself.
+template <class TH, class T, int PASSES>
 __global__ __launch_bounds__(256, (LossOcc<T>::N)) void loss_both(LossGradArgs h, LossGradArgs w) {
   __shared__ __attribute__((aligned(1024))) uint8_t ring[4 * LossOcc<T>::STAGE];
-  const int rows = const_int(h.count), R = loss_row_tiles(rows, T::BN);
+  const int rows = const_int(h.count), R = loss_row_tiles(rows, TH::BN);
   const int ch = h.splits * R * h.mt, cw = w.splits * w.mt * w.ntn;
   if ((int)blockIdx.x < ch)
-    dh_tile<T, PASSES>(h, lds_addr(ring), R, xcd_cell(ch, blockIdx.x));
+    dh_tile<TH, PASSES>(h, lds_addr(ring), R, xcd_cell(ch, blockIdx.x));
   else if ((int)blockIdx.x < ch + cw)
     dw_tile<T, PASSES>(w, lds_addr(ring), rows, xcd_cell(cw, blockIdx.x - ch), cw, cw);
 }
@@ -276,6 +276,7 @@ hipError_t launch_loss_dh_p(int BN, const LossGradArgs& a, hipStream_t st) {
   const dim3 gr(a.splits * (a.two > 0 ? 1 : loss_row_tiles(a.N, BN)) * a.mt), th(256);
   switch (BN) {
     case 256: loss_dh<LossT256, PASSES><<<gr, th, 0, st>>>(a); break;
+    case 192: loss_dh<LossT192, PASSES><<<gr, th, 0, st>>>(a); break;
     case 128: loss_dh<LossT128, PASSES><<<gr, th, 0, st>>>(a); break;
     case 64: loss_dh<LossT64, PASSES><<<gr, th, 0, st>>>(a); break;
     default: loss_dh<LossT32, PASSES><<<gr, th, 0, st>>>(a); break;
@@ -294,11 +295,14 @@ hipError_t launch_loss_dw_p(int BNh, const LossGradArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-// row tiles and state tiles of 256
+// row tiles of 192 or 256, state tiles of 256
 template <int PASSES>
-hipError_t launch_loss_both_p(const LossGradArgs& h, const LossGradArgs& w, hipStream_t st) {
-  const dim3 gr(h.splits * loss_row_tiles(h.N, 256) * h.mt + w.splits * w.mt * w.ntn), th(256);
-  loss_both<LossT256, PASSES><<<gr, th, 0, st>>>(h, w);
+hipError_t launch_loss_both_p(int BN, const LossGradArgs& h, const LossGradArgs& w, hipStream_t st) {
+  const dim3 gr(h.splits * loss_row_tiles(h.N, BN) * h.mt + w.splits * w.mt * w.ntn), th(256);
+  if (BN == 192)
+    loss_both<LossT192, LossT256, PASSES><<<gr, th, 0, st>>>(h, w);
+  else
+    loss_both<LossT256, LossT256, PASSES><<<gr, th, 0, st>>>(h, w);
   return hipGetLastError();
 }
 

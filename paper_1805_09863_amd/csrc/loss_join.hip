@@ -17,6 +17,7 @@ hipError_t launch_loss_join(bool bf16, const LossJoinArgs& a, LossJoinMore more,
   more.db_wg = more.db.db ? (more.db.V + 63) / 64 : 0;
   switch (a.BNt) {
     case 256: join<LossT256>(bf16, a, more, st); break;
+    case 192: join<LossT192>(bf16, a, more, st); break;
     case 128: join<LossT128>(bf16, a, more, st); break;
     case 64: join<LossT64>(bf16, a, more, st); break;
     default: join<LossT32>(bf16, a, more, st); break;

@@ -432,6 +432,12 @@ hipError_t launch_loss_logits_p(int BN, const LossLogitsArgs& a, int blocks, hip
         break;
       }
       return hipErrorInvalidValue;
+    case 192:
+      if constexpr (PLANES != 2) {
+        loss_logits<LossT192, PASSES, PLANES><<<gr, th, 0, st>>>(a);
+        break;
+      }
+      return hipErrorInvalidValue;
     case 128: loss_logits<LossT128, PASSES, PLANES><<<gr, th, 0, st>>>(a); break;
     case 64: loss_logits<LossT64, PASSES, PLANES><<<gr, th, 0, st>>>(a); break;
     default: loss_logits<LossT32, PASSES, PLANES><<<gr, th, 0, st>>>(a); break;

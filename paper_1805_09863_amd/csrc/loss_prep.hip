@@ -209,8 +209,9 @@ __global__ __launch_bounds__(kPackT) void loss_pack(LossPackArgs a) {
 #pragma unroll
           for (int u = 0; u < 4; ++u)
             if (t[u] >= 0 && t[u] < a.rows.V) {
-              const int ru = r + u * step, blk = ((t[u] & (wtm - 1)) >> 5) * NB + ((ru & (wtn - 1)) >> 5);
-              use(ru, row[u], t[u], ((ru >= wtn ? a.words0 : 0) + t[u] / wtm) * blocks + blk);
+              const int ru = r + u * step, second = ru >= wtn;  // of the wave's rows
+              const int blk = ((t[u] & (wtm - 1)) >> 5) * NB + ((ru - (second ? wtn : 0)) >> 5);
+              use(ru, row[u], t[u], ((second ? a.words0 : 0) + t[u] / wtm) * blocks + blk);
             }
         }
     };

@@ -156,6 +156,14 @@ def test_tiles_in_turn(kb, dtype, N, H, V):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,H,V", [(180, 40, 60001), (192, 32, 60000), (570, 64, 30000), (570, 300, 30001)])
+def test_tiles_of_192_rows(kb, dtype, N, H, V):
+    """Row tiles that are no power of two: one, and several; states of one tile, and of more (dh and dW in one launch)."""
+    check_ce(kb, dtype, N, H, V, smoothing=0.1)
+    check_kd(kb, dtype, N, H, V, 20, 2.0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("N,H,V", [(7, 1, 1), (3, 5, 2), (9, 31, 255), (40, 33, 257), (70, 200, 1001), (300, 130, 8), (1, 7, 3000)])
 def test_odd_sizes(kb, dtype, N, H, V):
     check_ce(kb, dtype, N, H, V)
