@@ -187,7 +187,7 @@ Plan make_plan(int dtype, int N, int H, int V, int K, bool teacher, bool grad, b
     if (p.both()) {
       // One launch: every workgroup about its share of all stages, and none of less than 16; dh's splits so that both are
       // done soonest, whether each takes its share or the workgroups fill whole rounds of the card (640 x 512 x 30,000
-      // in float32, a piece: 256 workgroups in 23 splits, 262 in 24; the training pass 654 us and 775).  A part's writing
+      // in float32, row tiles of 256, a piece: 256 workgroups in 23 splits, 262 in 24; the training pass 654 us and 775).  A part's writing
       // and reading costs the card 0.13 us, a sixth of a stage, and counts twice: a card that waits for its last
       // workgroups clocks higher (4,096 x 1,024 x 50,000 in whole rounds of four splits 1,504 us, in shares of two 1,484).
       const int start = p.bf16 ? 6 : 1;  // a tile's start and end, in stages
