@@ -298,6 +298,43 @@ def test_many_rows(kb, N):
     check_kd(kb, BF16, N, 32, 300, 3)
 
 
+def test_most_rows(kb):
+    """KB_LOSS_MAX_N rows, against float64 on the GPU: offsets of states, dlogits and parts past 2^31 bytes."""
+    N, H, V = 4194304, 8, 8
+    g = torch.Generator(device="cuda").manual_seed(3)
+    h = torch.randn((N, H), generator=g, device="cuda").to(BF16)
+    W = (torch.randn((H, V), generator=g, device="cuda") / 3).to(BF16)
+    b = torch.randn(V, generator=g, device="cuda")
+    target = torch.randint(-1, V, (N,), generator=g, device="cuda", dtype=torch.int32)
+    grad = torch.randn(N, generator=g, device="cuda")
+    loss, lse = kb.cross_entropy(h, W, b, target)
+    dh, dW, db = kb.cross_entropy_grad(h, W, b, target, lse, grad)
+    used = target >= 0
+    t = target.long().clamp_min(0)[:, None]
+    x = h.double() @ W.double() + b.double()
+    norm = torch.logsumexp(x, 1)
+    size = h.double().abs() @ W.double().abs() + b.double().abs()
+    # a logit: H + 3 roundings of what it sums; exponentials 2^-22, exponents 4 u of |x| twice, the sum V, the logarithm
+    off = (H + 3) * U * size.amax(1) + 8 * U * x.abs().amax(1) + 2.0 ** -22 + (V + 4) * U * (1 + norm.abs())
+    assert ((lse - norm).abs() <= off)[used].all() and (lse[~used] == 0).all()
+    want = norm - x.gather(1, t).squeeze(1)
+    assert ((loss - want).abs() <= 2 * off + 2 * U * want.abs())[used].all() and (loss[~used] == 0).all()
+    p = torch.exp(x - norm[:, None])
+    G = (p - torch.zeros_like(p).scatter_(1, t, 1.0)) * (grad.double() * used)[:, None]
+    e = (grad.double().abs() * used)[:, None] * p * torch.expm1(3 * off + 2.0 ** -21)[:, None] + 4 * U * G.abs() + 2.0 ** -126
+    r = 2.0 ** -8
+    Wd = W.double()
+    for name, got, want, tol, out in (
+            ("dh", dh, G @ Wd.t(), (e + (r + (V + 80) * U) * G.abs()) @ Wd.t().abs(), r),
+            # sums in 256 parts and 16 of them at a time: chains of N / 256 and 16 + 16 (db: 32 of a tile, then N / 2048 + 16)
+            ("dW", dW, h.double().t() @ G, h.double().abs().t() @ (e + (r + (N / 256 + 80) * U) * G.abs()), r),
+            ("db", db, G.sum(0), (e + (N / 2048 + 80) * U * G.abs()).sum(0), U)):
+        lim = tol + out * (want.abs() + tol) + 2.0 ** -126
+        err = (got.double() - want).abs()
+        assert (err <= lim).all(), f"{name}: off by {err.max().item()}"
+    assert (dh[~used] == 0).all()
+
+
 @pytest.mark.parametrize("N,H,V", [(5, 32, 262144), (40, 32, 262144), (2000, 32, 262144)])
 def test_largest_vocabulary(kb, N, H, V):
     _, h, W, b, target, grad = make(5, BF16, N, H, V, pad=0.0)
