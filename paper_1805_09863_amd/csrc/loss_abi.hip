@@ -101,6 +101,52 @@ long long all_done(long long nh, long long lh, long long nw, long long lw) {
   return hi;
 }
 
+struct Splits {
+  int dh, dw;
+  long long time;  // in stages of 32 steps
+};
+
+// dh and dW of a piece of `tiles` word tiles in one launch: stages of dh along the piece's words, of dW along the rows.
+// Every workgroup about its share of all stages, and none of less than 16; dh's splits so that both are done soonest,
+// whether each takes its share or the workgroups fill whole rounds of the card (640 x 512 x 30,000 in float32, row tiles
+// of 256, a piece: 256 workgroups in 23 splits, 262 in 24; the training pass 654 us and 775).  A part's writing and
+// reading costs the card 0.13 us, a sixth of a stage, and counts twice: a card that waits for its last workgroups clocks
+// higher (4,096 x 1,024 x 50,000 in whole rounds of four splits 1,504 us, in shares of two 1,484).
+Splits both_splits(const Plan& p, int tiles) {
+  const long long st_h = (long long)tiles * (kb::kLossM / kb::kLossStage), st_w = up(p.N, kb::kLossStage) / kb::kLossStage;
+  const long long n_h = (long long)p.Rd * p.dh_mt, n_w = (long long)tiles * p.dw_ntn;
+  const int start = p.bf16 ? 6 : 1;  // a tile's start and end, in stages
+  const long long share = std::max<long long>(16, (n_h * st_h + n_w * st_w) / 256);
+  Splits s{1, (int)std::max<long long>(1, (st_w + share / 2) / share), LLONG_MAX};
+  const long long nw = n_w * s.dw, lw = (st_w + s.dw - 1) / s.dw + start;
+  for (int k = 0; k <= 3; ++k) {
+    long long sh = k == 0 ? (st_h + share / 2) / share : (256 * k - nw) / n_h;
+    sh = std::max<long long>(1, std::min<long long>(std::min(sh, st_h / 16), tiles));
+    const long long time = all_done(n_h * sh, (st_h + sh - 1) / sh * p.BN / 256 + start, nw, lw) + n_h * sh / (p.bf16 ? 3 : 18);
+    if (time < s.time) s.time = time, s.dh = (int)sh;
+  }
+  return s;
+}
+
+// The products' time with pieces of `piece` word tiles, in stages of a tile of 256 rows: rounds of the logits' tiles, whose
+// epilogue takes 5 stages (13 with dlogits), the gradients' launch, and 6 for each launch.  Dlogits of more than 128 MB,
+// half the last-level cache, cost 7% (8,192 x 1,024 x 90,000, the gradients: 11 pieces of 128 MB and 44 rounds of the
+// logits' tiles 4,182 us, 2 pieces of 704 MB and 44 rounds 4,499, 6 of 236 MB and 48 rounds 4,596); rounds that are not
+// full cost more (5,000 x 512 x 32,001: 3 pieces of 110 MB and 12 rounds 800 us, 2 of 165 MB and 10 rounds 611; the loss of
+// 1,024 x 1,024 x 60,000 in float32: 3 pieces and 6 rounds 1,065, 2 and 4 rounds 769).
+long long pieces_time(const Plan& p, int piece, bool grad, size_t bytes) {
+  const int passes = p.bf16 ? 1 : 6;
+  auto one = [&](int tiles) {
+    const long long P = kb::loss_splits(p.grid, p.R, tiles), rounds = (tiles + P - 1) / P * ((p.R * P + p.grid - 1) / p.grid);
+    long long t = rounds * (p.Hk / kb::kLossStage * passes + (grad ? 13 : 5)) * p.BN / 256 + 6;
+    if (grad) t += (p.both() ? both_splits(p, tiles).time * passes : (long long)tiles * p.dh_mt) + 6;
+    return t;
+  };
+  const int full = p.vt / piece, rest = p.vt % piece;
+  const long long sum = full * one(piece) + (rest > 0 ? one(rest) : 0);
+  return grad && bytes > (size_t)128 << 20 ? sum + sum * 7 / 100 : sum;
+}
+
 // The plan of a call. `direct`: W is read where it lies; else its pieces are laid out first (float32 in bf16 pieces, odd
 // sizes and addresses with zeros filled up).
 Plan make_plan(int dtype, int N, int H, int V, int K, bool teacher, bool grad, bool w_aligned) {
@@ -138,17 +184,31 @@ Plan make_plan(int dtype, int N, int H, int V, int K, bool teacher, bool grad, b
   p.grid = std::max(p.BN == 32 ? 512 : 256, p.R);
   const bool shape = p.bf16 && H % kb::kLossStage == 0 && V % 8 == 0 && V >= kb::kLossM;
   p.direct = shape && w_aligned;
+  // two pieces of the dlogits: rows of one tile of dh, the second ones behind all of the first
+  p.two = p.g_planes == 2 ? p.R * p.BN : 0;
+  p.BNd = p.two == 0 ? p.BN : p.two <= 32 ? 64 : p.two <= 64 ? 128 : 256;
+  p.Rd = p.two == 0 ? p.R : 1;
+  p.dh_mt = (H + kb::kLossM - 1) / kb::kLossM;
+  p.dw_ntn = (H + p.BNh - 1) / p.BNh;
 
-  // A piece: as many words as keep its dlogits, and the part of W that is laid out, at 128 MB, half the last-level cache
-  // (8,192 x 1,024 x 90,000, a training pass: 5.87 ms; at 64 MB 6.37, 256 MB 6.12, 1 GB 6.29).
-  // (W at an odd address where its shape needs no laying out: small pieces, so that the workspace need not grow.)
-  const size_t most = (size_t)128 << 20;
+  // Pieces: as many as take the least time of those whose dlogits, and whose part of W that is laid out, have 64 to 256 MB.
+  // (W at an odd address where its shape needs no laying out: small pieces of it, so that the workspace need not grow.)
   const size_t w_tile = (size_t)p.Hk * kb::kLossM * 2 * p.planes, g_tile = (size_t)p.R * p.BN * kb::kLossM * 2 * p.g_planes;
-  size_t tiles = p.vt;
-  if (!p.direct) tiles = std::min(tiles, std::max<size_t>(1, (shape ? most / 16 : most) / w_tile));
-  if (grad) tiles = std::min(tiles, std::max<size_t>(1, most / g_tile));
-  p.pieces = (int)((p.vt + tiles - 1) / tiles);
-  p.piece = (p.vt + p.pieces - 1) / p.pieces;
+  auto tiles_of = [&](size_t most) {
+    size_t tiles = p.vt;
+    if (!p.direct) tiles = std::min(tiles, std::max<size_t>(1, (shape ? most / 16 : most) / w_tile));
+    if (grad) tiles = std::min(tiles, std::max<size_t>(1, most / g_tile));
+    return (int)tiles;
+  };
+  const int fewest = (p.vt + tiles_of((size_t)256 << 20) - 1) / tiles_of((size_t)256 << 20);
+  const int most = (p.vt + tiles_of((size_t)64 << 20) - 1) / tiles_of((size_t)64 << 20);
+  p.piece = (p.vt + fewest - 1) / fewest;
+  long long least = LLONG_MAX;
+  for (int k = fewest; k <= most && fewest < most; ++k) {
+    const int piece = (p.vt + k - 1) / k;
+    const long long time = pieces_time(p, piece, grad, piece * ((grad ? g_tile : 0) + (p.direct ? 0 : w_tile)));
+    if (time < least) p.piece = piece, least = time;
+  }
   p.pieces = (p.vt + p.piece - 1) / p.piece;
 
   Space s;
@@ -173,34 +233,13 @@ Plan make_plan(int dtype, int N, int H, int V, int K, bool teacher, bool grad, b
     p.xt = s.take((size_t)p.R * p.BN * K * 4);
   } else {
     p.rowp = s.take((size_t)p.R * p.BN * sizeof(float2));
-    // two pieces: rows of one tile of dh, the second ones behind all of the first
-    p.two = p.g_planes == 2 ? p.R * p.BN : 0;
-    p.BNd = p.two == 0 ? p.BN : p.two <= 32 ? 64 : p.two <= 64 ? 128 : 256;
-    p.Rd = p.two == 0 ? p.R : 1;
     p.g = s.take(p.two == 0 ? p.piece * g_tile : (size_t)p.piece * kb::kLossM * 2 * p.BNd);
     p.dbp = s.take((size_t)p.R * p.WN * p.vt * kb::kLossM * 4);
-    p.dh_mt = (H + kb::kLossM - 1) / kb::kLossM;
-    p.dw_ntn = (H + p.BNh - 1) / p.BNh;
-    // Stages of 32 steps: of dh along the piece's words, of dW along the rows.
-    const long long st_h = (long long)p.piece * (kb::kLossM / kb::kLossStage), st_w = up(N, kb::kLossStage) / kb::kLossStage;
-    const long long n_h = (long long)p.Rd * p.dh_mt, n_w = (long long)p.piece * p.dw_ntn;
+    const long long st_w = up(N, kb::kLossStage) / kb::kLossStage, n_w = (long long)p.piece * p.dw_ntn;
+    const long long n_h = (long long)p.Rd * p.dh_mt;
     if (p.both()) {
-      // One launch: every workgroup about its share of all stages, and none of less than 16; dh's splits so that both are
-      // done soonest, whether each takes its share or the workgroups fill whole rounds of the card (640 x 512 x 30,000
-      // in float32, row tiles of 256, a piece: 256 workgroups in 23 splits, 262 in 24; the training pass 654 us and 775).  A part's writing
-      // and reading costs the card 0.13 us, a sixth of a stage, and counts twice: a card that waits for its last
-      // workgroups clocks higher (4,096 x 1,024 x 50,000 in whole rounds of four splits 1,504 us, in shares of two 1,484).
-      const int start = p.bf16 ? 6 : 1;  // a tile's start and end, in stages
-      const long long share = std::max<long long>(16, (n_h * st_h + n_w * st_w) / 256);
-      p.dw_splits = (int)std::max<long long>(1, (st_w + share / 2) / share);
-      const long long nw = n_w * p.dw_splits, lw = (st_w + p.dw_splits - 1) / p.dw_splits + start;
-      long long least = LLONG_MAX;
-      for (int k = 0; k <= 3; ++k) {
-        long long sh = k == 0 ? (st_h + share / 2) / share : (256 * k - nw) / n_h;
-        sh = std::max<long long>(1, std::min<long long>(std::min(sh, st_h / 16), p.piece));
-        const long long time = all_done(n_h * sh, (st_h + sh - 1) / sh * p.BN / 256 + start, nw, lw) + n_h * sh / (p.bf16 ? 3 : 18);
-        if (time < least) least = time, p.dh_splits = (int)sh;
-      }
+      const Splits both = both_splits(p, p.piece);
+      p.dh_splits = both.dh, p.dw_splits = both.dw;
     } else {
       p.dh_splits = (int)std::max<long long>(1, std::min<long long>((p.BNd == 32 ? 512 : 256) / n_h, p.piece));
       p.dw_splits = (int)std::max<long long>(1, std::min<long long>(256 / n_w, st_w / 8));
