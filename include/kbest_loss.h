@@ -106,9 +106,9 @@ kb_status kb_cross_entropy_grad(int dtype, int N, int H, int V, const void* h, c
  *   token, logit  N x K int32 and float32, row-major, in any order: the
  *                 teacher's words and their logits (log-probabilities serve
  *                 as well: a row's constant drops out).  An entry whose token
- *                 is outside 0 .. V - 1 or whose logit is -inf counts for
+ *                 is outside 0 .. V - 1 or whose logit / T is -inf counts for
  *                 nothing; entries of a row with the same token add up.
- *   temperature   T > 0.
+ *   temperature   1e-6 <= T <= 1e6; the logits / T must be finite.
  * The rest as for kb_cross_entropy; the workspace of K.
  */
 kb_status kb_distill(int dtype, int N, int H, int V, int K, const void* h, const void* W, const float* b,

@@ -1065,9 +1065,9 @@ def distill(h: torch.Tensor, W: torch.Tensor, b: torch.Tensor, token: torch.Tens
 
     ``token``, ``logit``: N x K int32 and float32, the teacher's words for every row and their logits (or
     log-probabilities, as ``kbest_step`` scores them), in any order; a token outside 0 .. V - 1 or a logit of
-    -inf is no entry, and a row without one is left out.  The loss is temperature^2 times the divergence of
-    softmax(student / temperature) from softmax(logit / temperature); lse is the log-sum-exp of the student's
-    logits / temperature.
+    -inf is no entry, and a row without one is left out.  ``temperature`` is 1e-6 to 1e6; the loss is its square
+    times the divergence of softmax(student / temperature) from softmax(logit / temperature); lse is the log-sum-exp
+    of the student's logits / temperature.
     """
     dev, _, code, N, H, V, hp, Wp, bp = _loss_layer(h, W, b)
     K, tp, yp = _loss_teacher(token, logit, N, dev)

@@ -88,9 +88,9 @@ template <int BASE, int NOP>
 __device__ __forceinline__ void dma_i(const uint32_t* off, int i, const void* src, uint32_t lds) {
   switch (i) {
     case 0: dma16_at<BASE, NOP>(off[0], src, lds); break;
-    case 1: dma16_at<BASE + 1024, NOP>(off[1], src, lds); break;
-    case 2: dma16_at<BASE + 2048, NOP>(off[2], src, lds); break;
-    default: dma16_at<BASE + 3072, NOP>(off[3], src, lds); break;
+    case 1: dma16_at<BASE + 1 * 1024, NOP>(off[1], src, lds); break;
+    case 2: dma16_at<BASE + 2 * 1024, NOP>(off[2], src, lds); break;
+    default: dma16_at<BASE + 3 * 1024, NOP>(off[3], src, lds); break;
   }
 }
 
