@@ -1,4 +1,4 @@
-// The losses of at most eight rows: W is read once (twice for its gradient) and everything else is small, so the
+// The losses of at most eight rows (of float32, scored: sixteen, in two turns): W is read once (twice for its gradient) and everything else is small, so the
 // vector ALUs do, in float32 whatever the operands' type, and W needs no laying out, whatever its alignment.
 //
 // A workgroup takes chunks of 16 (few words: 8) x 16 bytes of words: threads of 16 bytes each along the words, and 16 or

@@ -156,6 +156,13 @@ def test_tiles_in_turn(kb, dtype, N, H, V):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,H,V", [(9, 100, 3001), (13, 64, 1000), (16, 256, 30000), (17, 64, 1000)])
+def test_a_few_rows_more(kb, dtype, N, H, V):
+    check_ce(kb, dtype, N, H, V, smoothing=0.1)
+    check_kd(kb, dtype, N, H, V, 70, 2.0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("N,H,V", [(180, 40, 60001), (192, 32, 60000), (570, 64, 30000), (570, 300, 30001)])
 def test_tiles_of_192_rows(kb, dtype, N, H, V):
     """Row tiles that are no power of two: one, and several; states of one tile, and of more (dh and dW in one launch)."""
