@@ -205,6 +205,12 @@ __global__ __launch_bounds__(256, (LossOcc<T>::N)) void loss_both(LossGradArgs h
     dw_tile<T, PASSES>(w, lds_addr(ring), rows, xcd_cell(cw, blockIdx.x - ch), cw, cw);
 }
 
+// Workgroups of a join, of at most 2^22 tiles (2^22 rows of 2^16 states) and 64 a tile.
+template <class T>
+__host__ __device__ constexpr int loss_join_blocks(int tiles) {
+  return tiles * (T::MB * T::NB * 4);
+}
+
 // The parts of a result added up in order and rounded once.  A workgroup takes a quarter of the registers of one block of
 // 32 x 32 of every wave of a tile: four groups of 256 threads add up every fourth part each, then the four sums.
 // Behind them, workgroups that fill the rows of dh that do not count with zeros, and some that add up the bias' sums.
@@ -214,20 +220,20 @@ __global__ __launch_bounds__(1024) void loss_join(LossJoinArgs a, LossJoinMore m
   const int tid = threadIdx.x & 255, grp = threadIdx.x >> 8, lane = tid & 63, half = lane >> 5, col = lane & 31;
   const int wave = tid >> 6, wm = wave % T::WM, wn = wave / T::WM;
   D* out = static_cast<D*>(a.out);
-  const int work = gridDim.x - more.zero_wg - more.db_wg;
-  if ((int)blockIdx.x >= work + more.zero_wg) {
-    sum_bias(more.db, blockIdx.x - work - more.zero_wg, reinterpret_cast<float*>(sums));
+  const int tiles = a.mt * a.ntn;  // dh: by rows, then states; dW: by words, then states
+  const int work = loss_join_blocks<T>(tiles), wg = blockIdx.y * gridDim.x + blockIdx.x;
+  if (wg >= work + more.zero_wg) {
+    if (wg < work + more.zero_wg + more.db_wg) sum_bias(more.db, wg - work - more.zero_wg, reinterpret_cast<float*>(sums));
     return;
   }
-  if ((int)blockIdx.x >= work) {
-    for (int n = blockIdx.x - work; n < more.N; n += more.zero_wg)
+  if (wg >= work) {
+    for (int n = wg - work; n < more.N; n += more.zero_wg)
       if (more.inv[n] < 0)
         for (int i = threadIdx.x; i < a.cols; i += 1024) out[(size_t)n * a.ld + i] = (D)0.f;
     return;
   }
   const int rows = a.is_dh ? *a.count : a.rows;
-  const int tiles = a.mt * a.ntn;  // dh: by rows, then states; dW: by words, then states
-  const int q = blockIdx.x & 3, unit = blockIdx.x >> 2;
+  const int q = wg & 3, unit = wg >> 2;
   const int tile = unit / (T::MB * T::NB), blk = unit % (T::MB * T::NB);
   const int m = blk / T::NB, n = blk % T::NB;
   const int mt = a.is_dh ? tile % a.mt : tile / a.ntn, nt = a.is_dh ? tile / a.mt : tile % a.ntn;

@@ -5,7 +5,9 @@ namespace kb {
 
 template <class T>
 void join(bool bf16, const LossJoinArgs& a, const LossJoinMore& more, hipStream_t st) {
-  const dim3 gr(a.mt * a.ntn * T::MB * T::NB * 4 + more.zero_wg + more.db_wg), th(1024);
+  // Fewer than 2^32 threads lie along a grid's axis: workgroups beyond 2^21 (2^21 rows of 1,024 states) in rows of 2^21.
+  const int blocks = loss_join_blocks<T>(a.mt * a.ntn) + more.zero_wg + more.db_wg, row = 1 << 21;
+  const dim3 gr(blocks < row ? blocks : row, (blocks + row - 1) / row), th(1024);
   if (bf16)
     loss_join<T, __bf16><<<gr, th, 0, st>>>(a, more);
   else
