@@ -1,5 +1,6 @@
 // Host side of the output layer's losses: argument validation, the plan of a
 // call and the entry points declared in include/kbest_loss.h.
+#include <float.h>
 #include <limits.h>
 #include <math.h>
 
@@ -290,6 +291,12 @@ struct Call {
   hipStream_t st;
 };
 
+// smoothing / V.  One that is 0 in float32 is the smallest value instead: it has no weight, but a word of b = -inf that the
+// labels name takes the loss to +inf all the same (0 x -inf has no value).
+float rest_of(const Call& c) {
+  return c.smoothing > 0.f ? std::max(c.smoothing / (float)c.V, FLT_TRUE_MIN) : 0.f;
+}
+
 kb_status check_call(const Call& c, const Plan& p) {
   if (!c.h || !c.W || !c.b || !c.token) return fail(KB_ERR_INVALID_ARG, "null h, W, b or words");
   if (!aligned(c.h, p.z) || !aligned(c.W, p.z) || !aligned(c.b, 4) || !aligned(c.token, 4) || !aligned(c.logit, 4))
@@ -403,7 +410,7 @@ kb::LossLogitsArgs logits_args(const Call& c, const Plan& p, const Work& w, cons
   a.words0 = p.words0;
   a.wt0 = t0 * (kb::kLossM / p.WTM);
   a.K = c.K;
-  a.rest = c.smoothing / (float)c.V;
+  a.rest = rest_of(c);
   return a;
 }
 
@@ -415,7 +422,7 @@ kb::LossFewArgs few_args(const Call& c, const Plan& p) {
   a.inv_t = 1.f / c.temperature;
   a.t2 = c.temperature * c.temperature;
   a.target_part = 1.f - c.smoothing;
-  a.rest = c.smoothing / (float)c.V;
+  a.rest = rest_of(c);
   a.grid = p.grid;
   return a;
 }
@@ -488,7 +495,7 @@ kb_status forward(const Call& c) {
   f.known = c.logit ? w.at<float>(p.known) : nullptr;
   f.scale = kb::kL2E / c.temperature;
   f.inv_t = 1.f / c.temperature;
-  f.rest = c.smoothing / (float)c.V;
+  f.rest = rest_of(c);
   f.t2 = c.temperature * c.temperature;
   f.loss = c.loss;
   f.lse = c.lse;
