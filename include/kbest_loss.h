@@ -58,10 +58,16 @@ extern "C" {
 
 /*
  * Workspace bytes of kb_cross_entropy (K = 1) and kb_distill, and of their
- * gradients.  0 for N = 0 and for sizes that the calls refuse.  The gradients'
- * grows with N * H and, for db, by N * V / 32 bytes (a row of sums for every
- * 128 rows); with the logits' N * V and with H * V only as far as a piece of
- * the vocabulary goes.
+ * gradients, whichever of the three are asked for.  0 for N = 0 and for sizes
+ * that the calls refuse.  Never less for more rows, other sizes equal: a
+ * workspace for the most rows that a program has at once serves all its
+ * batches.
+ * They grow with N * H (the states in bf16 pieces; gradients: dh in float32),
+ * with N * K, and by N * V / 512 bytes (where the lists of the rows' words
+ * begin); the gradients' by up to N * V / 8 besides (db's sums: a row for every
+ * 32 rows, in large batches, N * V / 32, for every 128).  With the logits'
+ * N * V and with H * V only as far as a piece of the vocabulary goes: of either
+ * at most 256 MiB, or 256 words.
  */
 size_t kb_loss_workspace_bytes(int dtype, int N, int H, int V, int K);
 size_t kb_loss_grad_workspace_bytes(int dtype, int N, int H, int V, int K);

@@ -948,12 +948,12 @@ def _loss_bytes(name: str, *shape: int) -> int:
 
 
 def loss_workspace_bytes(dtype: int, N: int, H: int, V: int, K: int = 1) -> int:
-    """Workspace of ``cross_entropy`` (K = 1) and ``distill``."""
+    """Workspace of ``cross_entropy`` (K = 1) and ``distill``; that of the most rows serves fewer as well."""
     return _loss_bytes("kb_loss_workspace_bytes", dtype, N, H, V, K)
 
 
 def loss_grad_workspace_bytes(dtype: int, N: int, H: int, V: int, K: int = 1) -> int:
-    """Workspace of ``cross_entropy_grad`` (K = 1) and ``distill_grad``."""
+    """Workspace of ``cross_entropy_grad`` (K = 1) and ``distill_grad``; that of the most rows serves fewer as well."""
     return _loss_bytes("kb_loss_grad_workspace_bytes", dtype, N, H, V, K)
 
 

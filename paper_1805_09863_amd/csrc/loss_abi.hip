@@ -148,6 +148,22 @@ long long pieces_time(const Plan& p, int piece, bool grad, size_t bytes) {
   return grad && bytes > (size_t)128 << 20 ? sum + sum * 7 / 100 : sum;
 }
 
+// A batch's tiles, pieces and splits are chosen as for the next step of rows: every number up to 16, multiples of 32 up
+// to 2,048, from there 32 steps to each doubling.  Within a step the workspace only grows with the rows.
+int plan_rows(int N) {
+  if (N <= 16) return N;
+  int q = 32;
+  while (q * 64 < N) q *= 2;
+  return up(N, q);
+}
+constexpr int kPlanSteps = 16 + 64 + 32 * 11;  // up to KB_LOSS_MAX_N = 2,048 x 2^11
+int step_rows(int i) {
+  if (i < 16) return i + 1;
+  if (i < 80) return 32 * (i - 15);
+  const int doubling = (i - 80) / 32;
+  return (32 + (i - 80) % 32 + 1) * (64 << doubling);
+}
+
 // The plan of a call. `direct`: W is read where it lies; else its pieces are laid out first (float32 in bf16 pieces, odd
 // sizes and addresses with zeros filled up).
 Plan make_plan(int dtype, int N, int H, int V, int K, bool teacher, bool grad, bool w_aligned) {
@@ -176,8 +192,7 @@ Plan make_plan(int dtype, int N, int H, int V, int K, bool teacher, bool grad, b
     return p;
   }
   p.vt = (V + kb::kLossM - 1) / kb::kLossM;
-  p.BN = row_tile(N, p.vt);
-  p.R = kb::loss_row_tiles(N, p.BN);
+  p.BN = row_tile(plan_rows(N), p.vt);
   p.WN = p.BN >= 128 ? 2 : 1;
   p.WTM = kb::loss_wtm(p.BN);
   p.WTN = kb::loss_wtn(p.BN);
@@ -186,19 +201,25 @@ Plan make_plan(int dtype, int N, int H, int V, int K, bool teacher, bool grad, b
   p.Hk = up(H, kb::kLossStage);
   p.words0 = p.vt * (kb::kLossM / p.WTM);
   p.nb = p.BN / p.WTN * p.words0 * kb::loss_blocks(p.BN);
-  p.grid = std::max(p.BN == 32 ? 512 : 256, p.R);
   const bool shape = p.bf16 && H % kb::kLossStage == 0 && V % 8 == 0 && V >= kb::kLossM;
   p.direct = shape && w_aligned;
-  // two pieces of the dlogits: rows of one tile of dh, the second ones behind all of the first
-  p.two = p.g_planes == 2 ? p.R * p.BN : 0;
-  p.BNd = p.two == 0 ? p.BN : p.two <= 32 ? 64 : p.two <= 64 ? 128 : 256;
-  p.Rd = p.two == 0 ? p.R : 1;
+  auto set_rows = [&](int rows) {
+    p.N = rows;
+    p.R = kb::loss_row_tiles(rows, p.BN);
+    p.grid = std::max(p.BN == 32 ? 512 : 256, p.R);
+    // two pieces of the dlogits: rows of one tile of dh, the second ones behind all of the first
+    p.two = p.g_planes == 2 ? p.R * p.BN : 0;
+    p.BNd = p.two == 0 ? p.BN : p.two <= 32 ? 64 : p.two <= 64 ? 128 : 256;
+    p.Rd = p.two == 0 ? p.R : 1;
+  };
+  set_rows(plan_rows(N));
   p.dh_mt = (H + kb::kLossM - 1) / kb::kLossM;
   p.dw_ntn = (H + p.BNh - 1) / p.BNh;
 
   // Pieces: as many as take the least time of those whose dlogits, and whose part of W that is laid out, have 64 to 256 MB.
   // (W at an odd address where its shape needs no laying out: small pieces of it, so that the workspace need not grow.)
-  const size_t w_tile = (size_t)p.Hk * kb::kLossM * 2 * p.planes, g_tile = (size_t)p.R * p.BN * kb::kLossM * 2 * p.g_planes;
+  const size_t w_tile = (size_t)p.Hk * kb::kLossM * 2 * p.planes;
+  size_t g_tile = (size_t)p.R * p.BN * kb::kLossM * 2 * p.g_planes;
   auto tiles_of = [&](size_t most) {
     size_t tiles = p.vt;
     if (!p.direct) tiles = std::min(tiles, std::max<size_t>(1, (shape ? most / 16 : most) / w_tile));
@@ -215,7 +236,23 @@ Plan make_plan(int dtype, int N, int H, int V, int K, bool teacher, bool grad, b
     if (time < least) p.piece = piece, least = time;
   }
   p.pieces = (p.vt + p.piece - 1) / p.piece;
+  if (grad) {
+    const long long st_w = up(p.N, kb::kLossStage) / kb::kLossStage, n_w = (long long)p.piece * p.dw_ntn;
+    const long long n_h = (long long)p.Rd * p.dh_mt;
+    if (p.both()) {
+      const Splits both = both_splits(p, p.piece);
+      p.dh_splits = both.dh, p.dw_splits = both.dw;
+    } else {
+      p.dh_splits = (int)std::max<long long>(1, std::min<long long>((p.BNd == 32 ? 512 : 256) / n_h, p.piece));
+      p.dw_splits = (int)std::max<long long>(1, std::min<long long>(256 / n_w, st_w / 8));
+    }
+    // few stages a tile: a workgroup takes several tiles, the next one's loads under way while it writes one
+    p.dw_grid = (int)(n_w * p.dw_splits);
+    if (p.dw_splits == 1 && st_w * p.g_planes <= 16) p.dw_grid = std::min(p.dw_grid, p.BNh == 64 ? 512 : 256);
+  }
 
+  set_rows(N);
+  g_tile = (size_t)p.R * p.BN * kb::kLossM * 2 * p.g_planes;
   Space s;
   p.count = s.take(4);
   p.map = s.take((size_t)N * 4);
@@ -240,20 +277,8 @@ Plan make_plan(int dtype, int N, int H, int V, int K, bool teacher, bool grad, b
     p.rowp = s.take((size_t)p.R * p.BN * sizeof(float2));
     p.g = s.take(p.two == 0 ? p.piece * g_tile : (size_t)p.piece * kb::kLossM * 2 * p.BNd);
     p.dbp = s.take((size_t)p.R * p.WN * p.vt * kb::kLossM * 4);
-    const long long st_w = up(N, kb::kLossStage) / kb::kLossStage, n_w = (long long)p.piece * p.dw_ntn;
-    const long long n_h = (long long)p.Rd * p.dh_mt;
-    if (p.both()) {
-      const Splits both = both_splits(p, p.piece);
-      p.dh_splits = both.dh, p.dw_splits = both.dw;
-    } else {
-      p.dh_splits = (int)std::max<long long>(1, std::min<long long>((p.BNd == 32 ? 512 : 256) / n_h, p.piece));
-      p.dw_splits = (int)std::max<long long>(1, std::min<long long>(256 / n_w, st_w / 8));
-    }
-    // few stages a tile: a workgroup takes several tiles, the next one's loads under way while it writes one
-    p.dw_grid = (int)(n_w * p.dw_splits);
-    if (p.dw_splits == 1 && st_w * p.g_planes <= 16) p.dw_grid = std::min(p.dw_grid, p.BNh == 64 ? 512 : 256);
-    p.dh_part = s.take((size_t)p.dh_splits * n_h * kb::kLossM * p.BNd * 4);
-    if (p.dw_splits > 1) p.dw_part = s.take((size_t)p.dw_splits * n_w * kb::kLossM * p.BNh * 4);
+    p.dh_part = s.take((size_t)p.dh_splits * p.Rd * p.dh_mt * kb::kLossM * p.BNd * 4);
+    if (p.dw_splits > 1) p.dw_part = s.take((size_t)p.dw_splits * p.piece * p.dw_ntn * kb::kLossM * p.BNh * 4);
   }
   p.bytes = s.at;
   return p;
@@ -268,10 +293,25 @@ kb_status check_sizes(int dtype, int N, int H, int V, int K) {
   return KB_OK;
 }
 
+// What the largest of all batches of up to N rows takes, so that a workspace for a program's largest batch serves the
+// smaller ones: pieces are chosen by their time, and 5,825 rows of 1,024 x 90,000 have larger ones than 8,192.  The steps
+// that were worked out for the last layer are kept, by its sizes alone (all of them up to 8,192 rows of 1,024 x 90,000: 1.8 ms).
 size_t workspace_bytes(int dtype, int N, int H, int V, int K, bool grad) {
   if (check_sizes(dtype, N, H, V, K) != KB_OK || N == 0) return 0;
-  return std::max(make_plan(dtype, N, H, V, K, true, grad, true).bytes,
-                  make_plan(dtype, N, H, V, K, true, grad, false).bytes);
+  static thread_local struct {
+    int dtype, H, V, K, grad, n;
+    size_t most[kPlanSteps];
+  } t = {};
+  if (t.n == 0 || t.dtype != dtype || t.H != H || t.V != V || t.K != K || t.grad != grad)
+    t.dtype = dtype, t.H = H, t.V = V, t.K = K, t.grad = grad, t.n = 0;
+  int i = 0;
+  while (step_rows(i) < N) ++i;
+  for (; t.n <= i; ++t.n) {
+    size_t most = t.n > 0 ? t.most[t.n - 1] : 0;
+    for (bool aligned : {true, false}) most = std::max(most, make_plan(dtype, step_rows(t.n), H, V, K, true, grad, aligned).bytes);
+    t.most[t.n] = most;
+  }
+  return t.most[i];
 }
 
 // What the two losses have in common.
