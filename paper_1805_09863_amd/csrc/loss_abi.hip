@@ -440,7 +440,6 @@ kb::LossLogitsArgs logits_args(const Call& c, const Plan& p, const Work& w, cons
   a.b = w.at<float>(p.b) + (size_t)t0 * kb::kLossM;
   a.words = c.V - t0 * kb::kLossM;
   a.vt = tiles;
-  a.N = c.N;
   a.count = w.rows.count;
   a.grid = p.grid;
   a.scale = kb::kL2E / c.temperature;

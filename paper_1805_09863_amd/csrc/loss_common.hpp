@@ -105,7 +105,6 @@ struct LossLogitsArgs {
   const float* b;        // bias of the piece's first word on
   int words;             // words of the piece that exist
   int vt;                // its word tiles
-  int N;
   const int32_t* count;
   int grid;              // workgroups that share the tiles
   float scale;           // log2(e) / T

@@ -296,11 +296,19 @@ hipError_t launch_loss_dh_p(int BN, const LossGradArgs& a, hipStream_t st) {
 template <int PASSES>
 hipError_t launch_loss_dw_p(int BNh, const LossGradArgs& a, hipStream_t st) {
   const dim3 gr(a.grid), th(256);
-  switch (BNh) {
-    case 256: loss_dw<LossT256, PASSES><<<gr, th, 0, st>>>(a); break;
-    case 128: loss_dw<LossT128, PASSES><<<gr, th, 0, st>>>(a); break;
-    default: loss_dw<LossT64, PASSES><<<gr, th, 0, st>>>(a); break;
+  if constexpr (PASSES != 2) {  // dlogits in two pieces are those of at most 128 rows, whose state tiles are 64 wide
+    if (BNh == 256) {
+      loss_dw<LossT256, PASSES><<<gr, th, 0, st>>>(a);
+      return hipGetLastError();
+    }
+    if (BNh == 128) {
+      loss_dw<LossT128, PASSES><<<gr, th, 0, st>>>(a);
+      return hipGetLastError();
+    }
+  } else if (BNh != 64) {
+    return hipErrorInvalidValue;
   }
+  loss_dw<LossT64, PASSES><<<gr, th, 0, st>>>(a);
   return hipGetLastError();
 }
 

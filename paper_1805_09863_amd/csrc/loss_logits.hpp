@@ -35,11 +35,6 @@ __device__ __forceinline__ int const_int(const int32_t* p) {
   return *(const KB_CONST int32_t*)(uintptr_t)uniform_ptr(p);
 }
 
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ i32x4 const_int4(const void* p) {
-  return *(const KB_CONST i32x4*)(uintptr_t)uniform_ptr(p);
-}
-
 // Workgroup b of the R x P cells: those of an XCD (every eighth workgroup) are neighbours, groups of four row tiles
 // walked split by split, so that one L2 sees the tiles of W asked for by several row tiles at about the same time.
 __device__ __forceinline__ void loss_cell(int R, int P, int b, int& rt, int& sp) {
