@@ -13,6 +13,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "loss_load.hpp"
 #include "loss_teacher.hpp"
 
 namespace kb {
@@ -24,37 +25,15 @@ struct FewWords {
   static constexpr int N = 16 / sizeof(S);  // of a thread
 };
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4f __attribute__((ext_vector_type(4)));
-typedef u32x4 Raw16b __attribute__((aligned(2)));  // 16 bytes at any element
-typedef f32x4f Raw16f __attribute__((aligned(4)));
-
 // A thread's words of a row of W: by one load (of any alignment) where all of them exist (ALL), else the `left` ones.
 template <bool ALL, class S>
 __device__ __forceinline__ void few_load(const S* p, int left, float (&x)[FewWords<S>::N]) {
   constexpr int NW = FewWords<S>::N;
   if constexpr (!ALL) {
 #pragma unroll
-    for (int i = 0; i < NW; ++i) {
-      x[i] = 0.f;
-      if (i < left) {
-        if constexpr (sizeof(S) == 2)
-          x[i] = __uint_as_float((uint32_t)p[i] << 16);
-        else
-          x[i] = p[i];
-      }
-    }
-  } else if constexpr (sizeof(S) == 2) {
-    const u32x4 r = *reinterpret_cast<const Raw16b*>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(r[i] << 16);
-      x[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
-    }
+    for (int i = 0; i < NW; ++i) x[i] = i < left ? widen(p, i) : 0.f;
   } else {
-    const f32x4f r = *reinterpret_cast<const Raw16f*>(p);
-#pragma unroll
-    for (int i = 0; i < NW; ++i) x[i] = r[i];
+    load16(p, x);
   }
 }
 
@@ -66,27 +45,19 @@ __device__ __forceinline__ void few_store(S* p, int left, const float (&x)[FewWo
 #pragma unroll
     for (int i = 0; i < NW; ++i) r[i] = (__bf16)x[i];
     if constexpr (ALL) {
-      *reinterpret_cast<Raw16b*>(p) = __builtin_bit_cast(u32x4, r);
+      *reinterpret_cast<AnyU32x4*>(p) = __builtin_bit_cast(u32x4, r);
     } else {
 #pragma unroll
       for (int i = 0; i < NW; ++i)
         if (i < left) reinterpret_cast<__bf16*>(p)[i] = r[i];
     }
   } else if constexpr (ALL) {
-    *reinterpret_cast<Raw16f*>(p) = f32x4f{x[0], x[1], x[2], x[3]};
+    *reinterpret_cast<AnyF32x4*>(p) = f32x4{x[0], x[1], x[2], x[3]};
   } else {
 #pragma unroll
     for (int i = 0; i < NW; ++i)
       if (i < left) p[i] = x[i];
   }
-}
-
-__device__ __forceinline__ float few_value(const uint16_t* p, size_t i) { return __uint_as_float((uint32_t)p[i] << 16); }
-__device__ __forceinline__ float few_value(const float* p, size_t i) { return p[i]; }
-
-template <int CTRL>
-__device__ __forceinline__ float dpp(float x) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
 }
 
 // v[0 .. NR) summed over TW lanes in a row, 16 or 8 (i: the lane among them); lane i gets the value that its bits name
@@ -108,10 +79,10 @@ __device__ __forceinline__ float few_sum(float (&v)[NR], int i) {
   };
   auto half = [](int n) { return n > 1 ? n / 2 : 1; };
   constexpr int n3 = TW == 16 ? half(NR) : NR, n2 = half(n3), n1 = half(n2);
-  if constexpr (TW == 16) step(std::integral_constant<int, NR>{}, (i & 8) != 0, [](float x) { return dpp<0x140>(x); });  // row_mirror
-  step(std::integral_constant<int, n3>{}, (i & 4) != 0, [](float x) { return dpp<0x141>(x); });  // row_half_mirror
-  step(std::integral_constant<int, n2>{}, (i & 2) != 0, [](float x) { return dpp<0x1b>(x); });   // quad_perm 3 2 1 0
-  step(std::integral_constant<int, n1>{}, (i & 1) != 0, [](float x) { return dpp<0xb1>(x); });   // quad_perm 1 0 3 2
+  if constexpr (TW == 16) step(std::integral_constant<int, NR>{}, (i & 8) != 0, [](float x) { return dpp_of<0x140>(x); });  // row_mirror
+  step(std::integral_constant<int, n3>{}, (i & 4) != 0, [](float x) { return dpp_of<0x141>(x); });  // row_half_mirror
+  step(std::integral_constant<int, n2>{}, (i & 2) != 0, [](float x) { return dpp_of<0x1b>(x); });   // quad_perm 3 2 1 0
+  step(std::integral_constant<int, n1>{}, (i & 1) != 0, [](float x) { return dpp_of<0xb1>(x); });   // quad_perm 1 0 3 2
   return v[0];
 }
 
@@ -173,7 +144,7 @@ __global__ __launch_bounds__(256) void loss_few(LossFewArgs a) {
   for (int i = tid; i < H * NR; i += 256) {
     const int k = i / NR, n = i % NR;
     // rows left out are not read
-    hs[i] = n < N && (GRAD ? rowv[2 * n] != INFINITY : rowv[2 * n + 1] != 0.f) ? few_value(h, (size_t)n * H + k) : 0.f;
+    hs[i] = n < N && (GRAD ? rowv[2 * n] != INFINITY : rowv[2 * n + 1] != 0.f) ? widen(h, (size_t)n * H + k) : 0.f;
     if (GRAD) dhs[i] = 0.f;
   }
   __syncthreads();
@@ -230,7 +201,7 @@ __global__ __launch_bounds__(256) void loss_few(LossFewArgs a) {
     for (int n = 0; n < NR; ++n) {
 #pragma unroll
       for (int i = 0; i < NW; ++i) {
-        if (TW == 8) acc[n][i] += dpp<0x128>(acc[n][i]);  // row_ror by 8
+        if (TW == 8) acc[n][i] += dpp_of<0x128>(acc[n][i]);  // row_ror by 8
         acc[n][i] += __shfl_xor(acc[n][i], 16, 64);
         acc[n][i] += __shfl_xor(acc[n][i], 32, 64);
       }

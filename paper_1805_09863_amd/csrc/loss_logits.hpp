@@ -22,6 +22,7 @@
 // dlogits written); 640 x 512 x 30,000 of float32 140 and 168.
 #pragma once
 
+#include "loss_load.hpp"
 #include "loss_mm.hpp"
 
 namespace kb {
@@ -76,11 +77,6 @@ __device__ __forceinline__ void store_rows(uint32_t mine, Value value, Write wri
     const bf16x8 v = *(const KB_LDS bf16x8*)(uintptr_t)(mine + (uint32_t)(row * 64 + (c ^ hswz(row)) * 16));
     write(row, c * 8, v);
   }
-}
-
-template <int CTRL>
-__device__ __forceinline__ float dpp_of(float x) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
 }
 
 // s[0 .. 16) summed over each half's 32 lanes: lane i gets value (i & 31) / 2.  Rows of 16 lanes swap halves of the

@@ -5,6 +5,7 @@
 #include "k3_scan.hpp"
 #include "loss_bias.hpp"
 #include "loss_common.hpp"
+#include "loss_load.hpp"
 #include "loss_teacher.hpp"
 
 namespace kb {
@@ -69,30 +70,12 @@ __device__ __forceinline__ void write_pieces(const float (&x)[8], uint16_t* out,
   }
 }
 
-__device__ __forceinline__ float widen(const uint16_t* p, size_t i) { return __uint_as_float((uint32_t)p[i] << 16); }
-__device__ __forceinline__ float widen(const float* p, size_t i) { return p[i]; }
-
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4p __attribute__((ext_vector_type(4)));
-typedef u32x4 Raw16b __attribute__((aligned(2)));  // 16 bytes at any element
-typedef f32x4p Raw16f __attribute__((aligned(4)));
-
 // n of 8 values from p on, the rest zeros; all of them by loads of 16 bytes, at any address.
 template <class S>
 __device__ __forceinline__ void load8(const S* p, int n, float (&x)[8]) {
   if (n >= 8) {
-    if constexpr (sizeof(S) == 2) {
-      const u32x4 w = *reinterpret_cast<const Raw16b*>(p);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x[2 * i] = __uint_as_float(w[i] << 16);
-        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-      }
-    } else {
-      const f32x4p v = *reinterpret_cast<const Raw16f*>(p), u = *reinterpret_cast<const Raw16f*>(p + 4);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = v[i], x[4 + i] = u[i];
-    }
+    load16(p, x);
+    if constexpr (sizeof(S) == 4) load16(p + 4, x + 4);
     return;
   }
 #pragma unroll
