@@ -94,9 +94,10 @@ kb_status kb_cross_entropy(int dtype, int N, int H, int V, const void* h, const 
  *   dW            nullable, H x V of the type of W.
  *   db            nullable, V float32.
  * Outputs are overwritten, not added to, and may not overlap the inputs.  The
- * products take the logits' gradients rounded once to the type of h (float32
- * to 2^-24); db is summed from them in float32 before that.  N = 0 gives zeros
- * in dW and db.
+ * products take the logits' gradients rounded once: in bf16 to 2^-8, a
+ * rounding as large as the results' own, for N <= 128 to 2^-17; in float32 to
+ * 2^-24.  db is summed from them in float32 before that.  N = 0 gives zeros in
+ * dW and db.
  *   workspace     kb_loss_grad_workspace_bytes(dtype, N, H, V, 1) bytes,
  *                 256-byte aligned.
  */

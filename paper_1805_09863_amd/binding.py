@@ -1032,6 +1032,9 @@ def cross_entropy(h: torch.Tensor, W: torch.Tensor, b: torch.Tensor, target: tor
     ``target`` N int32, the word of every row (outside 0 .. V - 1: the row is left out, its loss and lse are
     0).  ``smoothing``: the part of the labels that is spread over all words.  ``out`` may supply (loss, lse),
     ``ws`` a workspace of at least ``loss_workspace_bytes`` bytes.
+
+    Nothing is recorded for ``backward()``, whether h, W or b require gradients or not: the gradients are what
+    ``cross_entropy_grad`` returns.
     """
     dev, _, code, N, H, V, hp, Wp, bp = _loss_layer(h, W, b)
     tp = _loss_need(target, "target", _I32, (N,), dev)
@@ -1048,7 +1051,9 @@ def cross_entropy_grad(h: torch.Tensor, W: torch.Tensor, b: torch.Tensor, target
     (kb_cross_entropy_grad): returns (dh, dW, db), of the types and shapes of h, W and b.
 
     ``lse`` is what ``cross_entropy`` returned, ``grad`` N float32.  ``out`` may supply (dh, dW, db), with None
-    for what is not wanted; ``ws`` a workspace of at least ``loss_grad_workspace_bytes`` bytes.
+    for what is not wanted; ``ws`` a workspace of at least ``loss_grad_workspace_bytes`` bytes.  The results stand by
+    themselves: no tensor's ``.grad`` is set or added to.  In bfloat16 the logits' gradients are rounded to 2^-8 before
+    the products, of at most 128 rows to 2^-17.
     """
     dev, _, code, N, H, V, hp, Wp, bp = _loss_layer(h, W, b)
     tp = _loss_need(target, "target", _I32, (N,), dev)
@@ -1068,6 +1073,8 @@ def distill(h: torch.Tensor, W: torch.Tensor, b: torch.Tensor, token: torch.Tens
     -inf is no entry, and a row without one is left out.  ``temperature`` is 1e-6 to 1e6; the loss is its square
     times the divergence of softmax(student / temperature) from softmax(logit / temperature); lse is the log-sum-exp
     of the student's logits / temperature.
+
+    Nothing is recorded for ``backward()``: the gradients are what ``distill_grad`` returns.
     """
     dev, _, code, N, H, V, hp, Wp, bp = _loss_layer(h, W, b)
     K, tp, yp = _loss_teacher(token, logit, N, dev)

@@ -295,7 +295,7 @@ kb_status check_sizes(int dtype, int N, int H, int V, int K) {
 
 // What the largest of all batches of up to N rows takes, so that a workspace for a program's largest batch serves the
 // smaller ones: pieces are chosen by their time, and 5,825 rows of 1,024 x 90,000 have larger ones than 8,192.  The steps
-// that were worked out for the last layer are kept, by its sizes alone (all of them up to 8,192 rows of 1,024 x 90,000: 1.8 ms).
+// that were worked out for the last layer are kept, by its sizes alone (all up to 8,192 rows of 1,024 x 90,000: 1.8 ms).
 size_t workspace_bytes(int dtype, int N, int H, int V, int K, bool grad) {
   if (check_sizes(dtype, N, H, V, K) != KB_OK || N == 0) return 0;
   static thread_local struct {
@@ -308,7 +308,7 @@ size_t workspace_bytes(int dtype, int N, int H, int V, int K, bool grad) {
   while (step_rows(i) < N) ++i;
   for (; t.n <= i; ++t.n) {
     size_t most = t.n > 0 ? t.most[t.n - 1] : 0;
-    for (bool aligned : {true, false}) most = std::max(most, make_plan(dtype, step_rows(t.n), H, V, K, true, grad, aligned).bytes);
+    for (bool at16 : {true, false}) most = std::max(most, make_plan(dtype, step_rows(t.n), H, V, K, true, grad, at16).bytes);
     t.most[t.n] = most;
   }
   return t.most[i];

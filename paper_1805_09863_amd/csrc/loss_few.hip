@@ -1,5 +1,6 @@
-// The losses of at most eight rows (of float32, scored: sixteen, in two turns): W is read once (twice for its gradient) and everything else is small, so the
-// vector ALUs do, in float32 whatever the operands' type, and W needs no laying out, whatever its alignment.
+// The losses of at most eight rows (of float32, scored: sixteen, in two turns): W is read once (twice for its gradient)
+// and everything else is small, so the vector ALUs do, in float32 whatever the operands' type, and W needs no laying out,
+// whatever its alignment.
 //
 // A workgroup takes chunks of 16 (few words: 8) x 16 bytes of words: threads of 16 bytes each along the words, and 16 or
 // 32 slices along the states.  Forward: every thread sums its words' products over its slice's states for all rows, the
@@ -8,8 +9,9 @@
 // states gives dW (a product over the rows, written as it comes) and the chunk's part of dh (summed over the threads
 // along the words by halving what a lane keeps), which the workgroup adds up over its chunks in LDS.
 //
-// 8 rows of float32, 1,024 x 32,000: 42 us (3.2 TB/s, one reading of W), with gradients 141 (3.7 TB/s, three passes over
-// its size); 5 x 256 x 8,000 is bound by the launches (11 and 4 us of kernels; with gradients 37 in four).
+// 8 rows of float32, 1,024 x 32,000: 55 us from memory (2.4 TB/s, one reading of W), 36 with W in the last-level cache; the
+// gradients 77 (5.1 TB/s, three passes over its size, the second reading from that cache); 5 x 256 x 8,000 is bound by the
+// launches (10 and 4 us of kernels; with gradients 35 in four).
 #include <algorithm>
 #include <type_traits>
 
@@ -94,8 +96,9 @@ __global__ __launch_bounds__(256) void loss_few(LossFewArgs a) {
   constexpr int NW = FewWords<S>::N, CH = TW * NW, NS = 256 / TW;  // words of a chunk, slices
   extern __shared__ __align__(16) float dyn[];
   const size_t held = few_states(a.H, NR);
-  // Eight rows' values of a state are read by 16 bytes; scored in float32, in pairs (8 x 1,024 x 32,000: 40.8 us, by 16 bytes,
-  // with fewer registers and fewer loads under way, 42.7; bf16 and gradients are 1 to 6% faster by 16 bytes).
+  // Eight rows' values of a state are read by 16 bytes; scored in float32, in pairs (8 x 1,024 x 32,000, W in the last-level
+  // cache, a call: 40.8 us, by 16 bytes, with fewer registers and fewer loads under way, 42.7; bf16 and gradients are 1 to
+  // 6% faster by 16 bytes).
   uint32_t first = 0;
   if constexpr (!GRAD && sizeof(S) == 4) asm("" : "+s"(first));  // the compiler does not know where they lie
   float* hs = dyn + first;                // H x NR states
