@@ -23,7 +23,7 @@ path (k = 5): --dtype f32 (aligned shapes, H 256-2048, multiples of 64, V
 (the DMA pipeline, H 512-2048, V 8k-90k, 12-2,560 rows: kBf16DmaCosts) and
 bf16reg (H 500-2000, odd V of 8,001-90,001, 12-2,560 rows: kBf16Costs).
 
-    python -m paper_1805_09863_amd.tune_planner --dtype bf16 --out gpurun_out/tune_bf16.json
+    python -m paper_1805_09863_amd.tune_planner --dtype bf16 --out tune_bf16.json
 
 Operands are drawn on the device (normal h, W scaled by 1/sqrt(H), small
 uniform bias); times do not depend on their values beyond the candidate
